@@ -111,7 +111,7 @@ def draw(rng):
         most = 4096 * 4096 * 8192 // 2 // (6 if t == "fp32" else 1)  # the largest listed one's work
         M = _log(rng, 1, 1 << 17)
         K, N = _width(rng, 64, 8192), _width(rng, 64, 8192)
-        while M * K * N * (2 if op == "dense_backward" else 1) > most:
+        while M * K * N * (2 if op == "dense_backward" else 1) > most or M * max(K, N) > 1 << 25:
             M, K, N = _size(M // 2 + 1), _size(max(64, K * 4 // 5)), _size(max(64, N * 4 // 5))
         act, order, bias = rng.choice(ACTS), rng.choice(("io", "oi")), rng.random() < 0.8
         if op == "dense_backward":
