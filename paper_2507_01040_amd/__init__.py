@@ -32,7 +32,11 @@ BLOCK_AUTO, BLOCK_TWO_LAUNCH, BLOCK_FUSED = 0, 1, 2
 EXPORTED = ("clifford_conv_nd", "clifford_conv_nd_algo", "clifford_linear",
             "multivector_act", "cliffconv_cayley_table", "cliffconv_status_string",
             "cliffconv_mfma_peak_probe", "clifford_block2_nd", "clifford_block2_nd_path",
-            "clifford_block2_nd_noalloc")
+            "clifford_block2_nd_noalloc",
+            "cliffconv_dense", "cliffconv_dense_workspace", "cliffconv_dense_backward",
+            "cliffconv_dense_backward_workspace", "cliffconv_layer_norm",
+            "cliffconv_layer_norm_backward", "cliffconv_layer_norm_backward_workspace",
+            "cliffconv_dropout")
 
 
 class CliffActDesc(ctypes.Structure):
@@ -88,6 +92,7 @@ def load(path: str = LIB_PATH):
                  "multivector_act", "cliffconv_cayley_table", "cliffconv_mfma_peak_probe",
                  "clifford_block2_nd", "clifford_block2_nd_path", "clifford_block2_nd_noalloc"):
         getattr(lib, name).restype = i32
+    feed_forward.declare(lib)
     _lib = lib
     return lib
 
@@ -549,3 +554,12 @@ def block_forward(x, layers, g: Sequence[int], outs=None, stream=None):
         y = conv_nd(y, f, b, g, act=a, out=None if outs is None else outs[li],
                     stream=stream)
     return y
+
+
+# the residual feed-forward operators (include/cliffconv_ff.h); they build on
+# the names above
+from . import feed_forward  # noqa: E402
+from .feed_forward import (  # noqa: E402,F401
+    ACT_GELU, ACT_NONE, ACT_RELU, ACT_SILU, dense, dense_backward, dense_backward_plan, dense_plan,
+    dropout, dropout_plan, layer_norm, layer_norm_backward, layer_norm_backward_plan,
+    layer_norm_plan)

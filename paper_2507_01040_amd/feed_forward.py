@@ -1,0 +1,496 @@
+"""Residual feed-forward operators of libcliffconv.so (include/cliffconv_ff.h):
+what stands between the Clifford linear layers of a network, for training and
+serving -- layer norm, dense layers with bias, activation, dropout and residual
+in their epilogue, dropout by itself, and their gradients.
+
+Rows are the leading axes of a tensor, features its last one; a multivector
+tensor [B, C, N_B] of ``linear`` is taken as ``x.flatten(1)``.  Tensors are
+float32, bfloat16 or float16, one type per call, and may be views whose rows
+have one stride and contiguous features.  As everywhere in the package, torch
+provides device memory and streams only; every tensor's shape, type, layout and
+device is checked before the library is called.  ``*_plan`` functions do the
+checks once, for a call that is repeated on the same buffers.
+"""
+from __future__ import annotations
+
+import ctypes
+from typing import Optional, Tuple
+
+import paper_2507_01040_amd as _pkg
+
+ACT_NONE, ACT_RELU, ACT_GELU, ACT_SILU = 0, 1, 2, 3
+F32, BF16, F16 = 0, 1, 2
+
+
+class CliffDropoutDesc(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_double), ("rng", ctypes.c_void_p)]
+
+
+def declare(lib) -> None:
+    """Argument and result types of the entry points."""
+    i64, vp, i32 = ctypes.c_int64, ctypes.c_void_p, ctypes.c_int
+    drop = ctypes.POINTER(CliffDropoutDesc)
+    mat = [vp, i64]
+    lib.cliffconv_dense.argtypes = [i32, i64, i64, i64, *mat, *mat, i32, vp, i32, drop,
+                                    *mat, *mat, *mat, vp, i64, vp]
+    lib.cliffconv_dense_backward.argtypes = [i32, i64, i64, i64, *mat, *mat, *mat, i32, *mat, i32,
+                                             drop, *mat, *mat, vp, vp, i64, vp]
+    lib.cliffconv_layer_norm.argtypes = [i32, i64, i64, *mat, vp, vp, ctypes.c_double, *mat, vp, vp,
+                                         vp]
+    lib.cliffconv_layer_norm_backward.argtypes = [i32, i64, i64, *mat, *mat, vp, vp, vp, *mat, *mat,
+                                                  vp, vp, vp, i64, vp]
+    lib.cliffconv_dropout.argtypes = [i32, i64, i64, *mat, drop, *mat, *mat, vp]
+    lib.cliffconv_dense_workspace.argtypes = [i32, i64, i64, i64]
+    lib.cliffconv_dense_backward_workspace.argtypes = [i32, i64, i64, i64]
+    lib.cliffconv_layer_norm_backward_workspace.argtypes = [i32, i64, i64]
+    for name in EXPORTED:
+        getattr(lib, name).restype = i64 if name.endswith("_workspace") else i32
+
+
+EXPORTED = ("cliffconv_dense", "cliffconv_dense_workspace", "cliffconv_dense_backward",
+            "cliffconv_dense_backward_workspace", "cliffconv_layer_norm",
+            "cliffconv_layer_norm_backward", "cliffconv_layer_norm_backward_workspace",
+            "cliffconv_dropout")
+
+
+# ---------------------------------------------------------------------------
+# Checks
+# ---------------------------------------------------------------------------
+
+def _shape(t) -> Tuple[int, ...]:
+    return tuple(getattr(t, "shape", ()))
+
+
+def _check_rows(t, shape, name: str) -> None:
+    if _shape(t) != tuple(shape):
+        raise ValueError("%s has shape %s, expected %s" % (name, _shape(t), tuple(shape)))
+
+
+def _row_stride(t, name: str) -> int:
+    """The one stride of t's rows (all axes but the last, which is contiguous)."""
+    shape, strides = t.shape, t.stride()
+    d = shape[-1]
+    if 0 in shape[:-1]:
+        return d
+    if d > 1 and strides[-1] != 1:
+        raise ValueError("%s: features are not contiguous (strides %s)" % (name, tuple(strides)))
+    ld = None
+    for size, stride in zip(reversed(shape[:-1]), reversed(strides[:-1])):
+        if size == 1:
+            continue
+        if ld is None:
+            ld, run = stride, stride * size
+            if ld < d:
+                raise ValueError("%s: rows overlap (strides %s)" % (name, tuple(strides)))
+        elif stride != run:
+            raise ValueError("%s: rows have no single stride (shape %s, strides %s)"
+                             % (name, tuple(shape), tuple(strides)))
+        else:
+            run = stride * size
+    return d if ld is None else ld
+
+
+def _type_of(x, name: str) -> int:
+    import torch
+    codes = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
+    if x.dtype not in codes:
+        raise ValueError("%s has type %s, expected float32, bfloat16 or float16" % (name, x.dtype))
+    return codes[x.dtype]
+
+
+def _check_dev(t, name: str, like=None, dtype=None) -> None:
+    import torch
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise ValueError("%s must be a GPU tensor" % name)
+    if like is not None and t.device != like.device:
+        raise ValueError("%s is on %s, not on %s with the input" % (name, t.device, like.device))
+    want = dtype if dtype is not None else like.dtype if like is not None else None
+    if want is not None and t.dtype != want:
+        raise ValueError("%s has type %s, expected %s" % (name, t.dtype, want))
+
+
+def _check_vector(t, n: int, name: str) -> None:
+    if t is not None:
+        _check_rows(t, (n,), name)
+
+
+def _check_vector_dev(t, name: str, like, dtype=None) -> None:
+    if t is not None:
+        _check_dev(t, name, like, dtype)
+        if not t.is_contiguous():
+            raise ValueError("%s must be contiguous" % name)
+
+
+def _rows_of(shape) -> int:
+    n = 1
+    for s in shape[:-1]:
+        n *= s
+    return n
+
+
+def _check_features(x, name: str) -> None:
+    if len(_shape(x)) < 1 or x.shape[-1] < 1:
+        raise ValueError("%s has shape %s, expected [..., features]" % (name, _shape(x)))
+
+
+def _check_dropout(dropout, name: str = "dropout") -> None:
+    if dropout is None:
+        return
+    p, rng = dropout
+    if not 0.0 <= p <= 1.0:
+        raise ValueError("%s: probability %r is not in [0, 1]" % (name, p))
+    _check_rows(rng, (2,), name + " rng")
+
+
+def _check_dropout_dev(dropout, like, name: str = "dropout") -> None:
+    if dropout is not None:
+        import torch
+        _check_vector_dev(dropout[1], name + " rng", like, torch.int64)
+
+
+def _drop_desc(dropout):
+    if dropout is None:
+        return None
+    d = CliffDropoutDesc()
+    d.p, d.rng = float(dropout[0]), dropout[1].data_ptr()
+    return d
+
+
+def _check_act(act) -> None:
+    if act not in (ACT_NONE, ACT_RELU, ACT_GELU, ACT_SILU):
+        raise ValueError("unknown activation %r" % (act,))
+
+
+def _ref(desc):
+    return ctypes.byref(desc) if desc is not None else None
+
+
+def _ptr(t):
+    return t.data_ptr() if t is not None else None
+
+
+def _weight_order(w, name: str = "weight") -> Tuple[int, int]:
+    """(w_out_in, row stride) of a weight [K, N]: stored as it is, or the
+    transposed view of a stored [N, K]."""
+    K, N = w.shape
+    sk, sn = w.stride()
+    if (sn == 1 or N == 1) and (sk >= N or K == 1):
+        return 0, sk if K > 1 else N
+    if (sk == 1 or K == 1) and (sn >= K or N == 1):
+        return 1, sn if N > 1 else K
+    raise ValueError("%s: neither axis is contiguous (shape %s, strides %s)" % (name, (K, N), (sk, sn)))
+
+
+class FeedForwardPlan(_pkg.Plan):
+    """A Plan whose output may be a tuple of tensors.  Called for another
+    stream, it tells torch's allocator that its buffers are used there."""
+
+    def __call__(self, stream=None):
+        if stream is not None and hasattr(stream, "cuda_stream"):
+            for t in self._own:
+                t.record_stream(stream)
+        return super().__call__(stream)
+
+
+def _plan(fn_name: str, args, out, keep, own, stream) -> FeedForwardPlan:
+    """The call as a plan; args end with the stream's place.  ``own``: tensors
+    allocated here, which another stream than the current one may use."""
+    if stream is not None and hasattr(stream, "cuda_stream"):
+        for t in own:
+            t.record_stream(stream)
+    args = (*args, _pkg._stream_ptr(stream) or None)
+    p = FeedForwardPlan(getattr(_pkg.load(), fn_name), args, len(args) - 1, fn_name, out, keep)
+    p._own = own
+    return p
+
+
+class _Buffers:
+    """Outputs and workspace of a call: the caller's, or allocated here."""
+
+    def __init__(self, like):
+        self.like = like
+        self.own = []
+
+    def empty(self, given, shape, name: str, dtype=None):
+        import torch
+        if given is not None:
+            _check_dev(given, name, self.like, dtype)
+            return given
+        t = torch.empty(shape, dtype=dtype or self.like.dtype, device=self.like.device)
+        self.own.append(t)
+        return t
+
+    def workspace(self, given, need: int):
+        import torch
+        if given is not None:
+            _check_dev(given, "workspace", self.like, torch.uint8)
+            if given.numel() < need or not given.is_contiguous():
+                raise ValueError("workspace holds %d bytes, expected %d contiguous ones"
+                                 % (given.numel(), need))
+            return given, given.numel()
+        if need == 0:
+            return None, 0
+        t = torch.empty(need, dtype=torch.uint8, device=self.like.device)
+        self.own.append(t)
+        return t, need
+
+
+# ---------------------------------------------------------------------------
+# Dense layer
+# ---------------------------------------------------------------------------
+
+def dense_plan(x, weight, bias=None, act: int = ACT_NONE, dropout=None, residual=None, pre=None,
+               out=None, workspace=None, stream=None) -> FeedForwardPlan:
+    """dense as a plan."""
+    _check_features(x, "x")
+    K = x.shape[-1]
+    if len(_shape(weight)) != 2 or weight.shape[0] != K or weight.shape[1] < 1:
+        raise ValueError("weight has shape %s, expected [%d, features out]" % (_shape(weight), K))
+    N = weight.shape[1]
+    shape = tuple(x.shape[:-1]) + (N,)
+    want_pre = pre is not None and pre is not False
+    given_pre = None if pre is True or not want_pre else pre
+    _check_vector(bias, N, "bias")
+    _check_act(act)
+    _check_dropout(dropout)
+    for t, name in ((residual, "residual"), (given_pre, "pre"), (out, "out")):
+        if t is not None:
+            _check_rows(t, shape, name)
+    _check_dev(x, "x")
+    code = _type_of(x, "x")
+    _check_dev(weight, "weight", x)
+    _check_vector_dev(bias, "bias", x)
+    _check_dropout_dev(dropout, x)
+    if residual is not None:
+        _check_dev(residual, "residual", x)
+    order, ldw = _weight_order(weight)
+    b = _Buffers(x)
+    pre_t = b.empty(given_pre, shape, "pre") if want_pre else None
+    out = b.empty(out, shape, "out")
+    M = _rows_of(x.shape)
+    lib = _pkg.load()
+    ws, ws_bytes = b.workspace(workspace, lib.cliffconv_dense_workspace(code, M, K, N))
+    desc = _drop_desc(dropout)
+    args = (code, M, K, N, _ptr(x), _row_stride(x, "x"), _ptr(weight), ldw, order, _ptr(bias), act,
+            _ref(desc), _ptr(residual), _row_stride(residual, "residual") if residual is not None else 0,
+            _ptr(pre_t), _row_stride(pre_t, "pre") if want_pre else 0, _ptr(out),
+            _row_stride(out, "out"), _ptr(ws), ws_bytes)
+    return _plan("cliffconv_dense", args, (out, pre_t) if want_pre else out,
+                 (x, weight, bias, dropout, residual, pre_t, out, ws, desc), b.own, stream)
+
+
+def dense(x, weight, bias=None, act: int = ACT_NONE, dropout=None, residual=None, pre=None,
+          out=None, workspace=None, stream=None):
+    """Dense layer residual + dropout(f(x weight + bias)) of x [..., K] and
+    weight [K, N] (or the transposed view of a stored [N, K]), bias [N] or
+    None, residual [..., N] or None.  ``act`` is one of ACT_NONE, ACT_RELU,
+    ACT_GELU, ACT_SILU; ``dropout`` is None or (p, rng) with rng an int64 GPU
+    tensor (key, step).  Returns the output [..., N]; with ``pre`` True or a
+    tensor also the pre-activations that the gradient needs: (out, pre)."""
+    return dense_plan(x, weight, bias, act, dropout, residual, pre, out, workspace, stream)()
+
+
+def dense_backward_plan(dy, x, weight, pre=None, act: int = ACT_NONE, dropout=None,
+                        bias: bool = True, dx=None, dweight=None, dbias=None, workspace=None,
+                        stream=None) -> FeedForwardPlan:
+    """dense_backward as a plan."""
+    _check_features(x, "x")
+    K = x.shape[-1]
+    if len(_shape(weight)) != 2 or weight.shape[0] != K or weight.shape[1] < 1:
+        raise ValueError("weight has shape %s, expected [%d, features out]" % (_shape(weight), K))
+    N = weight.shape[1]
+    _check_rows(dy, tuple(x.shape[:-1]) + (N,), "dy")
+    _check_act(act)
+    _check_dropout(dropout)
+    if act != ACT_NONE:
+        if pre is None:
+            raise ValueError("an activation's gradient needs the pre-activations")
+        _check_rows(pre, dy.shape, "pre")
+    else:
+        pre = None
+    for t, like, name in ((dx, x, "dx"), (dweight, weight, "dweight")):
+        if t is not None and t is not False:
+            _check_rows(t, like.shape, name)
+    if dbias is not None:
+        _check_vector(dbias, N, "dbias")
+    _check_dev(dy, "dy")
+    code = _type_of(dy, "dy")
+    for t, name in ((x, "x"), (weight, "weight")):
+        _check_dev(t, name, dy)
+    if pre is not None:
+        _check_dev(pre, "pre", dy)
+    _check_dropout_dev(dropout, dy)
+    order, ldw = _weight_order(weight)
+    b = _Buffers(dy)
+    dx = None if dx is False else b.empty(dx, tuple(x.shape), "dx")
+    if dweight is False:
+        dweight = None
+    elif dweight is None:  # in the order of the weight
+        dweight = b.empty(None, (N, K), "dweight").t() if order else b.empty(None, (K, N), "dweight")
+    else:
+        b.empty(dweight, (K, N), "dweight")
+    lddw = N
+    if dweight is not None:
+        o, lddw = _weight_order(dweight, "dweight")
+        if o != order and K > 1 and N > 1:
+            raise ValueError("dweight is not stored in the order of the weight")
+    if bias:
+        dbias = b.empty(dbias, (N,), "dbias")
+        _check_vector_dev(dbias, "dbias", dy)
+    else:
+        dbias = None
+    M = _rows_of(x.shape)
+    lib = _pkg.load()
+    ws, ws_bytes = b.workspace(workspace, lib.cliffconv_dense_backward_workspace(code, M, K, N))
+    desc = _drop_desc(dropout)
+    args = (code, M, K, N, _ptr(dy), _row_stride(dy, "dy"), _ptr(x), _row_stride(x, "x"),
+            _ptr(weight), ldw, order, _ptr(pre), _row_stride(pre, "pre") if pre is not None else 0,
+            act, _ref(desc), _ptr(dx), _row_stride(dx, "dx") if dx is not None else 0,
+            _ptr(dweight), lddw, _ptr(dbias), _ptr(ws), ws_bytes)
+    outs = tuple(t for t, want in ((dx, dx is not None), (dweight, dweight is not None),
+                                   (dbias, bool(bias))) if want)
+    return _plan("cliffconv_dense_backward", args, outs,
+                 (dy, x, weight, pre, dropout, dx, dweight, dbias, ws, desc), b.own, stream)
+
+
+def dense_backward(dy, x, weight, pre=None, act: int = ACT_NONE, dropout=None, bias: bool = True,
+                   dx=None, dweight=None, dbias=None, workspace=None, stream=None):
+    """Gradient of dense for the output's gradient dy [..., N]: returns (dx
+    [..., K], dweight [K, N] stored in the order of the weight, dbias [N]),
+    without dbias where ``bias`` is False, and without dx or dweight where they
+    are given as False.  ``pre`` is the forward call's (needed with an
+    activation), ``act`` and ``dropout`` as there.  The residual's gradient is
+    dy itself."""
+    return dense_backward_plan(dy, x, weight, pre, act, dropout, bias, dx, dweight, dbias, workspace,
+                               stream)()
+
+
+# ---------------------------------------------------------------------------
+# Layer norm
+# ---------------------------------------------------------------------------
+
+def layer_norm_plan(x, weight=None, bias=None, eps: float = 1e-5, out=None, mean=None, rstd=None,
+                    stream=None) -> FeedForwardPlan:
+    """layer_norm as a plan."""
+    import torch
+    _check_features(x, "x")
+    d, rows = x.shape[-1], _rows_of(x.shape)
+    _check_vector(weight, d, "weight")
+    _check_vector(bias, d, "bias")
+    _check_vector(mean, rows, "mean")
+    _check_vector(rstd, rows, "rstd")
+    if not eps >= 0.0:
+        raise ValueError("eps %r is negative" % (eps,))
+    if out is not None:
+        _check_rows(out, x.shape, "out")
+    _check_dev(x, "x")
+    code = _type_of(x, "x")
+    _check_vector_dev(weight, "weight", x)
+    _check_vector_dev(bias, "bias", x)
+    _check_vector_dev(mean, "mean", x, torch.float32)
+    _check_vector_dev(rstd, "rstd", x, torch.float32)
+    b = _Buffers(x)
+    out = b.empty(out, tuple(x.shape), "out")
+    mean = b.empty(mean, (rows,), "mean", torch.float32)
+    rstd = b.empty(rstd, (rows,), "rstd", torch.float32)
+    args = (code, rows, d, _ptr(x), _row_stride(x, "x"), _ptr(weight), _ptr(bias), float(eps),
+            _ptr(out), _row_stride(out, "out"), _ptr(mean), _ptr(rstd))
+    return _plan("cliffconv_layer_norm", args, (out, mean, rstd),
+                 (x, weight, bias, out, mean, rstd), b.own, stream)
+
+
+def layer_norm(x, weight=None, bias=None, eps: float = 1e-5, out=None, mean=None, rstd=None,
+               stream=None):
+    """Layer norm of x [..., d] over its last axis with weight and bias [d] (or
+    None).  Returns (out, mean, rstd): the statistics are float32, one for each
+    row, for the gradient.  ``out`` may be x."""
+    return layer_norm_plan(x, weight, bias, eps, out, mean, rstd, stream)()
+
+
+def layer_norm_backward_plan(dy, x, mean, rstd, weight=None, dresidual=None, params: bool = True,
+                             dx=None, dweight=None, dbias=None, workspace=None,
+                             stream=None) -> FeedForwardPlan:
+    """layer_norm_backward as a plan."""
+    import torch
+    _check_features(x, "x")
+    d, rows = x.shape[-1], _rows_of(x.shape)
+    _check_rows(dy, x.shape, "dy")
+    _check_rows(mean, (rows,), "mean")
+    _check_rows(rstd, (rows,), "rstd")
+    _check_vector(weight, d, "weight")
+    _check_vector(dweight, d, "dweight")
+    _check_vector(dbias, d, "dbias")
+    for t, name in ((dresidual, "dresidual"), (dx, "dx")):
+        if t is not None:
+            _check_rows(t, x.shape, name)
+    _check_dev(dy, "dy")
+    code = _type_of(dy, "dy")
+    _check_dev(x, "x", dy)
+    _check_vector_dev(mean, "mean", dy, torch.float32)
+    _check_vector_dev(rstd, "rstd", dy, torch.float32)
+    _check_vector_dev(weight, "weight", dy)
+    if dresidual is not None:
+        _check_dev(dresidual, "dresidual", dy)
+    b = _Buffers(dy)
+    dx = b.empty(dx, tuple(x.shape), "dx")
+    ws, ws_bytes = None, 0
+    if params:
+        dweight = b.empty(dweight, (d,), "dweight")
+        dbias = b.empty(dbias, (d,), "dbias")
+        _check_vector_dev(dweight, "dweight", dy)
+        _check_vector_dev(dbias, "dbias", dy)
+        ws, ws_bytes = b.workspace(
+            workspace, _pkg.load().cliffconv_layer_norm_backward_workspace(code, rows, d))
+    else:
+        dweight = dbias = None
+    args = (code, rows, d, _ptr(dy), _row_stride(dy, "dy"), _ptr(x), _row_stride(x, "x"), _ptr(mean),
+            _ptr(rstd), _ptr(weight), _ptr(dresidual),
+            _row_stride(dresidual, "dresidual") if dresidual is not None else 0, _ptr(dx),
+            _row_stride(dx, "dx"), _ptr(dweight), _ptr(dbias), _ptr(ws), ws_bytes)
+    return _plan("cliffconv_layer_norm_backward", args, (dx, dweight, dbias) if params else dx,
+                 (dy, x, mean, rstd, weight, dresidual, dx, dweight, dbias, ws), b.own, stream)
+
+
+def layer_norm_backward(dy, x, mean, rstd, weight=None, dresidual=None, params: bool = True, dx=None,
+                        dweight=None, dbias=None, workspace=None, stream=None):
+    """Gradient of layer_norm for the output's gradient dy: returns (dx,
+    dweight, dbias), or dx alone where ``params`` is False.  ``mean`` and
+    ``rstd`` are the forward call's.  ``dresidual`` (the gradient that x gets
+    past the norm) is added to dx before its rounding.  ``dx`` may be dy or
+    dresidual."""
+    return layer_norm_backward_plan(dy, x, mean, rstd, weight, dresidual, params, dx, dweight, dbias,
+                                    workspace, stream)()
+
+
+# ---------------------------------------------------------------------------
+# Dropout
+# ---------------------------------------------------------------------------
+
+def dropout_plan(x, p: float, rng, residual=None, out=None, stream=None) -> FeedForwardPlan:
+    """dropout as a plan."""
+    _check_features(x, "x")
+    _check_dropout((p, rng))
+    for t, name in ((residual, "residual"), (out, "out")):
+        if t is not None:
+            _check_rows(t, x.shape, name)
+    _check_dev(x, "x")
+    code = _type_of(x, "x")
+    _check_dropout_dev((p, rng), x)
+    if residual is not None:
+        _check_dev(residual, "residual", x)
+    b = _Buffers(x)
+    out = b.empty(out, tuple(x.shape), "out")
+    desc = _drop_desc((p, rng))
+    args = (code, _rows_of(x.shape), x.shape[-1], _ptr(x), _row_stride(x, "x"), _ref(desc),
+            _ptr(residual), _row_stride(residual, "residual") if residual is not None else 0,
+            _ptr(out), _row_stride(out, "out"))
+    return _plan("cliffconv_dropout", args, out, (x, rng, residual, out, desc), b.own, stream)
+
+
+def dropout(x, p: float, rng, residual: Optional[object] = None, out=None, stream=None):
+    """residual + dropout(x) of x [..., d]: elements are dropped with
+    probability p and scaled by 1 / (1 - p) otherwise.  ``rng`` is an int64 GPU
+    tensor (key, step); the mask depends on it, p and the element's row and
+    column only and is never stored: the gradient is the same call on dy
+    (without the residual).  ``out`` may be x or residual."""
+    return dropout_plan(x, p, rng, residual, out, stream)()
