@@ -1,20 +1,37 @@
-// Dense layer with its epilogue, and its gradient.
+// Dense layer with its epilogue, and its gradient: three matrix products
+//   y = x w,  dx = g w^T,  dw = x^T g
+// of one kernel, which takes either operand contiguous along the contraction or
+// along the output (Stage::KM).
 #include <stdio.h>
 
 #include <algorithm>
 
+#include "dense_geom.hpp"
 #include "ff_common.hpp"
+#include "split.hpp"
 
 namespace cliff {
 namespace {
 
-// C[m, n] = sum_k A(m, k) B(k, n), operands by two strides each.
+typedef float f4 __attribute__((ext_vector_type(4)));
+typedef float f16v __attribute__((ext_vector_type(16)));
+typedef short s4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+typedef __bf16 b8 __attribute__((ext_vector_type(8)));
+typedef _Float16 h8 __attribute__((ext_vector_type(8)));
+typedef __attribute__((address_space(3))) void lds_void;
+
+// C[m, n] = sum_k A(m, k) B(n, k): operand X is [R, K] with row stride ld
+// (KM) or [K, R] with it.
 struct ProductArgs {
-    int64_t M, K, N;
+    int64_t M, N, K;
     const void* a;
-    int64_t am, ak;
+    int64_t lda;
     const void* b;
-    int64_t bk, bn;
+    int64_t ldb;
+    int splits;       // parts of the contraction, each by its own workgroups ...
+    int64_t k_part;   // ... of this many values (a multiple of the stage's)
+    float* partial;   // splits > 1: fp32 [splits][M][N], joined by another kernel
     // epilogue
     const void* bias;
     int act;
@@ -25,107 +42,648 @@ struct ProductArgs {
     int64_t ldp;
     void* y;
     int64_t ldy;
+    int vec;  // whole groups of four columns, aligned to their size, in every one of them
 };
 
-// 32 x 32 outputs per workgroup, one per thread in four passes.
 template <typename T>
-__global__ __launch_bounds__(256) void product_kernel(ProductArgs p)
+struct Vec4 {
+    typedef T t __attribute__((ext_vector_type(4)));
+};
+
+// Four neighbouring columns, some of which may not exist (have < 4).
+template <typename T>
+__device__ inline f4 load4(const T* p, bool vec, int have)
 {
-    __shared__ float as[32][33], bs[32][33];
-    const int64_t tn = (p.N + 31) / 32;
-    const int64_t m0 = blockIdx.x / tn * 32, n0 = blockIdx.x % tn * 32;
-    const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
-    float acc[4] = {};
-    for (int64_t k0 = 0; k0 < p.K; k0 += 32) {
-        for (int i = 0; i < 4; ++i) {
-            const int row = ty + 8 * i;
-            const int64_t m = m0 + row, k = k0 + tx, kb = k0 + row, n = n0 + tx;
-            as[row][tx] = m < p.M && k < p.K ? (float)static_cast<const T*>(p.a)[m * p.am + k * p.ak] : 0.f;
-            bs[row][tx] = kb < p.K && n < p.N ? (float)static_cast<const T*>(p.b)[kb * p.bk + n * p.bn] : 0.f;
-        }
-        __syncthreads();
-        for (int k = 0; k < 32; ++k)
-            for (int i = 0; i < 4; ++i) acc[i] += as[ty + 8 * i][k] * bs[k][tx];
-        __syncthreads();
+    typedef typename Vec4<T>::t v4;
+    if (vec) return __builtin_convertvector(*reinterpret_cast<const v4*>(p), f4);
+    f4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (e < have) v[e] = (float)p[e];
+    return v;
+}
+template <typename T>
+__device__ inline void store4(T* p, const f4& v, bool vec, int have)
+{
+    typedef typename Vec4<T>::t v4;
+    if (vec) {
+        *reinterpret_cast<v4*>(p) = __builtin_convertvector(v, v4);
+        return;
     }
-    const int64_t n = n0 + tx;
-    if (n >= p.N) return;
-    for (int i = 0; i < 4; ++i) {
-        const int64_t m = m0 + ty + 8 * i;
-        if (m >= p.M) continue;
-        float v = acc[i] + (p.bias ? (float)static_cast<const T*>(p.bias)[n] : 0.f);
-        if (p.pre) static_cast<T*>(p.pre)[m * p.ldp + n] = (T)v;
-        v = activate(p.act, v);
-        if (p.drop.rng) {
-            const Words w = philox((uint64_t)p.drop.rng[0], (uint32_t)p.drop.rng[1], (uint32_t)(n >> 2), m);
-            v = w.w[n & 3] <= p.drop.last ? 0.f : v * p.drop.scale;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (e < have) p[e] = (T)v[e];
+}
+
+__device__ inline void activate4(int act, f4& v)
+{
+    switch (act) {
+#define EACH(A)                                      \
+    case A:                                          \
+        for (int e = 0; e < 4; ++e) v[e] = activate(A, v[e]); \
+        break;
+        EACH(CLIFF_ACT_RELU)
+        EACH(CLIFF_ACT_GELU)
+        EACH(CLIFF_ACT_SILU)
+#undef EACH
+    }
+}
+__device__ inline void slope4(int act, f4& v, const f4& pre)
+{
+    switch (act) {
+#define EACH(A)                                                  \
+    case A:                                                      \
+        for (int e = 0; e < 4; ++e) v[e] *= activate_slope(A, pre[e]); \
+        break;
+        EACH(CLIFF_ACT_RELU)
+        EACH(CLIFF_ACT_GELU)
+        EACH(CLIFF_ACT_SILU)
+#undef EACH
+    }
+}
+__device__ inline void drop4(const DropArgs& d, uint64_t key, uint32_t step, int64_t r, int64_t c, f4& v)
+{
+    const Words w = philox(key, step, (uint32_t)(c >> 2), r);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = w.w[e] <= d.last ? 0.f : v[e] * d.scale;
+}
+
+// The epilogue of columns n to n + 3 of row m.
+template <typename T>
+__device__ inline void finish4(const ProductArgs& p, int64_t m, int64_t n, f4 v, const f4& bias)
+{
+    const int have = p.N - n < 4 ? (int)(p.N - n) : 4;
+    v += bias;
+    if (p.pre) store4(static_cast<T*>(p.pre) + m * p.ldp + n, v, p.vec, have);
+    activate4(p.act, v);
+    if (p.drop.rng) drop4(p.drop, (uint64_t)p.drop.rng[0], (uint32_t)p.drop.rng[1], m, n, v);
+    if (p.residual) v += load4(static_cast<const T*>(p.residual) + m * p.ldr + n, p.vec, have);
+    store4(static_cast<T*>(p.y) + m * p.ldy + n, v, p.vec, have);
+}
+
+template <typename T>
+__device__ inline f4 bias4(const ProductArgs& p, int64_t n)
+{
+    f4 b = {0.f, 0.f, 0.f, 0.f};
+    if (p.bias)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (n + e < p.N) b[e] = (float)static_cast<const T*>(p.bias)[n + e];
+    return b;
+}
+
+// Eight elements from memory that is aligned to an element: `have` of them,
+// then zeros.
+template <typename T>
+struct Chunk {  // 16-bit types: as they are; fp32: two halves
+    u4 v[sizeof(T) / 2];
+};
+template <typename T>
+__device__ inline Chunk<T> load_chunk(const T* p, int have)
+{
+    Chunk<T> c;
+    if (have >= 8) {
+        __builtin_memcpy(&c, p, 8 * sizeof(T));
+        return c;
+    }
+    T t[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        t[e] = (T)0.f;
+        if (e < have) t[e] = p[e];
+    }
+    __builtin_memcpy(&c, t, sizeof c);
+    return c;
+}
+
+// A Stage as a type, so that its shape is known when a function is compiled.
+template <int R_, int KT_, bool KM_>
+struct StageOf {
+    static constexpr Stage s{R_, KT_, KM_};
+    static constexpr bool KM = KM_;
+};
+
+constexpr uint32_t NOWHERE = 0x80000000u;  // past every descriptor's end: loads zeros
+
+// Until this wave's direct loads have arrived (vmcnt 0).
+__device__ inline void wait_direct() { __builtin_amdgcn_s_waitcnt(0x0f70); }
+
+// Stages of one operand's tile, from its first row and contraction value.
+template <typename T, typename SO, int NT>
+struct Operand {
+    static constexpr Stage S = SO::s;
+    static constexpr int L = S.slots() / NT;  // slots per thread
+    static_assert(S.slots() % NT == 0, "whole slots");
+    const T* x;
+    int64_t ld;
+    int rows;      // of the tile that exist
+    int64_t vals;  // contraction values that exist
+
+    // Byte offsets of a thread's slots from a stage's start (direct loads).
+    __device__ void offsets(uint32_t (&off)[L], int tid) const
+    {
+#pragma unroll
+        for (int i = 0; i < L; ++i) {
+            const int e = i * NT + tid, r = S.slot_row(e), k = S.slot_k(e);
+            off[i] = r < rows ? (uint32_t)((S.KM ? r * ld + k : k * ld + r) * 2) : NOWHERE;
         }
-        if (p.residual) v += (float)static_cast<const T*>(p.residual)[m * p.ldr + n];
-        static_cast<T*>(p.y)[m * p.ldy + n] = (T)v;
+    }
+    // Stage s straight to LDS; slots past the last value become zeros.  The
+    // loads are inline asm without outputs: as builtins, every transposing read
+    // of LDS, of the other buffer too, waits for all of them.  The caller waits
+    // (wait_direct) before the barrier that makes the stage readable.
+    __device__ void direct(const uint32_t (&off)[L], int s, char* to, int tid, int wave) const
+    {
+        const T* const base = x + (S.KM ? (int64_t)s * S.KT : (int64_t)s * S.KT * ld);
+        const uint64_t address = (uint64_t)base;
+        const u4 d = {(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)address),
+                      (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(address >> 32)) & 0xffffu, 0x7fffffffu,
+                      0x00020000u};
+        const int64_t left = vals - (int64_t)s * S.KT;
+        const uint32_t lds = (uint32_t)(uintptr_t)(lds_void*)to + wave * 1024;
+#pragma unroll
+        for (int i = 0; i < L; ++i) {
+            uint32_t o = off[i];
+            if (left < S.KT && S.slot_k(i * NT + tid) >= (int)left) o = NOWHERE;
+            __asm__ volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+                             :
+                             : "s"(lds + i * NT * 16), "v"(o), "s"(d)
+                             : "memory", "m0");
+        }
+    }
+    // Stage s into registers ...
+    __device__ void fetch(Chunk<T> (&c)[L], int s, int tid) const
+    {
+        const int64_t k1 = (int64_t)s * S.KT;
+        const int left = (int)(vals - k1 < S.KT ? vals - k1 : S.KT);
+#pragma unroll
+        for (int i = 0; i < L; ++i) {
+            const int e = i * NT + tid, r = S.slot_row(e), k = S.slot_k(e);
+            c[i] = load_chunk(x + (S.KM ? r * ld + k1 + k : (k1 + k) * ld + r), S.slot_have(e, rows, left));
+        }
+    }
+    // ... and from there to LDS, fp32 as three planes.
+    static __device__ void store(const Chunk<T> (&c)[L], char* to, int tid)
+    {
+#pragma unroll
+        for (int i = 0; i < L; ++i) {
+            char* const at = to + (i * NT + tid) * 16;
+            if constexpr (sizeof(T) == 4) {
+                u4 t[3];
+#pragma unroll
+                for (int h = 0; h < 4; ++h) {
+                    const f4 v = __builtin_bit_cast(f4, c[i].v[h >> 1]);
+                    const Parts q = split2(v[2 * (h & 1)], v[2 * (h & 1) + 1]);
+#pragma unroll
+                    for (int u = 0; u < 3; ++u) t[u][h] = q.t[u];
+                }
+#pragma unroll
+                for (int u = 0; u < 3; ++u) *reinterpret_cast<u4*>(at + u * S.bytes()) = t[u];
+            } else {
+                *reinterpret_cast<u4*>(at) = c[i].v[0];
+            }
+        }
+    }
+    // The fragment of rows row0 to + 31 and values k to + 15 of a stage in LDS.
+    static __device__ u4 frag(const char* from, int row0, int k, int lane)
+    {
+        if constexpr (SO::KM) {
+            return *reinterpret_cast<const u4*>(from + frag_byte(S, row0, k, lane, 0));
+        } else {
+            typedef __attribute__((address_space(3))) s4 ls4;
+            struct {
+                s4 x, y;
+            } z{__builtin_amdgcn_ds_read_tr16_b64_v4i16((ls4*)(from + frag_byte(S, row0, k, lane, 0))),
+                __builtin_amdgcn_ds_read_tr16_b64_v4i16((ls4*)(from + frag_byte(S, row0, k, lane, 1)))};
+            return __builtin_bit_cast(u4, z);
+        }
+    }
+    // element (r, k), zero outside
+    __device__ float at(int r, int64_t k) const
+    {
+        return r < rows && k < vals ? (float)x[S.KM ? r * ld + k : k * ld + r] : 0.f;
+    }
+};
+
+// BM x BN outputs per workgroup of WR x WC waves; a stage is KT contraction
+// values.  DIRECT: 16-bit operands whose rows are 16-byte aligned and whole
+// chunks go from memory straight to LDS, one stage ahead in the other of two
+// buffers.  Otherwise chunks go through registers, one stage ahead, and fp32
+// ones become three bf16 planes (split.hpp).
+template <typename T, bool AKM, bool BKM, int BM, int BN, int WR, int WC, int KT, bool DIRECT>
+__global__ __launch_bounds__(64 * WR * WC) void product_kernel(ProductArgs p)
+{
+    constexpr bool F32 = sizeof(T) == 4;
+    constexpr int P = F32 ? 3 : 1, NT = 64 * WR * WC, WM = BM / WR, WN = BN / WC, MI = WM / 32, NI = WN / 32;
+    static_assert(!(F32 && DIRECT) && WN == 64, "shape");
+    using A = Operand<T, StageOf<BM, KT, AKM>, NT>;
+    using B = Operand<T, StageOf<BN, KT, BKM>, NT>;
+    constexpr int PA = A::S.bytes(), PB = B::S.bytes(), BUF = P * (PA + PB), KK = KT / 16;
+    extern __shared__ u4 smem4[];
+    char* const smem = reinterpret_cast<char*>(smem4);
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wm = wave / WC * WM, wn = wave % WC * WN;
+
+    const TileId id = tile_of(blockIdx.x, (uint32_t)((p.M + BM - 1) / BM), (uint32_t)((p.N + BN - 1) / BN), p.splits);
+    const int64_t m0 = (int64_t)id.m * BM, n0 = (int64_t)id.n * BN, k0 = id.split * p.k_part;
+    const int64_t kn = p.K - k0 < p.k_part ? p.K - k0 : p.k_part;
+    const int steps = kn > 0 ? (int)((kn + KT - 1) / KT) : 0;
+    const A a{static_cast<const T*>(p.a) + (AKM ? m0 * p.lda + k0 : k0 * p.lda + m0), p.lda,
+              (int)(p.M - m0 < BM ? p.M - m0 : BM), kn};
+    const B b{static_cast<const T*>(p.b) + (BKM ? n0 * p.ldb + k0 : k0 * p.ldb + n0), p.ldb,
+              (int)(p.N - n0 < BN ? p.N - n0 : BN), kn};
+
+    f16v acc[MI][NI];
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+        for (int j = 0; j < NI; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+    u4 fa[2][MI][P], fb[2][NI][P];
+    auto read = [&](int set, const char* buf, int kk) {
+#pragma unroll
+        for (int q = 0; q < P; ++q) {
+#pragma unroll
+            for (int i = 0; i < MI; ++i) fa[set][i][q] = A::frag(buf + q * PA, wm + 32 * i, 16 * kk, lane);
+#pragma unroll
+            for (int j = 0; j < NI; ++j) fb[set][j][q] = B::frag(buf + P * PA + q * PB, wn + 32 * j, 16 * kk, lane);
+        }
+    };
+    // The output's columns are the matrix instruction's rows: a lane's groups of
+    // four accumulators are neighbours in memory.
+    auto multiply = [&](int set) {
+        constexpr int QA[6] = {2, 0, 1, 1, 0, 0}, QB[6] = {0, 2, 1, 0, 1, 0};
+#pragma unroll
+        for (int q = 0; q < (F32 ? 6 : 1); ++q)
+#pragma unroll
+            for (int i = 0; i < MI; ++i)
+#pragma unroll
+                for (int j = 0; j < NI; ++j) {
+                    const u4 &x = fb[set][j][F32 ? QB[q] : 0], &y = fa[set][i][F32 ? QA[q] : 0];
+                    if constexpr (__is_same(T, _Float16))
+                        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
+                            __builtin_bit_cast(h8, x), __builtin_bit_cast(h8, y), acc[i][j], 0, 0, 0);
+                    else
+                        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                            __builtin_bit_cast(b8, x), __builtin_bit_cast(b8, y), acc[i][j], 0, 0, 0);
+                }
+    };
+
+    // Two fragment reads before each product, while there are any.
+    auto interleave = [&] {
+        constexpr int RD = P * (MI * (AKM ? 1 : 2) + NI * (BKM ? 1 : 2)), MF = MI * NI * (F32 ? 6 : 1);
+#pragma unroll
+        for (int i = 0; i < MF; ++i) {
+            if (2 * i < RD) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    };
+
+    if constexpr (DIRECT) {
+        // The wait for a stage and the barrier stand before the last group of
+        // products of the one before it, when that one's fragments have all been
+        // read: the first fragments of the new stage come while those products run.
+        uint32_t offa[A::L], offb[B::L];
+        a.offsets(offa, tid);
+        b.offsets(offb, tid);
+        auto issue = [&](int s) {
+            char* const to = smem + (s & 1) * BUF;
+            a.direct(offa, s, to, tid, wave);
+            b.direct(offb, s, to + PA, tid, wave);
+        };
+        if (steps > 0) issue(0);
+        wait_direct();
+        __syncthreads();
+        if (steps > 1) issue(1);
+        if (steps > 0) read(0, smem, 0);
+        for (int s = 0; s < steps; ++s) {
+            const char* const buf = smem + (s & 1) * BUF;
+#pragma unroll
+            for (int kk = 0; kk + 1 < KK; ++kk) {
+                read((kk + 1) & 1, buf, kk + 1);
+                multiply(kk & 1);
+                interleave();
+            }
+            wait_direct();
+            __syncthreads();
+            if (s + 2 < steps) issue(s + 2);
+            static_assert(KK % 2 == 0, "fragment sets");
+            if (s + 1 < steps) read(0, smem + ((s + 1) & 1) * BUF, 0);
+            multiply(1);
+        }
+    } else {
+        Chunk<T> ca[A::L], cb[B::L];
+        if (steps > 0) {
+            a.fetch(ca, 0, tid);
+            b.fetch(cb, 0, tid);
+        }
+        for (int s = 0; s < steps; ++s) {
+            __syncthreads();
+            A::store(ca, smem, tid);
+            B::store(cb, smem + P * PA, tid);
+            __syncthreads();
+            if (s + 1 < steps) {
+                a.fetch(ca, s + 1, tid);
+                b.fetch(cb, s + 1, tid);
+            }
+#pragma unroll
+            for (int kk = 0; kk < KK; ++kk) {
+                read(kk & 1, smem, kk);
+                multiply(kk & 1);
+            }
+        }
+        if constexpr (F32) {
+            // Sums that are infinite or NaN, or that the parts cannot hold, again
+            // as fp32 products, operands straight from memory (this wave's tile).
+            float z = 0.f;
+#pragma unroll
+            for (int i = 0; i < MI; ++i)
+#pragma unroll
+                for (int j = 0; j < NI; ++j) {
+                    acc[i][j] *= SPLIT_UNSCALE;
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) z = fmaf(acc[i][j][e], 0.f, z);
+                }
+            if (__ballot(z != 0.f)) {
+#pragma unroll
+                for (int i = 0; i < MI; ++i)
+#pragma unroll
+                    for (int j = 0; j < NI; ++j)
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+                for (int64_t k = lane >> 5; k - (lane >> 5) < kn; k += 2) {
+                    float va[MI], vb[NI];
+#pragma unroll
+                    for (int i = 0; i < MI; ++i) va[i] = a.at(wm + 32 * i + (lane & 31), k);
+#pragma unroll
+                    for (int j = 0; j < NI; ++j) vb[j] = b.at(wn + 32 * j + (lane & 31), k);
+#pragma unroll
+                    for (int i = 0; i < MI; ++i)
+#pragma unroll
+                        for (int j = 0; j < NI; ++j)
+                            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(vb[j], va[i], acc[i][j], 0, 0, 0);
+                }
+            }
+        }
+    }
+
+    // Epilogue: 32 rows at a time through LDS, so that 16 lanes hold 64
+    // neighbouring columns of a row.
+    __syncthreads();
+    constexpr int EW = WN + 4;  // floats per row there
+    float* const tile = reinterpret_cast<float*>(smem) + wave * 32 * EW;
+    const int64_t n = n0 + wn + 4 * (lane & 15);
+    const f4 bias = p.splits > 1 ? f4{0.f, 0.f, 0.f, 0.f} : bias4<T>(p, n);
+#pragma unroll
+    for (int i = 0; i < MI; ++i) {
+#pragma unroll
+        for (int j = 0; j < NI; ++j)
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+                *reinterpret_cast<f4*>(tile + (lane & 31) * EW + 32 * j + 8 * g + 4 * (lane >> 5)) =
+                    f4{acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll 1
+        for (int h = 0; h < 8; ++h) {
+            const int r = 4 * h + (lane >> 4);
+            const int64_t m = m0 + wm + 32 * i + r;
+            const f4 v = *reinterpret_cast<const f4*>(tile + r * EW + 4 * (lane & 15));
+            if (m < p.M && n < p.N) {
+                if (p.splits > 1) {
+                    float* const q = p.partial + (id.split * p.M + m) * p.N + n;
+                    if (p.N % 4 == 0)
+                        *reinterpret_cast<f4*>(q) = v;
+                    else
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (n + e < p.N) q[e] = v[e];
+                } else {
+                    finish4<T>(p, m, n, v, bias);
+                }
+            }
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
     }
 }
 
-// g = dropout(dy) f'(pre) into the workspace [M, N].
+// Joins the parts of a split contraction in order and finishes the outputs:
+// one thread per four columns of a row.
 template <typename T>
-__global__ __launch_bounds__(256) void slope_kernel(DenseBackwardArgs a, T* g)
+__global__ __launch_bounds__(256) void join_kernel(ProductArgs p)
 {
-    const int64_t n = a.M * a.N;
-    for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < n; i += gridDim.x * 256ll) {
-        const int64_t r = i / a.N, c = i % a.N;
-        float v = (float)static_cast<const T*>(a.dy)[r * a.lddy + c];
-        if (a.act != CLIFF_ACT_NONE)
-            v *= activate_slope(a.act, (float)static_cast<const T*>(a.pre)[r * a.ldp + c]);
-        if (a.drop.rng) {
-            const Words w = philox((uint64_t)a.drop.rng[0], (uint32_t)a.drop.rng[1], (uint32_t)(c >> 2), r);
-            v = w.w[c & 3] <= a.drop.last ? 0.f : v * a.drop.scale;
+    const int64_t nq = (p.N + 3) / 4, n_all = p.M * nq, plane = p.M * p.N;
+    for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < n_all; i += gridDim.x * 256ll) {
+        const int64_t m = i / nq, n = i % nq * 4;
+        const float* q = p.partial + m * p.N + n;
+        f4 v = {0.f, 0.f, 0.f, 0.f};
+        if (p.N % 4 == 0) {
+#pragma unroll 4
+            for (int s = 0; s < p.splits; ++s) v += *reinterpret_cast<const f4*>(q + s * plane);
+        } else {
+            for (int s = 0; s < p.splits; ++s)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (n + e < p.N) v[e] += q[s * plane + e];
         }
-        g[i] = (T)v;
+        finish4<T>(p, m, n, v, bias4<T>(p, n));
     }
 }
 
+// g = dropout(dy) f'(pre) into g [M, N] (unless NULL), and its column sums over
+// a share of the rows into sums [part][N] (unless NULL).  A workgroup takes 256
+// columns; its four waves every fourth row each.
 template <typename T>
-__global__ __launch_bounds__(64) void bias_kernel(DenseBackwardArgs a)
+__global__ __launch_bounds__(256) void slope_kernel(DenseBackwardArgs a, T* g, float* sums, int64_t rows_per_part,
+                                                    int vec)
 {
-    const int64_t c = blockIdx.x;
+    __shared__ f4 part[4][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t c = blockIdx.x * 256ll + 4 * lane;
+    const int64_t r0 = blockIdx.y * rows_per_part, r1 = r0 + rows_per_part < a.M ? r0 + rows_per_part : a.M;
+    uint64_t key = 0;
+    uint32_t step = 0;
+    if (a.drop.rng) {
+        key = (uint64_t)a.drop.rng[0];
+        step = (uint32_t)a.drop.rng[1];
+    }
+    f4 t = {0.f, 0.f, 0.f, 0.f};
+    const int have = a.N - c < 4 ? (int)(a.N - c) : 4;
+    if (c < a.N) {
+#pragma unroll 2
+        for (int64_t r = r0 + wave; r < r1; r += 4) {
+            f4 v = load4(static_cast<const T*>(a.dy) + r * a.lddy + c, vec, have);
+            if (a.act != CLIFF_ACT_NONE)
+                slope4(a.act, v, load4(static_cast<const T*>(a.pre) + r * a.ldp + c, vec, have));
+            if (a.drop.rng) drop4(a.drop, key, step, r, c, v);
+            if (g) store4(g + r * a.N + c, v, a.N % 4 == 0, have);
+            t += v;
+        }
+    }
+    if (!sums) return;
+    part[wave][lane] = t;
+    __syncthreads();
+    if (wave) return;
+    t = part[0][lane] + part[1][lane] + part[2][lane] + part[3][lane];
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (c + e < a.N) sums[blockIdx.y * a.N + c + e] = t[e];
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void bias_kernel(const float* sums, int parts, int64_t N, T* dbias)
+{
+    const int64_t c = blockIdx.x * 256ll + threadIdx.x;
+    if (c >= N) return;
     float t = 0.f;
-    for (int64_t r = threadIdx.x; r < a.M; r += 64) {
-        float v = (float)static_cast<const T*>(a.dy)[r * a.lddy + c];
-        if (a.act != CLIFF_ACT_NONE)
-            v *= activate_slope(a.act, (float)static_cast<const T*>(a.pre)[r * a.ldp + c]);
-        if (a.drop.rng) {
-            const Words w = philox((uint64_t)a.drop.rng[0], (uint32_t)a.drop.rng[1], (uint32_t)(c >> 2), r);
-            v = w.w[c & 3] <= a.drop.last ? 0.f : v * a.drop.scale;
+    for (int i = 0; i < parts; ++i) t += sums[i * N + c];
+    dbias[c] = (T)t;
+}
+
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// How a product is cut: tiles of 256 x 256 or 128 x 128, and parts of the
+// contraction.
+struct Cut {
+    bool large;
+    int splits;
+    int64_t k_part;
+};
+
+Cut cut(int dtype, int64_t M, int64_t N, int64_t K, bool direct)
+{
+    const int cus = std::max(device_cus(), 1);
+    const int KT = dtype == CLIFF_F32 ? 32 : 64;
+    Cut best{false, 1, 0};
+    double least = 0;
+    for (int large = 0; large <= (direct ? 1 : 0); ++large) {
+        const int B = large ? 256 : 128;
+        const int64_t tiles = ceil_div(M, B) * ceil_div(N, B), steps = std::max<int64_t>(1, ceil_div(K, KT));
+        for (int64_t want = 1; want <= 64 && want <= steps; ++want) {
+            const int64_t per = ceil_div(steps, want), splits = ceil_div(steps, per);
+            if (splits != want) continue;
+            // cycles: of a step with the compute unit to itself, rounds of workgroups
+            const double step = large ? 2700 : dtype == CLIFF_F32 ? 2100 : 760;
+            const int64_t wgs = tiles * splits, slots = large ? cus : 2 * cus;
+            const double share = large ? 1.0 : wgs > cus ? 2.0 : 1.25;
+            double t = (double)ceil_div(wgs, slots) * (share * step * per + (large ? 12000 : 6000));
+            if (splits > 1) t += 6000 + (double)M * N * 4 * (2 * splits) / 2000;
+            if (least == 0 || t < least) {
+                least = t;
+                best = Cut{large != 0, (int)splits, per * KT};
+            }
         }
-        t += v;
     }
-    for (int o = 32; o; o >>= 1) t += __shfl_xor(t, o);
-    if (threadIdx.x == 0) static_cast<T*>(a.dbias)[c] = (T)t;
+    return best;
+}
+
+int64_t partial_bytes(int dtype, int64_t M, int64_t N, int64_t K)
+{
+    int64_t n = 0;
+    for (int direct = 0; direct <= (dtype == CLIFF_F32 ? 0 : 1); ++direct) {
+        const Cut c = cut(dtype, M, N, K, direct != 0);
+        if (c.splits > 1) n = std::max(n, c.splits * M * N * 4);
+    }
+    return ceil_div(n, 256) * 256;
+}
+
+bool aligned_rows(const void* x, int64_t ld, int64_t width)
+{
+    return ((uintptr_t)x & 15) == 0 && ld % 8 == 0 && width % 8 == 0 && ld <= (1 << 21);
 }
 
 template <typename T>
-cliff_status product(const ProductArgs& p, hipStream_t stream)
+int whole_quads(int64_t N, std::initializer_list<std::pair<const void*, int64_t>> ms)
 {
-    const int64_t blocks = (p.M + 31) / 32 * ((p.N + 31) / 32);
-    if (blocks >= (int64_t)1 << 31) return CLIFF_EUNSUPPORTED;
-    hipLaunchKernelGGL(product_kernel<T>, dim3((unsigned)blocks), dim3(256), 0, stream, p);
+    if (N % 4) return 0;
+    for (const auto& m : ms)
+        if (m.first && (((uintptr_t)m.first & (4 * sizeof(T) - 1)) || m.second % 4)) return 0;
+    return 1;
+}
+
+template <typename T, bool AKM, bool BKM, int BM, int BN, int WR, int WC, int KT, bool DIRECT>
+cliff_status run(const ProductArgs& p, hipStream_t stream)
+{
+    constexpr int P = sizeof(T) == 4 ? 3 : 1;
+    constexpr int stage = P * KT * 2 * (BM + BN) * (DIRECT ? 2 : 1), epi = WR * WC * 32 * (BN / WC + 4) * 4;
+    constexpr int lds = stage > epi ? stage : epi;
+    static_assert(lds <= 160 * 1024, "LDS");
+    const int64_t wgs = ceil_div(p.M, BM) * ceil_div(p.N, BN) * p.splits;
+    if (wgs >= (int64_t)1 << 31) return CLIFF_EUNSUPPORTED;
+    const auto k = product_kernel<T, AKM, BKM, BM, BN, WR, WC, KT, DIRECT>;
+    if (debug_enabled())
+        fprintf(stderr, "cliffconv: product %lld x %lld x %lld tile %d x %d x %d%s, %lld workgroups, %d splits\n",
+                (long long)p.M, (long long)p.N, (long long)p.K, BM, BN, KT, DIRECT ? " direct" : "",
+                (long long)wgs, p.splits);
+    hipLaunchKernelGGL(k, dim3((unsigned)wgs), dim3(64 * WR * WC), lds, stream, p);
     return launched();
+}
+
+// A product and, where its contraction is split, the join.
+template <typename T, bool AKM, bool BKM>
+cliff_status product(int dtype, ProductArgs p, hipStream_t stream)
+{
+    const bool direct = sizeof(T) == 2 && aligned_rows(p.a, p.lda, AKM ? p.K : p.M) &&
+                        aligned_rows(p.b, p.ldb, BKM ? p.K : p.N);
+    const Cut c = cut(dtype, p.M, p.N, p.K, direct);
+    p.splits = c.splits;
+    p.k_part = c.k_part;
+    p.vec = whole_quads<T>(p.N, {{p.pre, p.ldp}, {p.residual, p.ldr}, {p.y, p.ldy}});
+    cliff_status s;
+    if constexpr (sizeof(T) == 4) {
+        s = run<T, AKM, BKM, 128, 128, 2, 2, 32, false>(p, stream);
+    } else {
+        if (!direct)
+            s = run<T, AKM, BKM, 128, 128, 2, 2, 64, false>(p, stream);
+        else if (c.large)
+            s = run<T, AKM, BKM, 256, 256, 2, 4, 64, true>(p, stream);
+        else
+            s = run<T, AKM, BKM, 128, 128, 2, 2, 64, true>(p, stream);
+    }
+    if (s != CLIFF_OK || p.splits == 1) return s;
+    const int64_t blocks = std::min<int64_t>(ceil_div(p.M * ceil_div(p.N, 4), 256), 1 << 16);
+    hipLaunchKernelGGL(join_kernel<T>, dim3((unsigned)blocks), dim3(256), 0, stream, p);
+    return launched();
+}
+
+// Workspace of the backward pass: g, the bias's partial sums, partial products.
+struct BackwardSpace {
+    int64_t g, sums, partial, all;
+    int parts;
+};
+BackwardSpace backward_space(int dtype, int64_t M, int64_t K, int64_t N)
+{
+    BackwardSpace w;
+    const int64_t cols = ceil_div(N, 256);
+    w.parts = (int)std::max<int64_t>(1, std::min<int64_t>(ceil_div(M, 16), ceil_div(2048, cols)));
+    w.g = 0;
+    w.sums = ceil_div(M * N * (dtype == CLIFF_F32 ? 4 : 2), 256) * 256;
+    w.partial = w.sums + ceil_div(w.parts * N * 4, 256) * 256;
+    w.all = w.partial + std::max({partial_bytes(dtype, M, K, N), partial_bytes(dtype, K, N, M),
+                                  partial_bytes(dtype, N, K, M)});
+    return w;
 }
 
 }  // namespace
 
-int64_t dense_workspace(int, int64_t, int64_t, int64_t) { return 0; }
-int64_t dense_backward_workspace(int dtype, int64_t M, int64_t, int64_t N)
+int64_t dense_workspace(int dtype, int64_t M, int64_t K, int64_t N) { return partial_bytes(dtype, M, N, K); }
+int64_t dense_backward_workspace(int dtype, int64_t M, int64_t K, int64_t N)
 {
-    return (M * N * (dtype == CLIFF_F32 ? 4 : 2) + 15) / 16 * 16;
+    return backward_space(dtype, M, K, N).all;
 }
 
 cliff_status launch_dense(int dtype, const DenseArgs& a, hipStream_t stream)
 {
     clear_hip_error();
     return with_type(dtype, [&](auto t) {
-        ProductArgs p{a.M, a.K, a.N, a.x, a.ldx, 1, a.w, a.w_out_in ? 1 : a.ldw, a.w_out_in ? a.ldw : 1,
-                      a.bias, a.act, a.drop, a.residual, a.ldr, a.pre, a.ldp, a.y, a.ldy};
-        return product<decltype(t)>(p, stream);
+        using T = decltype(t);
+        ProductArgs p{a.M, a.N, a.K, a.x, a.ldx, a.w, a.ldw, 1, 0, static_cast<float*>(a.workspace),
+                      a.bias, a.act, a.drop, a.residual, a.ldr, a.pre, a.ldp, a.y, a.ldy, 0};
+        return a.w_out_in ? product<T, true, true>(dtype, p, stream) : product<T, true, false>(dtype, p, stream);
     });
 }
 
@@ -134,39 +692,41 @@ cliff_status launch_dense_backward(int dtype, const DenseBackwardArgs& a, hipStr
     clear_hip_error();
     return with_type(dtype, [&](auto t) {
         using T = decltype(t);
-        const void* g = a.dy;
-        int64_t ldg = a.lddy;
-        if (a.M && (a.act != CLIFF_ACT_NONE || a.drop.rng)) {
-            T* gw = static_cast<T*>(a.workspace);
-            const int64_t blocks = std::min<int64_t>((a.M * a.N + 255) / 256, 1 << 20);
-            hipLaunchKernelGGL(slope_kernel<T>, dim3((unsigned)blocks), dim3(256), 0, stream, a, gw);
-            g = gw;
-            ldg = a.N;
-        }
+        const BackwardSpace w = backward_space(dtype, a.M, a.K, a.N);
+        char* const ws = static_cast<char*>(a.workspace);
+        const bool change = a.act != CLIFF_ACT_NONE || a.drop.rng;
+        const void* g = change ? ws + w.g : a.dy;
+        const int64_t ldg = change ? a.N : a.lddy;
+        float* const sums = reinterpret_cast<float*>(ws + w.sums);
+        float* const partial = reinterpret_cast<float*>(ws + w.partial);
         cliff_status s = CLIFF_OK;
-        const DropArgs none{nullptr, 0, 1.f};
-        if (a.dbias) {
-            hipLaunchKernelGGL(bias_kernel<T>, dim3((unsigned)a.N), dim3(64), 0, stream, a);
+        if (a.dbias || (change && (a.dx || a.dw))) {
+            const int vec = whole_quads<T>(a.N, {{a.dy, a.lddy}, {a.pre, a.ldp}});
+            hipLaunchKernelGGL(slope_kernel<T>, dim3((unsigned)ceil_div(a.N, 256), (unsigned)w.parts), dim3(256), 0,
+                               stream, a, change && (a.dx || a.dw) ? reinterpret_cast<T*>(ws + w.g) : nullptr,
+                               a.dbias ? sums : nullptr, ceil_div(a.M, w.parts), vec);
             s = launched();
         }
+        if (s == CLIFF_OK && a.dbias) {
+            hipLaunchKernelGGL(bias_kernel<T>, dim3((unsigned)ceil_div(a.N, 256)), dim3(256), 0, stream, sums,
+                               w.parts, a.N, static_cast<T*>(a.dbias));
+            s = launched();
+        }
+        const DropArgs none{nullptr, 0, 1.f};
+        auto plain = [&](int64_t M, int64_t N, int64_t K, const void* x, int64_t ldx, const void* y, int64_t ldy,
+                         void* out, int64_t ldo) {
+            return ProductArgs{M, N, K, x, ldx, y, ldy, 1, 0, partial, nullptr, CLIFF_ACT_NONE,
+                               none, nullptr, 0, nullptr, 0, out, ldo, 0};
+        };
         if (s == CLIFF_OK && a.dx && a.M) {
-            ProductArgs p{a.M, a.N, a.K, g, ldg, 1, a.w, a.w_out_in ? a.ldw : 1, a.w_out_in ? 1 : a.ldw,
-                          nullptr, CLIFF_ACT_NONE, none, nullptr, 0, nullptr, 0, a.dx, a.lddx};
-            s = product<T>(p, stream);
+            const ProductArgs p = plain(a.M, a.K, a.N, g, ldg, a.w, a.ldw, a.dx, a.lddx);
+            s = a.w_out_in ? product<T, true, false>(dtype, p, stream) : product<T, true, true>(dtype, p, stream);
         }
-        if (s == CLIFF_OK && a.dw) {
-            // in the order of w: [K, N] = x^T g or [N, K] = g^T x
-            ProductArgs p{a.K, a.M, a.N, a.x, 1, a.ldx, g, ldg, 1, nullptr, CLIFF_ACT_NONE, none, nullptr, 0,
-                          nullptr, 0, a.dw, a.lddw};
-            if (a.w_out_in) {
-                std::swap(p.M, p.N);
-                p.a = g;
-                p.ak = ldg;
-                p.b = a.x;
-                p.bk = a.ldx;
-            }
-            s = product<T>(p, stream);
-        }
+        if (s == CLIFF_OK && a.dw)  // in the order of w: [K, N] = x^T g or [N, K] = g^T x
+            s = product<T, false, false>(dtype,
+                                         a.w_out_in ? plain(a.N, a.K, a.M, g, ldg, a.x, a.ldx, a.dw, a.lddw)
+                                                    : plain(a.K, a.N, a.M, a.x, a.ldx, g, ldg, a.dw, a.lddw),
+                                         stream);
         return s;
     });
 }
