@@ -42,7 +42,6 @@ struct ProductArgs {
     int64_t ldp;
     void* y;
     int64_t ldy;
-    int vec;  // whole groups of four columns, aligned to their size, in every one of them
 };
 
 template <typename T>
@@ -50,29 +49,33 @@ struct Vec4 {
     typedef T t __attribute__((ext_vector_type(4)));
 };
 
-// Four neighbouring columns, some of which may not exist (have < 4).
+// Four neighbouring columns, of which some may not exist (have < 4).
 template <typename T>
-__device__ inline f4 load4(const T* p, bool vec, int have)
+__device__ inline f4 load4(const T* p, int have)
 {
-    typedef typename Vec4<T>::t v4;
-    if (vec) return __builtin_convertvector(*reinterpret_cast<const v4*>(p), f4);
-    f4 v = {0.f, 0.f, 0.f, 0.f};
+    typename Vec4<T>::t v;
+    if (have >= 4) {
+        __builtin_memcpy(&v, p, sizeof v);
+    } else {
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-        if (e < have) v[e] = (float)p[e];
-    return v;
+        for (int e = 0; e < 4; ++e) {
+            v[e] = (T)0.f;
+            if (e < have) v[e] = p[e];
+        }
+    }
+    return __builtin_convertvector(v, f4);
 }
 template <typename T>
-__device__ inline void store4(T* p, const f4& v, bool vec, int have)
+__device__ inline void store4(T* p, const f4& v, int have)
 {
-    typedef typename Vec4<T>::t v4;
-    if (vec) {
-        *reinterpret_cast<v4*>(p) = __builtin_convertvector(v, v4);
-        return;
-    }
+    const typename Vec4<T>::t t = __builtin_convertvector(v, typename Vec4<T>::t);
+    if (have >= 4) {
+        __builtin_memcpy(p, &t, sizeof t);
+    } else {
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-        if (e < have) p[e] = (T)v[e];
+        for (int e = 0; e < 4; ++e)
+            if (e < have) p[e] = t[e];
+    }
 }
 
 __device__ inline void activate4(int act, f4& v)
@@ -114,47 +117,25 @@ __device__ inline void finish4(const ProductArgs& p, int64_t m, int64_t n, f4 v,
 {
     const int have = p.N - n < 4 ? (int)(p.N - n) : 4;
     v += bias;
-    if (p.pre) store4(static_cast<T*>(p.pre) + m * p.ldp + n, v, p.vec, have);
+    if (p.pre) store4(static_cast<T*>(p.pre) + m * p.ldp + n, v, have);
     activate4(p.act, v);
     if (p.drop.rng) drop4(p.drop, (uint64_t)p.drop.rng[0], (uint32_t)p.drop.rng[1], m, n, v);
-    if (p.residual) v += load4(static_cast<const T*>(p.residual) + m * p.ldr + n, p.vec, have);
-    store4(static_cast<T*>(p.y) + m * p.ldy + n, v, p.vec, have);
+    if (p.residual) v += load4(static_cast<const T*>(p.residual) + m * p.ldr + n, have);
+    store4(static_cast<T*>(p.y) + m * p.ldy + n, v, have);
 }
 
 template <typename T>
 __device__ inline f4 bias4(const ProductArgs& p, int64_t n)
 {
-    f4 b = {0.f, 0.f, 0.f, 0.f};
-    if (p.bias)
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (n + e < p.N) b[e] = (float)static_cast<const T*>(p.bias)[n + e];
-    return b;
+    if (!p.bias || n >= p.N) return f4{0.f, 0.f, 0.f, 0.f};
+    return load4(static_cast<const T*>(p.bias) + n, p.N - n < 4 ? (int)(p.N - n) : 4);
 }
 
-// Eight elements from memory that is aligned to an element: `have` of them,
-// then zeros.
+// Eight elements in 16-byte pieces (load16): one of a 16-bit type, two of fp32.
 template <typename T>
-struct Chunk {  // 16-bit types: as they are; fp32: two halves
-    u4 v[sizeof(T) / 2];
+struct Chunk {
+    raw16 v[sizeof(T) / 2];
 };
-template <typename T>
-__device__ inline Chunk<T> load_chunk(const T* p, int have)
-{
-    Chunk<T> c;
-    if (have >= 8) {
-        __builtin_memcpy(&c, p, 8 * sizeof(T));
-        return c;
-    }
-    T t[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        t[e] = (T)0.f;
-        if (e < have) t[e] = p[e];
-    }
-    __builtin_memcpy(&c, t, sizeof c);
-    return c;
-}
 
 // A Stage as a type, so that its shape is known when a function is compiled.
 template <int R_, int KT_, bool KM_>
@@ -178,6 +159,7 @@ struct Operand {
     int64_t ld;
     int rows;      // of the tile that exist
     int64_t vals;  // contraction values that exist
+    int64_t width;  // elements of a line of memory up to and with the tile's last
 
     // Byte offsets of a thread's slots from a stage's start (direct loads).
     __device__ void offsets(uint32_t (&off)[L], int tid) const
@@ -219,14 +201,24 @@ struct Operand {
 #pragma unroll
         for (int i = 0; i < L; ++i) {
             const int e = i * NT + tid, r = S.slot_row(e), k = S.slot_k(e);
-            c[i] = load_chunk(x + (S.KM ? r * ld + k1 + k : (k1 + k) * ld + r), S.slot_have(e, rows, left));
+            const int have = S.slot_have(e, rows, left);
+            const T* const p = x + (S.KM ? r * ld + k1 + k : (k1 + k) * ld + r);
+#pragma unroll
+            for (int h = 0; h < (int)sizeof(T) / 2; ++h)
+                c[i].v[h] = load16(p + h * per16<T>, have - h * per16<T>, width);
         }
     }
     // ... and from there to LDS, fp32 as three planes.
-    static __device__ void store(const Chunk<T> (&c)[L], char* to, int tid)
+    __device__ void store(Chunk<T> (&c)[L], int s, char* to, int tid) const
     {
+        const int64_t k1 = (int64_t)s * S.KT;
+        const int left = (int)(vals - k1 < S.KT ? vals - k1 : S.KT);
 #pragma unroll
         for (int i = 0; i < L; ++i) {
+            const int have = S.slot_have(i * NT + tid, rows, left);
+#pragma unroll
+            for (int h = 0; h < (int)sizeof(T) / 2; ++h)
+                settle16<T>(c[i].v[h], have - h * per16<T>, width);
             char* const at = to + (i * NT + tid) * 16;
             if constexpr (sizeof(T) == 4) {
                 u4 t[3];
@@ -290,9 +282,9 @@ __global__ __launch_bounds__(64 * WR * WC) void product_kernel(ProductArgs p)
     const int64_t kn = p.K - k0 < p.k_part ? p.K - k0 : p.k_part;
     const int steps = kn > 0 ? (int)((kn + KT - 1) / KT) : 0;
     const A a{static_cast<const T*>(p.a) + (AKM ? m0 * p.lda + k0 : k0 * p.lda + m0), p.lda,
-              (int)(p.M - m0 < BM ? p.M - m0 : BM), kn};
+              (int)(p.M - m0 < BM ? p.M - m0 : BM), kn, AKM ? k0 + kn : p.M};
     const B b{static_cast<const T*>(p.b) + (BKM ? n0 * p.ldb + k0 : k0 * p.ldb + n0), p.ldb,
-              (int)(p.N - n0 < BN ? p.N - n0 : BN), kn};
+              (int)(p.N - n0 < BN ? p.N - n0 : BN), kn, BKM ? k0 + kn : p.N};
 
     f16v acc[MI][NI];
 #pragma unroll
@@ -382,8 +374,8 @@ __global__ __launch_bounds__(64 * WR * WC) void product_kernel(ProductArgs p)
         }
         for (int s = 0; s < steps; ++s) {
             __syncthreads();
-            A::store(ca, smem, tid);
-            B::store(cb, smem + P * PA, tid);
+            a.store(ca, s, smem, tid);
+            b.store(cb, s, smem + P * PA, tid);
             __syncthreads();
             if (s + 1 < steps) {
                 a.fetch(ca, s + 1, tid);
@@ -454,13 +446,7 @@ __global__ __launch_bounds__(64 * WR * WC) void product_kernel(ProductArgs p)
             const f4 v = *reinterpret_cast<const f4*>(tile + r * EW + 4 * (lane & 15));
             if (m < p.M && n < p.N) {
                 if (p.splits > 1) {
-                    float* const q = p.partial + (id.split * p.M + m) * p.N + n;
-                    if (p.N % 4 == 0)
-                        *reinterpret_cast<f4*>(q) = v;
-                    else
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            if (n + e < p.N) q[e] = v[e];
+                    store4(p.partial + (id.split * p.M + m) * p.N + n, v, p.N - n < 4 ? (int)(p.N - n) : 4);
                 } else {
                     finish4<T>(p, m, n, v, bias);
                 }
@@ -480,16 +466,10 @@ __global__ __launch_bounds__(256) void join_kernel(ProductArgs p)
     for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < n_all; i += gridDim.x * 256ll) {
         const int64_t m = i / nq, n = i % nq * 4;
         const float* q = p.partial + m * p.N + n;
+        const int have = p.N - n < 4 ? (int)(p.N - n) : 4;
         f4 v = {0.f, 0.f, 0.f, 0.f};
-        if (p.N % 4 == 0) {
 #pragma unroll 4
-            for (int s = 0; s < p.splits; ++s) v += *reinterpret_cast<const f4*>(q + s * plane);
-        } else {
-            for (int s = 0; s < p.splits; ++s)
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (n + e < p.N) v[e] += q[s * plane + e];
-        }
+        for (int s = 0; s < p.splits; ++s) v += load4(q + s * plane, have);
         finish4<T>(p, m, n, v, bias4<T>(p, n));
     }
 }
@@ -498,8 +478,7 @@ __global__ __launch_bounds__(256) void join_kernel(ProductArgs p)
 // a share of the rows into sums [part][N] (unless NULL).  A workgroup takes 256
 // columns; its four waves every fourth row each.
 template <typename T>
-__global__ __launch_bounds__(256) void slope_kernel(DenseBackwardArgs a, T* g, float* sums, int64_t rows_per_part,
-                                                    int vec)
+__global__ __launch_bounds__(256) void slope_kernel(DenseBackwardArgs a, T* g, float* sums, int64_t rows_per_part)
 {
     __shared__ f4 part[4][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -514,13 +493,13 @@ __global__ __launch_bounds__(256) void slope_kernel(DenseBackwardArgs a, T* g, f
     f4 t = {0.f, 0.f, 0.f, 0.f};
     const int have = a.N - c < 4 ? (int)(a.N - c) : 4;
     if (c < a.N) {
-#pragma unroll 2
+#pragma unroll 4
         for (int64_t r = r0 + wave; r < r1; r += 4) {
-            f4 v = load4(static_cast<const T*>(a.dy) + r * a.lddy + c, vec, have);
+            f4 v = load4(static_cast<const T*>(a.dy) + r * a.lddy + c, have);
             if (a.act != CLIFF_ACT_NONE)
-                slope4(a.act, v, load4(static_cast<const T*>(a.pre) + r * a.ldp + c, vec, have));
+                slope4(a.act, v, load4(static_cast<const T*>(a.pre) + r * a.ldp + c, have));
             if (a.drop.rng) drop4(a.drop, key, step, r, c, v);
-            if (g) store4(g + r * a.N + c, v, a.N % 4 == 0, have);
+            if (g) store4(g + r * a.N + c, v, have);
             t += v;
         }
     }
@@ -534,13 +513,24 @@ __global__ __launch_bounds__(256) void slope_kernel(DenseBackwardArgs a, T* g, f
         if (c + e < a.N) sums[blockIdx.y * a.N + c + e] = t[e];
 }
 
+// Joins the parts [part][N] in a fixed order: 64 columns per workgroup, every
+// 16th part per wave.
 template <typename T>
-__global__ __launch_bounds__(256) void bias_kernel(const float* sums, int parts, int64_t N, T* dbias)
+__global__ __launch_bounds__(1024) void bias_kernel(const float* sums, int parts, int64_t N, T* dbias)
 {
-    const int64_t c = blockIdx.x * 256ll + threadIdx.x;
-    if (c >= N) return;
+    __shared__ float s[16][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t c = blockIdx.x * 64ll + lane;
     float t = 0.f;
-    for (int i = 0; i < parts; ++i) t += sums[i * N + c];
+    if (c < N) {
+#pragma unroll 8
+        for (int i = wave; i < parts; i += 16) t += sums[i * N + c];
+    }
+    s[wave][lane] = t;
+    __syncthreads();
+    if (wave || c >= N) return;
+    t = 0.f;
+    for (int i = 0; i < 16; ++i) t += s[i][lane];
     dbias[c] = (T)t;
 }
 
@@ -596,15 +586,6 @@ bool aligned_rows(const void* x, int64_t ld, int64_t width)
     return ((uintptr_t)x & 15) == 0 && ld % 8 == 0 && width % 8 == 0 && ld <= (1 << 21);
 }
 
-template <typename T>
-int whole_quads(int64_t N, std::initializer_list<std::pair<const void*, int64_t>> ms)
-{
-    if (N % 4) return 0;
-    for (const auto& m : ms)
-        if (m.first && (((uintptr_t)m.first & (4 * sizeof(T) - 1)) || m.second % 4)) return 0;
-    return 1;
-}
-
 template <typename T, bool AKM, bool BKM, int BM, int BN, int WR, int WC, int KT, bool DIRECT>
 cliff_status run(const ProductArgs& p, hipStream_t stream)
 {
@@ -632,7 +613,6 @@ cliff_status product(int dtype, ProductArgs p, hipStream_t stream)
     const Cut c = cut(dtype, p.M, p.N, p.K, direct);
     p.splits = c.splits;
     p.k_part = c.k_part;
-    p.vec = whole_quads<T>(p.N, {{p.pre, p.ldp}, {p.residual, p.ldr}, {p.y, p.ldy}});
     cliff_status s;
     if constexpr (sizeof(T) == 4) {
         s = run<T, AKM, BKM, 128, 128, 2, 2, 32, false>(p, stream);
@@ -682,7 +662,7 @@ cliff_status launch_dense(int dtype, const DenseArgs& a, hipStream_t stream)
     return with_type(dtype, [&](auto t) {
         using T = decltype(t);
         ProductArgs p{a.M, a.N, a.K, a.x, a.ldx, a.w, a.ldw, 1, 0, static_cast<float*>(a.workspace),
-                      a.bias, a.act, a.drop, a.residual, a.ldr, a.pre, a.ldp, a.y, a.ldy, 0};
+                      a.bias, a.act, a.drop, a.residual, a.ldr, a.pre, a.ldp, a.y, a.ldy};
         return a.w_out_in ? product<T, true, true>(dtype, p, stream) : product<T, true, false>(dtype, p, stream);
     });
 }
@@ -701,14 +681,13 @@ cliff_status launch_dense_backward(int dtype, const DenseBackwardArgs& a, hipStr
         float* const partial = reinterpret_cast<float*>(ws + w.partial);
         cliff_status s = CLIFF_OK;
         if (a.dbias || (change && (a.dx || a.dw))) {
-            const int vec = whole_quads<T>(a.N, {{a.dy, a.lddy}, {a.pre, a.ldp}});
             hipLaunchKernelGGL(slope_kernel<T>, dim3((unsigned)ceil_div(a.N, 256), (unsigned)w.parts), dim3(256), 0,
                                stream, a, change && (a.dx || a.dw) ? reinterpret_cast<T*>(ws + w.g) : nullptr,
-                               a.dbias ? sums : nullptr, ceil_div(a.M, w.parts), vec);
+                               a.dbias ? sums : nullptr, ceil_div(a.M, w.parts));
             s = launched();
         }
         if (s == CLIFF_OK && a.dbias) {
-            hipLaunchKernelGGL(bias_kernel<T>, dim3((unsigned)ceil_div(a.N, 256)), dim3(256), 0, stream, sums,
+            hipLaunchKernelGGL(bias_kernel<T>, dim3((unsigned)ceil_div(a.N, 64)), dim3(1024), 0, stream, sums,
                                w.parts, a.N, static_cast<T*>(a.dbias));
             s = launched();
         }
@@ -716,7 +695,7 @@ cliff_status launch_dense_backward(int dtype, const DenseBackwardArgs& a, hipStr
         auto plain = [&](int64_t M, int64_t N, int64_t K, const void* x, int64_t ldx, const void* y, int64_t ldy,
                          void* out, int64_t ldo) {
             return ProductArgs{M, N, K, x, ldx, y, ldy, 1, 0, partial, nullptr, CLIFF_ACT_NONE,
-                               none, nullptr, 0, nullptr, 0, out, ldo, 0};
+                               none, nullptr, 0, nullptr, 0, out, ldo};
         };
         if (s == CLIFF_OK && a.dx && a.M) {
             const ProductArgs p = plain(a.M, a.K, a.N, g, ldg, a.w, a.ldw, a.dx, a.lddx);

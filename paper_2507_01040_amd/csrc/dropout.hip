@@ -35,12 +35,13 @@ __global__ __launch_bounds__(256) void dropout_kernel(DropoutArgs a, uint32_t pi
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) {
         const int h = r0 + r < a.rows ? have : 0;
-        x[r] = load16(static_cast<const T*>(a.x) + (r0 + r) * a.ldx + col, h);
-        if (a.residual) res[r] = load16(static_cast<const T*>(a.residual) + (r0 + r) * a.ldr + col, h);
+        x[r] = load16(static_cast<const T*>(a.x) + (r0 + r) * a.ldx + col, h, a.d);
+        if (a.residual) res[r] = load16(static_cast<const T*>(a.residual) + (r0 + r) * a.ldr + col, h, a.d);
     }
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) {
         float v[E], u[E];
+        settle16<T>(x[r], have, a.d);
         unpack16<T>(x[r], v);
         if (a.drop.rng)
 #pragma unroll
@@ -51,6 +52,7 @@ __global__ __launch_bounds__(256) void dropout_kernel(DropoutArgs a, uint32_t pi
                     v[4 * q + e] = w.w[e] <= a.drop.last ? 0.f : v[4 * q + e] * a.drop.scale;
             }
         if (a.residual) {
+            settle16<T>(res[r], have, a.d);
             unpack16<T>(res[r], u);
 #pragma unroll
             for (int e = 0; e < E; ++e) v[e] += u[e];

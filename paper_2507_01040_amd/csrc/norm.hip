@@ -16,6 +16,24 @@ namespace {
 
 constexpr int wg_threads(int TPR) { return TPR > 256 ? TPR : 256; }
 
+template <typename T, int TPR, int R, int C>
+__device__ inline void settle_rows(raw16 (&x)[R][C], int t, int64_t d)
+{
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int c = 0; c < C; ++c) settle16<T>(x[r][c], (int)d - (c * TPR + t) * per16<T>, d);
+}
+
+// The elements of a vector [d] from column col on.
+template <typename T>
+__device__ inline void load_vector(const T* v, int col, int64_t d, float* to)
+{
+    raw16 r = load16(v + col, (int)d - col, d);
+    settle16<T>(r, (int)d - col, d);
+    unpack16<T>(r, to);
+}
+
 // Rows per workgroup and pass: wg_threads / TPR groups of R.
 template <typename T, int TPR, int EL, int R>
 __global__ __launch_bounds__(wg_threads(TPR)) void norm_kernel(NormArgs a)
@@ -35,8 +53,9 @@ __global__ __launch_bounds__(wg_threads(TPR)) void norm_kernel(NormArgs a)
             for (int c = 0; c < C; ++c) {
                 const int col = (c * TPR + t) * E;
                 x[r][c] = load16(static_cast<const T*>(a.x) + (rg + r) * a.ldx + col,
-                                 rg + r < a.rows ? (int)a.d - col : 0);
+                                 rg + r < a.rows ? (int)a.d - col : 0, a.d);
             }
+        settle_rows<T, TPR, R, C>(x, t, a.d);
         float mean[R], sq[R];
 #pragma unroll
         for (int r = 0; r < R; ++r) {
@@ -79,8 +98,8 @@ __global__ __launch_bounds__(wg_threads(TPR)) void norm_kernel(NormArgs a)
         for (int c = 0; c < C; ++c) {
             const int col = (c * TPR + t) * E, have = (int)a.d - col;
             float vw[E], vb[E];
-            if (w) unpack16<T>(load16(w + col, have), vw);
-            if (b) unpack16<T>(load16(b + col, have), vb);
+            if (w) load_vector(w, col, a.d, vw);
+            if (b) load_vector(b, col, a.d, vb);
 #pragma unroll
             for (int r = 0; r < R; ++r) {
                 float v[E];
@@ -126,25 +145,24 @@ __global__ __launch_bounds__(wg_threads(TPR), 2) void norm_backward_kernel(NormB
 #pragma unroll
             for (int c = 0; c < C; ++c) {
                 const int col = (c * TPR + t) * E, have = row ? (int)a.d - col : 0;
-                x[r][c] = load16(static_cast<const T*>(a.x) + (rg + r) * a.ldx + col, have);
-                dy[r][c] = load16(static_cast<const T*>(a.dy) + (rg + r) * a.lddy + col, have);
+                x[r][c] = load16(static_cast<const T*>(a.x) + (rg + r) * a.ldx + col, have, a.d);
+                dy[r][c] = load16(static_cast<const T*>(a.dy) + (rg + r) * a.lddy + col, have, a.d);
                 if (a.dresidual)
-                    res[r][c] = load16(static_cast<const T*>(a.dresidual) + (rg + r) * a.ldr + col, have);
+                    res[r][c] = load16(static_cast<const T*>(a.dresidual) + (rg + r) * a.ldr + col, have, a.d);
             }
         }
+        settle_rows<T, TPR, R, C>(x, t, a.d);
+        settle_rows<T, TPR, R, C>(dy, t, a.d);
+        if (a.dresidual) settle_rows<T, TPR, R, C>(res, t, a.d);
         // sums of q and of q h; elements that do not exist are zeros
         float s[2 * R];
 #pragma unroll
         for (int r = 0; r < R; ++r) s[2 * r] = s[2 * r + 1] = 0.f;
-        raw16 vw[C];
 #pragma unroll
         for (int c = 0; c < C; ++c) {
             const int col = (c * TPR + t) * E;
             float wf[E];
-            if (w) {
-                vw[c] = load16(w + col, (int)a.d - col);
-                unpack16<T>(vw[c], wf);
-            }
+            if (w) load_vector(w, col, a.d, wf);
 #pragma unroll
             for (int r = 0; r < R; ++r) {
                 float xv[E], dv[E];
@@ -165,7 +183,7 @@ __global__ __launch_bounds__(wg_threads(TPR), 2) void norm_backward_kernel(NormB
         for (int c = 0; c < C; ++c) {
             const int col = (c * TPR + t) * E, have = (int)a.d - col;
             float wf[E];
-            if (w) unpack16<T>(vw[c], wf);
+            if (w) load_vector(w, col, a.d, wf);
 #pragma unroll
             for (int r = 0; r < R; ++r) {
                 float xv[E], dv[E], v[E];
@@ -329,7 +347,7 @@ bool with_spread(int64_t d, F&& f)
     else if (d <= 64 * 16) f.template operator()<64, 16, 2>();
     else if (d <= 256 * 8) f.template operator()<256, 8, 4>();
     else if (d <= 256 * 16) f.template operator()<256, 16, 2>();
-    else if (d <= 256 * 32) f.template operator()<256, 32, 1>();
+    else if (d <= 512 * 16) f.template operator()<512, 16, 1>();
     else if constexpr (BACKWARD) return false;
     else if (d <= 1024 * 16) f.template operator()<1024, 16, 1>();
     else return false;

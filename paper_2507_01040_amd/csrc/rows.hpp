@@ -6,32 +6,6 @@
 
 namespace cliff {
 
-typedef uint32_t raw16 __attribute__((ext_vector_type(4)));  // 16 bytes of a row
-
-template <typename T>
-constexpr int per16 = 16 / (int)sizeof(T);  // elements in them
-
-// The elements from p on, as far as they exist (`have` of them; zeros then).
-// p is aligned to an element only.
-template <typename T>
-__device__ inline raw16 load16(const T* p, int have)
-{
-    constexpr int E = per16<T>;
-    raw16 r = {0, 0, 0, 0};
-    if (have >= E) {
-        __builtin_memcpy(&r, p, 16);
-    } else if (have > 0) {
-        T t[E];
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-            t[e] = (T)0.f;
-            if (e < have) t[e] = p[e];
-        }
-        __builtin_memcpy(&r, t, 16);
-    }
-    return r;
-}
-
 template <typename T>
 __device__ inline void unpack16(const raw16& r, float* v)
 {
