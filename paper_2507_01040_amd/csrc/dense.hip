@@ -5,6 +5,7 @@
 #include <stdio.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "dense_geom.hpp"
 #include "ff_common.hpp"
@@ -170,55 +171,71 @@ struct Operand {
             off[i] = r < rows ? (uint32_t)((S.KM ? r * ld + k : k * ld + r) * 2) : NOWHERE;
         }
     }
-    // Stage s straight to LDS; slots past the last value become zeros.  The
-    // loads are inline asm without outputs: as builtins, every transposing read
-    // of LDS, of the other buffer too, waits for all of them.  The caller waits
-    // (wait_direct) before the barrier that makes the stage readable.
-    __device__ void direct(const uint32_t (&off)[L], int s, char* to, int tid, int wave) const
+    // Piece i of L of stage s straight to LDS; slots past the last value become
+    // zeros.  The load is inline asm without outputs: as a builtin, every
+    // transposing read of LDS, of the other buffer too, waits for all of them.
+    // The caller waits (wait_direct) before the barrier that makes the stage
+    // readable.
+    __device__ void direct(uint32_t off, int i, int s, char* to, int tid, int wave) const
     {
-        const T* const base = x + (S.KM ? (int64_t)s * S.KT : (int64_t)s * S.KT * ld);
-        const uint64_t address = (uint64_t)base;
+        const uint64_t address = (uint64_t)(x + (S.KM ? (int64_t)s * S.KT : (int64_t)s * S.KT * ld));
         const u4 d = {(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)address),
                       (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(address >> 32)) & 0xffffu, 0x7fffffffu,
                       0x00020000u};
-        const int64_t left = vals - (int64_t)s * S.KT;
-        const uint32_t lds = (uint32_t)(uintptr_t)(lds_void*)to + wave * 1024;
-#pragma unroll
-        for (int i = 0; i < L; ++i) {
-            uint32_t o = off[i];
-            if (left < S.KT && S.slot_k(i * NT + tid) >= (int)left) o = NOWHERE;
-            __asm__ volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
-                             :
-                             : "s"(lds + i * NT * 16), "v"(o), "s"(d)
-                             : "memory", "m0");
-        }
+        const int n = left(s);
+        if (n < S.KT && S.slot_k(i * NT + tid) >= n) off = NOWHERE;
+        __asm__ volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+                         :
+                         : "s"((uint32_t)(uintptr_t)(lds_void*)to + wave * 1024 + i * NT * 16), "v"(off), "s"(d)
+                         : "memory", "m0");
     }
-    // Stage s into registers ...
-    __device__ void fetch(Chunk<T> (&c)[L], int s, int tid) const
+    __device__ int left(int s) const  // of a stage's values, those that exist
     {
-        const int64_t k1 = (int64_t)s * S.KT;
-        const int left = (int)(vals - k1 < S.KT ? vals - k1 : S.KT);
+        const int64_t n = vals - (int64_t)s * S.KT;
+        return n < S.KT ? (int)n : S.KT;
+    }
+    // A thread's slots of the first stage (loads through registers); the next
+    // stage's are `advance` elements on.
+    __device__ void pointers(const T* (&at)[L], int tid) const
+    {
 #pragma unroll
         for (int i = 0; i < L; ++i) {
             const int e = i * NT + tid, r = S.slot_row(e), k = S.slot_k(e);
-            const int have = S.slot_have(e, rows, left);
-            const T* const p = x + (S.KM ? r * ld + k1 + k : (k1 + k) * ld + r);
+            at[i] = x + (S.KM ? r * ld + k : k * ld + r);
+        }
+    }
+    __device__ int64_t advance() const { return S.KM ? S.KT : S.KT * ld; }
+    // Stage s into registers ...
+    __device__ void fetch(Chunk<T> (&c)[L], const T* (&at)[L], int s, int tid) const
+    {
+        const int n = left(s);
 #pragma unroll
-            for (int h = 0; h < (int)sizeof(T) / 2; ++h)
-                c[i].v[h] = load16(p + h * per16<T>, have - h * per16<T>, width);
+        for (int i = 0; i < L; ++i) {
+            if (n == S.KT && rows == S.R) {
+                __builtin_memcpy(&c[i], at[i], sizeof c[i]);
+            } else {
+                const int have = S.slot_have(i * NT + tid, rows, n);
+#pragma unroll
+                for (int h = 0; h < (int)sizeof(T) / 2; ++h)
+                    c[i].v[h] = load16(at[i] + h * per16<T>, have - h * per16<T>, width);
+            }
+            at[i] += advance();
         }
     }
     // ... and from there to LDS, fp32 as three planes.
     __device__ void store(Chunk<T> (&c)[L], int s, char* to, int tid) const
     {
-        const int64_t k1 = (int64_t)s * S.KT;
-        const int left = (int)(vals - k1 < S.KT ? vals - k1 : S.KT);
+        const int n = left(s);
+        if (n < S.KT || rows < S.R)
+#pragma unroll
+            for (int i = 0; i < L; ++i) {
+                const int have = S.slot_have(i * NT + tid, rows, n);
+#pragma unroll
+                for (int h = 0; h < (int)sizeof(T) / 2; ++h)
+                    settle16<T>(c[i].v[h], have - h * per16<T>, width);
+            }
 #pragma unroll
         for (int i = 0; i < L; ++i) {
-            const int have = S.slot_have(i * NT + tid, rows, left);
-#pragma unroll
-            for (int h = 0; h < (int)sizeof(T) / 2; ++h)
-                settle16<T>(c[i].v[h], have - h * per16<T>, width);
             char* const at = to + (i * NT + tid) * 16;
             if constexpr (sizeof(T) == 4) {
                 u4 t[3];
@@ -267,7 +284,7 @@ __global__ __launch_bounds__(64 * WR * WC) void product_kernel(ProductArgs p)
 {
     constexpr bool F32 = sizeof(T) == 4;
     constexpr int P = F32 ? 3 : 1, NT = 64 * WR * WC, WM = BM / WR, WN = BN / WC, MI = WM / 32, NI = WN / 32;
-    static_assert(!(F32 && DIRECT) && WN == 64, "shape");
+    static_assert(!(F32 && DIRECT) && WN % 64 == 0, "shape");
     using A = Operand<T, StageOf<BM, KT, AKM>, NT>;
     using B = Operand<T, StageOf<BN, KT, BKM>, NT>;
     constexpr int PA = A::S.bytes(), PB = B::S.bytes(), BUF = P * (PA + PB), KK = KT / 16;
@@ -294,83 +311,117 @@ __global__ __launch_bounds__(64 * WR * WC) void product_kernel(ProductArgs p)
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
     u4 fa[2][MI][P], fb[2][NI][P];
+    auto read_one = [&](int set, const char* buf, int kk, int f) {  // columns' fragments first
+#pragma unroll
+        for (int q = 0; q < P; ++q)
+            if (f < NI) fb[set][f][q] = B::frag(buf + P * PA + q * PB, wn + 32 * f, 16 * kk, lane);
+            else fa[set][f - NI][q] = A::frag(buf + q * PA, wm + 32 * (f - NI), 16 * kk, lane);
+    };
     auto read = [&](int set, const char* buf, int kk) {
 #pragma unroll
-        for (int q = 0; q < P; ++q) {
-#pragma unroll
-            for (int i = 0; i < MI; ++i) fa[set][i][q] = A::frag(buf + q * PA, wm + 32 * i, 16 * kk, lane);
-#pragma unroll
-            for (int j = 0; j < NI; ++j) fb[set][j][q] = B::frag(buf + P * PA + q * PB, wn + 32 * j, 16 * kk, lane);
-        }
+        for (int f = 0; f < MI + NI; ++f) read_one(set, buf, kk, f);
     };
     // The output's columns are the matrix instruction's rows: a lane's groups of
     // four accumulators are neighbours in memory.
-    auto multiply = [&](int set) {
+    auto multiply_row = [&](int set, int i) {
         constexpr int QA[6] = {2, 0, 1, 1, 0, 0}, QB[6] = {0, 2, 1, 0, 1, 0};
 #pragma unroll
         for (int q = 0; q < (F32 ? 6 : 1); ++q)
 #pragma unroll
-            for (int i = 0; i < MI; ++i)
-#pragma unroll
-                for (int j = 0; j < NI; ++j) {
-                    const u4 &x = fb[set][j][F32 ? QB[q] : 0], &y = fa[set][i][F32 ? QA[q] : 0];
-                    if constexpr (__is_same(T, _Float16))
-                        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
-                            __builtin_bit_cast(h8, x), __builtin_bit_cast(h8, y), acc[i][j], 0, 0, 0);
-                    else
-                        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                            __builtin_bit_cast(b8, x), __builtin_bit_cast(b8, y), acc[i][j], 0, 0, 0);
-                }
+            for (int j = 0; j < NI; ++j) {
+                const u4 &x = fb[set][j][F32 ? QB[q] : 0], &y = fa[set][i][F32 ? QA[q] : 0];
+                if constexpr (__is_same(T, _Float16))
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
+                        __builtin_bit_cast(h8, x), __builtin_bit_cast(h8, y), acc[i][j], 0, 0, 0);
+                else
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                        __builtin_bit_cast(b8, x), __builtin_bit_cast(b8, y), acc[i][j], 0, 0, 0);
+            }
     };
-
-    // Two fragment reads before each product, while there are any.
-    auto interleave = [&] {
-        constexpr int RD = P * (MI * (AKM ? 1 : 2) + NI * (BKM ? 1 : 2)), MF = MI * NI * (F32 ? 6 : 1);
+    auto multiply = [&](int set) {
 #pragma unroll
-        for (int i = 0; i < MF; ++i) {
-            if (2 * i < RD) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
-            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-        }
-        __builtin_amdgcn_sched_barrier(0);
+        for (int i = 0; i < MI; ++i) multiply_row(set, i);
     };
 
     if constexpr (DIRECT) {
         // The wait for a stage and the barrier stand before the last group of
         // products of the one before it, when that one's fragments have all been
         // read: the first fragments of the new stage come while those products run.
+        // The loads of a stage are spread over the products of two groups (all at
+        // once they keep the waves from their products for a third of the step).
+        static_assert(KK % 2 == 0 && A::L == B::L && A::L % MI == 0, "groups");
         uint32_t offa[A::L], offb[B::L];
         a.offsets(offa, tid);
         b.offsets(offb, tid);
-        auto issue = [&](int s) {
-            char* const to = smem + (s & 1) * BUF;
-            a.direct(offa, s, to, tid, wave);
-            b.direct(offb, s, to + PA, tid, wave);
-        };
-        if (steps > 0) issue(0);
-        wait_direct();
-        __syncthreads();
-        if (steps > 1) issue(1);
-        if (steps > 0) read(0, smem, 0);
-        for (int s = 0; s < steps; ++s) {
-            const char* const buf = smem + (s & 1) * BUF;
+        auto load_a = [&](int s, int i) { a.direct(offa[i], i, s, smem + (s & 1) * BUF, tid, wave); };
+        auto load_b = [&](int s, int i) { b.direct(offb[i], i, s, smem + (s & 1) * BUF + PA, tid, wave); };
+        // Products of a group of 16 values, with the reads of the next one's
+        // fragments (next: its buffer) and half of the loads of a stage.
+        auto group = [&](int set, const char* next, int kk, auto loads) {
+            constexpr int F = MI + NI;
 #pragma unroll
-            for (int kk = 0; kk + 1 < KK; ++kk) {
-                read((kk + 1) & 1, buf, kk + 1);
-                multiply(kk & 1);
-                interleave();
+            for (int i = 0; i < MI; ++i) {
+#pragma unroll
+                for (int f = i * F / MI; f < (i + 1) * F / MI; ++f)
+                    read_one(set ^ 1, next, kk, f);
+                multiply_row(set, i);
+#pragma unroll
+                for (int l = i * A::L / MI; l < (i + 1) * A::L / MI; ++l) loads(l);
+                __builtin_amdgcn_sched_barrier(0);
             }
+        };
+        auto nothing = [](int) {};
+        if (steps > 0) {
+#pragma unroll
+            for (int i = 0; i < A::L; ++i) load_a(0, i);
+#pragma unroll
+            for (int i = 0; i < B::L; ++i) load_b(0, i);
             wait_direct();
             __syncthreads();
-            if (s + 2 < steps) issue(s + 2);
-            static_assert(KK % 2 == 0, "fragment sets");
-            if (s + 1 < steps) read(0, smem + ((s + 1) & 1) * BUF, 0);
-            multiply(1);
+            if (steps > 1)
+#pragma unroll
+                for (int i = 0; i < A::L; ++i) load_a(1, i);
+            read(0, smem, 0);
         }
+        // Step s; whether there are one and two more.
+        auto step = [&](int s, auto one, auto two) {
+            const char* const buf = smem + (s & 1) * BUF;
+            group(0, buf, 1, [&](int i) {
+                if constexpr (one) load_b(s + 1, i);
+            });
+#pragma unroll
+            for (int kk = 1; kk + 1 < KK; ++kk) group(kk & 1, buf, kk + 1, nothing);
+            wait_direct();
+            __syncthreads();
+            // (the last step reads what no product uses)
+            group(1, smem + ((s + 1) & 1) * BUF, 0, [&](int i) {
+                if constexpr (two) load_a(s + 2, i);
+            });
+        };
+        constexpr std::true_type yes;
+        constexpr std::false_type no;
+        int s = 0;
+        for (; s + 2 < steps; ++s) step(s, yes, yes);
+        if (s + 1 < steps) step(s++, yes, no);
+        if (s < steps) step(s, no, no);
     } else {
+        // Two fragment reads before each product, while there are any.
+        auto interleave = [&](bool reads) {
+            constexpr int RD = P * (MI * (AKM ? 1 : 2) + NI * (BKM ? 1 : 2)), MF = MI * NI * (F32 ? 6 : 1);
+#pragma unroll
+            for (int i = 0; i < MF; ++i) {
+                if (reads && 2 * i < RD) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        };
         Chunk<T> ca[A::L], cb[B::L];
+        const T *ata[A::L], *atb[B::L];
+        a.pointers(ata, tid);
+        b.pointers(atb, tid);
         if (steps > 0) {
-            a.fetch(ca, 0, tid);
-            b.fetch(cb, 0, tid);
+            a.fetch(ca, ata, 0, tid);
+            b.fetch(cb, atb, 0, tid);
         }
         for (int s = 0; s < steps; ++s) {
             __syncthreads();
@@ -378,13 +429,15 @@ __global__ __launch_bounds__(64 * WR * WC) void product_kernel(ProductArgs p)
             b.store(cb, s, smem + P * PA, tid);
             __syncthreads();
             if (s + 1 < steps) {
-                a.fetch(ca, s + 1, tid);
-                b.fetch(cb, s + 1, tid);
+                a.fetch(ca, ata, s + 1, tid);
+                b.fetch(cb, atb, s + 1, tid);
             }
+            read(0, smem, 0);
 #pragma unroll
             for (int kk = 0; kk < KK; ++kk) {
-                read(kk & 1, smem, kk);
+                if (kk + 1 < KK) read((kk + 1) & 1, smem, kk + 1);
                 multiply(kk & 1);
+                interleave(kk + 1 < KK);
             }
         }
         if constexpr (F32) {
@@ -425,35 +478,39 @@ __global__ __launch_bounds__(64 * WR * WC) void product_kernel(ProductArgs p)
     // Epilogue: 32 rows at a time through LDS, so that 16 lanes hold 64
     // neighbouring columns of a row.
     __syncthreads();
-    constexpr int EW = WN + 4;  // floats per row there
+    constexpr int EW = 64 + 4;  // floats per row there
     float* const tile = reinterpret_cast<float*>(smem) + wave * 32 * EW;
-    const int64_t n = n0 + wn + 4 * (lane & 15);
-    const f4 bias = p.splits > 1 ? f4{0.f, 0.f, 0.f, 0.f} : bias4<T>(p, n);
 #pragma unroll
-    for (int i = 0; i < MI; ++i) {
+    for (int jh = 0; jh < NI / 2; ++jh) {
+        const int64_t n = n0 + wn + 64 * jh + 4 * (lane & 15);
+        const f4 bias = p.splits > 1 ? f4{0.f, 0.f, 0.f, 0.f} : bias4<T>(p, n);
 #pragma unroll
-        for (int j = 0; j < NI; ++j)
+        for (int i = 0; i < MI; ++i) {
 #pragma unroll
-            for (int g = 0; g < 4; ++g)
-                *reinterpret_cast<f4*>(tile + (lane & 31) * EW + 32 * j + 8 * g + 4 * (lane >> 5)) =
-                    f4{acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const f16v& c = acc[i][2 * jh + j];
+                    *reinterpret_cast<f4*>(tile + (lane & 31) * EW + 32 * j + 8 * g + 4 * (lane >> 5)) =
+                        f4{c[4 * g], c[4 * g + 1], c[4 * g + 2], c[4 * g + 3]};
+                }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
 #pragma unroll 1
-        for (int h = 0; h < 8; ++h) {
-            const int r = 4 * h + (lane >> 4);
-            const int64_t m = m0 + wm + 32 * i + r;
-            const f4 v = *reinterpret_cast<const f4*>(tile + r * EW + 4 * (lane & 15));
-            if (m < p.M && n < p.N) {
-                if (p.splits > 1) {
-                    store4(p.partial + (id.split * p.M + m) * p.N + n, v, p.N - n < 4 ? (int)(p.N - n) : 4);
-                } else {
-                    finish4<T>(p, m, n, v, bias);
+            for (int h = 0; h < 8; ++h) {
+                const int r = 4 * h + (lane >> 4);
+                const int64_t m = m0 + wm + 32 * i + r;
+                const f4 v = *reinterpret_cast<const f4*>(tile + r * EW + 4 * (lane & 15));
+                if (m < p.M && n < p.N) {
+                    if (p.splits > 1)
+                        store4(p.partial + (id.split * p.M + m) * p.N + n, v, p.N - n < 4 ? (int)(p.N - n) : 4);
+                    else
+                        finish4<T>(p, m, n, v, bias);
                 }
             }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
         }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
     }
 }
 
@@ -590,7 +647,7 @@ template <typename T, bool AKM, bool BKM, int BM, int BN, int WR, int WC, int KT
 cliff_status run(const ProductArgs& p, hipStream_t stream)
 {
     constexpr int P = sizeof(T) == 4 ? 3 : 1;
-    constexpr int stage = P * KT * 2 * (BM + BN) * (DIRECT ? 2 : 1), epi = WR * WC * 32 * (BN / WC + 4) * 4;
+    constexpr int stage = P * KT * 2 * (BM + BN) * (DIRECT ? 2 : 1), epi = WR * WC * 32 * (64 + 4) * 4;
     constexpr int lds = stage > epi ? stage : epi;
     static_assert(lds <= 160 * 1024, "LDS");
     const int64_t wgs = ceil_div(p.M, BM) * ceil_div(p.N, BN) * p.splits;

@@ -12,9 +12,10 @@ namespace cliff {
 // contiguous along the contraction, and a slot holds 8 of its values of one
 // row; otherwise memory is contiguous along the rows, and a slot holds 8 rows
 // of one contraction value.  Slots of a line (a row, or a contraction value)
-// are permuted by an XOR so that the lanes of a fragment read, which walk down
-// the lines, spread over the banks; a direct load to LDS writes the slots in
-// order and permutes the addresses that it reads instead.
+// are permuted by an XOR so that the lanes that a fragment read serves at once
+// (16 of 16 bytes, 32 of 8), which walk down the lines, touch all 64 banks once
+// (two-way conflicts cost 30 % of the read rate); a direct load to LDS writes the
+// slots in order and permutes the addresses that it reads instead.
 struct Stage {
     int R, KT;
     bool KM;
@@ -23,7 +24,8 @@ struct Stage {
     __host__ __device__ constexpr int bytes() const { return R * KT * 2; }
     __host__ __device__ constexpr int swizzle(int l) const
     {
-        return KM ? (l / (8 / line() > 0 ? 8 / line() : 1)) & (line() - 1) : ((l & 7) << 1) & (line() - 1);
+        return KM ? (l / (16 / line())) & (line() - 1)
+                  : ((l & 3) << 2 | (l >> 2 & 2)) & (line() - 1);
     }
     // first row and contraction value of slot e
     __host__ __device__ constexpr int slot_row(int e) const

@@ -71,13 +71,15 @@ static void stage(const Stage& s)
                     REQUIRE(x.row == row0 + (lane & 31) && x.k == k0 + 8 * (lane >> 5) + i,
                             "lane %d value %d: (%d, %d) at %d, %d", lane, i, x.row, x.k, row0, k0);
                 }
-    // banks: 16 lanes of a transposing read, 8 of a 16-byte read, in one pass of 128 bytes
-    for (int lane = 0; lane < 64; lane += s.KM ? 8 : 16) {
-        std::set<int> banks;
-        for (int l = lane; l < lane + (s.KM ? 8 : 16); ++l)
-            for (int w = 0; w < (s.KM ? 4 : 2); ++w) banks.insert((frag_byte(s, 0, 0, l, 0) / 4 + w) % 32);
-        if (s.line() >= 8 || s.KM) REQUIRE(banks.size() == 32, "lanes from %d touch %d banks", lane, (int)banks.size());
-    }
+    // banks: 32 lanes of a transposing read, 16 of a 16-byte read, at once
+    const int at_once = s.KM ? 16 : 32;
+    if (s.KM || s.line() >= 16)
+        for (int lane = 0; lane < 64; lane += at_once) {
+            std::set<int> banks;
+            for (int l = lane; l < lane + at_once; ++l)
+                for (int w = 0; w < 64 / at_once; ++w) banks.insert((frag_byte(s, 0, 0, l, 0) / 4 + w) % 64);
+            REQUIRE(banks.size() == 64, "lanes from %d touch %d banks", lane, (int)banks.size());
+        }
 }
 
 static void tiles(uint32_t tm, uint32_t tn, uint32_t splits)
