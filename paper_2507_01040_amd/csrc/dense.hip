@@ -138,6 +138,15 @@ struct Chunk {
     raw16 v[sizeof(T) / 2];
 };
 
+template <typename T>
+__device__ inline f16v mma(const u4& x, const u4& y, const f16v& c)
+{
+    if constexpr (__is_same(T, _Float16))
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(h8, x), __builtin_bit_cast(h8, y), c, 0, 0, 0);
+    else
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(b8, x), __builtin_bit_cast(b8, y), c, 0, 0, 0);
+}
+
 // A Stage as a type, so that its shape is known when a function is compiled.
 template <int R_, int KT_, bool KM_>
 struct StageOf {
@@ -205,35 +214,31 @@ struct Operand {
         }
     }
     __device__ int64_t advance() const { return S.KM ? S.KT : S.KT * ld; }
-    // Stage s into registers ...
+    // A stage into registers ...
+    __device__ void fetch_whole(Chunk<T> (&c)[L], const T* (&at)[L]) const
+    {
+#pragma unroll
+        for (int i = 0; i < L; ++i) {
+            __builtin_memcpy(&c[i], at[i], sizeof c[i]);
+            at[i] += advance();
+        }
+    }
     __device__ void fetch(Chunk<T> (&c)[L], const T* (&at)[L], int s, int tid) const
     {
         const int n = left(s);
+        if (n == S.KT && rows == S.R) return fetch_whole(c, at);
 #pragma unroll
         for (int i = 0; i < L; ++i) {
-            if (n == S.KT && rows == S.R) {
-                __builtin_memcpy(&c[i], at[i], sizeof c[i]);
-            } else {
-                const int have = S.slot_have(i * NT + tid, rows, n);
+            const int have = S.slot_have(i * NT + tid, rows, n);
 #pragma unroll
-                for (int h = 0; h < (int)sizeof(T) / 2; ++h)
-                    c[i].v[h] = load16(at[i] + h * per16<T>, have - h * per16<T>, width);
-            }
+            for (int h = 0; h < (int)sizeof(T) / 2; ++h)
+                c[i].v[h] = load16(at[i] + h * per16<T>, have - h * per16<T>, width);
             at[i] += advance();
         }
     }
     // ... and from there to LDS, fp32 as three planes.
-    __device__ void store(Chunk<T> (&c)[L], int s, char* to, int tid) const
+    static __device__ void put(const Chunk<T> (&c)[L], char* to, int tid)
     {
-        const int n = left(s);
-        if (n < S.KT || rows < S.R)
-#pragma unroll
-            for (int i = 0; i < L; ++i) {
-                const int have = S.slot_have(i * NT + tid, rows, n);
-#pragma unroll
-                for (int h = 0; h < (int)sizeof(T) / 2; ++h)
-                    settle16<T>(c[i].v[h], have - h * per16<T>, width);
-            }
 #pragma unroll
         for (int i = 0; i < L; ++i) {
             char* const at = to + (i * NT + tid) * 16;
@@ -252,6 +257,19 @@ struct Operand {
                 *reinterpret_cast<u4*>(at) = c[i].v[0];
             }
         }
+    }
+    __device__ void store(Chunk<T> (&c)[L], int s, char* to, int tid) const
+    {
+        const int n = left(s);
+        if (n < S.KT || rows < S.R)
+#pragma unroll
+            for (int i = 0; i < L; ++i) {
+                const int have = S.slot_have(i * NT + tid, rows, n);
+#pragma unroll
+                for (int h = 0; h < (int)sizeof(T) / 2; ++h)
+                    settle16<T>(c[i].v[h], have - h * per16<T>, width);
+            }
+        put(c, to, tid);
     }
     // The fragment of rows row0 to + 31 and values k to + 15 of a stage in LDS.
     static __device__ u4 frag(const char* from, int row0, int k, int lane)
@@ -274,20 +292,62 @@ struct Operand {
     }
 };
 
+// The outputs of a wave's MI x NI blocks of 32 x 32 from row m1, column n1 on: 32
+// rows at a time through LDS, so that 16 lanes hold 64 neighbouring columns of a
+// row.  Begins with a barrier: the stages there are done with.
+template <typename T, int MI, int NI>
+__device__ inline void write_tile(const ProductArgs& p, const TileId& id, int64_t m1, int64_t n1,
+                                  const f16v (&acc)[MI][NI], char* smem, int lane, int wave)
+{
+    __syncthreads();
+    constexpr int EW = 64 + 4;  // floats per row there
+    float* const tile = reinterpret_cast<float*>(smem) + wave * 32 * EW;
+#pragma unroll
+    for (int jh = 0; jh < NI / 2; ++jh) {
+        const int64_t n = n1 + 64 * jh + 4 * (lane & 15);
+        const f4 bias = p.splits > 1 ? f4{0.f, 0.f, 0.f, 0.f} : bias4<T>(p, n);
+#pragma unroll
+        for (int i = 0; i < MI; ++i) {
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const f16v& c = acc[i][2 * jh + j];
+                    *reinterpret_cast<f4*>(tile + (lane & 31) * EW + 32 * j + 8 * g + 4 * (lane >> 5)) =
+                        f4{c[4 * g], c[4 * g + 1], c[4 * g + 2], c[4 * g + 3]};
+                }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll 1
+            for (int h = 0; h < 8; ++h) {
+                const int r = 4 * h + (lane >> 4);
+                const int64_t m = m1 + 32 * i + r;
+                const f4 v = *reinterpret_cast<const f4*>(tile + r * EW + 4 * (lane & 15));
+                if (m < p.M && n < p.N) {
+                    if (p.splits > 1)
+                        store4(p.partial + (id.split * p.M + m) * p.N + n, v, p.N - n < 4 ? (int)(p.N - n) : 4);
+                    else
+                        finish4<T>(p, m, n, v, bias);
+                }
+            }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+        }
+    }
+}
+
 // BM x BN outputs per workgroup of WR x WC waves; a stage is KT contraction
-// values.  DIRECT: 16-bit operands whose rows are 16-byte aligned and whole
-// chunks go from memory straight to LDS, one stage ahead in the other of two
-// buffers.  Otherwise chunks go through registers, one stage ahead, and fp32
-// ones become three bf16 planes (split.hpp).
+// values of 16 bits.  DIRECT: operands whose rows are 16-byte aligned and whole
+// slots go from memory straight to LDS, one stage ahead in the other of two
+// buffers.  Otherwise slots go through registers, one stage ahead.
 template <typename T, bool AKM, bool BKM, int BM, int BN, int WR, int WC, int KT, bool DIRECT>
 __global__ __launch_bounds__(64 * WR * WC) void product_kernel(ProductArgs p)
 {
-    constexpr bool F32 = sizeof(T) == 4;
-    constexpr int P = F32 ? 3 : 1, NT = 64 * WR * WC, WM = BM / WR, WN = BN / WC, MI = WM / 32, NI = WN / 32;
-    static_assert(!(F32 && DIRECT) && WN % 64 == 0, "shape");
+    constexpr int NT = 64 * WR * WC, WM = BM / WR, WN = BN / WC, MI = WM / 32, NI = WN / 32;
+    static_assert(sizeof(T) == 2 && WN % 64 == 0, "shape");
     using A = Operand<T, StageOf<BM, KT, AKM>, NT>;
     using B = Operand<T, StageOf<BN, KT, BKM>, NT>;
-    constexpr int PA = A::S.bytes(), PB = B::S.bytes(), BUF = P * (PA + PB), KK = KT / 16;
+    constexpr int PA = A::S.bytes(), BUF = PA + B::S.bytes(), KK = KT / 16;
     extern __shared__ u4 smem4[];
     char* const smem = reinterpret_cast<char*>(smem4);
     const int tid = threadIdx.x, lane = tid & 63;
@@ -310,12 +370,10 @@ __global__ __launch_bounds__(64 * WR * WC) void product_kernel(ProductArgs p)
         for (int j = 0; j < NI; ++j)
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
-    u4 fa[2][MI][P], fb[2][NI][P];
+    u4 fa[2][MI], fb[2][NI];
     auto read_one = [&](int set, const char* buf, int kk, int f) {  // columns' fragments first
-#pragma unroll
-        for (int q = 0; q < P; ++q)
-            if (f < NI) fb[set][f][q] = B::frag(buf + P * PA + q * PB, wn + 32 * f, 16 * kk, lane);
-            else fa[set][f - NI][q] = A::frag(buf + q * PA, wm + 32 * (f - NI), 16 * kk, lane);
+        if (f < NI) fb[set][f] = B::frag(buf + PA, wn + 32 * f, 16 * kk, lane);
+        else fa[set][f - NI] = A::frag(buf, wm + 32 * (f - NI), 16 * kk, lane);
     };
     auto read = [&](int set, const char* buf, int kk) {
 #pragma unroll
@@ -324,19 +382,8 @@ __global__ __launch_bounds__(64 * WR * WC) void product_kernel(ProductArgs p)
     // The output's columns are the matrix instruction's rows: a lane's groups of
     // four accumulators are neighbours in memory.
     auto multiply_row = [&](int set, int i) {
-        constexpr int QA[6] = {2, 0, 1, 1, 0, 0}, QB[6] = {0, 2, 1, 0, 1, 0};
 #pragma unroll
-        for (int q = 0; q < (F32 ? 6 : 1); ++q)
-#pragma unroll
-            for (int j = 0; j < NI; ++j) {
-                const u4 &x = fb[set][j][F32 ? QB[q] : 0], &y = fa[set][i][F32 ? QA[q] : 0];
-                if constexpr (__is_same(T, _Float16))
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
-                        __builtin_bit_cast(h8, x), __builtin_bit_cast(h8, y), acc[i][j], 0, 0, 0);
-                else
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                        __builtin_bit_cast(b8, x), __builtin_bit_cast(b8, y), acc[i][j], 0, 0, 0);
-            }
+        for (int j = 0; j < NI; ++j) acc[i][j] = mma<T>(fb[set][j], fa[set][i], acc[i][j]);
     };
     auto multiply = [&](int set) {
 #pragma unroll
@@ -407,7 +454,7 @@ __global__ __launch_bounds__(64 * WR * WC) void product_kernel(ProductArgs p)
     } else {
         // Two fragment reads before each product, while there are any.
         auto interleave = [&](bool reads) {
-            constexpr int RD = P * (MI * (AKM ? 1 : 2) + NI * (BKM ? 1 : 2)), MF = MI * NI * (F32 ? 6 : 1);
+            constexpr int RD = MI * (AKM ? 1 : 2) + NI * (BKM ? 1 : 2), MF = MI * NI;
 #pragma unroll
             for (int i = 0; i < MF; ++i) {
                 if (reads && 2 * i < RD) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
@@ -426,7 +473,7 @@ __global__ __launch_bounds__(64 * WR * WC) void product_kernel(ProductArgs p)
         for (int s = 0; s < steps; ++s) {
             __syncthreads();
             a.store(ca, s, smem, tid);
-            b.store(cb, s, smem + P * PA, tid);
+            b.store(cb, s, smem + PA, tid);
             __syncthreads();
             if (s + 1 < steps) {
                 a.fetch(ca, ata, s + 1, tid);
@@ -440,78 +487,159 @@ __global__ __launch_bounds__(64 * WR * WC) void product_kernel(ProductArgs p)
                 interleave(kk + 1 < KK);
             }
         }
-        if constexpr (F32) {
-            // Sums that are infinite or NaN, or that the parts cannot hold, again
-            // as fp32 products, operands straight from memory (this wave's tile).
-            float z = 0.f;
+    }
+    write_tile<T, MI, NI>(p, id, m0 + wm, n0 + wn, acc, smem, lane, wave);
+}
+
+// The same for fp32: every operand as three bf16 parts (split.hpp), a product as
+// six, 128 x 128 outputs per workgroup of 2 x 2 waves, stages of 16 values.
+// While a wave multiplies stage s, it reads the fragments of stage s + 1, splits
+// stage s + 2 from registers into the LDS buffer that stage s has left, and
+// loads stage s + 4, so a step has one barrier.
+template <bool AKM, bool BKM>
+__global__ __launch_bounds__(256, 2) void split_product_kernel(ProductArgs p)
+{
+    constexpr int BM = 128, BN = 128, KT = 16, MI = 2, NI = 2, NT = 256;
+    using A = Operand<float, StageOf<BM, KT, AKM>, NT>;
+    using B = Operand<float, StageOf<BN, KT, BKM>, NT>;
+    constexpr int PA = A::S.bytes(), PB = B::S.bytes(), BUF = 3 * (PA + PB);
+    static_assert(A::L == 1 && B::L == 1, "one slot per thread");
+    extern __shared__ u4 smem4[];
+    char* const smem = reinterpret_cast<char*>(smem4);
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wm = wave / 2 * 64, wn = wave % 2 * 64;
+
+    const TileId id = tile_of(blockIdx.x, (uint32_t)((p.M + BM - 1) / BM), (uint32_t)((p.N + BN - 1) / BN), p.splits);
+    const int64_t m0 = (int64_t)id.m * BM, n0 = (int64_t)id.n * BN, k0 = id.split * p.k_part;
+    const int64_t kn = p.K - k0 < p.k_part ? p.K - k0 : p.k_part;
+    const int steps = kn > 0 ? (int)((kn + KT - 1) / KT) : 0;
+    const A a{static_cast<const float*>(p.a) + (AKM ? m0 * p.lda + k0 : k0 * p.lda + m0), p.lda,
+              (int)(p.M - m0 < BM ? p.M - m0 : BM), kn, AKM ? k0 + kn : p.M};
+    const B b{static_cast<const float*>(p.b) + (BKM ? n0 * p.ldb + k0 : k0 * p.ldb + n0), p.ldb,
+              (int)(p.N - n0 < BN ? p.N - n0 : BN), kn, BKM ? k0 + kn : p.N};
+
+    f16v acc[MI][NI];
+    auto clear = [&] {
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+#pragma unroll
+            for (int j = 0; j < NI; ++j)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+    };
+    clear();
+    u4 fa[2][MI][3], fb[2][NI][3];
+    auto read = [&](int set, const char* buf) {
+#pragma unroll
+        for (int q = 0; q < 3; ++q) {
+#pragma unroll
+            for (int j = 0; j < NI; ++j) fb[set][j][q] = B::frag(buf + 3 * PA + q * PB, wn + 32 * j, 0, lane);
+#pragma unroll
+            for (int i = 0; i < MI; ++i) fa[set][i][q] = A::frag(buf + q * PA, wm + 32 * i, 0, lane);
+        }
+    };
+    auto multiply = [&](int set) {
+        constexpr int QA[6] = {2, 0, 1, 1, 0, 0}, QB[6] = {0, 2, 1, 0, 1, 0};
+#pragma unroll
+        for (int q = 0; q < 6; ++q)
 #pragma unroll
             for (int i = 0; i < MI; ++i)
 #pragma unroll
-                for (int j = 0; j < NI; ++j) {
-                    acc[i][j] *= SPLIT_UNSCALE;
+                for (int j = 0; j < NI; ++j) acc[i][j] = mma<float>(fb[set][j][QB[q]], fa[set][i][QA[q]], acc[i][j]);
+    };
+    Chunk<float> ca[2][1], cb[2][1];
+    const float *ata[1], *atb[1];
+    a.pointers(ata, tid);
+    b.pointers(atb, tid);
+    auto fetch = [&](int s) {
+        if (s >= steps) return;
+        a.fetch(ca[s & 1], ata, s, tid);
+        b.fetch(cb[s & 1], atb, s, tid);
+    };
+    auto store = [&](int s) {
+        if (s >= steps) return;
+        a.store(ca[s & 1], s, smem + (s & 1) * BUF, tid);
+        b.store(cb[s & 1], s, smem + (s & 1) * BUF + 3 * PA, tid);
+    };
+    // Step s of parity s & 1 = set; plain: stages s + 2 and s + 4 are whole.
+    auto step = [&](int s, auto set, auto plain) {
+        char* const own = smem + set * BUF;
+        read(set ^ 1, smem + (set ^ 1) * BUF);
+        if constexpr (plain) {
+            A::put(ca[set], own, tid);
+            B::put(cb[set], own + 3 * PA, tid);
+            a.fetch_whole(ca[set], ata);
+            b.fetch_whole(cb[set], atb);
+        } else {
+            store(s + 2);
+            fetch(s + 4);
+        }
+        multiply(set);
+        if constexpr (plain) {
+            // a product, then a read or two and what splitting takes
+            constexpr int RD = 3 * (MI * (AKM ? 1 : 2) + NI * (BKM ? 1 : 2));
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) z = fmaf(acc[i][j][e], 0.f, z);
-                }
-            if (__ballot(z != 0.f)) {
-#pragma unroll
-                for (int i = 0; i < MI; ++i)
-#pragma unroll
-                    for (int j = 0; j < NI; ++j)
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
-                for (int64_t k = lane >> 5; k - (lane >> 5) < kn; k += 2) {
-                    float va[MI], vb[NI];
-#pragma unroll
-                    for (int i = 0; i < MI; ++i) va[i] = a.at(wm + 32 * i + (lane & 31), k);
-#pragma unroll
-                    for (int j = 0; j < NI; ++j) vb[j] = b.at(wn + 32 * j + (lane & 31), k);
-#pragma unroll
-                    for (int i = 0; i < MI; ++i)
-#pragma unroll
-                        for (int j = 0; j < NI; ++j)
-                            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(vb[j], va[i], acc[i][j], 0, 0, 0);
-                }
+            for (int i = 0; i < 24; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                if (i < 12) __builtin_amdgcn_sched_group_barrier(0x100, RD / 12, 0);
+                __builtin_amdgcn_sched_group_barrier(0x002, 5, 0);
+                if (i % 4 == 3) __builtin_amdgcn_sched_group_barrier(0x200, 1, 0);
             }
         }
+        __syncthreads();
+    };
+    constexpr std::integral_constant<int, 0> even;
+    constexpr std::integral_constant<int, 1> odd;
+    constexpr std::true_type yes;
+    constexpr std::false_type no;
+    fetch(0);
+    fetch(1);
+    store(0);
+    store(1);
+    fetch(2);
+    fetch(3);
+    __syncthreads();
+    read(0, smem);
+    __syncthreads();  // stage 2 takes the place of stage 0
+    const int whole = a.rows == BM && b.rows == BN ? (int)(kn / KT) : 0;  // whole stages
+    int s = 0;
+    for (; s + 5 < whole; s += 2) {
+        step(s, even, yes);
+        step(s + 1, odd, yes);
+    }
+    for (; s < steps; s += 2) {
+        step(s, even, no);
+        if (s + 1 < steps) step(s + 1, odd, no);
     }
 
-    // Epilogue: 32 rows at a time through LDS, so that 16 lanes hold 64
-    // neighbouring columns of a row.
-    __syncthreads();
-    constexpr int EW = 64 + 4;  // floats per row there
-    float* const tile = reinterpret_cast<float*>(smem) + wave * 32 * EW;
+    // Sums that are infinite or NaN, or that the parts cannot hold, again as fp32
+    // products, operands straight from memory (this wave's tile).
+    float z = 0.f;
 #pragma unroll
-    for (int jh = 0; jh < NI / 2; ++jh) {
-        const int64_t n = n0 + wn + 64 * jh + 4 * (lane & 15);
-        const f4 bias = p.splits > 1 ? f4{0.f, 0.f, 0.f, 0.f} : bias4<T>(p, n);
+    for (int i = 0; i < MI; ++i)
 #pragma unroll
-        for (int i = 0; i < MI; ++i) {
+        for (int j = 0; j < NI; ++j) {
+            acc[i][j] *= SPLIT_UNSCALE;
 #pragma unroll
-            for (int j = 0; j < 2; ++j)
+            for (int e = 0; e < 16; ++e) z = fmaf(acc[i][j][e], 0.f, z);
+        }
+    if (__ballot(z != 0.f)) {
+        clear();
+        for (int64_t k = lane >> 5; k - (lane >> 5) < kn; k += 2) {
+            float va[MI], vb[NI];
 #pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    const f16v& c = acc[i][2 * jh + j];
-                    *reinterpret_cast<f4*>(tile + (lane & 31) * EW + 32 * j + 8 * g + 4 * (lane >> 5)) =
-                        f4{c[4 * g], c[4 * g + 1], c[4 * g + 2], c[4 * g + 3]};
-                }
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-            __builtin_amdgcn_wave_barrier();
-#pragma unroll 1
-            for (int h = 0; h < 8; ++h) {
-                const int r = 4 * h + (lane >> 4);
-                const int64_t m = m0 + wm + 32 * i + r;
-                const f4 v = *reinterpret_cast<const f4*>(tile + r * EW + 4 * (lane & 15));
-                if (m < p.M && n < p.N) {
-                    if (p.splits > 1)
-                        store4(p.partial + (id.split * p.M + m) * p.N + n, v, p.N - n < 4 ? (int)(p.N - n) : 4);
-                    else
-                        finish4<T>(p, m, n, v, bias);
-                }
-            }
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-            __builtin_amdgcn_wave_barrier();
+            for (int i = 0; i < MI; ++i) va[i] = a.at(wm + 32 * i + (lane & 31), k);
+#pragma unroll
+            for (int j = 0; j < NI; ++j) vb[j] = b.at(wn + 32 * j + (lane & 31), k);
+#pragma unroll
+            for (int i = 0; i < MI; ++i)
+#pragma unroll
+                for (int j = 0; j < NI; ++j)
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(vb[j], va[i], acc[i][j], 0, 0, 0);
         }
     }
+    write_tile<float, MI, NI>(p, id, m0 + wm, n0 + wn, acc, smem, lane, wave);
 }
 
 // Joins the parts of a split contraction in order and finishes the outputs:
@@ -604,7 +732,7 @@ struct Cut {
 Cut cut(int dtype, int64_t M, int64_t N, int64_t K, bool direct)
 {
     const int cus = std::max(device_cus(), 1);
-    const int KT = dtype == CLIFF_F32 ? 32 : 64;
+    const int KT = dtype == CLIFF_F32 ? 16 : 64;
     Cut best{false, 1, 0};
     double least = 0;
     for (int large = 0; large <= (direct ? 1 : 0); ++large) {
@@ -614,7 +742,7 @@ Cut cut(int dtype, int64_t M, int64_t N, int64_t K, bool direct)
             const int64_t per = ceil_div(steps, want), splits = ceil_div(steps, per);
             if (splits != want) continue;
             // cycles: of a step with the compute unit to itself, rounds of workgroups
-            const double step = large ? 2700 : dtype == CLIFF_F32 ? 2100 : 760;
+            const double step = large ? 2700 : dtype == CLIFF_F32 ? 1050 : 760;
             const int64_t wgs = tiles * splits, slots = large ? cus : 2 * cus;
             const double share = large ? 1.0 : wgs > cus ? 2.0 : 1.25;
             double t = (double)ceil_div(wgs, slots) * (share * step * per + (large ? 12000 : 6000));
@@ -643,21 +771,17 @@ bool aligned_rows(const void* x, int64_t ld, int64_t width)
     return ((uintptr_t)x & 15) == 0 && ld % 8 == 0 && width % 8 == 0 && ld <= (1 << 21);
 }
 
-template <typename T, bool AKM, bool BKM, int BM, int BN, int WR, int WC, int KT, bool DIRECT>
-cliff_status run(const ProductArgs& p, hipStream_t stream)
+// Enqueues kernel k for tiles of B x B; its stages take `stage` bytes of LDS.
+template <typename K>
+cliff_status run(K k, const char* name, int B, int threads, int stage, const ProductArgs& p, hipStream_t stream)
 {
-    constexpr int P = sizeof(T) == 4 ? 3 : 1;
-    constexpr int stage = P * KT * 2 * (BM + BN) * (DIRECT ? 2 : 1), epi = WR * WC * 32 * (64 + 4) * 4;
-    constexpr int lds = stage > epi ? stage : epi;
-    static_assert(lds <= 160 * 1024, "LDS");
-    const int64_t wgs = ceil_div(p.M, BM) * ceil_div(p.N, BN) * p.splits;
+    const int lds = std::max(stage, threads / 64 * 32 * (64 + 4) * 4);  // or what write_tile takes
+    const int64_t wgs = ceil_div(p.M, B) * ceil_div(p.N, B) * p.splits;
     if (wgs >= (int64_t)1 << 31) return CLIFF_EUNSUPPORTED;
-    const auto k = product_kernel<T, AKM, BKM, BM, BN, WR, WC, KT, DIRECT>;
     if (debug_enabled())
-        fprintf(stderr, "cliffconv: product %lld x %lld x %lld tile %d x %d x %d%s, %lld workgroups, %d splits\n",
-                (long long)p.M, (long long)p.N, (long long)p.K, BM, BN, KT, DIRECT ? " direct" : "",
-                (long long)wgs, p.splits);
-    hipLaunchKernelGGL(k, dim3((unsigned)wgs), dim3(64 * WR * WC), lds, stream, p);
+        fprintf(stderr, "cliffconv: product %lld x %lld x %lld, %s tiles of %d, %lld workgroups, %d splits\n",
+                (long long)p.M, (long long)p.N, (long long)p.K, name, B, (long long)wgs, p.splits);
+    hipLaunchKernelGGL(k, dim3((unsigned)wgs), dim3(threads), lds, stream, p);
     return launched();
 }
 
@@ -672,14 +796,14 @@ cliff_status product(int dtype, ProductArgs p, hipStream_t stream)
     p.k_part = c.k_part;
     cliff_status s;
     if constexpr (sizeof(T) == 4) {
-        s = run<T, AKM, BKM, 128, 128, 2, 2, 32, false>(p, stream);
+        s = run(split_product_kernel<AKM, BKM>, "split", 128, 256, 2 * 3 * 2 * 128 * 16 * 2, p, stream);
     } else {
         if (!direct)
-            s = run<T, AKM, BKM, 128, 128, 2, 2, 64, false>(p, stream);
+            s = run(product_kernel<T, AKM, BKM, 128, 128, 2, 2, 64, false>, "staged", 128, 256, 2 * 128 * 64 * 2, p, stream);
         else if (c.large)
-            s = run<T, AKM, BKM, 256, 256, 2, 4, 64, true>(p, stream);
+            s = run(product_kernel<T, AKM, BKM, 256, 256, 2, 4, 64, true>, "direct", 256, 512, 2 * 2 * 256 * 64 * 2, p, stream);
         else
-            s = run<T, AKM, BKM, 128, 128, 2, 2, 64, true>(p, stream);
+            s = run(product_kernel<T, AKM, BKM, 128, 128, 2, 2, 64, true>, "direct", 128, 256, 2 * 2 * 128 * 64 * 2, p, stream);
     }
     if (s != CLIFF_OK || p.splits == 1) return s;
     const int64_t blocks = std::min<int64_t>(ceil_div(p.M * ceil_div(p.N, 4), 256), 1 << 16);

@@ -97,7 +97,7 @@ static void tiles(uint32_t tm, uint32_t tn, uint32_t splits)
 int main()
 {
     for (int R : {32, 64, 128, 256})
-        for (int KT : {32, 64})
+        for (int KT : {16, 32, 64})
             for (bool km : {false, true}) stage(Stage{R, KT, km});
     for (uint32_t tm : {1, 2, 7, 8, 9, 17, 64})
         for (uint32_t tn : {1, 3, 8, 31})
