@@ -112,19 +112,6 @@ __device__ inline void drop4(const DropArgs& d, uint64_t key, uint32_t step, int
     for (int e = 0; e < 4; ++e) v[e] = w.w[e] <= d.last ? 0.f : v[e] * d.scale;
 }
 
-// The epilogue of columns n to n + 3 of row m.
-template <typename T>
-__device__ inline void finish4(const ProductArgs& p, int64_t m, int64_t n, f4 v, const f4& bias)
-{
-    const int have = p.N - n < 4 ? (int)(p.N - n) : 4;
-    v += bias;
-    if (p.pre) store4(static_cast<T*>(p.pre) + m * p.ldp + n, v, have);
-    activate4(p.act, v);
-    if (p.drop.rng) drop4(p.drop, (uint64_t)p.drop.rng[0], (uint32_t)p.drop.rng[1], m, n, v);
-    if (p.residual) v += load4(static_cast<const T*>(p.residual) + m * p.ldr + n, have);
-    store4(static_cast<T*>(p.y) + m * p.ldy + n, v, have);
-}
-
 template <typename T>
 __device__ inline f4 bias4(const ProductArgs& p, int64_t n)
 {
@@ -292,6 +279,30 @@ struct Operand {
     }
 };
 
+// Four rows of a group of four columns: rows m, m + step, ...
+template <typename T>
+__device__ inline void finish_rows(const ProductArgs& p, int64_t m, int step, int64_t n, const f4 (&v)[4],
+                                   const f4& bias)
+{
+    const int have = p.N - n < 4 ? (int)(p.N - n) : 4;
+    f4 res[4];
+    if (p.residual)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            if (m + r * step < p.M) res[r] = load4(static_cast<const T*>(p.residual) + (m + r * step) * p.ldr + n, have);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const int64_t row = m + r * step;
+        if (row >= p.M) break;
+        f4 u = v[r] + bias;
+        if (p.pre) store4(static_cast<T*>(p.pre) + row * p.ldp + n, u, have);
+        activate4(p.act, u);
+        if (p.drop.rng) drop4(p.drop, (uint64_t)p.drop.rng[0], (uint32_t)p.drop.rng[1], row, n, u);
+        if (p.residual) u += res[r];
+        store4(static_cast<T*>(p.y) + row * p.ldy + n, u, have);
+    }
+}
+
 // The outputs of a wave's MI x NI blocks of 32 x 32 from row m1, column n1 on: 32
 // rows at a time through LDS, so that 16 lanes hold 64 neighbouring columns of a
 // row.  Begins with a barrier: the stages there are done with.
@@ -302,37 +313,46 @@ __device__ inline void write_tile(const ProductArgs& p, const TileId& id, int64_
     __syncthreads();
     constexpr int EW = 64 + 4;  // floats per row there
     float* const tile = reinterpret_cast<float*>(smem) + wave * 32 * EW;
+    auto put = [&](const f16v& c, int j) {
 #pragma unroll
-    for (int jh = 0; jh < NI / 2; ++jh) {
-        const int64_t n = n1 + 64 * jh + 4 * (lane & 15);
-        const f4 bias = p.splits > 1 ? f4{0.f, 0.f, 0.f, 0.f} : bias4<T>(p, n);
-#pragma unroll
-        for (int i = 0; i < MI; ++i) {
-#pragma unroll
-            for (int j = 0; j < 2; ++j)
-#pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    const f16v& c = acc[i][2 * jh + j];
-                    *reinterpret_cast<f4*>(tile + (lane & 31) * EW + 32 * j + 8 * g + 4 * (lane >> 5)) =
-                        f4{c[4 * g], c[4 * g + 1], c[4 * g + 2], c[4 * g + 3]};
-                }
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-            __builtin_amdgcn_wave_barrier();
+        for (int g = 0; g < 4; ++g)
+            *reinterpret_cast<f4*>(tile + (lane & 31) * EW + 32 * j + 8 * g + 4 * (lane >> 5)) =
+                f4{c[4 * g], c[4 * g + 1], c[4 * g + 2], c[4 * g + 3]};
+    };
+    static_assert(MI <= 4 && NI == 2, "blocks");
 #pragma unroll 1
-            for (int h = 0; h < 8; ++h) {
-                const int r = 4 * h + (lane >> 4);
-                const int64_t m = m1 + 32 * i + r;
-                const f4 v = *reinterpret_cast<const f4*>(tile + r * EW + 4 * (lane & 15));
-                if (m < p.M && n < p.N) {
-                    if (p.splits > 1)
-                        store4(p.partial + (id.split * p.M + m) * p.N + n, v, p.N - n < 4 ? (int)(p.N - n) : 4);
-                    else
-                        finish4<T>(p, m, n, v, bias);
+    for (int i = 0; i < MI; ++i) {  // not unrolled: one copy of what follows the switch
+        switch (i) {
+        case 0: put(acc[0][0], 0); put(acc[0][1], 1); break;
+        case 1: if constexpr (MI > 1) { put(acc[1][0], 0); put(acc[1][1], 1); } break;
+        case 2: if constexpr (MI > 2) { put(acc[2][0], 0); put(acc[2][1], 1); } break;
+        case 3: if constexpr (MI > 3) { put(acc[3][0], 0); put(acc[3][1], 1); } break;
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        const int64_t n = n1 + 4 * (lane & 15);
+        if (n < p.N) {
+            const f4 bias = p.splits > 1 ? f4{0.f, 0.f, 0.f, 0.f} : bias4<T>(p, n);
+#pragma unroll 1
+            for (int h = 0; h < 2; ++h) {
+                const int r0 = 16 * h + (lane >> 4);
+                const int64_t m = m1 + 32 * i + r0;
+                f4 v[4];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) v[r] = *reinterpret_cast<const f4*>(tile + (r0 + 4 * r) * EW + 4 * (lane & 15));
+                if (p.splits > 1) {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        if (m + 4 * r < p.M)
+                            store4(p.partial + (id.split * p.M + m + 4 * r) * p.N + n, v[r],
+                                   p.N - n < 4 ? (int)(p.N - n) : 4);
+                } else {
+                    finish_rows<T>(p, m, 4, n, v, bias);
                 }
             }
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-            __builtin_amdgcn_wave_barrier();
         }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
     }
 }
 
@@ -643,20 +663,219 @@ __global__ __launch_bounds__(256, 2) void split_product_kernel(ProductArgs p)
 }
 
 // Joins the parts of a split contraction in order and finishes the outputs:
-// one thread per four columns of a row.
+// one thread per four columns of four rows.
 template <typename T>
 __global__ __launch_bounds__(256) void join_kernel(ProductArgs p)
 {
-    const int64_t nq = (p.N + 3) / 4, n_all = p.M * nq, plane = p.M * p.N;
-    for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < n_all; i += gridDim.x * 256ll) {
-        const int64_t m = i / nq, n = i % nq * 4;
-        const float* q = p.partial + m * p.N + n;
-        const int have = p.N - n < 4 ? (int)(p.N - n) : 4;
-        f4 v = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-        for (int s = 0; s < p.splits; ++s) v += load4(q + s * plane, have);
-        finish4<T>(p, m, n, v, bias4<T>(p, n));
+    const int64_t nq = (p.N + 3) / 4, i = blockIdx.x * 256ll + threadIdx.x, plane = p.M * p.N;
+    if (i >= (p.M + 3) / 4 * nq) return;
+    const int64_t m = i / nq * 4, n = i % nq * 4;
+    const int have = p.N - n < 4 ? (int)(p.N - n) : 4;
+    f4 v[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) v[r] = f4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 2
+    for (int s = 0; s < p.splits; ++s)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            if (m + r < p.M) v[r] += load4(p.partial + s * plane + (m + r) * p.N + n, have);
+    finish_rows<T>(p, m, 1, n, v, bias4<T>(p, n));
+}
+
+// The sums of eight waves for the same 32 MB x 32 outputs (a lane's
+// accumulators as in write_tile), joined in order and finished.
+template <typename T, int MB>
+__device__ inline void join_waves(const ProductArgs& p, int64_t n0, const f16v (&acc)[MB], float* lds, int lane, int wave)
+{
+    constexpr int EW = 32 + 4, PLANE = MB * 32 * EW;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < MB; ++i)
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+            *reinterpret_cast<f4*>(lds + wave * PLANE + (32 * i + (lane & 31)) * EW + 8 * g + 4 * (lane >> 5)) =
+                f4{acc[i][4 * g], acc[i][4 * g + 1], acc[i][4 * g + 2], acc[i][4 * g + 3]};
+    __syncthreads();
+    // 8 threads per row, four columns each; a thread takes four rows 8 MB apart
+    const int tid = threadIdx.x, c = 4 * (tid & 7), r0 = tid >> 3;
+    const int64_t n = n0 + c;
+    if (r0 >= 8 * MB || r0 >= p.M || n >= p.N) return;
+    const f4 bias = bias4<T>(p, n);
+    f4 v[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        v[r] = f4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < 8; ++w) v[r] += *reinterpret_cast<const f4*>(lds + w * PLANE + (r0 + 8 * MB * r) * EW + c);
     }
+    finish_rows<T>(p, r0, 8 * MB, n, v, bias);
+}
+
+// Few rows (32 MB at most): bound by the read of B, so every workgroup streams
+// 32 columns of it once, its eight waves an eighth of the contraction each, and
+// they join their sums in LDS.  16-bit B contiguous along the contraction is
+// loaded as fragments; otherwise a wave turns its slots through a piece of LDS of
+// its own, without barriers.  One stage of 64 values ahead.
+template <typename T, bool BKM, int MB>
+__global__ __launch_bounds__(512, 2) void rows_kernel(ProductArgs p)
+{
+    constexpr Stage S{32, 64, false};
+    constexpr int EW = 32 + 4;
+    __shared__ __align__(16) char smem[8 * (MB * 32 * EW * 4 > S.bytes() ? MB * 32 * EW * 4 : S.bytes())];
+    const int lane = threadIdx.x & 63, r = lane & 31, half = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t n0 = blockIdx.x * 32ll;
+    const int64_t part = (p.K + 511) / 512 * 64, k0 = wave * part;
+    const int64_t k1 = k0 + part < p.K ? k0 + part : p.K;
+    const T* const a = static_cast<const T*>(p.a);
+    const T* const b = static_cast<const T*>(p.b);
+    f16v acc[MB];
+#pragma unroll
+    for (int i = 0; i < MB; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[i][e] = 0.f;
+
+    // Slots of 8 values of rows of a matrix that is contiguous along the
+    // contraction: value 16 j + 8 half of a stage.
+    struct Stage64 {
+        raw16 x[MB][4], w[4];
+    };
+    char* const own = smem + wave * S.bytes();
+    auto have_k = [&](int64_t k, int j) { return (int)(k1 - k < 64 ? k1 - k : 64) - 16 * j - 8 * half; };
+    const int cols = (int)(p.N - n0 < 32 ? p.N - n0 : 32);
+    auto load = [&](Stage64& f, int64_t k) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+#pragma unroll
+            for (int i = 0; i < MB; ++i)
+                f.x[i][j] = load16(a + (32 * i + r) * p.lda + k + 16 * j + 8 * half, 32 * i + r < p.M ? have_k(k, j) : 0, k1);
+            if constexpr (BKM) {
+                f.w[j] = load16(b + (n0 + r) * p.ldb + k + 16 * j + 8 * half, r < cols ? have_k(k, j) : 0, k1);
+            } else {
+                const int e = 64 * j + lane, kr = S.slot_k(e), c = S.slot_row(e);
+                f.w[j] = load16(b + (k + kr) * p.ldb + n0 + c, k + kr < k1 ? cols - c : 0, n0 + cols);
+            }
+        }
+    };
+    auto settle = [&](Stage64& f, int64_t k) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if (k1 - k < 64) {
+#pragma unroll
+                for (int i = 0; i < MB; ++i) settle16<T>(f.x[i][j], 32 * i + r < p.M ? have_k(k, j) : 0, k1);
+                if constexpr (BKM) settle16<T>(f.w[j], r < cols ? have_k(k, j) : 0, k1);
+            }
+            if constexpr (!BKM)
+                if (cols < 32) settle16<T>(f.w[j], k + S.slot_k(64 * j + lane) < k1 ? cols - S.slot_row(64 * j + lane) : 0, n0 + cols);
+        }
+    };
+    auto use = [&](Stage64& f, int64_t k) {
+        settle(f, k);
+        u4 w[4];
+        if constexpr (BKM) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[j] = f.w[j];
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) *reinterpret_cast<u4*>(own + (64 * j + lane) * 16) = f.w[j];
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[j] = Operand<T, StageOf<32, 64, false>, 64>::frag(own, 0, 16 * j, lane);
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int i = 0; i < MB; ++i) acc[i] = mma<T>(w[j], f.x[i][j], acc[i]);
+    };
+    if (k0 < k1) {
+        Stage64 f[2];
+        load(f[0], k0);
+        int64_t k = k0;
+        for (; k + 64 < k1; k += 128) {
+            load(f[1], k + 64);
+            use(f[0], k);
+            if (k + 128 < k1) load(f[0], k + 128);
+            use(f[1], k + 64);
+        }
+        if (k < k1) use(f[0], k);
+    }
+    join_waves<T, MB>(p, n0, acc, reinterpret_cast<float*>(smem), lane, wave);
+}
+
+// The same in fp32, on the fp32 matrix cores (the memory is slower): value
+// 8 j + 4 half + e of a stage of 32 in the e-th of four instructions.
+template <bool BKM, int MB>
+__global__ __launch_bounds__(512, 2) void rows_fp32_kernel(ProductArgs p)
+{
+    constexpr int EW = 32 + 4;
+    __shared__ __align__(16) char smem[8 * MB * 32 * EW * 4];
+    const int lane = threadIdx.x & 63, r = lane & 31, half = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t n0 = blockIdx.x * 32ll;
+    const int64_t part = (p.K + 255) / 256 * 32, k0 = wave * part;
+    const int64_t k1 = k0 + part < p.K ? k0 + part : p.K;
+    const float* const a = static_cast<const float*>(p.a);
+    const float* const b = static_cast<const float*>(p.b);
+    const bool col = n0 + r < p.N;
+    f16v acc[MB];
+#pragma unroll
+    for (int i = 0; i < MB; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[i][e] = 0.f;
+    struct Stage32 {
+        raw16 x[MB][4], w[4];
+    };
+    auto have_k = [&](int64_t k, int j) { return (int)(k1 - k < 32 ? k1 - k : 32) - 8 * j - 4 * half; };
+    auto load = [&](Stage32& f, int64_t k) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int64_t kj = k + 8 * j + 4 * half;
+#pragma unroll
+            for (int i = 0; i < MB; ++i)
+                f.x[i][j] = load16(a + (32 * i + r) * p.lda + kj, 32 * i + r < p.M ? have_k(k, j) : 0, k1);
+            if constexpr (BKM) {
+                f.w[j] = load16(b + (n0 + r) * p.ldb + kj, col ? have_k(k, j) : 0, k1);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    f.w[j][e] = col && kj + e < k1 ? __builtin_bit_cast(uint32_t, b[(kj + e) * p.ldb + n0 + r]) : 0u;
+            }
+        }
+    };
+    auto use = [&](Stage32& f, int64_t k) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if (k1 - k < 32) {
+#pragma unroll
+                for (int i = 0; i < MB; ++i) settle16<float>(f.x[i][j], 32 * i + r < p.M ? have_k(k, j) : 0, k1);
+                if constexpr (BKM) settle16<float>(f.w[j], col ? have_k(k, j) : 0, k1);
+            }
+            const f4 w = __builtin_bit_cast(f4, f.w[j]);
+#pragma unroll
+            for (int i = 0; i < MB; ++i) {
+                const f4 x = __builtin_bit_cast(f4, f.x[i][j]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    acc[i] = __builtin_amdgcn_mfma_f32_32x32x2f32(w[e], x[e], acc[i], 0, 0, 0);
+            }
+        }
+    };
+    if (k0 < k1) {
+        Stage32 f[2];
+        load(f[0], k0);
+        int64_t k = k0;
+        for (; k + 32 < k1; k += 64) {
+            load(f[1], k + 32);
+            use(f[0], k);
+            if (k + 64 < k1) load(f[0], k + 64);
+            use(f[1], k + 32);
+        }
+        if (k < k1) use(f[0], k);
+    }
+    join_waves<float, MB>(p, n0, acc, reinterpret_cast<float*>(smem), lane, wave);
 }
 
 // g = dropout(dy) f'(pre) into g [M, N] (unless NULL), and its column sums over
@@ -729,36 +948,49 @@ struct Cut {
     int64_t k_part;
 };
 
+// Times in ns, measured (MI355X): of a stage with one workgroup on each compute
+// unit and with as many as fit, and of a workgroup's begin and end; the kernels
+// wait for memory most of the time when they are alone, so a second workgroup is
+// nearly free.
+struct TileTimes {
+    int B, KT, fit;
+    double alone, full, ends;
+};
+constexpr TileTimes T_DIRECT256{256, 64, 1, 1600, 1600, 9000}, T_DIRECT128{128, 64, 2, 950, 1150, 6000},
+    T_STAGED128{128, 64, 3, 2000, 2100, 7000}, T_SPLIT128{128, 16, 2, 950, 1350, 7000};
+
 Cut cut(int dtype, int64_t M, int64_t N, int64_t K, bool direct)
 {
-    const int cus = std::max(device_cus(), 1);
-    const int KT = dtype == CLIFF_F32 ? 16 : 64;
+    const int64_t cus = std::max(device_cus(), 1);
     Cut best{false, 1, 0};
     double least = 0;
     for (int large = 0; large <= (direct ? 1 : 0); ++large) {
-        const int B = large ? 256 : 128;
-        const int64_t tiles = ceil_div(M, B) * ceil_div(N, B), steps = std::max<int64_t>(1, ceil_div(K, KT));
+        const TileTimes& t = large ? T_DIRECT256 : dtype == CLIFF_F32 ? T_SPLIT128 : direct ? T_DIRECT128 : T_STAGED128;
+        const int64_t tiles = ceil_div(M, t.B) * ceil_div(N, t.B), steps = std::max<int64_t>(1, ceil_div(K, t.KT));
         for (int64_t want = 1; want <= 64 && want <= steps; ++want) {
             const int64_t per = ceil_div(steps, want), splits = ceil_div(steps, per);
             if (splits != want) continue;
-            // cycles: of a step with the compute unit to itself, rounds of workgroups
-            const double step = large ? 2700 : dtype == CLIFF_F32 ? 1050 : 760;
-            const int64_t wgs = tiles * splits, slots = large ? cus : 2 * cus;
-            const double share = large ? 1.0 : wgs > cus ? 2.0 : 1.25;
-            double t = (double)ceil_div(wgs, slots) * (share * step * per + (large ? 12000 : 6000));
-            if (splits > 1) t += 6000 + (double)M * N * 4 * (2 * splits) / 2000;
-            if (least == 0 || t < least) {
-                least = t;
-                best = Cut{large != 0, (int)splits, per * KT};
+            const int64_t wgs = tiles * splits, rounds = wgs / (cus * t.fit), rest = wgs % (cus * t.fit);
+            double ns = rounds * (per * t.full + t.ends);
+            if (rest) ns += per * (rest <= cus ? t.alone : t.full) + t.ends;
+            // the join: a launch, and the partial sums written and read
+            if (splits > 1) ns += 3500 + (double)M * N * 4 * (splits + 1) / 6000;
+            if (least == 0 || ns < least) {
+                least = ns;
+                best = Cut{large != 0, (int)splits, per * t.KT};
             }
         }
     }
     return best;
 }
 
-int64_t partial_bytes(int dtype, int64_t M, int64_t N, int64_t K)
+constexpr int64_t FEW_ROWS = 64;  // up to which rows_kernel runs
+
+// What a product of rows (y or dx) or a weight's gradient needs for its parts.
+int64_t partial_bytes(int dtype, int64_t M, int64_t N, int64_t K, bool rows)
 {
     int64_t n = 0;
+    if (rows && M <= FEW_ROWS) return 0;
     for (int direct = 0; direct <= (dtype == CLIFF_F32 ? 0 : 1); ++direct) {
         const Cut c = cut(dtype, M, N, K, direct != 0);
         if (c.splits > 1) n = std::max(n, c.splits * M * N * 4);
@@ -785,10 +1017,29 @@ cliff_status run(K k, const char* name, int B, int threads, int stage, const Pro
     return launched();
 }
 
+template <typename T, bool BKM>
+cliff_status few_rows(const ProductArgs& p, hipStream_t stream)
+{
+    const int64_t wgs = ceil_div(p.N, 32);
+    if (debug_enabled())
+        fprintf(stderr, "cliffconv: product %lld x %lld x %lld, few rows, %lld workgroups\n", (long long)p.M,
+                (long long)p.N, (long long)p.K, (long long)wgs);
+    const auto go = [&](auto k) {
+        hipLaunchKernelGGL(k, dim3((unsigned)wgs), dim3(512), 0, stream, p);
+        return launched();
+    };
+    if constexpr (sizeof(T) == 4)
+        return p.M <= 32 ? go(rows_fp32_kernel<BKM, 1>) : go(rows_fp32_kernel<BKM, 2>);
+    else
+        return p.M <= 32 ? go(rows_kernel<T, BKM, 1>) : go(rows_kernel<T, BKM, 2>);
+}
+
 // A product and, where its contraction is split, the join.
 template <typename T, bool AKM, bool BKM>
 cliff_status product(int dtype, ProductArgs p, hipStream_t stream)
 {
+    if constexpr (AKM)
+        if (p.M <= FEW_ROWS) return few_rows<T, BKM>(p, stream);
     const bool direct = sizeof(T) == 2 && aligned_rows(p.a, p.lda, AKM ? p.K : p.M) &&
                         aligned_rows(p.b, p.ldb, BKM ? p.K : p.N);
     const Cut c = cut(dtype, p.M, p.N, p.K, direct);
@@ -806,7 +1057,8 @@ cliff_status product(int dtype, ProductArgs p, hipStream_t stream)
             s = run(product_kernel<T, AKM, BKM, 128, 128, 2, 2, 64, true>, "direct", 128, 256, 2 * 2 * 128 * 64 * 2, p, stream);
     }
     if (s != CLIFF_OK || p.splits == 1) return s;
-    const int64_t blocks = std::min<int64_t>(ceil_div(p.M * ceil_div(p.N, 4), 256), 1 << 16);
+    const int64_t blocks = ceil_div(ceil_div(p.M, 4) * ceil_div(p.N, 4), 256);
+    if (blocks >= (int64_t)1 << 31) return CLIFF_EUNSUPPORTED;
     hipLaunchKernelGGL(join_kernel<T>, dim3((unsigned)blocks), dim3(256), 0, stream, p);
     return launched();
 }
@@ -824,14 +1076,14 @@ BackwardSpace backward_space(int dtype, int64_t M, int64_t K, int64_t N)
     w.g = 0;
     w.sums = ceil_div(M * N * (dtype == CLIFF_F32 ? 4 : 2), 256) * 256;
     w.partial = w.sums + ceil_div(w.parts * N * 4, 256) * 256;
-    w.all = w.partial + std::max({partial_bytes(dtype, M, K, N), partial_bytes(dtype, K, N, M),
-                                  partial_bytes(dtype, N, K, M)});
+    w.all = w.partial + std::max({partial_bytes(dtype, M, K, N, true), partial_bytes(dtype, K, N, M, false),
+                                  partial_bytes(dtype, N, K, M, false)});
     return w;
 }
 
 }  // namespace
 
-int64_t dense_workspace(int dtype, int64_t M, int64_t K, int64_t N) { return partial_bytes(dtype, M, N, K); }
+int64_t dense_workspace(int dtype, int64_t M, int64_t K, int64_t N) { return partial_bytes(dtype, M, N, K, true); }
 int64_t dense_backward_workspace(int dtype, int64_t M, int64_t K, int64_t N)
 {
     return backward_space(dtype, M, K, N).all;
