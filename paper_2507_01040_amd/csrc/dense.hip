@@ -156,7 +156,7 @@ struct Operand {
     int64_t ld;
     int rows;      // of the tile that exist
     int64_t vals;  // contraction values that exist
-    int64_t width;  // elements of a line of memory up to and with the tile's last
+    int64_t width;  // elements of a line of memory before the tile's end
 
     // Byte offsets of a thread's slots from a stage's start (direct loads).
     __device__ void offsets(uint32_t (&off)[L], int tid) const
@@ -210,16 +210,22 @@ struct Operand {
             at[i] += advance();
         }
     }
+    // (of a tile or stage that is not whole; what it lacks is zeroed in store)
     __device__ void fetch(Chunk<T> (&c)[L], const T* (&at)[L], int s, int tid) const
     {
         const int n = left(s);
         if (n == S.KT && rows == S.R) return fetch_whole(c, at);
 #pragma unroll
         for (int i = 0; i < L; ++i) {
-            const int have = S.slot_have(i * NT + tid, rows, n);
+            const int e = i * NT + tid, r = S.slot_row(e), k = S.slot_k(e);
+            // the slot's line, from the tile's first element there; lines that do
+            // not exist give way to the last one
+            const int line = S.KM ? r : k, lines = S.KM ? rows : n, pos = S.KM ? k : r, end = S.KM ? n : rows;
+            const T* const p = at[i] - pos + (line < lines ? 0 : (lines - 1 - line) * ld);
 #pragma unroll
             for (int h = 0; h < (int)sizeof(T) / 2; ++h)
-                c[i].v[h] = load16(at[i] + h * per16<T>, have - h * per16<T>, width);
+                c[i].v[h] = width < per16<T> ? load16_narrow(p, pos + h * per16<T>, end)
+                                             : load16(p, pos + h * per16<T>, end);
             at[i] += advance();
         }
     }
@@ -251,10 +257,11 @@ struct Operand {
         if (n < S.KT || rows < S.R)
 #pragma unroll
             for (int i = 0; i < L; ++i) {
-                const int have = S.slot_have(i * NT + tid, rows, n);
+                const int e = i * NT + tid, r = S.slot_row(e), k = S.slot_k(e);
 #pragma unroll
                 for (int h = 0; h < (int)sizeof(T) / 2; ++h)
-                    settle16<T>(c[i].v[h], have - h * per16<T>, width);
+                    if (!S.KM && k >= n) c[i].v[h] = raw16{0, 0, 0, 0};
+                    else if (width >= per16<T>) settle16<T>(c[i].v[h], (S.KM ? k : r) + h * per16<T>, S.KM ? n : rows);
             }
         put(c, to, tid);
     }
@@ -279,19 +286,19 @@ struct Operand {
     }
 };
 
-// Four rows of a group of four columns: rows m, m + step, ...
-template <typename T>
-__device__ inline void finish_rows(const ProductArgs& p, int64_t m, int step, int64_t n, const f4 (&v)[4],
+// R rows of a group of four columns: rows m, m + step, ...
+template <typename T, int R>
+__device__ inline void finish_rows(const ProductArgs& p, int64_t m, int step, int64_t n, const f4 (&v)[R],
                                    const f4& bias)
 {
     const int have = p.N - n < 4 ? (int)(p.N - n) : 4;
-    f4 res[4];
+    f4 res[R];
     if (p.residual)
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
+        for (int r = 0; r < R; ++r)
             if (m + r * step < p.M) res[r] = load4(static_cast<const T*>(p.residual) + (m + r * step) * p.ldr + n, have);
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
+    for (int r = 0; r < R; ++r) {
         const int64_t row = m + r * step;
         if (row >= p.M) break;
         f4 u = v[r] + bias;
@@ -347,7 +354,7 @@ __device__ inline void write_tile(const ProductArgs& p, const TileId& id, int64_
                             store4(p.partial + (id.split * p.M + m + 4 * r) * p.N + n, v[r],
                                    p.N - n < 4 ? (int)(p.N - n) : 4);
                 } else {
-                    finish_rows<T>(p, m, 4, n, v, bias);
+                    finish_rows<T, 4>(p, m, 4, n, v, bias);
                 }
             }
         }
@@ -662,220 +669,270 @@ __global__ __launch_bounds__(256, 2) void split_product_kernel(ProductArgs p)
     write_tile<float, MI, NI>(p, id, m0 + wm, n0 + wn, acc, smem, lane, wave);
 }
 
-// Joins the parts of a split contraction in order and finishes the outputs:
-// one thread per four columns of four rows.
+// Joins the parts of a split contraction in a fixed order and finishes the
+// outputs: a workgroup takes 64 groups of four columns, its four waves every
+// fourth part each.
 template <typename T>
 __global__ __launch_bounds__(256) void join_kernel(ProductArgs p)
 {
-    const int64_t nq = (p.N + 3) / 4, i = blockIdx.x * 256ll + threadIdx.x, plane = p.M * p.N;
-    if (i >= (p.M + 3) / 4 * nq) return;
-    const int64_t m = i / nq * 4, n = i % nq * 4;
+    __shared__ f4 part[4][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t nq = (p.N + 3) / 4, i = blockIdx.x * 64ll + lane, plane = p.M * p.N;
+    const int64_t m = i / nq, n = i % nq * 4;
     const int have = p.N - n < 4 ? (int)(p.N - n) : 4;
-    f4 v[4];
-#pragma unroll
-    for (int r = 0; r < 4; ++r) v[r] = f4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll 2
-    for (int s = 0; s < p.splits; ++s)
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-            if (m + r < p.M) v[r] += load4(p.partial + s * plane + (m + r) * p.N + n, have);
-    finish_rows<T>(p, m, 1, n, v, bias4<T>(p, n));
+    f4 v[1] = {f4{0.f, 0.f, 0.f, 0.f}};
+    if (m < p.M) {
+        const float* const q = p.partial + m * p.N + n;
+#pragma unroll 8
+        for (int s = wave; s < p.splits; s += 4) v[0] += load4(q + s * plane, have);
+    }
+    part[wave][lane] = v[0];
+    __syncthreads();
+    if (wave || m >= p.M) return;
+    v[0] = part[0][lane] + part[1][lane] + part[2][lane] + part[3][lane];
+    finish_rows<T, 1>(p, m, 1, n, v, bias4<T>(p, n));
 }
 
-// The sums of eight waves for the same 32 MB x 32 outputs (a lane's
-// accumulators as in write_tile), joined in order and finished.
-template <typename T, int MB>
-__device__ inline void join_waves(const ProductArgs& p, int64_t n0, const f16v (&acc)[MB], float* lds, int lane, int wave)
+// Few rows (16 MB at most): bound by the read of B, so every workgroup streams
+// 16 NS columns of it once, its eight waves an eighth of the contraction each, D
+// stages ahead, and they join their sums in LDS.  Matrix instructions of 16 x 16
+// outputs, B's columns as their rows.
+
+// The sums of the eight waves for the same outputs, joined in order and finished.
+template <typename T, int MB, int NS>
+__device__ inline void join_waves(const ProductArgs& p, int64_t n0, const f4 (&acc)[MB][NS], float* lds, int lane,
+                                  int wave)
 {
-    constexpr int EW = 32 + 4, PLANE = MB * 32 * EW;
+    constexpr int EW = 16 * NS + 4, PLANE = MB * 16 * EW;
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < MB; ++i)
 #pragma unroll
-        for (int g = 0; g < 4; ++g)
-            *reinterpret_cast<f4*>(lds + wave * PLANE + (32 * i + (lane & 31)) * EW + 8 * g + 4 * (lane >> 5)) =
-                f4{acc[i][4 * g], acc[i][4 * g + 1], acc[i][4 * g + 2], acc[i][4 * g + 3]};
+        for (int j = 0; j < NS; ++j)
+            *reinterpret_cast<f4*>(lds + wave * PLANE + (16 * i + (lane & 15)) * EW + 16 * j + 4 * (lane >> 4)) =
+                acc[i][j];
     __syncthreads();
-    // 8 threads per row, four columns each; a thread takes four rows 8 MB apart
-    const int tid = threadIdx.x, c = 4 * (tid & 7), r0 = tid >> 3;
+    const int r = threadIdx.x / (4 * NS), c = 4 * (threadIdx.x % (4 * NS));
     const int64_t n = n0 + c;
-    if (r0 >= 8 * MB || r0 >= p.M || n >= p.N) return;
-    const f4 bias = bias4<T>(p, n);
-    f4 v[4];
+    if (r >= 16 * MB || r >= p.M || n >= p.N) return;
+    f4 v[1] = {f4{0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-        v[r] = f4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int w = 0; w < 8; ++w) v[r] += *reinterpret_cast<const f4*>(lds + w * PLANE + (r0 + 8 * MB * r) * EW + c);
-    }
-    finish_rows<T>(p, r0, 8 * MB, n, v, bias);
+    for (int w = 0; w < 8; ++w) v[0] += *reinterpret_cast<const f4*>(lds + w * PLANE + r * EW + c);
+    finish_rows<T, 1>(p, r, 1, n, v, bias4<T>(p, n));
 }
 
-// Few rows (32 MB at most): bound by the read of B, so every workgroup streams
-// 32 columns of it once, its eight waves an eighth of the contraction each, and
-// they join their sums in LDS.  16-bit B contiguous along the contraction is
-// loaded as fragments; otherwise a wave turns its slots through a piece of LDS of
-// its own, without barriers.  One stage of 64 values ahead.
+// What the eight waves share: the workgroup's columns, and a wave's part of the
+// contraction (whole stages of KT but for the last).
+template <int KT>
+struct RowsPart {
+    int64_t n0, k0, k1;
+    int cols;
+    __device__ RowsPart(const ProductArgs& p, int columns, int wave)
+    {
+        n0 = (int64_t)xcd_run(blockIdx.x, gridDim.x) * columns;
+        cols = (int)(p.N - n0 < columns ? p.N - n0 : columns);
+        const int64_t part = (p.K + 8 * KT - 1) / (8 * KT) * KT;
+        k0 = wave * part;
+        k1 = k0 + part < p.K ? k0 + part : p.K;
+    }
+    // Calls load(stage, k) D stages ahead of use(stage, k).
+    template <int D, typename St, typename L, typename U>
+    __device__ void run(L load, U use) const
+    {
+        St f[D];
+#pragma unroll
+        for (int d = 0; d < D; ++d)
+            if (k0 + d * KT < k1) load(f[d], k0 + d * KT);
+        for (int64_t k = k0; k < k1; k += D * KT)
+#pragma unroll
+            for (int d = 0; d < D; ++d) {
+                const int64_t kd = k + d * KT;
+                if (kd < k1) use(f[d], kd);
+                if (kd + D * KT < k1) load(f[d], kd + D * KT);
+            }
+    }
+};
+
+// 16-bit types.  B contiguous along the contraction is loaded as fragments;
+// otherwise a wave turns its slots through a piece of LDS of its own, without
+// barriers.
 template <typename T, bool BKM, int MB>
 __global__ __launch_bounds__(512, 2) void rows_kernel(ProductArgs p)
 {
+    constexpr int NS = BKM ? 1 : 2, D = MB == 4 ? 2 : 4;
     constexpr Stage S{32, 64, false};
-    constexpr int EW = 32 + 4;
-    __shared__ __align__(16) char smem[8 * (MB * 32 * EW * 4 > S.bytes() ? MB * 32 * EW * 4 : S.bytes())];
-    const int lane = threadIdx.x & 63, r = lane & 31, half = lane >> 5;
+    constexpr int JOIN = MB * 16 * (16 * NS + 4) * 4;
+    __shared__ __align__(16) char smem[8 * (BKM || JOIN > S.bytes() ? JOIN : S.bytes())];
+    const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int64_t n0 = blockIdx.x * 32ll;
-    const int64_t part = (p.K + 511) / 512 * 64, k0 = wave * part;
-    const int64_t k1 = k0 + part < p.K ? k0 + part : p.K;
+    const RowsPart<64> part(p, 16 * NS, wave);
+    const int64_t n0 = part.n0, k1 = part.k1;
+    const int cols = part.cols;
     const T* const a = static_cast<const T*>(p.a);
     const T* const b = static_cast<const T*>(p.b);
-    f16v acc[MB];
+    f4 acc[MB][NS];
 #pragma unroll
     for (int i = 0; i < MB; ++i)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) acc[i][e] = 0.f;
-
-    // Slots of 8 values of rows of a matrix that is contiguous along the
-    // contraction: value 16 j + 8 half of a stage.
-    struct Stage64 {
-        raw16 x[MB][4], w[4];
+        for (int j = 0; j < NS; ++j) acc[i][j] = f4{0.f, 0.f, 0.f, 0.f};
+    // a lane's slots: values 32 j + 8 g of a row
+    struct St {
+        raw16 x[MB][2], w[2 * NS];
     };
     char* const own = smem + wave * S.bytes();
-    auto have_k = [&](int64_t k, int j) { return (int)(k1 - k < 64 ? k1 - k : 64) - 16 * j - 8 * half; };
-    const int cols = (int)(p.N - n0 < 32 ? p.N - n0 : 32);
-    auto load = [&](Stage64& f, int64_t k) {
+    // rows and columns that do not exist give way to the last ones
+    const T* arow[MB];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
+    for (int i = 0; i < MB; ++i) arow[i] = a + (16 * i + r < p.M ? 16 * i + r : p.M - 1) * p.lda;
+    const T* const bcol = b + (n0 + (r < cols ? r : cols - 1)) * p.ldb;
+    auto load = [&](St& f, int64_t k) {
 #pragma unroll
-            for (int i = 0; i < MB; ++i)
-                f.x[i][j] = load16(a + (32 * i + r) * p.lda + k + 16 * j + 8 * half, 32 * i + r < p.M ? have_k(k, j) : 0, k1);
-            if constexpr (BKM) {
-                f.w[j] = load16(b + (n0 + r) * p.ldb + k + 16 * j + 8 * half, r < cols ? have_k(k, j) : 0, k1);
-            } else {
-                const int e = 64 * j + lane, kr = S.slot_k(e), c = S.slot_row(e);
-                f.w[j] = load16(b + (k + kr) * p.ldb + n0 + c, k + kr < k1 ? cols - c : 0, n0 + cols);
-            }
+        for (int j = 0; j < 2; ++j) {
+#pragma unroll
+            for (int i = 0; i < MB; ++i) f.x[i][j] = load16(arow[i], k + 32 * j + 8 * g, k1);
+            if constexpr (BKM) f.w[j] = load16(bcol, k + 32 * j + 8 * g, k1);
         }
-    };
-    auto settle = [&](Stage64& f, int64_t k) {
+        if constexpr (!BKM)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            if (k1 - k < 64) {
-#pragma unroll
-                for (int i = 0; i < MB; ++i) settle16<T>(f.x[i][j], 32 * i + r < p.M ? have_k(k, j) : 0, k1);
-                if constexpr (BKM) settle16<T>(f.w[j], r < cols ? have_k(k, j) : 0, k1);
+            for (int j = 0; j < 4; ++j) {
+                const int e = 64 * j + lane;
+                const int64_t kr = k + S.slot_k(e);
+                f.w[j] = load16(b + (kr < k1 ? kr : k1 - 1) * p.ldb, n0 + S.slot_row(e), n0 + cols);
             }
-            if constexpr (!BKM)
-                if (cols < 32) settle16<T>(f.w[j], k + S.slot_k(64 * j + lane) < k1 ? cols - S.slot_row(64 * j + lane) : 0, n0 + cols);
-        }
     };
-    auto use = [&](Stage64& f, int64_t k) {
-        settle(f, k);
-        u4 w[4];
+    auto use = [&](St& f, int64_t k) {
+        if (k1 - k < 64)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+#pragma unroll
+                for (int i = 0; i < MB; ++i) settle16<T>(f.x[i][j], k + 32 * j + 8 * g, k1);
+                if constexpr (BKM) settle16<T>(f.w[j], k + 32 * j + 8 * g, k1);
+            }
+        if constexpr (!BKM)
+            if (cols < 32 || k1 - k < 64)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int e = 64 * j + lane;
+                    if (k + S.slot_k(e) >= k1) f.w[j] = raw16{0, 0, 0, 0};
+                    settle16<T>(f.w[j], S.slot_row(e), cols);
+                }
+        u4 w[2][NS];
         if constexpr (BKM) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) w[j] = f.w[j];
+            w[0][0] = f.w[0];
+            w[1][0] = f.w[1];
         } else {
 #pragma unroll
             for (int j = 0; j < 4; ++j) *reinterpret_cast<u4*>(own + (64 * j + lane) * 16) = f.w[j];
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             __builtin_amdgcn_wave_barrier();
 #pragma unroll
-            for (int j = 0; j < 4; ++j) w[j] = Operand<T, StageOf<32, 64, false>, 64>::frag(own, 0, 16 * j, lane);
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int h = 0; h < NS; ++h) {
+                    typedef __attribute__((address_space(3))) s4 ls4;
+                    struct {
+                        s4 x, y;
+                    } z{__builtin_amdgcn_ds_read_tr16_b64_v4i16((ls4*)(own + frag16_byte(S, 16 * h, 32 * j, lane, 0))),
+                        __builtin_amdgcn_ds_read_tr16_b64_v4i16((ls4*)(own + frag16_byte(S, 16 * h, 32 * j, lane, 1)))};
+                    w[j][h] = __builtin_bit_cast(u4, z);
+                }
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             __builtin_amdgcn_wave_barrier();
         }
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
+        for (int j = 0; j < 2; ++j)
 #pragma unroll
-            for (int i = 0; i < MB; ++i) acc[i] = mma<T>(w[j], f.x[i][j], acc[i]);
+            for (int i = 0; i < MB; ++i)
+#pragma unroll
+                for (int h = 0; h < NS; ++h) {
+                    if constexpr (__is_same(T, _Float16))
+                        acc[i][h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(
+                            __builtin_bit_cast(h8, w[j][h]), __builtin_bit_cast(h8, f.x[i][j]), acc[i][h], 0, 0, 0);
+                    else
+                        acc[i][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                            __builtin_bit_cast(b8, w[j][h]), __builtin_bit_cast(b8, f.x[i][j]), acc[i][h], 0, 0, 0);
+                }
     };
-    if (k0 < k1) {
-        Stage64 f[2];
-        load(f[0], k0);
-        int64_t k = k0;
-        for (; k + 64 < k1; k += 128) {
-            load(f[1], k + 64);
-            use(f[0], k);
-            if (k + 128 < k1) load(f[0], k + 128);
-            use(f[1], k + 64);
-        }
-        if (k < k1) use(f[0], k);
-    }
-    join_waves<T, MB>(p, n0, acc, reinterpret_cast<float*>(smem), lane, wave);
+    part.template run<D, St>(load, use);
+    join_waves<T, MB, NS>(p, n0, acc, reinterpret_cast<float*>(smem), lane, wave);
 }
 
-// The same in fp32, on the fp32 matrix cores (the memory is slower): value
-// 8 j + 4 half + e of a stage of 32 in the e-th of four instructions.
+// fp32, on the fp32 matrix cores (the memory is slower): value 16 j + 4 g + e of
+// a stage of 32 in the e-th of four instructions.
 template <bool BKM, int MB>
 __global__ __launch_bounds__(512, 2) void rows_fp32_kernel(ProductArgs p)
 {
-    constexpr int EW = 32 + 4;
-    __shared__ __align__(16) char smem[8 * MB * 32 * EW * 4];
-    const int lane = threadIdx.x & 63, r = lane & 31, half = lane >> 5;
+    constexpr int NS = 1, D = MB == 4 ? 2 : 4;
+    __shared__ __align__(16) char smem[8 * MB * 16 * (16 * NS + 4) * 4];
+    const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int64_t n0 = blockIdx.x * 32ll;
-    const int64_t part = (p.K + 255) / 256 * 32, k0 = wave * part;
-    const int64_t k1 = k0 + part < p.K ? k0 + part : p.K;
+    const RowsPart<32> part(p, 16 * NS, wave);
+    const int64_t n0 = part.n0, k1 = part.k1;
+    const int cols = part.cols;
     const float* const a = static_cast<const float*>(p.a);
     const float* const b = static_cast<const float*>(p.b);
-    const bool col = n0 + r < p.N;
-    f16v acc[MB];
+    f4 acc[MB][NS];
 #pragma unroll
     for (int i = 0; i < MB; ++i)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) acc[i][e] = 0.f;
-    struct Stage32 {
-        raw16 x[MB][4], w[4];
+        for (int j = 0; j < NS; ++j) acc[i][j] = f4{0.f, 0.f, 0.f, 0.f};
+    struct St {
+        raw16 x[MB][2], w[2][NS];
     };
-    auto have_k = [&](int64_t k, int j) { return (int)(k1 - k < 32 ? k1 - k : 32) - 8 * j - 4 * half; };
-    auto load = [&](Stage32& f, int64_t k) {
+    const float* arow[MB];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int64_t kj = k + 8 * j + 4 * half;
+    for (int i = 0; i < MB; ++i) arow[i] = a + (16 * i + r < p.M ? 16 * i + r : p.M - 1) * p.lda;
+    int col[NS];
 #pragma unroll
-            for (int i = 0; i < MB; ++i)
-                f.x[i][j] = load16(a + (32 * i + r) * p.lda + kj, 32 * i + r < p.M ? have_k(k, j) : 0, k1);
+    for (int h = 0; h < NS; ++h) col[h] = 16 * h + r < cols ? 16 * h + r : cols - 1;
+    auto load = [&](St& f, int64_t k) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int64_t kj = k + 16 * j + 4 * g;
+#pragma unroll
+            for (int i = 0; i < MB; ++i) f.x[i][j] = load16(arow[i], kj, k1);
             if constexpr (BKM) {
-                f.w[j] = load16(b + (n0 + r) * p.ldb + kj, col ? have_k(k, j) : 0, k1);
+                f.w[j][0] = load16(b + (n0 + col[0]) * p.ldb, kj, k1);
             } else {
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    f.w[j][e] = col && kj + e < k1 ? __builtin_bit_cast(uint32_t, b[(kj + e) * p.ldb + n0 + r]) : 0u;
+                for (int h = 0; h < NS; ++h)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        f.w[j][h][e] = __builtin_bit_cast(uint32_t, b[(kj + e < k1 ? kj + e : k1 - 1) * p.ldb + n0 + col[h]]);
             }
         }
     };
-    auto use = [&](Stage32& f, int64_t k) {
+    auto use = [&](St& f, int64_t k) {
+        if (k1 - k < 32)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            if (k1 - k < 32) {
+            for (int j = 0; j < 2; ++j) {
+                const int64_t kj = k + 16 * j + 4 * g;
 #pragma unroll
-                for (int i = 0; i < MB; ++i) settle16<float>(f.x[i][j], 32 * i + r < p.M ? have_k(k, j) : 0, k1);
-                if constexpr (BKM) settle16<float>(f.w[j], col ? have_k(k, j) : 0, k1);
+                for (int i = 0; i < MB; ++i) settle16<float>(f.x[i][j], kj, k1);
+                if constexpr (BKM) {
+                    settle16<float>(f.w[j][0], kj, k1);
+                } else {
+#pragma unroll
+                    for (int h = 0; h < NS; ++h)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (kj + e >= k1) f.w[j][h][e] = 0u;
+                }
             }
-            const f4 w = __builtin_bit_cast(f4, f.w[j]);
 #pragma unroll
-            for (int i = 0; i < MB; ++i) {
-                const f4 x = __builtin_bit_cast(f4, f.x[i][j]);
+        for (int j = 0; j < 2; ++j)
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    acc[i] = __builtin_amdgcn_mfma_f32_32x32x2f32(w[e], x[e], acc[i], 0, 0, 0);
-            }
-        }
+            for (int i = 0; i < MB; ++i)
+#pragma unroll
+                for (int h = 0; h < NS; ++h) {
+                    const f4 w = __builtin_bit_cast(f4, f.w[j][h]), x = __builtin_bit_cast(f4, f.x[i][j]);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        acc[i][h] = __builtin_amdgcn_mfma_f32_16x16x4f32(w[e], x[e], acc[i][h], 0, 0, 0);
+                }
     };
-    if (k0 < k1) {
-        Stage32 f[2];
-        load(f[0], k0);
-        int64_t k = k0;
-        for (; k + 32 < k1; k += 64) {
-            load(f[1], k + 32);
-            use(f[0], k);
-            if (k + 64 < k1) load(f[0], k + 64);
-            use(f[1], k + 32);
-        }
-        if (k < k1) use(f[0], k);
-    }
-    join_waves<float, MB>(p, n0, acc, reinterpret_cast<float*>(smem), lane, wave);
+    part.template run<D, St>(load, use);
+    join_waves<float, MB, NS>(p, n0, acc, reinterpret_cast<float*>(smem), lane, wave);
 }
 
 // g = dropout(dy) f'(pre) into g [M, N] (unless NULL), and its column sums over
@@ -956,8 +1013,8 @@ struct TileTimes {
     int B, KT, fit;
     double alone, full, ends;
 };
-constexpr TileTimes T_DIRECT256{256, 64, 1, 1600, 1600, 9000}, T_DIRECT128{128, 64, 2, 950, 1150, 6000},
-    T_STAGED128{128, 64, 3, 2000, 2100, 7000}, T_SPLIT128{128, 16, 2, 950, 1350, 7000};
+constexpr TileTimes T_DIRECT256{256, 64, 1, 1600, 1600, 9000}, T_DIRECT128{128, 64, 2, 700, 1000, 6000},
+    T_STAGED128{128, 64, 3, 1500, 2000, 7000}, T_SPLIT128{128, 16, 2, 720, 1330, 7000};
 
 Cut cut(int dtype, int64_t M, int64_t N, int64_t K, bool direct)
 {
@@ -967,14 +1024,14 @@ Cut cut(int dtype, int64_t M, int64_t N, int64_t K, bool direct)
     for (int large = 0; large <= (direct ? 1 : 0); ++large) {
         const TileTimes& t = large ? T_DIRECT256 : dtype == CLIFF_F32 ? T_SPLIT128 : direct ? T_DIRECT128 : T_STAGED128;
         const int64_t tiles = ceil_div(M, t.B) * ceil_div(N, t.B), steps = std::max<int64_t>(1, ceil_div(K, t.KT));
-        for (int64_t want = 1; want <= 64 && want <= steps; ++want) {
+        for (const int want : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64, 96, 128, 192, 256}) {
+            if (want > steps) break;
             const int64_t per = ceil_div(steps, want), splits = ceil_div(steps, per);
-            if (splits != want) continue;
             const int64_t wgs = tiles * splits, rounds = wgs / (cus * t.fit), rest = wgs % (cus * t.fit);
             double ns = rounds * (per * t.full + t.ends);
             if (rest) ns += per * (rest <= cus ? t.alone : t.full) + t.ends;
             // the join: a launch, and the partial sums written and read
-            if (splits > 1) ns += 3500 + (double)M * N * 4 * (splits + 1) / 6000;
+            if (splits > 1) ns += 6000 + (double)M * N * 4 * 2 * splits / 12000;
             if (least == 0 || ns < least) {
                 least = ns;
                 best = Cut{large != 0, (int)splits, per * t.KT};
@@ -990,7 +1047,6 @@ constexpr int64_t FEW_ROWS = 64;  // up to which rows_kernel runs
 int64_t partial_bytes(int dtype, int64_t M, int64_t N, int64_t K, bool rows)
 {
     int64_t n = 0;
-    if (rows && M <= FEW_ROWS) return 0;
     for (int direct = 0; direct <= (dtype == CLIFF_F32 ? 0 : 1); ++direct) {
         const Cut c = cut(dtype, M, N, K, direct != 0);
         if (c.splits > 1) n = std::max(n, c.splits * M * N * 4);
@@ -1020,7 +1076,7 @@ cliff_status run(K k, const char* name, int B, int threads, int stage, const Pro
 template <typename T, bool BKM>
 cliff_status few_rows(const ProductArgs& p, hipStream_t stream)
 {
-    const int64_t wgs = ceil_div(p.N, 32);
+    const int64_t wgs = ceil_div(p.N, BKM || sizeof(T) == 4 ? 16 : 32);
     if (debug_enabled())
         fprintf(stderr, "cliffconv: product %lld x %lld x %lld, few rows, %lld workgroups\n", (long long)p.M,
                 (long long)p.N, (long long)p.K, (long long)wgs);
@@ -1029,9 +1085,9 @@ cliff_status few_rows(const ProductArgs& p, hipStream_t stream)
         return launched();
     };
     if constexpr (sizeof(T) == 4)
-        return p.M <= 32 ? go(rows_fp32_kernel<BKM, 1>) : go(rows_fp32_kernel<BKM, 2>);
+        return p.M <= 16 ? go(rows_fp32_kernel<BKM, 1>) : p.M <= 32 ? go(rows_fp32_kernel<BKM, 2>) : go(rows_fp32_kernel<BKM, 4>);
     else
-        return p.M <= 32 ? go(rows_kernel<T, BKM, 1>) : go(rows_kernel<T, BKM, 2>);
+        return p.M <= 16 ? go(rows_kernel<T, BKM, 1>) : p.M <= 32 ? go(rows_kernel<T, BKM, 2>) : go(rows_kernel<T, BKM, 4>);
 }
 
 // A product and, where its contraction is split, the join.
@@ -1039,7 +1095,7 @@ template <typename T, bool AKM, bool BKM>
 cliff_status product(int dtype, ProductArgs p, hipStream_t stream)
 {
     if constexpr (AKM)
-        if (p.M <= FEW_ROWS) return few_rows<T, BKM>(p, stream);
+        if (p.M <= FEW_ROWS && p.K >= per16<T> && (BKM || p.N >= per16<T>)) return few_rows<T, BKM>(p, stream);
     const bool direct = sizeof(T) == 2 && aligned_rows(p.a, p.lda, AKM ? p.K : p.M) &&
                         aligned_rows(p.b, p.ldb, BKM ? p.K : p.N);
     const Cut c = cut(dtype, p.M, p.N, p.K, direct);
@@ -1057,7 +1113,7 @@ cliff_status product(int dtype, ProductArgs p, hipStream_t stream)
             s = run(product_kernel<T, AKM, BKM, 128, 128, 2, 2, 64, true>, "direct", 128, 256, 2 * 2 * 128 * 64 * 2, p, stream);
     }
     if (s != CLIFF_OK || p.splits == 1) return s;
-    const int64_t blocks = ceil_div(ceil_div(p.M, 4) * ceil_div(p.N, 4), 256);
+    const int64_t blocks = ceil_div(p.M * ceil_div(p.N, 4), 64);
     if (blocks >= (int64_t)1 << 31) return CLIFF_EUNSUPPORTED;
     hipLaunchKernelGGL(join_kernel<T>, dim3((unsigned)blocks), dim3(256), 0, stream, p);
     return launched();

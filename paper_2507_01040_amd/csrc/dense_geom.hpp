@@ -38,13 +38,6 @@ struct Stage {
         const int l = e / line(), s = (e % line()) ^ swizzle(l);
         return KM ? 8 * s : l;
     }
-    // elements of slot e that exist, of a tile of `rows` rows and `left`
-    // contraction values (8 or more: all; 0 or less: none)
-    __host__ __device__ constexpr int slot_have(int e, int rows, int left) const
-    {
-        const int r = slot_row(e), k = slot_k(e);
-        return KM ? (r < rows ? left - k : 0) : (k < left ? rows - r : 0);
-    }
     // byte of element (row, k)
     __host__ __device__ constexpr int at(int row, int k) const
     {
@@ -67,18 +60,32 @@ __host__ __device__ constexpr int frag_byte(const Stage& s, int row0, int k0, in
     return s.at(row0 + (lane & 16) + 4 * (t & 3), k0 + frag_k(lane) + 4 * j + (t >> 2));
 }
 
-// The tile and split of workgroup bid.  Workgroups go round the 8 XCDs, so
-// each XCD gets a run of consecutive tiles; those go down 8 rows of tiles
-// before the next column, so that what runs together shares operands in its
-// L2.
+// The same for fragments of 16 rows by 32 values (v_mfma_*_16x16x32): lane l
+// holds row l & 15, values 8 (l >> 4) to + 7.
+__host__ __device__ constexpr int frag16_byte(const Stage& s, int row0, int k0, int lane, int j)
+{
+    if (s.KM) return s.at(row0 + (lane & 15), k0 + 8 * (lane >> 4));
+    const int t = lane & 15;
+    return s.at(row0 + 4 * (t & 3), k0 + 8 * (lane >> 4) + 4 * j + (t >> 2));
+}
+
+// Workgroups go round the 8 XCDs; workgroup bid's place in an order in which
+// each XCD has a run of neighbours, which share lines of its L2.
+__host__ __device__ inline uint32_t xcd_run(uint32_t bid, uint32_t total)
+{
+    const uint32_t q = total / 8, r = total % 8, xcd = bid % 8;
+    return xcd * q + (xcd < r ? xcd : r) + bid / 8;
+}
+
+// The tile and split of workgroup bid.  Each XCD gets a run of consecutive
+// tiles; those go down 8 rows of tiles before the next column, so that what
+// runs together shares operands in its L2.
 struct TileId {
     int m, n, split;
 };
 __host__ __device__ inline TileId tile_of(uint32_t bid, uint32_t tm, uint32_t tn, uint32_t splits)
 {
-    const uint32_t total = tm * tn * splits, q = total / 8, r = total % 8;
-    const uint32_t xcd = bid % 8, i = bid / 8;
-    const uint32_t t = xcd * q + (xcd < r ? xcd : r) + i;
+    const uint32_t t = xcd_run(bid, tm * tn * splits);
     const uint32_t split = t / (tm * tn), u = t % (tm * tn);
     const uint32_t g = u / (8 * tn), first = 8 * g, v = u % (8 * tn);
     const uint32_t rows = tm - first < 8 ? tm - first : 8;

@@ -32,16 +32,20 @@ __global__ __launch_bounds__(256) void dropout_kernel(DropoutArgs a, uint32_t pi
         step = (uint32_t)a.drop.rng[1];
     }
     raw16 x[ROWS], res[ROWS];
+    auto piece = [&](const void* from, int64_t ld, int r) {
+        const int64_t row = r0 + r < a.rows ? r0 + r : a.rows - 1;
+        const T* const line = static_cast<const T*>(from) + row * ld;
+        return a.d < E ? load16_narrow(line, col, a.d) : load16(line, col, a.d);
+    };
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) {
-        const int h = r0 + r < a.rows ? have : 0;
-        x[r] = load16(static_cast<const T*>(a.x) + (r0 + r) * a.ldx + col, h, a.d);
-        if (a.residual) res[r] = load16(static_cast<const T*>(a.residual) + (r0 + r) * a.ldr + col, h, a.d);
+        x[r] = piece(a.x, a.ldx, r);
+        if (a.residual) res[r] = piece(a.residual, a.ldr, r);
     }
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) {
         float v[E], u[E];
-        settle16<T>(x[r], have, a.d);
+        if (a.d >= E) settle16<T>(x[r], col, a.d);
         unpack16<T>(x[r], v);
         if (a.drop.rng)
 #pragma unroll
@@ -52,7 +56,7 @@ __global__ __launch_bounds__(256) void dropout_kernel(DropoutArgs a, uint32_t pi
                     v[4 * q + e] = w.w[e] <= a.drop.last ? 0.f : v[4 * q + e] * a.drop.scale;
             }
         if (a.residual) {
-            settle16<T>(res[r], have, a.d);
+            if (a.d >= E) settle16<T>(res[r], col, a.d);
             unpack16<T>(res[r], u);
 #pragma unroll
             for (int e = 0; e < E; ++e) v[e] += u[e];

@@ -208,41 +208,44 @@ typedef uint32_t raw16 __attribute__((ext_vector_type(4)));
 template <typename T>
 constexpr int per16 = 16 / (int)sizeof(T);  // elements in them
 
-// The 16 bytes from p on, of which `have` elements exist, in two steps, so that
-// many loads can be under way: load16, and settle16 where the value is used.
-// p is aligned to an element only.  A piece that ends past the row is loaded
-// from further left, where the row has it whole (`width`: elements of the row
-// up to and with the existing ones, 16 bytes or more), and shifted.  Elements
-// that do not exist become zeros.
+// The 16 bytes from element pos of a line on (aligned to an element only), of a
+// line whose elements before `end` may be read, in two steps, so that many loads
+// can be under way: load16, and settle16 where the value is used.  A piece that
+// passes the end is loaded from further left, where the line has it whole, and
+// shifted; elements that do not exist become zeros.  The line has 16 bytes or
+// more before its end; load16_narrow is for those that have not.
 template <typename T>
-__device__ inline raw16 load16(const T* p, int have, int64_t width)
+__device__ inline raw16 load16(const T* line, int64_t pos, int64_t end)
 {
-    constexpr int E = per16<T>;
-    raw16 r = {0, 0, 0, 0};
-    if (width >= E) {
-        if (have > 0) __builtin_memcpy(&r, have < E ? p + (have - E) : p, 16);
-    } else {
-        T t[E];
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-            t[e] = (T)0.f;
-            if (e < have) t[e] = p[e];
-        }
-        __builtin_memcpy(&r, t, 16);
-    }
+    raw16 r;
+    __builtin_memcpy(&r, line + (pos < end - per16<T> ? pos : end - per16<T>), 16);
     return r;
 }
 template <typename T>
-__device__ inline void settle16(raw16& r, int have, int64_t width)
+__device__ inline void settle16(raw16& r, int64_t pos, int64_t end)
 {
     constexpr int E = per16<T>;
-    if (have > 0 && have < E && width >= E) {
-        const int s = (E - have) * 8 * (int)sizeof(T);  // 16 to 112
-        uint64_t lo = r[0] | (uint64_t)r[1] << 32, hi = r[2] | (uint64_t)r[3] << 32;
-        lo = s >= 64 ? hi >> (s - 64) : lo >> s | hi << (64 - s);
-        hi = s >= 64 ? 0 : hi >> s;
-        r = raw16{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
+    const int64_t over = pos + E - end;  // elements past the end
+    if (over <= 0) return;
+    const int s = over < E ? (int)over * 8 * (int)sizeof(T) : 128;
+    uint64_t lo = r[0] | (uint64_t)r[1] << 32, hi = r[2] | (uint64_t)r[3] << 32;
+    lo = s >= 128 ? 0 : s >= 64 ? hi >> (s - 64) : lo >> s | hi << (64 - s);
+    hi = s >= 64 ? 0 : hi >> s;
+    r = raw16{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
+}
+template <typename T>
+__device__ inline raw16 load16_narrow(const T* line, int64_t pos, int64_t end)
+{
+    constexpr int E = per16<T>;
+    T t[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+        t[e] = (T)0.f;
+        if (pos + e < end) t[e] = line[pos + e];
     }
+    raw16 r;
+    __builtin_memcpy(&r, t, 16);
+    return r;
 }
 
 }  // namespace cliff

@@ -16,21 +16,27 @@ namespace {
 
 constexpr int wg_threads(int TPR) { return TPR > 256 ? TPR : 256; }
 
+template <typename T>
+__device__ inline raw16 load_piece(const T* row, int col, int64_t d)
+{
+    return d < per16<T> ? load16_narrow(row, col, d) : load16(row, col, d);
+}
 template <typename T, int TPR, int R, int C>
 __device__ inline void settle_rows(raw16 (&x)[R][C], int t, int64_t d)
 {
+    if (d < per16<T> || d == (int64_t)C * TPR * per16<T>) return;
 #pragma unroll
     for (int r = 0; r < R; ++r)
 #pragma unroll
-        for (int c = 0; c < C; ++c) settle16<T>(x[r][c], (int)d - (c * TPR + t) * per16<T>, d);
+        for (int c = 0; c < C; ++c) settle16<T>(x[r][c], (c * TPR + t) * per16<T>, d);
 }
 
 // The elements of a vector [d] from column col on.
 template <typename T>
 __device__ inline void load_vector(const T* v, int col, int64_t d, float* to)
 {
-    raw16 r = load16(v + col, (int)d - col, d);
-    settle16<T>(r, (int)d - col, d);
+    raw16 r = load_piece(v, col, d);
+    if (d >= per16<T>) settle16<T>(r, col, d);
     unpack16<T>(r, to);
 }
 
@@ -46,14 +52,16 @@ __global__ __launch_bounds__(wg_threads(TPR)) void norm_kernel(NormArgs a)
     const float inv = 1.0f / (float)a.d;
     for (int64_t r0 = (int64_t)blockIdx.x * G * R; r0 < a.rows; r0 += (int64_t)gridDim.x * G * R) {
         const int64_t rg = r0 + (int64_t)g * R;
+        int64_t rows[R];  // those that do not exist give way to the last one
+#pragma unroll
+        for (int r = 0; r < R; ++r) rows[r] = rg + r < a.rows ? rg + r : a.rows - 1;
         raw16 x[R][C];
 #pragma unroll
         for (int r = 0; r < R; ++r)
 #pragma unroll
             for (int c = 0; c < C; ++c) {
                 const int col = (c * TPR + t) * E;
-                x[r][c] = load16(static_cast<const T*>(a.x) + (rg + r) * a.ldx + col,
-                                 rg + r < a.rows ? (int)a.d - col : 0, a.d);
+                x[r][c] = load_piece(static_cast<const T*>(a.x) + rows[r] * a.ldx, col, a.d);
             }
         settle_rows<T, TPR, R, C>(x, t, a.d);
         float mean[R], sq[R];
@@ -140,15 +148,17 @@ __global__ __launch_bounds__(wg_threads(TPR), 2) void norm_backward_kernel(NormB
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             const bool row = rg + r < a.rows;
-            mean[r] = row ? a.mean[rg + r] : 0.f;
-            rstd[r] = row ? a.rstd[rg + r] : 0.f;
+            const int64_t m = row ? rg + r : a.rows - 1;
+            mean[r] = row ? a.mean[m] : 0.f;
+            rstd[r] = row ? a.rstd[m] : 0.f;
 #pragma unroll
             for (int c = 0; c < C; ++c) {
-                const int col = (c * TPR + t) * E, have = row ? (int)a.d - col : 0;
-                x[r][c] = load16(static_cast<const T*>(a.x) + (rg + r) * a.ldx + col, have, a.d);
-                dy[r][c] = load16(static_cast<const T*>(a.dy) + (rg + r) * a.lddy + col, have, a.d);
+                const int col = (c * TPR + t) * E;
+                x[r][c] = load_piece(static_cast<const T*>(a.x) + m * a.ldx, col, a.d);
+                dy[r][c] = load_piece(static_cast<const T*>(a.dy) + m * a.lddy, col, a.d);
+                if (!row) x[r][c] = dy[r][c] = raw16{0, 0, 0, 0};  // adds nothing to the sums
                 if (a.dresidual)
-                    res[r][c] = load16(static_cast<const T*>(a.dresidual) + (rg + r) * a.ldr + col, have, a.d);
+                    res[r][c] = load_piece(static_cast<const T*>(a.dresidual) + m * a.ldr, col, a.d);
             }
         }
         settle_rows<T, TPR, R, C>(x, t, a.d);

@@ -1,7 +1,7 @@
 // CPU check of the matrix-product kernels' address arithmetic (dense_geom.hpp):
 // every slot of a stage is filled once, a fragment read returns the elements
-// that the matrix instruction's lane needs, slots that are loaded whole lie
-// inside the matrix, and every tile and split belongs to one workgroup.
+// that the matrix instruction's lane needs, the lanes that are served at once use
+// different banks, and every tile and split belongs to one workgroup.
 #define __host__
 #define __device__
 #include "dense_geom.hpp"
@@ -40,13 +40,6 @@ static void stage(const Stage& s)
             x.k = k + (s.KM ? i : 0);
             REQUIRE(s.at(x.row, x.k) == 16 * e + 2 * i, "element (%d, %d)", x.row, x.k);
         }
-        // ragged tiles: a slot that is loaded whole lies inside
-        for (int rows : {1, 7, 8, s.R - 8, s.R - 1, s.R})
-            for (int left : {1, 8, 13, s.KT - 8, s.KT})
-                for (int i = 0; i < 8; ++i) {
-                    const bool in = (s.KM ? r : r + i) < rows && (s.KM ? k + i : k) < left;
-                    REQUIRE(in == (i < s.slot_have(e, rows, left)), "slot %d of %d x %d", e, rows, left);
-                }
     }
     std::set<std::pair<int, int>> seen;
     for (const El& x : lds) seen.insert({x.row, x.k});
@@ -69,6 +62,22 @@ static void stage(const Stage& s)
                         x = lds[b / 2 + t % 4];
                     }
                     REQUIRE(x.row == row0 + (lane & 31) && x.k == k0 + 8 * (lane >> 5) + i,
+                            "lane %d value %d: (%d, %d) at %d, %d", lane, i, x.row, x.k, row0, k0);
+                }
+    for (int row0 = 0; row0 < s.R; row0 += 16)
+        for (int k0 = 0; k0 + 32 <= s.KT; k0 += 32)
+            for (int lane = 0; lane < 64; ++lane)
+                for (int i = 0; i < 8; ++i) {
+                    El x;
+                    if (s.KM) {
+                        x = lds[frag16_byte(s, row0, k0, lane, 0) / 2 + i];
+                    } else {
+                        const int t = lane & 15, from = (lane & 48) + 4 * (i & 3) + t / 4;
+                        const int b = frag16_byte(s, row0, k0, from, i / 4);
+                        REQUIRE(b % 8 == 0 && b + 8 <= s.bytes(), "fragment byte %d", b);
+                        x = lds[b / 2 + t % 4];
+                    }
+                    REQUIRE(x.row == row0 + (lane & 15) && x.k == k0 + 8 * (lane >> 4) + i,
                             "lane %d value %d: (%d, %d) at %d, %d", lane, i, x.row, x.k, row0, k0);
                 }
     // banks: 32 lanes of a transposing read, 16 of a 16-byte read, at once
