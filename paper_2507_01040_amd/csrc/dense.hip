@@ -112,13 +112,6 @@ __device__ inline void drop4(const DropArgs& d, uint64_t key, uint32_t step, int
     for (int e = 0; e < 4; ++e) v[e] = w.w[e] <= d.last ? 0.f : v[e] * d.scale;
 }
 
-template <typename T>
-__device__ inline f4 bias4(const ProductArgs& p, int64_t n)
-{
-    if (!p.bias || n >= p.N) return f4{0.f, 0.f, 0.f, 0.f};
-    return load4(static_cast<const T*>(p.bias) + n, p.N - n < 4 ? (int)(p.N - n) : 4);
-}
-
 // Eight elements in 16-byte pieces (load16): one of a 16-bit type, two of fp32.
 template <typename T>
 struct Chunk {
@@ -286,10 +279,30 @@ struct Operand {
     }
 };
 
+// What the epilogue of a group of four columns needs besides their sums, loaded
+// early.
+struct Ends {
+    f4 bias;
+    uint64_t key;
+    uint32_t step;
+};
+template <typename T>
+__device__ inline Ends load_ends(const ProductArgs& p, int64_t n)
+{
+    Ends e{f4{0.f, 0.f, 0.f, 0.f}, 0, 0};
+    if (p.splits > 1) return e;  // the join's
+    if (p.bias && n < p.N) e.bias = load4(static_cast<const T*>(p.bias) + n, p.N - n < 4 ? (int)(p.N - n) : 4);
+    if (p.drop.rng) {
+        e.key = (uint64_t)p.drop.rng[0];
+        e.step = (uint32_t)p.drop.rng[1];
+    }
+    return e;
+}
+
 // R rows of a group of four columns: rows m, m + step, ...
 template <typename T, int R>
 __device__ inline void finish_rows(const ProductArgs& p, int64_t m, int step, int64_t n, const f4 (&v)[R],
-                                   const f4& bias)
+                                   const Ends& e)
 {
     const int have = p.N - n < 4 ? (int)(p.N - n) : 4;
     f4 res[R];
@@ -301,10 +314,10 @@ __device__ inline void finish_rows(const ProductArgs& p, int64_t m, int step, in
     for (int r = 0; r < R; ++r) {
         const int64_t row = m + r * step;
         if (row >= p.M) break;
-        f4 u = v[r] + bias;
+        f4 u = v[r] + e.bias;
         if (p.pre) store4(static_cast<T*>(p.pre) + row * p.ldp + n, u, have);
         activate4(p.act, u);
-        if (p.drop.rng) drop4(p.drop, (uint64_t)p.drop.rng[0], (uint32_t)p.drop.rng[1], row, n, u);
+        if (p.drop.rng) drop4(p.drop, e.key, e.step, row, n, u);
         if (p.residual) u += res[r];
         store4(static_cast<T*>(p.y) + row * p.ldy + n, u, have);
     }
@@ -317,6 +330,8 @@ template <typename T, int MI, int NI>
 __device__ inline void write_tile(const ProductArgs& p, const TileId& id, int64_t m1, int64_t n1,
                                   const f16v (&acc)[MI][NI], char* smem, int lane, int wave)
 {
+    const int64_t n = n1 + 4 * (lane & 15);
+    const Ends ends = load_ends<T>(p, n);
     __syncthreads();
     constexpr int EW = 64 + 4;  // floats per row there
     float* const tile = reinterpret_cast<float*>(smem) + wave * 32 * EW;
@@ -337,9 +352,7 @@ __device__ inline void write_tile(const ProductArgs& p, const TileId& id, int64_
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
-        const int64_t n = n1 + 4 * (lane & 15);
         if (n < p.N) {
-            const f4 bias = p.splits > 1 ? f4{0.f, 0.f, 0.f, 0.f} : bias4<T>(p, n);
 #pragma unroll 1
             for (int h = 0; h < 2; ++h) {
                 const int r0 = 16 * h + (lane >> 4);
@@ -354,7 +367,7 @@ __device__ inline void write_tile(const ProductArgs& p, const TileId& id, int64_
                             store4(p.partial + (id.split * p.M + m + 4 * r) * p.N + n, v[r],
                                    p.N - n < 4 ? (int)(p.N - n) : 4);
                 } else {
-                    finish_rows<T, 4>(p, m, 4, n, v, bias);
+                    finish_rows<T, 4>(p, m, 4, n, v, ends);
                 }
             }
         }
@@ -681,6 +694,9 @@ __global__ __launch_bounds__(256) void join_kernel(ProductArgs p)
     const int64_t m = i / nq, n = i % nq * 4;
     const int have = p.N - n < 4 ? (int)(p.N - n) : 4;
     f4 v[1] = {f4{0.f, 0.f, 0.f, 0.f}};
+    ProductArgs whole = p;
+    whole.splits = 1;
+    const Ends ends = load_ends<T>(whole, n);
     if (m < p.M) {
         const float* const q = p.partial + m * p.N + n;
 #pragma unroll 8
@@ -690,7 +706,7 @@ __global__ __launch_bounds__(256) void join_kernel(ProductArgs p)
     __syncthreads();
     if (wave || m >= p.M) return;
     v[0] = part[0][lane] + part[1][lane] + part[2][lane] + part[3][lane];
-    finish_rows<T, 1>(p, m, 1, n, v, bias4<T>(p, n));
+    finish_rows<T, 1>(p, m, 1, n, v, ends);
 }
 
 // Few rows (16 MB at most): bound by the read of B, so every workgroup streams
@@ -704,6 +720,9 @@ __device__ inline void join_waves(const ProductArgs& p, int64_t n0, const f4 (&a
                                   int wave)
 {
     constexpr int EW = 16 * NS + 4, PLANE = MB * 16 * EW;
+    const int r = threadIdx.x / (4 * NS), c = 4 * (threadIdx.x % (4 * NS));
+    const int64_t n = n0 + c;
+    const Ends ends = load_ends<T>(p, n);
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < MB; ++i)
@@ -712,13 +731,11 @@ __device__ inline void join_waves(const ProductArgs& p, int64_t n0, const f4 (&a
             *reinterpret_cast<f4*>(lds + wave * PLANE + (16 * i + (lane & 15)) * EW + 16 * j + 4 * (lane >> 4)) =
                 acc[i][j];
     __syncthreads();
-    const int r = threadIdx.x / (4 * NS), c = 4 * (threadIdx.x % (4 * NS));
-    const int64_t n = n0 + c;
     if (r >= 16 * MB || r >= p.M || n >= p.N) return;
     f4 v[1] = {f4{0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
     for (int w = 0; w < 8; ++w) v[0] += *reinterpret_cast<const f4*>(lds + w * PLANE + r * EW + c);
-    finish_rows<T, 1>(p, r, 1, n, v, bias4<T>(p, n));
+    finish_rows<T, 1>(p, r, 1, n, v, ends);
 }
 
 // What the eight waves share: the workgroup's columns, and a wave's part of the
