@@ -118,6 +118,18 @@ struct Chunk {
     raw16 v[sizeof(T) / 2];
 };
 
+// The three bf16 parts of eight floats.
+__device__ inline void split_chunk(const Chunk<float>& c, u4 (&t)[3])
+{
+#pragma unroll
+    for (int h = 0; h < 4; ++h) {
+        const f4 v = __builtin_bit_cast(f4, c.v[h >> 1]);
+        const Parts q = split2(v[2 * (h & 1)], v[2 * (h & 1) + 1]);
+#pragma unroll
+        for (int u = 0; u < 3; ++u) t[u][h] = q.t[u];
+    }
+}
+
 template <typename T>
 __device__ inline f16v mma(const u4& x, const u4& y, const f16v& c)
 {
@@ -230,13 +242,7 @@ struct Operand {
             char* const at = to + (i * NT + tid) * 16;
             if constexpr (sizeof(T) == 4) {
                 u4 t[3];
-#pragma unroll
-                for (int h = 0; h < 4; ++h) {
-                    const f4 v = __builtin_bit_cast(f4, c[i].v[h >> 1]);
-                    const Parts q = split2(v[2 * (h & 1)], v[2 * (h & 1) + 1]);
-#pragma unroll
-                    for (int u = 0; u < 3; ++u) t[u][h] = q.t[u];
-                }
+                split_chunk(c[i], t);
 #pragma unroll
                 for (int u = 0; u < 3; ++u) *reinterpret_cast<u4*>(at + u * S.bytes()) = t[u];
             } else {
@@ -952,6 +958,188 @@ __global__ __launch_bounds__(512, 2) void rows_fp32_kernel(ProductArgs p)
     join_waves<float, MB, NS>(p, n0, acc, reinterpret_cast<float*>(smem), lane, wave);
 }
 
+// Many rows and a short contraction: bound by the read of A and the write of y,
+// and a tile of the kernels above has too few stages to hide its begin and end.
+// So 128 columns of B stay in LDS (a panel, split for fp32), and each of eight
+// waves streams blocks of 32 rows past it without barriers, A from memory
+// straight into fragments, the next block's loads under the products of this one.
+// The panel lies as [plane][slot][column] in 16-byte slots, read without bank
+// conflicts; slot 2 kk + h has the 8 values of half-wave h in product group kk:
+// 16 kk + 8 h + i, or for fp32 (whose 8 are two loads) 16 kk + 4 h + i and 8 on,
+// so that a row's two lanes read neighbours.
+constexpr int PANEL = 128;
+template <typename T, bool BKM, int KK, bool WHOLE>
+__global__ __launch_bounds__(512, 2) void panel_kernel(ProductArgs p)
+{
+    constexpr bool F32 = sizeof(T) == 4;
+    constexpr int P = F32 ? 3 : 1, C = F32 ? 2 : 1, NJ = PANEL / 32, PLANE = 2 * KK * PANEL * 16, EW = 32 + 4,
+                  LINE = 128 / (16 * (int)sizeof(T)),  // product groups per line
+                  PF = F32 ? 4 : KK;                   // and those under way
+    extern __shared__ u4 smem4[];
+    char* const smem = reinterpret_cast<char*>(smem4);
+    const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const T* const a = static_cast<const T*>(p.a);
+    const T* const b = static_cast<const T*>(p.b);
+
+    const uint32_t panels = (uint32_t)((p.N + PANEL - 1) / PANEL), t = xcd_run(blockIdx.x, gridDim.x);
+    const int64_t n0 = (int64_t)(t % panels) * PANEL, stride = (int64_t)(gridDim.x / panels) * 8;
+    const int K = (int)p.K;
+    auto first = [&](int kk, int h, int c) { return 16 * kk + (F32 ? 4 * h + 8 * c : 8 * h); };
+    for (int i = tid; i < 2 * KK * PANEL; i += 512) {
+        const int col = i % PANEL, kk = i / PANEL / 2, h = i / PANEL % 2;
+        const int64_t n = n0 + col < p.N ? n0 + col : p.N - 1;  // (columns that do not exist are not written)
+        Chunk<T> v;
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            if constexpr (BKM) {
+                v.v[c] = load16(b + n * p.ldb, first(kk, h, c), K);
+                settle16<T>(v.v[c], first(kk, h, c), K);
+            } else {
+                T e[per16<T>];
+#pragma unroll
+                for (int u = 0; u < per16<T>; ++u) {
+                    const int k = first(kk, h, c) + u;
+                    e[u] = b[(k < K ? k : K - 1) * p.ldb + n];
+                    if (k >= K) e[u] = (T)0.f;
+                }
+                __builtin_memcpy(&v.v[c], e, 16);
+            }
+        }
+        if constexpr (F32) {
+            u4 s[3];
+            split_chunk(v, s);
+#pragma unroll
+            for (int q = 0; q < 3; ++q) *reinterpret_cast<u4*>(smem + q * PLANE + i * 16) = s[q];
+        } else {
+            *reinterpret_cast<u4*>(smem + i * 16) = v.v[0];
+        }
+    }
+    __syncthreads();
+
+    const int64_t blocks = (p.M + 31) / 32;
+    const int64_t b0 = (int64_t)(t / panels) * 8 + wave;
+    if (b0 >= blocks) return;
+    auto line = [&](int64_t blk) {
+        const int64_t row = 32 * blk + (lane & 31);
+        return a + (row < p.M ? row : p.M - 1) * p.lda;
+    };
+    const char* const mine = smem + (half * PANEL + (lane & 31)) * 16;
+    float* const tile = reinterpret_cast<float*>(smem + P * PLANE) + wave * 32 * EW;
+    Chunk<T> x[PF];
+    auto load = [&](const T* l, int kk) {
+#pragma unroll
+        for (int c = 0; c < C; ++c) x[kk % PF].v[c] = load16(l, first(kk, half, c), K);
+    };
+    auto fragment = [&](int kk, u4 (&to)[P]) {
+        if constexpr (!WHOLE)
+#pragma unroll
+            for (int c = 0; c < C; ++c) settle16<T>(x[kk % PF].v[c], first(kk, half, c), K);
+        if constexpr (F32) split_chunk(x[kk % PF], to);
+        else to[0] = x[kk % PF].v[0];
+    };
+    {
+        const T* const l = line(b0);
+#pragma unroll
+        for (int kk = 0; kk < PF; ++kk) load(l, kk);
+    }
+    for (int64_t blk = b0; blk < blocks; blk += stride) {
+        const T *const now = line(blk), *const next = line(blk + stride < blocks ? blk + stride : blk);
+        f16v acc[NJ];
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[j][e] = 0.f;
+        u4 w[2][P], xs[2][P];
+        auto read = [&](u4 (&to)[P], int kk, int j) {
+#pragma unroll
+            for (int q = 0; q < P; ++q)
+                to[q] = *reinterpret_cast<const u4*>(mine + q * PLANE + (2 * kk * PANEL + 32 * j) * 16);
+        };
+        read(w[0], 0, 0);
+        fragment(0, xs[0]);
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) {
+            if (kk % LINE == LINE - 1)  // whole lines of memory at once
+#pragma unroll
+                for (int l = kk - LINE + 1; l <= kk; ++l) {
+                    if (l + PF < KK) load(now, l + PF);
+                    else load(next, l + PF - KK);
+                }
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) {
+                const int u = (kk * NJ + j) & 1;
+                const bool last = j == NJ - 1;
+                if (!last) read(w[u ^ 1], kk, j + 1);
+                else if (kk + 1 < KK) read(w[u ^ 1], kk + 1, 0);
+                if (last && kk + 1 < KK) fragment(kk + 1, xs[(kk + 1) & 1]);
+                if constexpr (F32) {
+                    constexpr int QW[6] = {0, 2, 1, 0, 1, 0}, QX[6] = {2, 0, 1, 1, 0, 0};
+#pragma unroll
+                    for (int q = 0; q < 6; ++q) acc[j] = mma<T>(w[u][QW[q]], xs[kk & 1][QX[q]], acc[j]);
+                    if constexpr (WHOLE) {
+                        // the next fragments' reads, and the splitting, between the products
+#pragma unroll
+                        for (int q = 0; q < 6; ++q) {
+                            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                            if (q < 3) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                            if (last) __builtin_amdgcn_sched_group_barrier(0x002, 10, 0);
+                        }
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+                } else {
+                    acc[j] = mma<T>(w[u][0], xs[kk & 1][0], acc[j]);
+                }
+            }
+        }
+        if constexpr (F32) {
+            // sums that are infinite or NaN again as fp32 products, as above
+            float z = 0.f;
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) {
+                acc[j] *= SPLIT_UNSCALE;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) z = fmaf(acc[j][e], 0.f, z);
+            }
+            if (__ballot(z != 0.f)) {
+#pragma unroll
+                for (int j = 0; j < NJ; ++j)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) acc[j][e] = 0.f;
+                const T* const l = line(blk);
+                for (int k0 = 0; k0 < K; k0 += 2) {
+                    const int k = k0 + half;
+                    const float xv = k < K ? (float)l[k] : 0.f;
+#pragma unroll
+                    for (int j = 0; j < NJ; ++j) {
+                        const int64_t n = n0 + 32 * j + (lane & 31);
+                        const float wv = k < K && n < p.N ? (float)b[BKM ? n * p.ldb + k : k * p.ldb + n] : 0.f;
+                        acc[j] = __builtin_amdgcn_mfma_f32_32x32x2f32(wv, xv, acc[j], 0, 0, 0);
+                    }
+                }
+            }
+        }
+        // 32 columns at a time through LDS: 8 lanes hold a row's
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) {
+            const int64_t n = n0 + 32 * j + 4 * (lane & 7), m = 32 * blk + (lane >> 3);
+            const Ends ends = load_ends<T>(p, n);
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+                *reinterpret_cast<f4*>(tile + (lane & 31) * EW + 8 * g + 4 * half) =
+                    f4{acc[j][4 * g], acc[j][4 * g + 1], acc[j][4 * g + 2], acc[j][4 * g + 3]};
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+            f4 v[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) v[r] = *reinterpret_cast<const f4*>(tile + ((lane >> 3) + 8 * r) * EW + 4 * (lane & 7));
+            if (m < p.M && n < p.N) finish_rows<T, 4>(p, m, 8, n, v, ends);
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+        }
+    }
+}
+
 // g = dropout(dy) f'(pre) into g [M, N] (unless NULL), and its column sums over
 // a share of the rows into sums [part][N] (unless NULL).  A workgroup takes 256
 // columns; its four waves every fourth row each.
@@ -1107,12 +1295,41 @@ cliff_status few_rows(const ProductArgs& p, hipStream_t stream)
         return p.M <= 16 ? go(rows_kernel<T, BKM, 1>) : p.M <= 32 ? go(rows_kernel<T, BKM, 2>) : go(rows_kernel<T, BKM, 4>);
 }
 
+// Rows from which, and contraction up to which, the panel kernel is ahead of the
+// tiles, and its launch.
+constexpr int64_t PANEL_ROWS = 16384;
+constexpr int64_t PANEL_K = 128;
+
+template <typename T, bool BKM>
+cliff_status panel(const ProductArgs& p, hipStream_t stream)
+{
+    const int64_t panels = ceil_div(p.N, PANEL), cus = std::max(device_cus(), 1);
+    const int64_t groups = std::min(std::max<int64_t>(1, cus / panels), ceil_div(p.M, 32 * 8));
+    if (panels * groups >= (int64_t)1 << 31) return CLIFF_EUNSUPPORTED;
+    if (debug_enabled())
+        fprintf(stderr, "cliffconv: product %lld x %lld x %lld, panels, %lld workgroups\n", (long long)p.M,
+                (long long)p.N, (long long)p.K, (long long)(panels * groups));
+    const auto go = [&](auto k, int KK) {
+        const int lds = (sizeof(T) == 4 ? 3 : 1) * 2 * KK * PANEL * 16 + 8 * 32 * (32 + 4) * 4;
+        hipLaunchKernelGGL(k, dim3((unsigned)(panels * groups)), dim3(512), lds, stream, p);
+        return launched();
+    };
+    const auto sized = [&](auto kk) {
+        constexpr int KK = decltype(kk)::value;
+        return p.K == 16 * KK ? go(panel_kernel<T, BKM, KK, true>, KK) : go(panel_kernel<T, BKM, KK, false>, KK);
+    };
+    if (p.K <= 64) return sized(std::integral_constant<int, 4>{});
+    return sized(std::integral_constant<int, 8>{});
+}
+
 // A product and, where its contraction is split, the join.
 template <typename T, bool AKM, bool BKM>
 cliff_status product(int dtype, ProductArgs p, hipStream_t stream)
 {
     if constexpr (AKM)
         if (p.M <= FEW_ROWS && p.K >= per16<T> && (BKM || p.N >= per16<T>)) return few_rows<T, BKM>(p, stream);
+    if constexpr (AKM)
+        if (p.M >= PANEL_ROWS && p.K <= PANEL_K && p.K >= per16<T>) return panel<T, BKM>(p, stream);
     const bool direct = sizeof(T) == 2 && aligned_rows(p.a, p.lda, AKM ? p.K : p.M) &&
                         aligned_rows(p.b, p.ldb, BKM ? p.K : p.N);
     const Cut c = cut(dtype, p.M, p.N, p.K, direct);
