@@ -782,7 +782,7 @@ struct RowsPart {
 template <typename T, bool BKM, int MB>
 __global__ __launch_bounds__(512, 2) void rows_kernel(ProductArgs p)
 {
-    constexpr int NS = BKM ? 1 : 2, D = MB == 4 ? 2 : 4;
+    constexpr int NS = BKM ? 1 : 2, D = MB == 4 ? 2 : BKM ? 8 : 4;  // what the registers hold
     constexpr Stage S{32, 64, false};
     constexpr int JOIN = MB * 16 * (16 * NS + 4) * 4;
     __shared__ __align__(16) char smem[8 * (BKM || JOIN > S.bytes() ? JOIN : S.bytes())];

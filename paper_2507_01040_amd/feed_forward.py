@@ -14,6 +14,7 @@ checks once, for a call that is repeated on the same buffers.
 from __future__ import annotations
 
 import ctypes
+import functools
 from typing import Optional, Tuple
 
 import paper_2507_01040_amd as _pkg
@@ -185,8 +186,20 @@ class FeedForwardPlan(_pkg.Plan):
     """A Plan whose output may be a tuple of tensors.  Called for another
     stream, it tells torch's allocator that its buffers are used there."""
 
+    def __init__(self, fn, args, stream_index: int, name: str, out, keep, own=()):
+        # converted once: a call that is repeated is mostly this and the launch
+        args = [t(a) if isinstance(a, (int, float)) else a for t, a in zip(fn.argtypes, args)]
+        super().__init__(fn, args, stream_index, name, out, keep)
+        self._own = own
+        self._same_stream = functools.partial(fn, *args)
+
     def __call__(self, stream=None):
-        if stream is not None and hasattr(stream, "cuda_stream"):
+        if stream is None:
+            st = self._same_stream()
+            if st != _pkg.CLIFF_OK:
+                raise _pkg.CliffError(st, self._name)
+            return self.out
+        if hasattr(stream, "cuda_stream"):
             for t in self._own:
                 t.record_stream(stream)
         return super().__call__(stream)
@@ -199,9 +212,7 @@ def _plan(fn_name: str, args, out, keep, own, stream) -> FeedForwardPlan:
         for t in own:
             t.record_stream(stream)
     args = (*args, _pkg._stream_ptr(stream) or None)
-    p = FeedForwardPlan(getattr(_pkg.load(), fn_name), args, len(args) - 1, fn_name, out, keep)
-    p._own = own
-    return p
+    return FeedForwardPlan(getattr(_pkg.load(), fn_name), args, len(args) - 1, fn_name, out, keep, own)
 
 
 class _Buffers:
