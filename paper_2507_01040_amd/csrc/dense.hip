@@ -79,12 +79,13 @@ __device__ inline void store4(T* p, const f4& v, int have)
     }
 }
 
+template <bool FINE>
 __device__ inline void activate4(int act, f4& v)
 {
     switch (act) {
 #define EACH(A)                                      \
     case A:                                          \
-        for (int e = 0; e < 4; ++e) v[e] = activate(A, v[e]); \
+        for (int e = 0; e < 4; ++e) v[e] = activate<FINE>(A, v[e]); \
         break;
         EACH(CLIFF_ACT_RELU)
         EACH(CLIFF_ACT_GELU)
@@ -92,12 +93,13 @@ __device__ inline void activate4(int act, f4& v)
 #undef EACH
     }
 }
+template <bool FINE>
 __device__ inline void slope4(int act, f4& v, const f4& pre)
 {
     switch (act) {
 #define EACH(A)                                                  \
     case A:                                                      \
-        for (int e = 0; e < 4; ++e) v[e] *= activate_slope(A, pre[e]); \
+        for (int e = 0; e < 4; ++e) v[e] *= activate_slope<FINE>(A, pre[e]); \
         break;
         EACH(CLIFF_ACT_RELU)
         EACH(CLIFF_ACT_GELU)
@@ -322,7 +324,7 @@ __device__ inline void finish_rows(const ProductArgs& p, int64_t m, int step, in
         if (row >= p.M) break;
         f4 u = v[r] + e.bias;
         if (p.pre) store4(static_cast<T*>(p.pre) + row * p.ldp + n, u, have);
-        activate4(p.act, u);
+        activate4<sizeof(T) == 4>(p.act, u);
         if (p.drop.rng) drop4(p.drop, e.key, e.step, row, n, u);
         if (p.residual) u += res[r];
         store4(static_cast<T*>(p.y) + row * p.ldy + n, u, have);
@@ -1163,7 +1165,7 @@ __global__ __launch_bounds__(256) void slope_kernel(DenseBackwardArgs a, T* g, f
         for (int64_t r = r0 + wave; r < r1; r += 4) {
             f4 v = load4(static_cast<const T*>(a.dy) + r * a.lddy + c, have);
             if (a.act != CLIFF_ACT_NONE)
-                slope4(a.act, v, load4(static_cast<const T*>(a.pre) + r * a.ldp + c, have));
+                slope4<sizeof(T) == 4>(a.act, v, load4(static_cast<const T*>(a.pre) + r * a.ldp + c, have));
             if (a.drop.rng) drop4(a.drop, key, step, r, c, v);
             if (g) store4(g + r * a.N + c, v, have);
             t += v;

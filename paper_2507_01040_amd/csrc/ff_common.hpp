@@ -157,11 +157,19 @@ __device__ inline float reciprocal(float v) { return __builtin_amdgcn_rcpf(v); }
 // smoothly from 1/2 and is a polynomial in t = 1 / (1 + 0.3 |v|) without
 // constant term, fitted to the least relative error (1.5e-7 over the whole
 // axis, 5e-7 as evaluated), so that small values of the left tail keep their
-// digits.
+// digits.  FINE: what the exponent's rounding takes from e (4e-6 of it at |v| =
+// 12) is put back; 16-bit results do not show it.
+template <bool FINE>
 __device__ inline float gelu_cdf(float v, float& e)
 {
     const float a = fabsf(v), t = reciprocal(fmaf(0.3f, a, 1.0f));
-    e = __expf(-0.5f * v * v);
+    constexpr float C = -0.72134752f, C_REST = -9.62981495e-9f;  // -log2(e) / 2 = C + C_REST
+    const float s = v * v, x = s * C;
+    e = __builtin_amdgcn_exp2f(x);
+    if constexpr (FINE) {
+        const float rest = fmaf(s, C, -x) + fmaf(s, C_REST, fmaf(v, v, -s) * C);
+        if (s < 1e4f) e = fmaf(e, rest * 0.69314718f, e);
+    }
     float r = fmaf(0.0356758006f, t, -0.157207165f);
     r = fmaf(r, t, 0.206360237f);
     r = fmaf(r, t, -0.0536895875f);
@@ -173,24 +181,26 @@ __device__ inline float gelu_cdf(float v, float& e)
     return v < 0.f ? r : 1.0f - r;
 }
 
+template <bool FINE>
 __device__ inline float activate(int act, float v)
 {
     float e;
     switch (act) {
     case CLIFF_ACT_RELU: return v > 0.f ? v : 0.f;
-    case CLIFF_ACT_GELU: return v * gelu_cdf(v, e);
+    case CLIFF_ACT_GELU: return v * gelu_cdf<FINE>(v, e);
     case CLIFF_ACT_SILU: return v * reciprocal(1.0f + __expf(-v));
     }
     return v;
 }
 
+template <bool FINE>
 __device__ inline float activate_slope(int act, float v)
 {
     float e;
     switch (act) {
     case CLIFF_ACT_RELU: return v > 0.f ? 1.f : 0.f;
     case CLIFF_ACT_GELU: {
-        const float c = gelu_cdf(v, e);
+        const float c = gelu_cdf<FINE>(v, e);
         return fmaf(v * 0.39894228040143268f, e, c);
     }
     case CLIFF_ACT_SILU: {

@@ -53,11 +53,16 @@ def _times(v, m):
     return v if m is None else torch.where(m == 0, torch.zeros_like(v), v * m)
 
 
+def _phi(v):
+    # torch's ndtr loses the left tail to cancellation (1e-16 of 1)
+    return 0.5 * torch.special.erfc(-v * 0.5 ** 0.5)
+
+
 def act(a, v):
     if a == 1:
         return torch.clamp(v, min=0.0)
     if a == 2:
-        return v * torch.special.ndtr(v)
+        return v * _phi(v)
     if a == 3:
         return v * torch.sigmoid(v)
     return v
@@ -67,7 +72,7 @@ def slope(a, v):
     if a == 1:
         return (v > 0).double()
     if a == 2:
-        return torch.special.ndtr(v) + v * torch.exp(-v * v / 2) / np.sqrt(2 * np.pi)
+        return _phi(v) + v * torch.exp(-v * v / 2) / np.sqrt(2 * np.pi)
     if a == 3:
         s = torch.sigmoid(v)
         return s + v * s * (1 - s)

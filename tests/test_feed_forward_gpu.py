@@ -410,3 +410,95 @@ def test_leading_axes():
     y, _, _ = P.layer_norm(mv.flatten(1))
     assert y.shape == (10, 32)
     assert P.dense(x[0, 0], w).shape == (12,)
+
+
+# many rows and a short contraction: the panel kernel (rows from 16384, K up to 128)
+@pytest.mark.parametrize("order", ["io", "oi"])
+@pytest.mark.parametrize("size", [(16384, 128, 128), (16385, 64, 300), (20001, 100, 129), (16400, 13, 520), (40003, 17, 8),
+                                  (17000, 128, 1), (33333, 8, 257)], ids=str)
+@pytest.mark.parametrize("dtype", DTYPES, ids=ids)
+def test_dense_short_contraction(dtype, size, order):
+    M, K, N = size
+    d = Draw(M + K + N, dtype)
+    x, w, b, res = d.rows(M, K, 3), d.weight(K, N, order), d.vector(N), d.rows(M, N)
+    y, intact = guarded(M, N, dtype)
+    got, pre = P.dense(x, w, b, act=P.ACT_SILU, dropout=(0.2, rng()), residual=res, pre=True, out=y)
+    want, want_pre = O.dense(x, w, b, 3, (0.2, (KEY, STEP)), res, dtype)
+    O.check(pre, want_pre, "pre")
+    O.check(got, want, "y")
+    assert intact()
+
+
+@pytest.mark.parametrize("M,K,N", [(5, 96, 80), (40, 520, 48), (16390, 112, 80), (300, 640, 80)])
+def test_dense_not_finite_paths(M, K, N):
+    # fp32 by every kernel: few rows, panels, tiles (split contraction too):
+    # infinities stay in their rows and columns, and values that bf16 parts
+    # cannot hold come out as fp32 products give them
+    d = Draw(14, torch.float32)
+    x, w = d.rows(M, K), d.weight(K, N, "io")
+    x[2, 3] = float("inf")
+    x[3] = 0.0
+    x[3, 1] = 3e38
+    w[5, 7] = float("nan")
+    w[1, 9] = 2.0 ** -126
+    y = P.dense(x, w).cpu().double()
+    v, e = O.dense(x, w, None, 0, None, None, torch.float32)[0]
+    good = torch.isfinite(v)
+    big = v.abs() > 3.4e38
+    assert torch.equal(torch.isnan(y), torch.isnan(v))
+    assert not torch.isfinite(y[~good]).any() and (y[big & good].abs() > 3e38).all()
+    assert float(((y - v).abs() - e)[good & ~big].max()) <= 0
+
+
+def test_dense_split_contraction():
+    # few outputs and a long contraction: parts joined in order, the epilogue in the join
+    for dtype in DTYPES:
+        d = Draw(15, dtype)
+        for M, K, N, order in ((96, 8192, 72, "io"), (130, 5003, 61, "oi"), (72, 4096, 256, "oi")):
+            x, w, b, res = d.rows(M, K), d.weight(K, N, order), d.vector(N), d.rows(M, N)
+            y, intact = guarded(M, N, dtype)
+            P.dense(x, w, b, act=P.ACT_GELU, dropout=(0.15, rng()), residual=res, out=y)
+            O.check(y, O.dense(x, w, b, 2, (0.15, (KEY, STEP)), res, dtype)[0], str((M, K, N)))
+            assert intact()
+            again = P.dense(x, w, b, act=P.ACT_GELU, dropout=(0.15, rng()), residual=res)
+            assert torch.equal(again, y)
+
+
+def test_dense_large_tiles():
+    # 256 x 256 tiles with ragged edges, both orders, and their gradient
+    for dtype in (torch.bfloat16, torch.float16):
+        d = Draw(16, dtype)
+        M, K, N = 2100, 1096, 2008
+        for order in ("io", "oi"):
+            x, w, b = d.rows(M, K), d.weight(K, N, order), d.vector(N)
+            O.check(P.dense(x, w, b, act=P.ACT_RELU), O.dense(x, w, b, 1, None, None, dtype)[0], order)
+            dy = d.rows(M, N)
+            for got, v, name in zip(P.dense_backward(dy, x, w), O.dense_backward(dy, x, w, None, 0, None, dtype),
+                                    ("dx", "dw", "db")):
+                O.check(got, v, name)
+
+
+def test_dense_in_place_residual():
+    # y may be the residual, by every kernel
+    for M, K, N in ((3, 64, 72), (200, 96, 264), (100, 4096, 40), (16400, 64, 96)):
+        d = Draw(17, torch.bfloat16)
+        x, w, res = d.rows(M, K), d.weight(K, N, "io"), d.rows(M, N)
+        want = P.dense(x, w, residual=res)
+        assert torch.equal(P.dense(x, w, residual=res, out=res), want)
+
+
+def test_activations_over_the_range():
+    # values and slopes at every fp32 exponent that matters, at the ends too
+    v = torch.cat([torch.linspace(-12, 12, 4001), torch.tensor([-100.0, 100.0, -3e38, 3e38, 0.0, -0.0, 1e-30, -1e-30])])
+    x = v.to("cuda:0")[:, None]
+    one = torch.ones(1, 1, device="cuda:0")
+    for act in (P.ACT_RELU, P.ACT_GELU, P.ACT_SILU):
+        y = P.dense(x, one, act=act).cpu().double()[:, 0]
+        want = O.act(act, v.double())
+        # 16 roundings of the value, and of the value's size near zero
+        assert float(((y - want).abs() - 2.0 ** -20 * want.abs() - 1e-37)[v > -12.1].max()) <= 0, act
+        assert torch.isfinite(y).all()
+        g = P.dense_backward(torch.ones_like(x), x, one, pre=x, act=act)[0].cpu().double()[:, 0]
+        want = O.slope(act, v.double())
+        inside = v.abs() < 1e30
+        assert float((g - want).abs()[inside].max()) <= 2.0 ** -20 * 2, act
