@@ -197,14 +197,17 @@ struct Operand {
         const int64_t n = vals - (int64_t)s * S.KT;
         return n < S.KT ? (int)n : S.KT;
     }
-    // A thread's slots of the first stage (loads through registers); the next
-    // stage's are `advance` elements on.
+    // Loads through registers.  Whether the rows are whole slots: those that do
+    // not exist then give way to others, for nothing reads their products.
+    __device__ bool plain() const { return S.KM || rows == S.R || rows % 8 == 0; }
+    // A thread's slots of the first stage of a plain tile; the next stage's are
+    // `advance` elements on.
     __device__ void pointers(const T* (&at)[L], int tid) const
     {
 #pragma unroll
         for (int i = 0; i < L; ++i) {
-            const int e = i * NT + tid, r = S.slot_row(e), k = S.slot_k(e);
-            at[i] = x + (S.KM ? r * ld + k : k * ld + r);
+            const int e = i * NT + tid, r = S.slot_row(e), k = S.slot_k(e), last = S.KM ? rows - 1 : rows - 8;
+            at[i] = x + (S.KM ? (r < last ? r : last) * ld + k : k * ld + (r < last || last < 0 ? r : last));
         }
     }
     __device__ int64_t advance() const { return S.KM ? S.KT : S.KT * ld; }
@@ -217,18 +220,20 @@ struct Operand {
             at[i] += advance();
         }
     }
-    // (of a tile or stage that is not whole; what it lacks is zeroed in store)
+    // (of a tile that is not plain or a stage that is not whole; what it lacks is
+    // zeroed in store)
     __device__ void fetch(Chunk<T> (&c)[L], const T* (&at)[L], int s, int tid) const
     {
         const int n = left(s);
-        if (n == S.KT && rows == S.R) return fetch_whole(c, at);
+        if (n == S.KT && plain()) return fetch_whole(c, at);
+        const T* const stage = x + s * advance();
 #pragma unroll
         for (int i = 0; i < L; ++i) {
             const int e = i * NT + tid, r = S.slot_row(e), k = S.slot_k(e);
             // the slot's line, from the tile's first element there; lines that do
             // not exist give way to the last one
             const int line = S.KM ? r : k, lines = S.KM ? rows : n, pos = S.KM ? k : r, end = S.KM ? n : rows;
-            const T* const p = at[i] - pos + (line < lines ? 0 : (lines - 1 - line) * ld);
+            const T* const p = stage + (line < lines ? line : lines - 1) * ld;
 #pragma unroll
             for (int h = 0; h < (int)sizeof(T) / 2; ++h)
                 c[i].v[h] = width < per16<T> ? load16_narrow(p, pos + h * per16<T>, end)
@@ -255,7 +260,7 @@ struct Operand {
     __device__ void store(Chunk<T> (&c)[L], int s, char* to, int tid) const
     {
         const int n = left(s);
-        if (n < S.KT || rows < S.R)
+        if (n < S.KT || !plain())
 #pragma unroll
             for (int i = 0; i < L; ++i) {
                 const int e = i * NT + tid, r = S.slot_row(e), k = S.slot_k(e);
@@ -307,27 +312,32 @@ __device__ inline Ends load_ends(const ProductArgs& p, int64_t n)
     return e;
 }
 
-// R rows of a group of four columns: rows m, m + step, ...
-template <typename T, int R>
+// R rows of a group of four columns: rows m, m + step, ...  WHOLE: all of them
+// exist (no branches then, so that waits for earlier loads need not wait for
+// these stores).
+template <typename T, int R, bool WHOLE = false>
 __device__ inline void finish_rows(const ProductArgs& p, int64_t m, int step, int64_t n, const f4 (&v)[R],
                                    const Ends& e)
 {
-    const int have = p.N - n < 4 ? (int)(p.N - n) : 4;
+    const int have = WHOLE || p.N - n >= 4 ? 4 : (int)(p.N - n);
     f4 res[R];
-    if (p.residual)
+    if (p.residual) {
+        const T* const from = static_cast<const T*>(p.residual) + m * p.ldr + n;
 #pragma unroll
         for (int r = 0; r < R; ++r)
-            if (m + r * step < p.M) res[r] = load4(static_cast<const T*>(p.residual) + (m + r * step) * p.ldr + n, have);
+            if (WHOLE || m + r * step < p.M) res[r] = load4(from + r * (step * p.ldr), have);
+    }
+    T* const y = static_cast<T*>(p.y) + m * p.ldy + n;
+    T* const pre = static_cast<T*>(p.pre) + m * p.ldp + n;
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-        const int64_t row = m + r * step;
-        if (row >= p.M) break;
+        if (!WHOLE && m + r * step >= p.M) break;
         f4 u = v[r] + e.bias;
-        if (p.pre) store4(static_cast<T*>(p.pre) + row * p.ldp + n, u, have);
+        if (p.pre) store4(pre + r * (step * p.ldp), u, have);
         activate4<sizeof(T) == 4>(p.act, u);
-        if (p.drop.rng) drop4(p.drop, e.key, e.step, row, n, u);
+        if (p.drop.rng) drop4(p.drop, e.key, e.step, m + r * step, n, u);
         if (p.residual) u += res[r];
-        store4(static_cast<T*>(p.y) + row * p.ldy + n, u, have);
+        store4(y + r * (step * p.ldy), u, have);
     }
 }
 
@@ -650,7 +660,7 @@ __global__ __launch_bounds__(256, 2) void split_product_kernel(ProductArgs p)
     __syncthreads();
     read(0, smem);
     __syncthreads();  // stage 2 takes the place of stage 0
-    const int whole = a.rows == BM && b.rows == BN ? (int)(kn / KT) : 0;  // whole stages
+    const int whole = a.plain() && b.plain() ? (int)(kn / KT) : 0;  // whole stages
     int s = 0;
     for (; s + 5 < whole; s += 2) {
         step(s, even, yes);
@@ -976,7 +986,7 @@ __global__ __launch_bounds__(512, 2) void panel_kernel(ProductArgs p)
     constexpr bool F32 = sizeof(T) == 4;
     constexpr int P = F32 ? 3 : 1, C = F32 ? 2 : 1, NJ = PANEL / 32, PLANE = 2 * KK * PANEL * 16, EW = 32 + 4,
                   LINE = 128 / (16 * (int)sizeof(T)),  // product groups per line
-                  PF = F32 ? 4 : KK;                   // and those under way
+                  PF = F32 ? LINE : KK;                // and those under way
     extern __shared__ u4 smem4[];
     char* const smem = reinterpret_cast<char*>(smem4);
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
@@ -988,6 +998,8 @@ __global__ __launch_bounds__(512, 2) void panel_kernel(ProductArgs p)
     const int64_t n0 = (int64_t)(t % panels) * PANEL, stride = (int64_t)(gridDim.x / panels) * 8;
     const int K = (int)p.K;
     auto first = [&](int kk, int h, int c) { return 16 * kk + (F32 ? 4 * h + 8 * c : 8 * h); };
+    float* const bl = reinterpret_cast<float*>(smem + P * PLANE);
+    if (tid < PANEL) bl[tid] = p.bias && n0 + tid < p.N ? (float)static_cast<const T*>(p.bias)[n0 + tid] : 0.f;
     for (int i = tid; i < 2 * KK * PANEL; i += 512) {
         const int col = i % PANEL, kk = i / PANEL / 2, h = i / PANEL % 2;
         const int64_t n = n0 + col < p.N ? n0 + col : p.N - 1;  // (columns that do not exist are not written)
@@ -1027,7 +1039,8 @@ __global__ __launch_bounds__(512, 2) void panel_kernel(ProductArgs p)
         return a + (row < p.M ? row : p.M - 1) * p.lda;
     };
     const char* const mine = smem + (half * PANEL + (lane & 31)) * 16;
-    float* const tile = reinterpret_cast<float*>(smem + P * PLANE) + wave * 32 * EW;
+    float* const tile = bl + PANEL + wave * 32 * EW;
+    Ends ends = load_ends<T>(p, p.N);  // (the generator's; the bias is in LDS)
     Chunk<T> x[PF];
     auto load = [&](const T* l, int kk) {
 #pragma unroll
@@ -1121,23 +1134,43 @@ __global__ __launch_bounds__(512, 2) void panel_kernel(ProductArgs p)
                 }
             }
         }
-        // 32 columns at a time through LDS: 8 lanes hold a row's
-#pragma unroll
-        for (int j = 0; j < NJ; ++j) {
-            const int64_t n = n0 + 32 * j + 4 * (lane & 7), m = 32 * blk + (lane >> 3);
-            const Ends ends = load_ends<T>(p, n);
+        // 32 columns at a time through LDS: 8 lanes hold a row's.  A block that is
+        // not whole ends with a wait for all of its stores.
+        auto turn = [&](const f16v& c, f4 (&v)[4]) {
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
 #pragma unroll
             for (int g = 0; g < 4; ++g)
                 *reinterpret_cast<f4*>(tile + (lane & 31) * EW + 8 * g + 4 * half) =
-                    f4{acc[j][4 * g], acc[j][4 * g + 1], acc[j][4 * g + 2], acc[j][4 * g + 3]};
+                    f4{c[4 * g], c[4 * g + 1], c[4 * g + 2], c[4 * g + 3]};
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             __builtin_amdgcn_wave_barrier();
-            f4 v[4];
 #pragma unroll
             for (int r = 0; r < 4; ++r) v[r] = *reinterpret_cast<const f4*>(tile + ((lane >> 3) + 8 * r) * EW + 4 * (lane & 7));
-            if (m < p.M && n < p.N) finish_rows<T, 4>(p, m, 8, n, v, ends);
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-            __builtin_amdgcn_wave_barrier();
+        };
+        const int64_t m = 32 * blk + (lane >> 3);
+        f4 v[4];
+        if (32 * blk + 32 <= p.M && n0 + PANEL <= p.N) {
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) {
+                turn(acc[j], v);
+                ends.bias = *reinterpret_cast<const f4*>(bl + 32 * j + 4 * (lane & 7));
+                finish_rows<T, 4, true>(p, m, 8, n0 + 32 * j + 4 * (lane & 7), v, ends);
+            }
+        } else {
+#pragma unroll 1
+            for (int j = 0; j < NJ; ++j) {
+                switch (j) {
+                case 0: turn(acc[0], v); break;
+                case 1: turn(acc[1], v); break;
+                case 2: turn(acc[2], v); break;
+                case 3: turn(acc[3], v); break;
+                }
+                const int64_t n = n0 + 32 * j + 4 * (lane & 7);
+                ends.bias = *reinterpret_cast<const f4*>(bl + 32 * j + 4 * (lane & 7));
+                if (n < p.N) finish_rows<T, 4>(p, m, 8, n, v, ends);
+            }
+            wait_direct();
         }
     }
 }
@@ -1312,7 +1345,7 @@ cliff_status panel(const ProductArgs& p, hipStream_t stream)
         fprintf(stderr, "cliffconv: product %lld x %lld x %lld, panels, %lld workgroups\n", (long long)p.M,
                 (long long)p.N, (long long)p.K, (long long)(panels * groups));
     const auto go = [&](auto k, int KK) {
-        const int lds = (sizeof(T) == 4 ? 3 : 1) * 2 * KK * PANEL * 16 + 8 * 32 * (32 + 4) * 4;
+        const int lds = (sizeof(T) == 4 ? 3 : 1) * 2 * KK * PANEL * 16 + (PANEL + 8 * 32 * (32 + 4)) * 4;
         hipLaunchKernelGGL(k, dim3((unsigned)(panels * groups)), dim3(512), lds, stream, p);
         return launched();
     };

@@ -162,14 +162,12 @@ __device__ inline float reciprocal(float v) { return __builtin_amdgcn_rcpf(v); }
 template <bool FINE>
 __device__ inline float gelu_cdf(float v, float& e)
 {
-    const float a = fabsf(v), t = reciprocal(fmaf(0.3f, a, 1.0f));
+    const float a = fminf(fabsf(v), 16.f);  // e is zero there
+    const float t = reciprocal(fmaf(0.3f, a, 1.0f));
     constexpr float C = -0.72134752f, C_REST = -9.62981495e-9f;  // -log2(e) / 2 = C + C_REST
-    const float s = v * v, x = s * C;
+    const float s = a * a, x = s * C;
     e = __builtin_amdgcn_exp2f(x);
-    if constexpr (FINE) {
-        const float rest = fmaf(s, C, -x) + fmaf(s, C_REST, fmaf(v, v, -s) * C);
-        if (s < 1e4f) e = fmaf(e, rest * 0.69314718f, e);
-    }
+    if constexpr (FINE) e = fmaf(e, fmaf(fmaf(a, a, -s), C, fmaf(s, C_REST, fmaf(s, C, -x))) * 0.69314718f, e);
     float r = fmaf(0.0356758006f, t, -0.157207165f);
     r = fmaf(r, t, 0.206360237f);
     r = fmaf(r, t, -0.0536895875f);
