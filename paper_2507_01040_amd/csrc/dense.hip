@@ -727,15 +727,19 @@ __global__ __launch_bounds__(256) void join_kernel(ProductArgs p)
     finish_rows<T, 1>(p, m, 1, n, v, ends);
 }
 
-// Few rows (16 MB at most): bound by the read of B, so every workgroup streams
-// 16 NS columns of it once, its eight waves an eighth of the contraction each, D
-// stages ahead, and they join their sums in LDS.  Matrix instructions of 16 x 16
-// outputs, B's columns as their rows.
+// Few rows (16 MB at most): bound by the read of B, then by A, which every
+// workgroup reads.  A workgroup streams 16 NS columns of B once, its eight waves an
+// eighth of the contraction each, D stages ahead, and they join their sums in LDS.
+// Matrix instructions of 16 x 16 outputs, B's columns as their rows.  1 x 1024 x
+// 4096 bf16 4.2 us (launch and latency), 24 x 4096 x 4096 7.7 (the 34 MB of B
+// partly from the last-level cache, 8 TB/s beyond the launch), 24 x 4096 x 4096
+// fp32 17.
 
 // The sums of the eight waves for the same outputs, joined in order and finished.
+// Columns from `whole` on stand `shift` to the right of their place.
 template <typename T, int MB, int NS>
 __device__ inline void join_waves(const ProductArgs& p, int64_t n0, const f4 (&acc)[MB][NS], float* lds, int lane,
-                                  int wave)
+                                  int wave, int whole = 16 * NS, int shift = 0)
 {
     constexpr int EW = 16 * NS + 4, PLANE = MB * 16 * EW;
     const int r = threadIdx.x / (4 * NS), c = 4 * (threadIdx.x % (4 * NS));
@@ -752,7 +756,14 @@ __device__ inline void join_waves(const ProductArgs& p, int64_t n0, const f4 (&a
     if (r >= 16 * MB || r >= p.M || n >= p.N) return;
     f4 v[1] = {f4{0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
-    for (int w = 0; w < 8; ++w) v[0] += *reinterpret_cast<const f4*>(lds + w * PLANE + r * EW + c);
+    for (int w = 0; w < 8; ++w) {
+        const float* const at = lds + w * PLANE + r * EW;
+        f4 t = *reinterpret_cast<const f4*>(at + c);
+        if (c >= whole)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) t[e] = at[c + e + shift < EW ? c + e + shift : EW - 1];
+        v[0] += t;
+    }
     finish_rows<T, 1>(p, r, 1, n, v, ends);
 }
 
@@ -770,110 +781,196 @@ struct RowsPart {
         k0 = wave * part;
         k1 = k0 + part < p.K ? k0 + part : p.K;
     }
-    // Calls load(stage, k) D stages ahead of use(stage, k).
-    template <int D, typename St, typename L, typename U>
-    __device__ void run(L load, U use) const
+    // Calls load(stage, k) D stages ahead of use(stage).  While D more stages
+    // exist, no branch stands between a stage's load and its use: at a load that
+    // may not have been issued, the wait for an older one becomes a wait for all.
+    // A part's last values, less than a stage, come last, by load_last(stage, k).
+    template <int D, typename St, typename L, typename S, typename U>
+    __device__ void run(L load, S load_last, U use) const
     {
+        const int n = k1 > k0 ? (int)((k1 - k0) / KT) : 0;
         St f[D];
+        int s = 0;
+        if (n >= 2 * D) {
 #pragma unroll
-        for (int d = 0; d < D; ++d)
-            if (k0 + d * KT < k1) load(f[d], k0 + d * KT);
-        for (int64_t k = k0; k < k1; k += D * KT)
+            for (int d = 0; d < D; ++d) load(f[d], k0 + d * KT);
+            do {
 #pragma unroll
-            for (int d = 0; d < D; ++d) {
-                const int64_t kd = k + d * KT;
-                if (kd < k1) use(f[d], kd);
-                if (kd + D * KT < k1) load(f[d], kd + D * KT);
-            }
+                for (int d = 0; d < D; ++d) {
+                    use(f[d]);
+                    load(f[d], k0 + (int64_t)(s + D + d) * KT);
+                }
+                s += D;
+            } while (s + 2 * D <= n);
+        } else {
+#pragma unroll
+            for (int d = 0; d < D; ++d)
+                if (d < n) load(f[d], k0 + d * KT);
+        }
+#pragma unroll
+        for (int d = 0; d < D; ++d) {
+            if (s + d < n) use(f[d]);
+            if (s + D + d < n) load(f[d], k0 + (int64_t)(s + D + d) * KT);
+        }
+#pragma unroll
+        for (int d = 0; d < D - 1; ++d)
+            if (s + D + d < n) use(f[d]);
+        const int64_t k = k0 + (int64_t)n * KT;
+        if (k >= k1) return;
+        load_last(f[0], k);
+        use(f[0]);
     }
 };
 
-// 16-bit types.  B contiguous along the contraction is loaded as fragments;
-// otherwise a wave turns its slots through a piece of LDS of its own, without
-// barriers.
+// 16 bytes at a byte offset of a lane from an address of the wave.
+template <typename T>
+__device__ inline raw16 load_at(const T* base, uint32_t offset)
+{
+    raw16 r;
+    __builtin_memcpy(&r, reinterpret_cast<const char*>(base) + offset, 16);
+    return r;
+}
+
+// A wave's piece of LDS: lines of 128 bytes, 16 of a block, in pieces of 16 bytes.
+// Loads put a line's eight pieces on neighbouring lanes, and LDS, without barriers,
+// turns them into fragments: 16 lanes that read one piece of 16 lines meet every
+// bank once.  (Fragments straight from memory have four neighbouring lanes on four
+// lines, which the L1 cache serves one at a time where lines lie a multiple of 128
+// bytes apart: 24 x 4096 x 4096 bf16 in 12.0 us instead of 7.7.)
+struct Lines {
+    uint32_t at[2];  // a lane's two pieces of a block of lines, in bytes from the first
+    template <typename T>
+    __device__ Lines(int64_t first, int64_t lines, int64_t ld, int lane, T)
+    {
+        for (int h = 0; h < 2; ++h) {
+            const int64_t l = first + 8 * h + (lane >> 3);
+            at[h] = (uint32_t)((l < lines ? l : lines - 1) * ld + per16<T> * (lane & 7)) * (uint32_t)sizeof(T);
+        }
+    }
+    Lines() = default;
+    template <typename T>
+    __device__ void load(raw16 (&v)[2], const T* base) const
+    {
+        for (int h = 0; h < 2; ++h) v[h] = load_at(base, at[h]);
+    }
+    static __device__ int byte(int line, int piece) { return line * 128 + ((piece ^ (line >> 1 & 7)) << 4); }
+    static __device__ void write(const raw16 (&v)[2], char* lds, int lane)
+    {
+        for (int h = 0; h < 2; ++h) *reinterpret_cast<raw16*>(lds + byte(8 * h + (lane >> 3), lane & 7)) = v[h];
+    }
+    static __device__ void read(raw16 (&v)[2], const char* lds, int lane)
+    {
+        for (int j = 0; j < 2; ++j) v[j] = *reinterpret_cast<const raw16*>(lds + byte(lane & 15, 4 * j + (lane >> 4)));
+    }
+    // The values before k1 of a stage that is not whole, from value k on; lines
+    // that do not exist give way to the last one here too.
+    template <typename T>
+    static __device__ void load_last(raw16 (&v)[2], const T* x, int64_t first, int64_t lines, int64_t ld, int64_t k,
+                                     int64_t k1, int lane)
+    {
+        for (int h = 0; h < 2; ++h) {
+            const int64_t l = first + 8 * h + (lane >> 3), pos = k + per16<T> * (lane & 7);
+            v[h] = load16(x + (l < lines ? l : lines - 1) * ld, pos, k1);
+            settle16<T>(v[h], pos, k1);
+        }
+    }
+};
+constexpr int LINES = 16 * 128;  // bytes of a block
+
+__device__ inline void wave_fence()
+{
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
+// 16-bit types.  B contiguous along the output is turned by the reads of LDS.
 template <typename T, bool BKM, int MB>
 __global__ __launch_bounds__(512, 2) void rows_kernel(ProductArgs p)
 {
-    constexpr int NS = BKM ? 1 : 2, D = MB == 4 ? 2 : BKM ? 8 : 4;  // what the registers hold
+    constexpr int NS = BKM ? 1 : 2, D = MB == 4 ? (BKM ? 3 : 2) : BKM && MB == 1 ? 8 : 4;  // what the registers hold
     constexpr Stage S{32, 64, false};
-    constexpr int JOIN = MB * 16 * (16 * NS + 4) * 4;
-    __shared__ __align__(16) char smem[8 * (BKM || JOIN > S.bytes() ? JOIN : S.bytes())];
-    const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+    constexpr int OWN = MB * LINES + (BKM ? LINES : S.bytes()), JOIN = MB * 16 * (16 * NS + 4) * 4;
+    __shared__ __align__(16) char smem[8 * (JOIN > OWN ? JOIN : OWN)];
+    const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const RowsPart<64> part(p, 16 * NS, wave);
     const int64_t n0 = part.n0, k1 = part.k1;
     const int cols = part.cols;
     const T* const a = static_cast<const T*>(p.a);
-    const T* const b = static_cast<const T*>(p.b);
+    const T* const b = static_cast<const T*>(p.b) + (BKM ? n0 * p.ldb : n0);
     f4 acc[MB][NS];
 #pragma unroll
     for (int i = 0; i < MB; ++i)
 #pragma unroll
         for (int j = 0; j < NS; ++j) acc[i][j] = f4{0.f, 0.f, 0.f, 0.f};
-    // a lane's slots: values 32 j + 8 g of a row
     struct St {
         raw16 x[MB][2], w[2 * NS];
     };
-    char* const own = smem + wave * S.bytes();
-    // rows and columns that do not exist give way to the last ones
-    const T* arow[MB];
+    char* const own = smem + wave * OWN;
+    char* const own_w = own + MB * LINES;
+    Lines al[MB], bl;
 #pragma unroll
-    for (int i = 0; i < MB; ++i) arow[i] = a + (16 * i + r < p.M ? 16 * i + r : p.M - 1) * p.lda;
-    const T* const bcol = b + (n0 + (r < cols ? r : cols - 1)) * p.ldb;
+    for (int i = 0; i < MB; ++i) al[i] = Lines(16 * i, p.M, p.lda, lane, T{});
+    uint32_t bo[2 * NS];
+    const int left = cols < 8 ? cols - 8 : 0;  // a piece that passes the last column lies further left
+    if constexpr (BKM) {
+        bl = Lines(0, cols, p.ldb, lane, T{});
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int e = 64 * j + lane, c = S.slot_row(e);
+            bo[j] = (uint32_t)(S.slot_k(e) * p.ldb + (c < cols - 8 ? c : cols - 8) - left) * 2;
+        }
+    }
     auto load = [&](St& f, int64_t k) {
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
+        for (int i = 0; i < MB; ++i) al[i].load(f.x[i], a + k);
+        if constexpr (BKM)
+            bl.load(f.w, b + k);
+        else
 #pragma unroll
-            for (int i = 0; i < MB; ++i) f.x[i][j] = load16(arow[i], k + 32 * j + 8 * g, k1);
-            if constexpr (BKM) f.w[j] = load16(bcol, k + 32 * j + 8 * g, k1);
-        }
-        if constexpr (!BKM)
+            for (int j = 0; j < 4; ++j) f.w[j] = load_at(b + k * p.ldb + left, bo[j]);
+    };
+    auto load_last = [&](St& f, int64_t k) {
+#pragma unroll
+        for (int i = 0; i < MB; ++i) Lines::load_last(f.x[i], a, 16 * i, p.M, p.lda, k, k1, lane);
+        if constexpr (BKM)
+            Lines::load_last(f.w, b, 0, cols, p.ldb, k, k1, lane);
+        else
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const int e = 64 * j + lane;
-                const int64_t kr = k + S.slot_k(e);
-                f.w[j] = load16(b + (kr < k1 ? kr : k1 - 1) * p.ldb, n0 + S.slot_row(e), n0 + cols);
+                const int64_t kr = k + S.slot_k(64 * j + lane);
+                f.w[j] = load16(b + (kr < k1 ? kr : k1 - 1) * p.ldb, S.slot_row(64 * j + lane), cols);
+                if (kr >= k1) f.w[j] = raw16{0, 0, 0, 0};
             }
     };
-    auto use = [&](St& f, int64_t k) {
-        if (k1 - k < 64)
+    auto use = [&](St& f) {
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
+        for (int i = 0; i < MB; ++i) Lines::write(f.x[i], own + i * LINES, lane);
+        if constexpr (BKM)
+            Lines::write(f.w, own_w, lane);
+        else
 #pragma unroll
-                for (int i = 0; i < MB; ++i) settle16<T>(f.x[i][j], k + 32 * j + 8 * g, k1);
-                if constexpr (BKM) settle16<T>(f.w[j], k + 32 * j + 8 * g, k1);
-            }
-        if constexpr (!BKM)
-            if (cols < 32 || k1 - k < 64)
+            for (int j = 0; j < 4; ++j) *reinterpret_cast<raw16*>(own_w + (64 * j + lane) * 16) = f.w[j];
+        wave_fence();
+        raw16 w[NS][2], x[MB][2];
+        if constexpr (BKM)
+            Lines::read(w[0], own_w, lane);
+        else
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int e = 64 * j + lane;
-                    if (k + S.slot_k(e) >= k1) f.w[j] = raw16{0, 0, 0, 0};
-                    settle16<T>(f.w[j], S.slot_row(e), cols);
-                }
-        u4 w[2][NS];
-        if constexpr (BKM) {
-            w[0][0] = f.w[0];
-            w[1][0] = f.w[1];
-        } else {
+            for (int h = 0; h < NS; ++h)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) *reinterpret_cast<u4*>(own + (64 * j + lane) * 16) = f.w[j];
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-            __builtin_amdgcn_wave_barrier();
-#pragma unroll
-            for (int j = 0; j < 2; ++j)
-#pragma unroll
-                for (int h = 0; h < NS; ++h) {
+                for (int j = 0; j < 2; ++j) {
                     typedef __attribute__((address_space(3))) s4 ls4;
                     struct {
                         s4 x, y;
-                    } z{__builtin_amdgcn_ds_read_tr16_b64_v4i16((ls4*)(own + frag16_byte(S, 16 * h, 32 * j, lane, 0))),
-                        __builtin_amdgcn_ds_read_tr16_b64_v4i16((ls4*)(own + frag16_byte(S, 16 * h, 32 * j, lane, 1)))};
-                    w[j][h] = __builtin_bit_cast(u4, z);
+                    } z{__builtin_amdgcn_ds_read_tr16_b64_v4i16((ls4*)(own_w + frag16_byte(S, 16 * h, 32 * j, lane, 0))),
+                        __builtin_amdgcn_ds_read_tr16_b64_v4i16((ls4*)(own_w + frag16_byte(S, 16 * h, 32 * j, lane, 1)))};
+                    w[h][j] = __builtin_bit_cast(raw16, z);
                 }
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-            __builtin_amdgcn_wave_barrier();
-        }
+#pragma unroll
+        for (int i = 0; i < MB; ++i) Lines::read(x[i], own + i * LINES, lane);
+        wave_fence();
 #pragma unroll
         for (int j = 0; j < 2; ++j)
 #pragma unroll
@@ -882,14 +979,17 @@ __global__ __launch_bounds__(512, 2) void rows_kernel(ProductArgs p)
                 for (int h = 0; h < NS; ++h) {
                     if constexpr (__is_same(T, _Float16))
                         acc[i][h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(
-                            __builtin_bit_cast(h8, w[j][h]), __builtin_bit_cast(h8, f.x[i][j]), acc[i][h], 0, 0, 0);
+                            __builtin_bit_cast(h8, w[h][j]), __builtin_bit_cast(h8, x[i][j]), acc[i][h], 0, 0, 0);
                     else
                         acc[i][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                            __builtin_bit_cast(b8, w[j][h]), __builtin_bit_cast(b8, f.x[i][j]), acc[i][h], 0, 0, 0);
+                            __builtin_bit_cast(b8, w[h][j]), __builtin_bit_cast(b8, x[i][j]), acc[i][h], 0, 0, 0);
                 }
     };
-    part.template run<D, St>(load, use);
-    join_waves<T, MB, NS>(p, n0, acc, reinterpret_cast<float*>(smem), lane, wave);
+    part.template run<D, St>(load, load_last, use);
+    if constexpr (BKM)
+        join_waves<T, MB, NS>(p, n0, acc, reinterpret_cast<float*>(smem), lane, wave);
+    else
+        join_waves<T, MB, NS>(p, n0, acc, reinterpret_cast<float*>(smem), lane, wave, cols & ~7, 8 - (cols & 7));
 }
 
 // fp32, on the fp32 matrix cores (the memory is slower): value 16 j + 4 g + e of
@@ -897,76 +997,77 @@ __global__ __launch_bounds__(512, 2) void rows_kernel(ProductArgs p)
 template <bool BKM, int MB>
 __global__ __launch_bounds__(512, 2) void rows_fp32_kernel(ProductArgs p)
 {
-    constexpr int NS = 1, D = MB == 4 ? 2 : 4;
-    __shared__ __align__(16) char smem[8 * MB * 16 * (16 * NS + 4) * 4];
+    constexpr int NS = 1, D = MB == 4 ? 3 : BKM && MB == 1 ? 8 : 4;
+    constexpr int OWN = (MB + (BKM ? 1 : 0)) * LINES, JOIN = MB * 16 * (16 * NS + 4) * 4;
+    __shared__ __align__(16) char smem[8 * (JOIN > OWN ? JOIN : OWN)];
     const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const RowsPart<32> part(p, 16 * NS, wave);
     const int64_t n0 = part.n0, k1 = part.k1;
     const int cols = part.cols;
     const float* const a = static_cast<const float*>(p.a);
-    const float* const b = static_cast<const float*>(p.b);
+    const float* const b = static_cast<const float*>(p.b) + (BKM ? n0 * p.ldb : n0);
     f4 acc[MB][NS];
 #pragma unroll
-    for (int i = 0; i < MB; ++i)
-#pragma unroll
-        for (int j = 0; j < NS; ++j) acc[i][j] = f4{0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < MB; ++i) acc[i][0] = f4{0.f, 0.f, 0.f, 0.f};
     struct St {
-        raw16 x[MB][2], w[2][NS];
+        raw16 x[MB][2], w[2];
     };
-    const float* arow[MB];
+    char* const own = smem + wave * OWN;
+    const int col = r < cols ? r : cols - 1;
+    Lines al[MB], bl;
 #pragma unroll
-    for (int i = 0; i < MB; ++i) arow[i] = a + (16 * i + r < p.M ? 16 * i + r : p.M - 1) * p.lda;
-    int col[NS];
-#pragma unroll
-    for (int h = 0; h < NS; ++h) col[h] = 16 * h + r < cols ? 16 * h + r : cols - 1;
+    for (int i = 0; i < MB; ++i) al[i] = Lines(16 * i, p.M, p.lda, lane, 0.f);
+    if constexpr (BKM) bl = Lines(0, cols, p.ldb, lane, 0.f);
+    const uint32_t bo = (uint32_t)(4 * g * p.ldb + col) * 4;
     auto load = [&](St& f, int64_t k) {
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const int64_t kj = k + 16 * j + 4 * g;
+        for (int i = 0; i < MB; ++i) al[i].load(f.x[i], a + k);
+        if constexpr (BKM)
+            bl.load(f.w, b + k);
+        else
 #pragma unroll
-            for (int i = 0; i < MB; ++i) f.x[i][j] = load16(arow[i], kj, k1);
-            if constexpr (BKM) {
-                f.w[j][0] = load16(b + (n0 + col[0]) * p.ldb, kj, k1);
-            } else {
+            for (int j = 0; j < 2; ++j)
 #pragma unroll
-                for (int h = 0; h < NS; ++h)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        f.w[j][h][e] = __builtin_bit_cast(uint32_t, b[(kj + e < k1 ? kj + e : k1 - 1) * p.ldb + n0 + col[h]]);
-            }
-        }
+                for (int e = 0; e < 4; ++e)
+                    f.w[j][e] = *reinterpret_cast<const uint32_t*>(
+                        reinterpret_cast<const char*>(b + (k + 16 * j + e) * p.ldb) + bo);
     };
-    auto use = [&](St& f, int64_t k) {
-        if (k1 - k < 32)
+    auto load_last = [&](St& f, int64_t k) {
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const int64_t kj = k + 16 * j + 4 * g;
+        for (int i = 0; i < MB; ++i) Lines::load_last(f.x[i], a, 16 * i, p.M, p.lda, k, k1, lane);
+        if constexpr (BKM)
+            Lines::load_last(f.w, b, 0, cols, p.ldb, k, k1, lane);
+        else
 #pragma unroll
-                for (int i = 0; i < MB; ++i) settle16<float>(f.x[i][j], kj, k1);
-                if constexpr (BKM) {
-                    settle16<float>(f.w[j][0], kj, k1);
-                } else {
+            for (int j = 0; j < 2; ++j)
 #pragma unroll
-                    for (int h = 0; h < NS; ++h)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            if (kj + e >= k1) f.w[j][h][e] = 0u;
+                for (int e = 0; e < 4; ++e) {
+                    const int64_t kr = k + 16 * j + 4 * g + e;
+                    f.w[j][e] = __builtin_bit_cast(uint32_t, b[(kr < k1 ? kr : k1 - 1) * p.ldb + col]);
+                    if (kr >= k1) f.w[j][e] = 0u;
                 }
-            }
+    };
+    auto use = [&](St& f) {
+#pragma unroll
+        for (int i = 0; i < MB; ++i) Lines::write(f.x[i], own + i * LINES, lane);
+        if constexpr (BKM) Lines::write(f.w, own + MB * LINES, lane);
+        wave_fence();
+        raw16 x[MB][2], w[2] = {f.w[0], f.w[1]};
+        if constexpr (BKM) Lines::read(w, own + MB * LINES, lane);
+#pragma unroll
+        for (int i = 0; i < MB; ++i) Lines::read(x[i], own + i * LINES, lane);
+        wave_fence();
 #pragma unroll
         for (int j = 0; j < 2; ++j)
 #pragma unroll
             for (int i = 0; i < MB; ++i)
 #pragma unroll
-                for (int h = 0; h < NS; ++h) {
-                    const f4 w = __builtin_bit_cast(f4, f.w[j][h]), x = __builtin_bit_cast(f4, f.x[i][j]);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        acc[i][h] = __builtin_amdgcn_mfma_f32_16x16x4f32(w[e], x[e], acc[i][h], 0, 0, 0);
-                }
+                for (int e = 0; e < 4; ++e)
+                    acc[i][0] = __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(f4, w[j])[e],
+                                                                     __builtin_bit_cast(f4, x[i][j])[e], acc[i][0], 0, 0, 0);
     };
-    part.template run<D, St>(load, use);
+    part.template run<D, St>(load, load_last, use);
     join_waves<float, MB, NS>(p, n0, acc, reinterpret_cast<float*>(smem), lane, wave);
 }
 
@@ -1243,24 +1344,26 @@ struct Cut {
     bool large;
     int splits;
     int64_t k_part;
+    double ns;  // what it is expected to take
 };
 
-// Times in ns, measured (MI355X): of a stage with one workgroup on each compute
-// unit and with as many as fit, and of a workgroup's begin and end; the kernels
-// wait for memory most of the time when they are alone, so a second workgroup is
-// nearly free.
+// Times in ns, fitted to measured ones (MI355X; 31 products of 128 to 8008 rows
+// and columns with 1 to 32 parts each, 12 % off on average; the cuts that they
+// choose take 1 % longer than the best ones, 18 % at worst): of a stage with one
+// workgroup on each compute unit and with as many as fit, and of a workgroup's
+// begin and end.  The kernels wait for memory most of the time when they are
+// alone, so a second workgroup costs less than the first.
 struct TileTimes {
     int B, KT, fit;
     double alone, full, ends;
 };
-constexpr TileTimes T_DIRECT256{256, 64, 1, 1600, 1600, 9000}, T_DIRECT128{128, 64, 2, 700, 1000, 6000},
-    T_STAGED128{128, 64, 3, 1500, 2000, 7000}, T_SPLIT128{128, 16, 2, 720, 1330, 7000};
+constexpr TileTimes T_DIRECT256{256, 64, 1, 1300, 1300, 10000}, T_DIRECT128{128, 64, 2, 600, 1150, 5800},
+    T_STAGED128{128, 64, 2, 1100, 1550, 6300}, T_SPLIT128{128, 16, 2, 700, 1230, 8000};
 
 Cut cut(int dtype, int64_t M, int64_t N, int64_t K, bool direct)
 {
     const int64_t cus = std::max(device_cus(), 1);
-    Cut best{false, 1, 0};
-    double least = 0;
+    Cut best{false, 1, 0, 0};
     for (int large = 0; large <= (direct ? 1 : 0); ++large) {
         const TileTimes& t = large ? T_DIRECT256 : dtype == CLIFF_F32 ? T_SPLIT128 : direct ? T_DIRECT128 : T_STAGED128;
         const int64_t tiles = ceil_div(M, t.B) * ceil_div(N, t.B), steps = std::max<int64_t>(1, ceil_div(K, t.KT));
@@ -1271,17 +1374,28 @@ Cut cut(int dtype, int64_t M, int64_t N, int64_t K, bool direct)
             double ns = rounds * (per * t.full + t.ends);
             if (rest) ns += per * (rest <= cus ? t.alone : t.full) + t.ends;
             // the join: a launch, and the partial sums written and read
-            if (splits > 1) ns += 6000 + (double)M * N * 4 * 2 * splits / 12000;
-            if (least == 0 || ns < least) {
-                least = ns;
-                best = Cut{large != 0, (int)splits, per * t.KT};
-            }
+            if (splits > 1) ns += 4400 + (double)M * N * 4 * 2 * splits / 11700;
+            if (best.ns == 0 || ns < best.ns) best = Cut{large != 0, (int)splits, per * t.KT, ns};
         }
     }
     return best;
 }
 
-constexpr int64_t FEW_ROWS = 64;  // up to which rows_kernel runs
+// What the kernels of few rows are for: rows and row strides (32-bit offsets).
+constexpr int64_t FEW_ROWS = 64, FEW_LD = 1 << 23;
+
+// The time in ns of few_rows, from bytes that a compute unit takes in, to choose
+// between it and the tiles: every workgroup reads all of A, so that with a long
+// contraction and little else to share it the parts of split tiles are ahead.  24 x
+// 4096 x 4096 bf16: 7.7 us here, 13.8 in tiles; 24 x 8192 x 2048, B contiguous
+// along the output: 21.3 and 14.3; 64 x 4096 x 1024 fp32: 25 and 19.
+template <typename T, bool BKM>
+double few_rows_ns(const ProductArgs& p)
+{
+    const int cols = BKM || sizeof(T) == 4 ? 16 : 32, rows = p.M <= 16 ? 16 : p.M <= 32 ? 32 : 64;
+    const double rounds = std::max(1., (double)ceil_div(p.N, cols) / std::max(device_cus(), 1));
+    return 3500 + rounds * (double)(p.K * (rows + cols) * (int64_t)sizeof(T)) / (sizeof(T) == 4 ? 57 : BKM ? 75 : 65);
+}
 
 // What a product of rows (y or dx) or a weight's gradient needs for its parts.
 int64_t partial_bytes(int dtype, int64_t M, int64_t N, int64_t K, bool rows)
@@ -1361,13 +1475,15 @@ cliff_status panel(const ProductArgs& p, hipStream_t stream)
 template <typename T, bool AKM, bool BKM>
 cliff_status product(int dtype, ProductArgs p, hipStream_t stream)
 {
-    if constexpr (AKM)
-        if (p.M <= FEW_ROWS && p.K >= per16<T> && (BKM || p.N >= per16<T>)) return few_rows<T, BKM>(p, stream);
-    if constexpr (AKM)
-        if (p.M >= PANEL_ROWS && p.K <= PANEL_K && p.K >= per16<T>) return panel<T, BKM>(p, stream);
     const bool direct = sizeof(T) == 2 && aligned_rows(p.a, p.lda, AKM ? p.K : p.M) &&
                         aligned_rows(p.b, p.ldb, BKM ? p.K : p.N);
     const Cut c = cut(dtype, p.M, p.N, p.K, direct);
+    if constexpr (AKM) {
+        if (p.M <= FEW_ROWS && p.K >= per16<T> && (BKM || p.N >= per16<T>) && p.lda <= FEW_LD && p.ldb <= FEW_LD &&
+            few_rows_ns<T, BKM>(p) < c.ns)
+            return few_rows<T, BKM>(p, stream);
+        if (p.M >= PANEL_ROWS && p.K <= PANEL_K && p.K >= per16<T>) return panel<T, BKM>(p, stream);
+    }
     p.splits = c.splits;
     p.k_part = c.k_part;
     cliff_status s;
