@@ -397,7 +397,17 @@ __device__ inline void write_tile(const ProductArgs& p, const TileId& id, int64_
 // BM x BN outputs per workgroup of WR x WC waves; a stage is KT contraction
 // values of 16 bits.  DIRECT: operands whose rows are 16-byte aligned and whole
 // slots go from memory straight to LDS, one stage ahead in the other of two
-// buffers.  Otherwise slots go through registers, one stage ahead.
+// buffers.  Otherwise slots go through registers, one stage ahead (two ahead cost
+// the second workgroup of a compute unit: 4000 x 4001 x 4096 in 275 us, not 182).
+//
+// Bound by the matrix cores and LDS together: a 32 x 32 x 16 product takes 32
+// cycles of one of four SIMDs, a fragment 8 cycles of LDS (1 KB at 128 bytes a
+// cycle).  For 16 contraction values a tile of 256 x 256 has 64 products (512
+// cycles), 48 fragment reads and 16 KB of writes (512 cycles); one of 128 x 128 has
+// 16 products (128 cycles) and 192 cycles of LDS.  So tiles are large where there
+// are enough of them: 4000 x 4008 x 4096 bf16 112 us, 144 with 128 x 128; 1008 x 784
+// x 1536, one round either way, 24.4 and 13.4.  8192^3 bf16 1290 to 1336 TFLOP/s;
+// 4096 x 4096 x 8192 with GELU, dropout and both outputs 250 us, 1100 TFLOP/s.
 template <typename T, bool AKM, bool BKM, int BM, int BN, int WR, int WC, int KT, bool DIRECT>
 __global__ __launch_bounds__(64 * WR * WC) void product_kernel(ProductArgs p)
 {
@@ -553,7 +563,9 @@ __global__ __launch_bounds__(64 * WR * WC) void product_kernel(ProductArgs p)
 // six, 128 x 128 outputs per workgroup of 2 x 2 waves, stages of 16 values.
 // While a wave multiplies stage s, it reads the fragments of stage s + 1, splits
 // stage s + 2 from registers into the LDS buffer that stage s has left, and
-// loads stage s + 4, so a step has one barrier.
+// loads stage s + 4, so a step has one barrier.  Bound by the matrix cores (six
+// products at bf16's rate) with the vector instructions of the splitting beside
+// them: 4096^3 190 to 204 TFLOP/s, where the fp32 matrix cores' peak is 157.
 template <bool AKM, bool BKM>
 __global__ __launch_bounds__(256, 2) void split_product_kernel(ProductArgs p)
 {
@@ -701,15 +713,17 @@ __global__ __launch_bounds__(256, 2) void split_product_kernel(ProductArgs p)
 }
 
 // Joins the parts of a split contraction in a fixed order and finishes the
-// outputs: a workgroup takes 64 groups of four columns, its four waves every
-// fourth part each.
-template <typename T>
+// outputs: bound by the read of the parts.  WAVES == 1: a thread for each group of
+// four columns; few groups of many parts would keep too few loads in flight so, and
+// WAVES == 4 has a workgroup take 64 groups, its four waves every fourth part each.
+template <typename T, int WAVES>
 __global__ __launch_bounds__(256) void join_kernel(ProductArgs p)
 {
-    __shared__ f4 part[4][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t nq = (p.N + 3) / 4, i = blockIdx.x * 64ll + lane, plane = p.M * p.N;
-    const int64_t m = i / nq, n = i % nq * 4;
+    __shared__ f4 part[4][WAVES == 4 ? 64 : 1];
+    const int lane = threadIdx.x & 63, wave = WAVES == 4 ? threadIdx.x >> 6 : 0;
+    const int64_t nq = (p.N + 3) / 4, plane = p.M * p.N;
+    const int64_t i = WAVES == 4 ? blockIdx.x * 64ll + lane : blockIdx.x * 256ll + threadIdx.x;
+    const int64_t m = i >> 32 ? i / nq : (int64_t)((uint32_t)i / (uint32_t)nq), n = (i - m * nq) * 4;
     const int have = p.N - n < 4 ? (int)(p.N - n) : 4;
     f4 v[1] = {f4{0.f, 0.f, 0.f, 0.f}};
     ProductArgs whole = p;
@@ -718,13 +732,15 @@ __global__ __launch_bounds__(256) void join_kernel(ProductArgs p)
     if (m < p.M) {
         const float* const q = p.partial + m * p.N + n;
 #pragma unroll 8
-        for (int s = wave; s < p.splits; s += 4) v[0] += load4(q + s * plane, have);
+        for (int s = wave; s < p.splits; s += WAVES) v[0] += load4(q + s * plane, have);
     }
-    part[wave][lane] = v[0];
-    __syncthreads();
-    if (wave || m >= p.M) return;
-    v[0] = part[0][lane] + part[1][lane] + part[2][lane] + part[3][lane];
-    finish_rows<T, 1>(p, m, 1, n, v, ends);
+    if constexpr (WAVES == 4) {
+        part[wave][lane] = v[0];
+        __syncthreads();
+        if (wave) return;
+        v[0] = part[0][lane] + part[1][lane] + part[2][lane] + part[3][lane];
+    }
+    if (m < p.M) finish_rows<T, 1>(p, m, 1, n, v, ends);
 }
 
 // Few rows (16 MB at most): bound by the read of B, then by A, which every
@@ -1079,7 +1095,9 @@ __global__ __launch_bounds__(512, 2) void rows_fp32_kernel(ProductArgs p)
 // The panel lies as [plane][slot][column] in 16-byte slots, read without bank
 // conflicts; slot 2 kk + h has the 8 values of half-wave h in product group kk:
 // 16 kk + 8 h + i, or for fp32 (whose 8 are two loads) 16 kk + 4 h + i and 8 on,
-// so that a row's two lanes read neighbours.
+// so that a row's two lanes read neighbours.  131072 x 128 x 512 fp32: 120 us (2.8
+// TB/s, and 145 TFLOP/s of products), 150 with bias and GELU, whose vector
+// instructions the products do not hide; bf16 42 us (4.0 TB/s).
 constexpr int PANEL = 128;
 template <typename T, bool BKM, int KK, bool WHOLE>
 __global__ __launch_bounds__(512, 2) void panel_kernel(ProductArgs p)
@@ -1278,7 +1296,9 @@ __global__ __launch_bounds__(512, 2) void panel_kernel(ProductArgs p)
 
 // g = dropout(dy) f'(pre) into g [M, N] (unless NULL), and its column sums over
 // a share of the rows into sums [part][N] (unless NULL).  A workgroup takes 256
-// columns; its four waves every fourth row each.
+// columns; its four waves every fourth row each.  Bound by the vector instructions
+// of f' and the generator: 8192 x 2048 bf16, GELU and dropout, 34 us (3 TB/s); 65536
+// x 512 fp32, SiLU, 85 us (4.7 TB/s, memory).
 template <typename T>
 __global__ __launch_bounds__(256) void slope_kernel(DenseBackwardArgs a, T* g, float* sums, int64_t rows_per_part)
 {
@@ -1444,8 +1464,10 @@ cliff_status few_rows(const ProductArgs& p, hipStream_t stream)
         return p.M <= 16 ? go(rows_kernel<T, BKM, 1>) : p.M <= 32 ? go(rows_kernel<T, BKM, 2>) : go(rows_kernel<T, BKM, 4>);
 }
 
-// Rows from which, and contraction up to which, the panel kernel is ahead of the
-// tiles, and its launch.
+// Rows from which the panel kernel is ahead of the tiles (N 512, K 128, fp32, us:
+// 8192 rows 17.2 and 16.7 in tiles, 16384 rows 19.9 and 22.9, 131072 rows 120 and
+// 166; bf16 10.9 and 9.4, 12.2 and 11.9, 42 and 59), the contraction whose panel
+// fits LDS and whose rows fit registers, and its launch.
 constexpr int64_t PANEL_ROWS = 16384;
 constexpr int64_t PANEL_K = 128;
 
@@ -1470,6 +1492,11 @@ cliff_status panel(const ProductArgs& p, hipStream_t stream)
     if (p.K <= 64) return sized(std::integral_constant<int, 4>{});
     return sized(std::integral_constant<int, 8>{});
 }
+
+// Groups of four outputs from which a thread joins all of a group's parts: 1003 x
+// 777 x 1531 bf16 (384,000 groups, 2 parts) in 21.8 us with it and 24.3 with four
+// waves, 128 x 2048 x 512 fp32 (16,000 groups) in 19.9 and 17.4.
+constexpr int64_t JOIN_GROUPS = 1 << 17;
 
 // A product and, where its contraction is split, the join.
 template <typename T, bool AKM, bool BKM>
@@ -1498,9 +1525,11 @@ cliff_status product(int dtype, ProductArgs p, hipStream_t stream)
             s = run(product_kernel<T, AKM, BKM, 128, 128, 2, 2, 64, true>, "direct", 128, 256, 2 * 2 * 128 * 64 * 2, p, stream);
     }
     if (s != CLIFF_OK || p.splits == 1) return s;
-    const int64_t blocks = ceil_div(p.M * ceil_div(p.N, 4), 64);
+    const int64_t groups = p.M * ceil_div(p.N, 4);
+    const bool one = groups >= JOIN_GROUPS;
+    const int64_t blocks = ceil_div(groups, one ? 256 : 64);
     if (blocks >= (int64_t)1 << 31) return CLIFF_EUNSUPPORTED;
-    hipLaunchKernelGGL(join_kernel<T>, dim3((unsigned)blocks), dim3(256), 0, stream, p);
+    hipLaunchKernelGGL((one ? join_kernel<T, 1> : join_kernel<T, 4>), dim3((unsigned)blocks), dim3(256), 0, stream, p);
     return launched();
 }
 
