@@ -502,3 +502,43 @@ def test_activations_over_the_range():
         want = O.slope(act, v.double())
         inside = v.abs() < 1e30
         assert float((g - want).abs()[inside].max()) <= 2.0 ** -20 * 2, act
+
+
+# few rows past a long contraction: whole stages in rounds, a rest of rounds and
+# of a stage, and 1 to 31 columns in the last workgroup; NaN beside the operands
+@pytest.mark.parametrize("order", ["io", "oi"])
+@pytest.mark.parametrize("size", [(1, 520, 4096 + 5), (3, 8200, 4100), (16, 5003, 4106), (24, 4167, 4123), (50, 4101, 4097),
+                                  (64, 2303, 2079), (7, 1024, 33), (31, 700, 15)], ids=str)
+@pytest.mark.parametrize("dtype", DTYPES, ids=ids)
+def test_dense_few_rows(dtype, size, order):
+    M, K, N = size
+    d = Draw(M + K + N, dtype)
+    x, w = d.rows(M, K), d.weight(K, N, order)
+
+    def beside(t, pad):
+        big = torch.full((t.shape[0] + 1, t.shape[1] + pad), float("nan"), dtype=dtype, device="cuda:0")
+        big[:-1, :t.shape[1]] = t
+        return big[:-1, :t.shape[1]]
+    xs = beside(x, 5)
+    ws = beside(w, 3) if order == "io" else beside(w.t(), 3).t()
+    b, res = d.vector(N), d.rows(M, N)
+    drop = (0.25, rng())
+    want, want_pre = O.dense(x, w, b, 1, (0.25, (KEY, STEP)), res, dtype)
+    for left, right in ((x, w), (xs, ws)):
+        y, intact = guarded(M, N, dtype)
+        got, pre = P.dense(left, right, b, act=P.ACT_RELU, dropout=drop, residual=res, pre=True, out=y)
+        O.check(pre, want_pre, "pre")
+        O.check(got, want, "y")
+        assert intact()
+
+
+def test_joins_of_many_outputs():
+    # the two joins of split contractions, groups of four columns that end inside
+    for dtype in DTYPES:
+        d = Draw(18, dtype)
+        for M, K, N in ((1003, 1531, 777), (130, 4099, 250), (1001, 1601, 1022)):
+            x, w, b, res = d.rows(M, K), d.weight(K, N, "io"), d.vector(N), d.rows(M, N)
+            y, intact = guarded(M, N, dtype)
+            P.dense(x, w, b, act=P.ACT_SILU, dropout=(0.15, rng()), residual=res, out=y)
+            O.check(y, O.dense(x, w, b, 3, (0.15, (KEY, STEP)), res, dtype)[0], str((M, K, N)))
+            assert intact()
