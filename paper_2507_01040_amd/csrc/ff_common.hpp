@@ -127,6 +127,16 @@ cliff_status with_type(int dtype, F f)
     return CLIFF_EINVAL;
 }
 
+// a ^ b ^ c, in one instruction
+__host__ __device__ inline uint32_t xor3(uint32_t a, uint32_t b, uint32_t c)
+{
+#ifdef __HIP_DEVICE_COMPILE__
+    return __builtin_amdgcn_bitop3_b32(a, b, c, 0x96);
+#else
+    return a ^ b ^ c;
+#endif
+}
+
 // The four words of Philox4x32-7 for elements 4 q to 4 q + 3 of row r.
 // Seven rounds are the fewest that its authors found to pass every test of
 // theirs; a round is two 32 x 32 -> 64 products.
@@ -140,9 +150,9 @@ __host__ __device__ inline Words philox(uint64_t key, uint32_t step, uint32_t q,
 #pragma unroll
     for (int i = 0; i < 7; ++i) {
         const uint64_t a = (uint64_t)0xD2511F53u * c0, b = (uint64_t)0xCD9E8D57u * c2;
-        c0 = (uint32_t)(b >> 32) ^ c1 ^ k0;
+        c0 = xor3((uint32_t)(b >> 32), c1, k0);
         c1 = (uint32_t)b;
-        c2 = (uint32_t)(a >> 32) ^ c3 ^ k1;
+        c2 = xor3((uint32_t)(a >> 32), c3, k1);
         c3 = (uint32_t)a;
         k0 += 0x9E3779B9u;
         k1 += 0xBB67AE85u;
