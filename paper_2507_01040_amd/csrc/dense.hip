@@ -1297,7 +1297,7 @@ __global__ __launch_bounds__(512, 2) void panel_kernel(ProductArgs p)
 // g = dropout(dy) f'(pre) into g [M, N] (unless NULL), and its column sums over
 // a share of the rows into sums [part][N] (unless NULL).  A workgroup takes 256
 // columns; its four waves every fourth row each.  Bound by the vector instructions
-// of f' and the generator: 8192 x 2048 bf16, GELU and dropout, 34 us (3 TB/s); 65536
+// of f' and the generator: 8192 x 2048 bf16, GELU and dropout, 33 us (3 TB/s); 65536
 // x 512 fp32, SiLU, 85 us (4.7 TB/s, memory).
 template <typename T>
 __global__ __launch_bounds__(256) void slope_kernel(DenseBackwardArgs a, T* g, float* sums, int64_t rows_per_part)
