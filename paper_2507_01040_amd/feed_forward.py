@@ -170,16 +170,31 @@ def _ptr(t):
     return t.data_ptr() if t is not None else None
 
 
-def _weight_order(w, name: str = "weight") -> Tuple[int, int]:
-    """(w_out_in, row stride) of a weight [K, N]: stored as it is, or the
-    transposed view of a stored [N, K]."""
+def _stride_in_order(w, order: int) -> Optional[int]:
+    """The row stride of a weight [K, N] read as stored in that order (0: as it
+    is; 1: the transposed view of a stored [N, K]); None where it is not."""
     K, N = w.shape
     sk, sn = w.stride()
-    if (sn == 1 or N == 1) and (sk >= N or K == 1):
-        return 0, sk if K > 1 else N
-    if (sk == 1 or K == 1) and (sn >= K or N == 1):
-        return 1, sn if N > 1 else K
-    raise ValueError("%s: neither axis is contiguous (shape %s, strides %s)" % (name, (K, N), (sk, sn)))
+    rows, cols, ld, step = (N, K, sn, sk) if order else (K, N, sk, sn)
+    if (step != 1 and cols > 1) or (ld < cols and rows > 1):
+        return None
+    return ld if rows > 1 else cols
+
+
+def _weight_order(w, name: str = "weight", like=None) -> Tuple[int, int]:
+    """(w_out_in, row stride) of a weight [K, N].  One input or output feature
+    can have the strides of both orders: the one is taken that holds ``like``
+    too, its gradient, where that is given."""
+    for order in (0, 1):
+        ld = _stride_in_order(w, order)
+        if ld is not None and (like is None or _stride_in_order(like, order) is not None):
+            return order, ld
+    shape, strides = tuple(w.shape), tuple(w.stride())
+    if like is None:
+        raise ValueError("%s: neither axis is contiguous (shape %s, strides %s)" % (name, shape, strides))
+    _weight_order(w, name)
+    raise ValueError("d%s is not stored in the order of the %s (shape %s, strides %s and %s)"
+                     % (name, name, shape, tuple(like.stride()), strides))
 
 
 class FeedForwardPlan(_pkg.Plan):
@@ -331,7 +346,7 @@ def dense_backward_plan(dy, x, weight, pre=None, act: int = ACT_NONE, dropout=No
     if pre is not None:
         _check_dev(pre, "pre", dy)
     _check_dropout_dev(dropout, dy)
-    order, ldw = _weight_order(weight)
+    order, ldw = _weight_order(weight, like=None if dweight is False else dweight)
     b = _Buffers(dy)
     dx = None if dx is False else b.empty(dx, tuple(x.shape), "dx")
     if dweight is False:
@@ -340,11 +355,7 @@ def dense_backward_plan(dy, x, weight, pre=None, act: int = ACT_NONE, dropout=No
         dweight = b.empty(None, (N, K), "dweight").t() if order else b.empty(None, (K, N), "dweight")
     else:
         b.empty(dweight, (K, N), "dweight")
-    lddw = N
-    if dweight is not None:
-        o, lddw = _weight_order(dweight, "dweight")
-        if o != order and K > 1 and N > 1:
-            raise ValueError("dweight is not stored in the order of the weight")
+    lddw = _stride_in_order(dweight, order) if dweight is not None else N
     if bias:
         dbias = b.empty(dbias, (N,), "dbias")
         _check_vector_dev(dbias, "dbias", dy)

@@ -1,0 +1,96 @@
+"""What the feed-forward binding passes to the library, without a GPU: the
+calls' arguments are taken where the library would be called, and CPU tensors
+stand for those on the GPU."""
+import pytest
+import torch
+
+import paper_2507_01040_amd as P
+from paper_2507_01040_amd import feed_forward as F
+
+DENSE_BACKWARD = ("dtype M K N dy lddy x ldx w ldw order pre ldp act drop dx lddx dw lddw dbias ws "
+                  "ws_bytes stream").split()
+
+
+class _Library:
+    """Entry points that record their arguments; workspaces of 256 bytes."""
+
+    def __init__(self):
+        self.calls = []
+
+    def __getattr__(self, name):
+        if name.endswith("_workspace"):
+            return lambda *a: 256
+
+        def entry(*args):
+            self.calls.append((name, args))
+            return P.CLIFF_OK
+        entry.argtypes = [lambda v: v] * 40
+        return entry
+
+
+@pytest.fixture
+def library(monkeypatch):
+    lib = _Library()
+    monkeypatch.setattr(P, "load", lambda *a: lib)
+    monkeypatch.setattr(P, "_stream_ptr", lambda stream: 0)
+    monkeypatch.setattr(F, "_check_dev", lambda *a, **kw: None)
+    return lib
+
+
+def _stored(order, ld, K, N):
+    """A weight [K, N] of the order with that row stride, inside a larger buffer."""
+    if order:
+        return torch.zeros(N + 1, ld)[:N, :K].t()
+    return torch.zeros(K + 1, ld)[:K, :N]
+
+
+def _written(args, K, N):
+    """Byte offset from dw of every element (k, n) as the header lays them out."""
+    k, n = torch.arange(K)[:, None], torch.arange(N)[None, :]
+    return (n * args["lddw"] + k if args["order"] else k * args["lddw"] + n) * 4
+
+
+def _meant(t):
+    K, N = t.shape
+    return (torch.arange(K)[:, None] * t.stride(0) + torch.arange(N)[None, :] * t.stride(1)) * 4
+
+
+@pytest.mark.parametrize("given", [None, "io", "oi", "wide"])
+@pytest.mark.parametrize("order", ["io", "oi"])
+@pytest.mark.parametrize("K,N,pad", [(1, 512, 6), (1, 512, 0), (512, 1, 6), (512, 1, 0), (1, 1, 3), (1, 2, 0), (2, 1, 5),
+                                     (7, 5, 0), (7, 5, 2)], ids=str)
+def test_weight_gradient_goes_where_its_tensor_is(library, K, N, pad, order, given):
+    # one input or output feature: the strides of [K, N] and of a stored [N, K] do
+    # not tell the order
+    w = _stored(order == "oi", (K if order == "oi" else N) + pad, K, N)
+    dweight = None
+    if given == "wide":
+        dweight = _stored(order == "oi", (K if order == "oi" else N) + 9, K, N)
+    elif given:
+        dweight = _stored(given == "oi", K if given == "oi" else N, K, N)
+    x, dy = torch.zeros(3, K), torch.zeros(3, N)
+    try:
+        out = P.dense_backward(dy, x, w, dweight=dweight)[1]
+    except ValueError as e:
+        # refused: only a gradient that the weight's order cannot hold
+        assert "order of the weight" in str(e) and given in ("io", "oi") and min(K, N) > 0
+        got_order = F._weight_order(w)[0]
+        sk, sn = dweight.stride()
+        assert (sk != 1 and K > 1 or sn < K and N > 1) if got_order else (sn != 1 and N > 1 or sk < N and K > 1)
+        return
+    name, args = library.calls[-1]
+    assert name == "cliffconv_dense_backward"
+    args = dict(zip(DENSE_BACKWARD, args))
+    assert args["dw"] == out.data_ptr() and out.shape == (K, N)
+    if dweight is not None:
+        assert out is dweight
+    assert torch.equal(_written(args, K, N), _meant(out))
+    # and inside its storage
+    last = out.storage_offset() * 4 + int(_written(args, K, N).max()) + 4
+    assert last <= out.untyped_storage().nbytes()
+    # the weight is read where it is, in the same order
+    k, n = torch.arange(K)[:, None], torch.arange(N)[None, :]
+    read = (n * args["ldw"] + k if args["order"] else k * args["ldw"] + n) * 4
+    assert torch.equal(read, _meant(w))
+    least = K if args["order"] else N
+    assert args["ldw"] >= least and args["lddw"] >= least
