@@ -275,6 +275,30 @@ def _stream_ptr(stream) -> int:
     return int(s.cuda_stream)
 
 
+def _torch_stream(stream, device):
+    """A torch stream of what a caller may name one by: itself, an object with
+    its handle as ``cuda_stream``, or the raw handle."""
+    import torch
+    if isinstance(stream, torch.cuda.Stream):
+        return stream
+    handle = int(stream.cuda_stream) if hasattr(stream, "cuda_stream") else int(stream)
+    return torch.cuda.ExternalStream(handle, device) if handle else torch.cuda.default_stream(device)
+
+
+def _empty(shape, dtype, device, stream=None):
+    """Memory for a call on ``stream`` (None: the current one).  It is that
+    stream's own: what the allocator takes for another stream may have just
+    been freed there, with that stream's work on it still to come.  The current
+    stream, whose caller reads it, is noted too."""
+    import torch
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(_torch_stream(stream, device)):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    t.record_stream(torch.cuda.current_stream(device))
+    return t
+
+
 def from_paper_protocol(filters, bias=None):
     """Filters (N_B, C_in, C_out, d_f^k) and bias (N_B, C_out) in the paper's
     input/output protocol ("Optimization Performed", convolutional layers:

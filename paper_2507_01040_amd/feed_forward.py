@@ -199,7 +199,9 @@ def _weight_order(w, name: str = "weight", like=None) -> Tuple[int, int]:
 
 class FeedForwardPlan(_pkg.Plan):
     """A Plan whose output may be a tuple of tensors.  Called for another
-    stream, it tells torch's allocator that its buffers are used there."""
+    stream, it tells torch's allocator that its buffers are used there; they
+    are the plan's stream's, so that the other one has to wait for it first, as
+    for every tensor of another stream."""
 
     def __init__(self, fn, args, stream_index: int, name: str, out, keep, own=()):
         # converted once: a call that is repeated is mostly this and the launch
@@ -214,35 +216,31 @@ class FeedForwardPlan(_pkg.Plan):
             if st != _pkg.CLIFF_OK:
                 raise _pkg.CliffError(st, self._name)
             return self.out
-        if hasattr(stream, "cuda_stream"):
-            for t in self._own:
-                t.record_stream(stream)
+        for t in self._own:
+            t.record_stream(_pkg._torch_stream(stream, t.device))
         return super().__call__(stream)
 
 
 def _plan(fn_name: str, args, out, keep, own, stream) -> FeedForwardPlan:
     """The call as a plan; args end with the stream's place.  ``own``: tensors
-    allocated here, which another stream than the current one may use."""
-    if stream is not None and hasattr(stream, "cuda_stream"):
-        for t in own:
-            t.record_stream(stream)
+    allocated here, which another stream than the plan's may use."""
     args = (*args, _pkg._stream_ptr(stream) or None)
     return FeedForwardPlan(getattr(_pkg.load(), fn_name), args, len(args) - 1, fn_name, out, keep, own)
 
 
 class _Buffers:
-    """Outputs and workspace of a call: the caller's, or allocated here."""
+    """Outputs and workspace of a call: the caller's, or allocated here for the
+    stream it runs on."""
 
-    def __init__(self, like):
-        self.like = like
+    def __init__(self, like, stream):
+        self.like, self.stream = like, stream
         self.own = []
 
     def empty(self, given, shape, name: str, dtype=None):
-        import torch
         if given is not None:
             _check_dev(given, name, self.like, dtype)
             return given
-        t = torch.empty(shape, dtype=dtype or self.like.dtype, device=self.like.device)
+        t = _pkg._empty(shape, dtype or self.like.dtype, self.like.device, self.stream)
         self.own.append(t)
         return t
 
@@ -256,7 +254,7 @@ class _Buffers:
             return given, given.numel()
         if need == 0:
             return None, 0
-        t = torch.empty(need, dtype=torch.uint8, device=self.like.device)
+        t = _pkg._empty(need, torch.uint8, self.like.device, self.stream)
         self.own.append(t)
         return t, need
 
@@ -290,7 +288,7 @@ def dense_plan(x, weight, bias=None, act: int = ACT_NONE, dropout=None, residual
     if residual is not None:
         _check_dev(residual, "residual", x)
     order, ldw = _weight_order(weight)
-    b = _Buffers(x)
+    b = _Buffers(x, stream)
     pre_t = b.empty(given_pre, shape, "pre") if want_pre else None
     out = b.empty(out, shape, "out")
     M = _rows_of(x.shape)
@@ -347,7 +345,7 @@ def dense_backward_plan(dy, x, weight, pre=None, act: int = ACT_NONE, dropout=No
         _check_dev(pre, "pre", dy)
     _check_dropout_dev(dropout, dy)
     order, ldw = _weight_order(weight, like=None if dweight is False else dweight)
-    b = _Buffers(dy)
+    b = _Buffers(dy, stream)
     dx = None if dx is False else b.empty(dx, tuple(x.shape), "dx")
     if dweight is False:
         dweight = None
@@ -411,7 +409,7 @@ def layer_norm_plan(x, weight=None, bias=None, eps: float = 1e-5, out=None, mean
     _check_vector_dev(bias, "bias", x)
     _check_vector_dev(mean, "mean", x, torch.float32)
     _check_vector_dev(rstd, "rstd", x, torch.float32)
-    b = _Buffers(x)
+    b = _Buffers(x, stream)
     out = b.empty(out, tuple(x.shape), "out")
     mean = b.empty(mean, (rows,), "mean", torch.float32)
     rstd = b.empty(rstd, (rows,), "rstd", torch.float32)
@@ -453,7 +451,7 @@ def layer_norm_backward_plan(dy, x, mean, rstd, weight=None, dresidual=None, par
     _check_vector_dev(weight, "weight", dy)
     if dresidual is not None:
         _check_dev(dresidual, "dresidual", dy)
-    b = _Buffers(dy)
+    b = _Buffers(dy, stream)
     dx = b.empty(dx, tuple(x.shape), "dx")
     ws, ws_bytes = None, 0
     if params:
@@ -500,7 +498,7 @@ def dropout_plan(x, p: float, rng, residual=None, out=None, stream=None) -> Feed
     _check_dropout_dev((p, rng), x)
     if residual is not None:
         _check_dev(residual, "residual", x)
-    b = _Buffers(x)
+    b = _Buffers(x, stream)
     out = b.empty(out, tuple(x.shape), "out")
     desc = _drop_desc((p, rng))
     args = (code, _rows_of(x.shape), x.shape[-1], _ptr(x), _row_stride(x, "x"), _ref(desc),

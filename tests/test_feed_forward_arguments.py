@@ -94,3 +94,66 @@ def test_weight_gradient_goes_where_its_tensor_is(library, K, N, pad, order, giv
     assert torch.equal(read, _meant(w))
     least = K if args["order"] else N
     assert args["ldw"] >= least and args["lddw"] >= least
+
+
+class _Stream:
+    cuda_stream = 0x1234
+
+
+@pytest.fixture
+def streams(monkeypatch):
+    """Streams by name: which one is current, where tensors were allocated and
+    which ones they were recorded on."""
+    log = dict(current="first", made=[], recorded=[])
+
+    class Use:
+        def __init__(self, s):
+            self.s = s
+
+        def __enter__(self):
+            self.before, log["current"] = log["current"], self.s
+
+        def __exit__(self, *a):
+            log["current"] = self.before
+    empty = torch.empty
+
+    def noted(*a, **kw):
+        t = empty(*a, **kw)
+        log["made"].append((t.data_ptr(), log["current"]))
+        return t
+    monkeypatch.setattr(torch.cuda, "stream", Use)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda *a: log["current"])
+    monkeypatch.setattr(P, "_torch_stream", lambda s, d: "handle %x" % (s if isinstance(s, int) else s.cuda_stream))
+    monkeypatch.setattr(torch, "empty", noted)
+    monkeypatch.setattr(torch.Tensor, "record_stream", lambda t, s: log["recorded"].append((t.data_ptr(), s)))
+    return log
+
+
+def _calls(stream):
+    x, w, r = torch.zeros(6, 8), torch.zeros(8, 5), torch.zeros(2, dtype=torch.int64)
+    dy, v = torch.zeros(6, 5), torch.zeros(6)
+    return {"dense": lambda: P.dense_plan(x, w, pre=True, stream=stream),
+            "dense_backward": lambda: P.dense_backward_plan(dy, x, w, stream=stream),
+            "layer_norm": lambda: P.layer_norm_plan(x, stream=stream),
+            "layer_norm_backward": lambda: P.layer_norm_backward_plan(x, x, v, v, stream=stream),
+            "dropout": lambda: P.dropout_plan(x, 0.5, r, stream=stream)}
+
+
+@pytest.mark.parametrize("op", _calls(None))
+def test_buffers_are_the_streams_own(library, streams, op):
+    # memory that the current stream has freed may still be read there: what a
+    # call on another stream writes is allocated for that one
+    for stream, name in ((None, "first"), (_Stream(), "handle 1234")):
+        call = _calls(stream)[op]
+        streams["made"].clear()
+        streams["recorded"].clear()
+        plan = call()
+        assert streams["made"] and {s for _, s in streams["made"]} == {name}
+        assert streams["current"] == "first"
+        # and the caller, who reads it on the current stream, may free it at any time
+        assert streams["recorded"] == ([] if stream is None else [(p, "first") for p, _ in streams["made"]])
+        # a plan's call on a third stream, as torch's or by its handle
+        for third in (7, type("S", (), {"cuda_stream": 7})()):
+            streams["recorded"].clear()
+            plan(third)
+            assert sorted(streams["recorded"]) == sorted((p, "handle 7") for p, _ in streams["made"])
