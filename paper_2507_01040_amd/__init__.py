@@ -316,7 +316,7 @@ def from_paper_protocol(filters, bias=None):
     return last(filters), last(bias)
 
 
-def _conv_checked(x, filters, bias, g: Sequence[int], act, out):
+def _conv_checked(x, filters, bias, g: Sequence[int], act, out, stream=None):
     """conv_nd's checks; returns the call's sizes, the output tensor and the
     activation descriptor."""
     import torch
@@ -336,7 +336,7 @@ def _conv_checked(x, filters, bias, g: Sequence[int], act, out):
         _check_dev(bias, "bias", x.device)
     _check_act_dev(act, x.device, "act")
     if out is None:
-        out = torch.empty(shape, dtype=torch.float32, device=x.device)
+        out = _empty(shape, torch.float32, x.device, stream)
     _check_dev(out, "out", x.device)
     return (k, B, C_in, C_out, d_image, d_filter), out, _act_desc(act)
 
@@ -351,7 +351,7 @@ def conv_nd(x, filters, bias, g: Sequence[int], act: Optional[Tuple] = None,
     checked before the library is called: the C ABI takes raw pointers and
     cannot check the buffers behind them."""
     (k, B, C_in, C_out, d_image, d_filter), out, desc = _conv_checked(x, filters, bias, g,
-                                                                       act, out)
+                                                                       act, out, stream)
     st = clifford_conv_nd_algo(k, g, B, C_in, C_out, d_image, d_filter,
                                x.data_ptr(), filters.data_ptr(),
                                bias.data_ptr() if bias is not None else 0,
@@ -368,9 +368,12 @@ class Plan:
     for, ``plan(stream)`` on another torch stream (or raw stream handle); a
     status other than CLIFF_OK raises CliffError.  The library checks its
     arguments on every call as usual.  The plan holds references to its
-    tensors and descriptors; ``plan.out`` is the output tensor."""
+    tensors and descriptors; ``plan.out`` is the output tensor.  Those of them
+    that were allocated for the plan (``own``) are its stream's: another stream
+    has to wait for that one first, as for every tensor of another stream, and
+    torch's allocator is told that they are used there."""
 
-    def __init__(self, fn, args, stream_index: int, name: str, out, keep):
+    def __init__(self, fn, args, stream_index: int, name: str, out, keep, own=()):
         self._fn = fn
         self._args = list(args)
         self._si = stream_index
@@ -378,11 +381,14 @@ class Plan:
         self._name = name
         self.out = out
         self._keep = keep
+        self._own = own
 
     def __call__(self, stream=None):
         if stream is None:
             self._args[self._si] = self._stream
         else:
+            for t in self._own:
+                t.record_stream(_torch_stream(stream, t.device))
             handle = int(stream.cuda_stream) if hasattr(stream, "cuda_stream") else int(stream)
             self._args[self._si] = handle or None
         st = self._fn(*self._args)
@@ -395,14 +401,15 @@ def conv_plan(x, filters, bias, g: Sequence[int], act: Optional[Tuple] = None,
               out=None, stream=None, algo: int = ALGO_AUTO) -> Plan:
     """conv_nd as a Plan: the checks of conv_nd once, then each call only the
     C ABI call (``out`` is allocated here unless given)."""
+    own_out = out is None
     (k, B, C_in, C_out, d_image, d_filter), out, desc = _conv_checked(x, filters, bias, g,
-                                                                       act, out)
+                                                                       act, out, stream)
     garr = _g_array(g)
     args = (k, garr, B, C_in, C_out, d_image, d_filter, x.data_ptr(), filters.data_ptr(),
             bias.data_ptr() if bias is not None else None, out.data_ptr(),
             ctypes.byref(desc) if desc is not None else None, _stream_ptr(stream) or None, algo)
     return Plan(load().clifford_conv_nd_algo, args, 12, "clifford_conv_nd", out,
-                (x, filters, bias, act, garr, desc))
+                (x, filters, bias, act, garr, desc), (out,) if own_out else ())
 
 
 def linear(x, weight, bias, g: Sequence[int], act: Optional[Tuple] = None,
@@ -431,7 +438,7 @@ def linear(x, weight, bias, g: Sequence[int], act: Optional[Tuple] = None,
         _check_dev(bias, "bias", x.device)
     _check_act_dev(act, x.device, "act")
     if out is None:
-        out = torch.empty((B, C_out, nb), dtype=torch.float32, device=x.device)
+        out = _empty((B, C_out, nb), torch.float32, x.device, stream)
     _check_dev(out, "out", x.device)
     desc = _act_desc(act)
     st = clifford_linear(k, g, B, C_in, C_out, x.data_ptr(), weight.data_ptr(),
@@ -462,7 +469,7 @@ def act_nd(x, mode: int, blades: Sequence[int], weight=None, bias=None,
     _check_dev(x, "x")
     _check_act_dev((mode, blades, weight, bias), x.device, "activation")
     if out is None:
-        out = torch.empty_like(x)
+        out = _empty(xs, x.dtype, x.device, stream)
     _check_dev(out, "out", x.device)
     desc = _act_desc((mode, blades, weight, bias))
     st = multivector_act(nb, B, C, P, desc, x.data_ptr(), out.data_ptr(),
@@ -480,7 +487,7 @@ def _act_desc(act):
                          ab.data_ptr() if ab is not None else 0)
 
 
-def _block2_checked(x, layer1, layer2, g: Sequence[int], out, workspace):
+def _block2_checked(x, layer1, layer2, g: Sequence[int], out, workspace, stream=None):
     """block2's checks; returns the call's sizes, the workspace and output
     tensors and both activation descriptors."""
     import torch
@@ -520,9 +527,9 @@ def _block2_checked(x, layer1, layer2, g: Sequence[int], out, workspace):
     _check_act_dev(a1, x.device, "act1")
     _check_act_dev(a2, x.device, "act2")
     if workspace is None:
-        workspace = torch.empty(ws_shape, dtype=torch.float32, device=x.device)
+        workspace = _empty(ws_shape, torch.float32, x.device, stream)
     if out is None:
-        out = torch.empty(out_shape, dtype=torch.float32, device=x.device)
+        out = _empty(out_shape, torch.float32, x.device, stream)
     _check_dev(workspace, "workspace", x.device)
     _check_dev(out, "out", x.device)
     return ((k, B, C_in, C_mid, C_out, d_image, d_filter), workspace, out, _act_desc(a1),
@@ -538,7 +545,7 @@ def block2(x, layer1, layer2, g: Sequence[int], out=None, workspace=None, stream
     is called."""
     (f1, b1, _), (f2, b2, _) = layer1, layer2
     (k, B, C_in, C_mid, C_out, d_image, d_filter), workspace, out, d1, d2 = _block2_checked(
-        x, layer1, layer2, g, out, workspace)
+        x, layer1, layer2, g, out, workspace, stream)
     st = clifford_block2_nd_path(k, g, B, C_in, C_mid, C_out, d_image, d_filter,
                                  x.data_ptr(), f1.data_ptr(),
                                  b1.data_ptr() if b1 is not None else 0, d1,
@@ -554,8 +561,9 @@ def block2_plan(x, layer1, layer2, g: Sequence[int], out=None, workspace=None, s
                 path: int = 0) -> Plan:
     """block2 as a Plan: the checks once, then each call only the C ABI call."""
     (f1, b1, a1), (f2, b2, a2) = layer1, layer2
+    given = (workspace, out)
     (k, B, C_in, C_mid, C_out, d_image, d_filter), workspace, out, d1, d2 = _block2_checked(
-        x, layer1, layer2, g, out, workspace)
+        x, layer1, layer2, g, out, workspace, stream)
     garr = _g_array(g)
     args = (k, garr, B, C_in, C_mid, C_out, d_image, d_filter, x.data_ptr(), f1.data_ptr(),
             b1.data_ptr() if b1 is not None else None,
@@ -564,7 +572,8 @@ def block2_plan(x, layer1, layer2, g: Sequence[int], out=None, workspace=None, s
             ctypes.byref(d2) if d2 is not None else None, workspace.data_ptr(), out.data_ptr(),
             _stream_ptr(stream) or None, path)
     return Plan(load().clifford_block2_nd_path, args, 17, "clifford_block2_nd", out,
-                (x, layer1, layer2, workspace, garr, d1, d2))
+                (x, layer1, layer2, workspace, garr, d1, d2),
+                [t for t, of in zip((workspace, out), given) if of is None])
 
 
 def block_forward(x, layers, g: Sequence[int], outs=None, stream=None):

@@ -198,16 +198,12 @@ def _weight_order(w, name: str = "weight", like=None) -> Tuple[int, int]:
 
 
 class FeedForwardPlan(_pkg.Plan):
-    """A Plan whose output may be a tuple of tensors.  Called for another
-    stream, it tells torch's allocator that its buffers are used there; they
-    are the plan's stream's, so that the other one has to wait for it first, as
-    for every tensor of another stream."""
+    """A Plan whose output may be a tuple of tensors."""
 
     def __init__(self, fn, args, stream_index: int, name: str, out, keep, own=()):
         # converted once: a call that is repeated is mostly this and the launch
         args = [t(a) if isinstance(a, (int, float)) else a for t, a in zip(fn.argtypes, args)]
-        super().__init__(fn, args, stream_index, name, out, keep)
-        self._own = own
+        super().__init__(fn, args, stream_index, name, out, keep, own)
         self._same_stream = functools.partial(fn, *args)
 
     def __call__(self, stream=None):
@@ -216,8 +212,6 @@ class FeedForwardPlan(_pkg.Plan):
             if st != _pkg.CLIFF_OK:
                 raise _pkg.CliffError(st, self._name)
             return self.out
-        for t in self._own:
-            t.record_stream(_pkg._torch_stream(stream, t.device))
         return super().__call__(stream)
 
 
