@@ -52,7 +52,7 @@ extern "C" {
 
 typedef enum { CLIFF_F32 = 0, CLIFF_BF16 = 1, CLIFF_F16 = 2 } cliff_dtype;
 
-/* Pointwise activations f of a dense layer. */
+/* Pointwise activations f of a dense layer.  f(NaN) and f'(NaN) are NaN. */
 typedef enum {
     CLIFF_ACT_NONE = 0,
     CLIFF_ACT_RELU = 1, /* max(v, 0); slope 0 at 0 */

@@ -194,7 +194,7 @@ __device__ inline float activate(int act, float v)
 {
     float e;
     switch (act) {
-    case CLIFF_ACT_RELU: return v > 0.f ? v : 0.f;
+    case CLIFF_ACT_RELU: return v <= 0.f ? 0.f : v;  // NaN stays
     case CLIFF_ACT_GELU: return v * gelu_cdf<FINE>(v, e);
     case CLIFF_ACT_SILU: return v * reciprocal(1.0f + __expf(-v));
     }
@@ -206,7 +206,7 @@ __device__ inline float activate_slope(int act, float v)
 {
     float e;
     switch (act) {
-    case CLIFF_ACT_RELU: return v > 0.f ? 1.f : 0.f;
+    case CLIFF_ACT_RELU: return v > 0.f ? 1.f : v <= 0.f ? 0.f : v;  // NaN stays
     case CLIFF_ACT_GELU: {
         const float c = gelu_cdf<FINE>(v, e);
         return fmaf(v * 0.39894228040143268f, e, c);

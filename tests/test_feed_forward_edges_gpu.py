@@ -65,3 +65,42 @@ def test_buffers_of_a_call_on_another_stream():
     got = plan(side.cuda_stream)
     torch.cuda.current_stream().wait_stream(side)
     assert torch.equal(got, want)
+
+
+# each kernel of the dense layer: few rows, tiles, panels, a split contraction
+@pytest.mark.parametrize("M,K,N", [(3, 64, 72), (200, 96, 136), (16400, 64, 40), (72, 4096, 40)])
+@pytest.mark.parametrize("act", [P.ACT_NONE, P.ACT_RELU, P.ACT_GELU, P.ACT_SILU])
+@pytest.mark.parametrize("dtype", DTYPES, ids=ids)
+def test_nan_passes_the_activations(dtype, act, M, K, N):
+    # a NaN in a row of x stays in that row of y, whatever the activation; so does
+    # one of the pre-activations in the gradient, where its element is kept
+    d = Draw(21, dtype)
+    x, w, res = d.rows(M, K), d.weight(K, N, "io"), d.rows(M, N)
+    x[2, K - 1] = float("nan")
+    y, pre = P.dense(x, w, act=act, residual=res, pre=True)
+    bad = torch.zeros(M, N, dtype=torch.bool, device="cuda:0")
+    bad[2] = True
+    assert torch.equal(torch.isnan(y), bad) and torch.equal(torch.isnan(pre), bad)
+    if act == P.ACT_NONE:
+        return
+    x[2, K - 1] = 0.0
+    pre = d.rows(M, N)
+    pre[2, 5] = float("nan")
+    keep = torch.from_numpy(O.philox_words(KEY, STEP, 3, 8)[2, 5:6] >= 2 ** 31).to("cuda:0")
+    for drop, kept in ((None, True), ((0.5, rng()), bool(keep))):
+        dx, dw, db = P.dense_backward(res, x, w, pre=pre, act=act, dropout=drop)
+        row, col = torch.zeros(M, dtype=torch.bool, device="cuda:0"), torch.zeros(N, dtype=torch.bool, device="cuda:0")
+        row[2], col[5] = kept, kept
+        assert torch.equal(torch.isnan(dx), row[:, None].expand(M, K))
+        assert torch.equal(torch.isnan(dw), col[None, :].expand(K, N))
+        assert torch.equal(torch.isnan(db), col)
+
+
+def test_relu_values():
+    v = torch.tensor([-0.0, 0.0, 1e-40, -1e-40, 3e38, -3e38, float("inf"), float("-inf"), float("nan")], device="cuda:0")
+    one = torch.ones(1, 1, device="cuda:0")
+    y = P.dense(v[:, None], one, act=P.ACT_RELU)[:, 0]
+    assert torch.equal(y[:-1], torch.tensor([0.0, 0.0, 1e-40, 0.0, 3e38, 0.0, float("inf"), 0.0], device="cuda:0"))
+    assert torch.isnan(y[-1])
+    g = P.dense_backward(torch.ones_like(v)[:, None], v[:, None], one, pre=v[:, None], act=P.ACT_RELU)[0][:, 0]
+    assert g[:-1].tolist() == [0.0, 0.0, 1.0, 0.0, 1.0, 0.0, 1.0, 0.0] and torch.isnan(g[-1])
