@@ -22,7 +22,7 @@ typedef __bf16 b8 __attribute__((ext_vector_type(8)));
 typedef _Float16 h8 __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) void lds_void;
 
-// C[m, n] = sum_k A(m, k) B(n, k): operand X is [R, K] with row stride ld
+// C[m, n] = scale sum_k A(m, k) B(n, k): operand X is [R, K] with row stride ld
 // (KM) or [K, R] with it.
 struct ProductArgs {
     int64_t M, N, K;
@@ -34,6 +34,7 @@ struct ProductArgs {
     int64_t k_part;   // ... of this many values (a multiple of the stage's)
     float* partial;   // splits > 1: fp32 [splits][M][N], joined by another kernel
     // epilogue
+    float scale;
     const void* bias;
     int act;
     DropArgs drop;
@@ -332,7 +333,9 @@ __device__ inline void finish_rows(const ProductArgs& p, int64_t m, int step, in
 #pragma unroll
     for (int r = 0; r < R; ++r) {
         if (!WHOLE && m + r * step >= p.M) break;
-        f4 u = v[r] + e.bias;
+        f4 u;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) u[i] = fmaf(v[r][i], p.scale, e.bias[i]);
         if (p.pre) store4(pre + r * (step * p.ldp), u, have);
         activate4<sizeof(T) == 4>(p.act, u);
         if (p.drop.rng) drop4(p.drop, e.key, e.step, m + r * step, n, u);
@@ -1294,9 +1297,21 @@ __global__ __launch_bounds__(512, 2) void panel_kernel(ProductArgs p)
     }
 }
 
-// g = dropout(dy) f'(pre) into g [M, N] (unless NULL), and its column sums over
-// a share of the rows into sums [part][N] (unless NULL).  A workgroup takes 256
-// columns; its four waves every fourth row each.  Bound by the vector instructions
+// What a product of g is multiplied by: the dropout's 1 / (1 - p), and 1 / fit_slope.
+// Both are left out of the 16-bit g, so that it is exact without an activation and
+// with ReLU (dy or zero), and does not overflow where dx and dw do not: the slopes
+// of GELU and SiLU are at most 1.13, which fp16 would not hold times its largest
+// dy.  Otherwise g's one rounding is at most 2^-8 (bf16) or 2^-11 (fp16) of it.
+constexpr float FIT_SLOPE = 0.875f;
+template <typename T>
+constexpr float fit_slope(int act)
+{
+    return __is_same(T, _Float16) && (act == CLIFF_ACT_GELU || act == CLIFF_ACT_SILU) ? FIT_SLOPE : 1.f;
+}
+
+// g = keep dy f'(pre) fit_slope into g [M, N] (unless NULL), and the column sums
+// of keep dy f'(pre) over a share of the rows into sums [part][N] (unless NULL).  A
+// workgroup takes 256 columns; its four waves every fourth row each.  Bound by the vector instructions
 // of f' and the generator: 8192 x 2048 bf16, GELU and dropout, 33 us (3 TB/s); 65536
 // x 512 fp32, SiLU, 85 us (4.7 TB/s, memory).
 template <typename T>
@@ -1312,6 +1327,8 @@ __global__ __launch_bounds__(256) void slope_kernel(DenseBackwardArgs a, T* g, f
         key = (uint64_t)a.drop.rng[0];
         step = (uint32_t)a.drop.rng[1];
     }
+    DropArgs keep = a.drop;
+    keep.scale = 1.f;
     f4 t = {0.f, 0.f, 0.f, 0.f};
     const int have = a.N - c < 4 ? (int)(a.N - c) : 4;
     if (c < a.N) {
@@ -1320,9 +1337,9 @@ __global__ __launch_bounds__(256) void slope_kernel(DenseBackwardArgs a, T* g, f
             f4 v = load4(static_cast<const T*>(a.dy) + r * a.lddy + c, have);
             if (a.act != CLIFF_ACT_NONE)
                 slope4<sizeof(T) == 4>(a.act, v, load4(static_cast<const T*>(a.pre) + r * a.ldp + c, have));
-            if (a.drop.rng) drop4(a.drop, key, step, r, c, v);
-            if (g) store4(g + r * a.N + c, v, have);
+            if (keep.rng) drop4(keep, key, step, r, c, v);
             t += v;
+            if (g) store4(g + r * a.N + c, v * fit_slope<T>(a.act), have);
         }
     }
     if (!sums) return;
@@ -1335,10 +1352,10 @@ __global__ __launch_bounds__(256) void slope_kernel(DenseBackwardArgs a, T* g, f
         if (c + e < a.N) sums[blockIdx.y * a.N + c + e] = t[e];
 }
 
-// Joins the parts [part][N] in a fixed order: 64 columns per workgroup, every
-// 16th part per wave.
+// dbias: scale times the parts [part][N], joined in a fixed order: 64 columns per
+// workgroup, every 16th part per wave.
 template <typename T>
-__global__ __launch_bounds__(1024) void bias_kernel(const float* sums, int parts, int64_t N, T* dbias)
+__global__ __launch_bounds__(1024) void bias_kernel(const float* sums, int parts, int64_t N, float scale, T* dbias)
 {
     __shared__ float s[16][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -1353,7 +1370,7 @@ __global__ __launch_bounds__(1024) void bias_kernel(const float* sums, int parts
     if (wave || c >= N) return;
     t = 0.f;
     for (int i = 0; i < 16; ++i) t += s[i][lane];
-    dbias[c] = (T)t;
+    dbias[c] = (T)(t * scale);
 }
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
@@ -1565,7 +1582,7 @@ cliff_status launch_dense(int dtype, const DenseArgs& a, hipStream_t stream)
     return with_type(dtype, [&](auto t) {
         using T = decltype(t);
         ProductArgs p{a.M, a.N, a.K, a.x, a.ldx, a.w, a.ldw, 1, 0, static_cast<float*>(a.workspace),
-                      a.bias, a.act, a.drop, a.residual, a.ldr, a.pre, a.ldp, a.y, a.ldy};
+                      1.f, a.bias, a.act, a.drop, a.residual, a.ldr, a.pre, a.ldp, a.y, a.ldy};
         return a.w_out_in ? product<T, true, true>(dtype, p, stream) : product<T, true, false>(dtype, p, stream);
     });
 }
@@ -1582,6 +1599,7 @@ cliff_status launch_dense_backward(int dtype, const DenseBackwardArgs& a, hipStr
         const int64_t ldg = change ? a.N : a.lddy;
         float* const sums = reinterpret_cast<float*>(ws + w.sums);
         float* const partial = reinterpret_cast<float*>(ws + w.partial);
+        const float scale = a.drop.rng ? a.drop.scale : 1.f;
         cliff_status s = CLIFF_OK;
         if (a.dbias || (change && (a.dx || a.dw))) {
             hipLaunchKernelGGL(slope_kernel<T>, dim3((unsigned)ceil_div(a.N, 256), (unsigned)w.parts), dim3(256), 0,
@@ -1591,14 +1609,14 @@ cliff_status launch_dense_backward(int dtype, const DenseBackwardArgs& a, hipStr
         }
         if (s == CLIFF_OK && a.dbias) {
             hipLaunchKernelGGL(bias_kernel<T>, dim3((unsigned)ceil_div(a.N, 64)), dim3(1024), 0, stream, sums,
-                               w.parts, a.N, static_cast<T*>(a.dbias));
+                               w.parts, a.N, scale, static_cast<T*>(a.dbias));
             s = launched();
         }
         const DropArgs none{nullptr, 0, 1.f};
         auto plain = [&](int64_t M, int64_t N, int64_t K, const void* x, int64_t ldx, const void* y, int64_t ldy,
                          void* out, int64_t ldo) {
-            return ProductArgs{M, N, K, x, ldx, y, ldy, 1, 0, partial, nullptr, CLIFF_ACT_NONE,
-                               none, nullptr, 0, nullptr, 0, out, ldo};
+            return ProductArgs{M, N, K, x, ldx, y, ldy, 1, 0, partial, scale / fit_slope<T>(a.act), nullptr,
+                               CLIFF_ACT_NONE, none, nullptr, 0, nullptr, 0, out, ldo};
         };
         if (s == CLIFF_OK && a.dx && a.M) {
             const ProductArgs p = plain(a.M, a.K, a.N, g, ldg, a.w, a.ldw, a.dx, a.lddx);

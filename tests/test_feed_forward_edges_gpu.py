@@ -104,3 +104,53 @@ def test_relu_values():
     assert torch.isnan(y[-1])
     g = P.dense_backward(torch.ones_like(v)[:, None], v[:, None], one, pre=v[:, None], act=P.ACT_RELU)[0][:, 0]
     assert g[:-1].tolist() == [0.0, 0.0, 1.0, 0.0, 1.0, 0.0, 1.0, 0.0] and torch.isnan(g[-1])
+
+
+def _exact_gradient(dy, x, w, pre, act, dropout, dtype):
+    """((dx, bound), (dw, bound), (db, bound)) where g is rounded nowhere: fp32 sums
+    of exact products, the scale and one rounding to the type (bounds as in
+    ff_oracle.py)."""
+    dy, x, w = (v.detach().cpu().double() for v in (dy, x, w))
+    M, N = dy.shape
+    g = dy if not act else dy * O.slope(act, pre.detach().cpu().double())
+    if dropout is not None:
+        g = g * O.mask(dropout, M, N)
+    u, t = O.UNIT[dtype], O.TINY[dtype]
+
+    def out(v, size, n):
+        e = (O.LAMBDA * n ** 0.5 + O.COST) * O.U * size
+        return v, e * (1 + u) + 2 * u * v.abs() + t
+    return (out(g @ w.t(), g.abs() @ w.abs().t(), N), out(x.t() @ g, x.abs().t() @ g.abs(), M),
+            out(g.sum(0), g.abs().sum(0), M))
+
+
+@pytest.mark.parametrize("size", [(40, 64, 520), (300, 512, 256), (16400, 40, 96)], ids=str)
+@pytest.mark.parametrize("act", [P.ACT_NONE, P.ACT_RELU])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16], ids=ids)
+def test_gradient_without_rounding(dtype, act, size):
+    # a dropped layer without an activation or with ReLU: g is dy or zero, and the
+    # dropout's 1 / (1 - p), no value of the type, multiplies the fp32 sums
+    M, K, N = size
+    d = Draw(M + N, dtype)
+    x, w, dy, pre = d.rows(M, K), d.weight(K, N, "io"), d.rows(M, N), d.rows(M, N)
+    got = P.dense_backward(dy, x, w, pre=pre, act=act, dropout=(0.3, rng()))
+    for g, v, name in zip(got, _exact_gradient(dy, x, w, pre, act, (0.3, (KEY, STEP)), dtype), ("dx", "dw", "db")):
+        O.check(g, v, name)
+
+
+@pytest.mark.parametrize("act", [P.ACT_NONE, P.ACT_RELU, P.ACT_GELU, P.ACT_SILU])
+def test_fp16_gradient_of_large_values(act):
+    # output gradients up to fp16's largest value: dx and dw are far below it, and
+    # finite, though dy f'(pre) / (1 - p) is not an fp16 value
+    M, K, N = 70, 48, 80
+    d = Draw(22, torch.float16)
+    x, w = d.rows(M, K, scale=1e-3), d.weight(K, N, "io") * 0.01
+    dy = torch.where(d.rows(M, N) > 0, 65504.0, -65504.0).half()
+    pre = d.rows(M, N, scale=0.1, shift=1.5)  # about the steepest point of GELU
+    for p in (0.0, 0.6):
+        drop = (p, (KEY, STEP)) if p else None
+        dx, dw, db = P.dense_backward(dy, x, w, pre=pre, act=act, dropout=(p, rng()) if p else None)
+        want = O.dense_backward(dy, x, w, pre, act, drop, torch.float16)
+        assert float(want[0][0].abs().max()) < 65504 and float(want[1][0].abs().max()) < 65504
+        O.check(dx, want[0], "dx p %g" % p)
+        O.check(dw, want[1], "dw p %g" % p)
