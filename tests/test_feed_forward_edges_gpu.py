@@ -154,3 +154,21 @@ def test_fp16_gradient_of_large_values(act):
         assert float(want[0][0].abs().max()) < 65504 and float(want[1][0].abs().max()) < 65504
         O.check(dx, want[0], "dx p %g" % p)
         O.check(dw, want[1], "dw p %g" % p)
+
+
+def test_silu_keeps_the_digits_of_its_left_tail():
+    # e = exp(-|v|), 1 + e, its reciprocal and three products round to about 8 units
+    # of 2^-24 of the value (16 allowed); the slope's 1 + v (1 - s) adds as many times
+    # |v| (1 - s) / |1 + v (1 - s)|, at most 2.4 from v = -2 on (32 allowed).  Results
+    # below the smallest normal float are multiples of 2^-149.
+    v = torch.cat([torch.linspace(-104, 12, 8001), torch.linspace(-89, -86, 2000)])
+    x = v.to("cuda:0")[:, None]
+    one = torch.ones(1, 1, device="cuda:0")
+    y = P.dense(x, one, act=P.ACT_SILU).cpu().double()[:, 0]
+    want = O.act(3, v.double())
+    assert float(((y - want).abs() - 2.0 ** -20 * want.abs() - 110 * 2.0 ** -149).max()) <= 0
+    g = P.dense_backward(torch.ones_like(x), x, one, pre=x, act=P.ACT_SILU)[0].cpu().double()[:, 0]
+    want = O.slope(3, v.double())
+    tail = v <= -2
+    assert float(((g - want).abs() - 2.0 ** -19 * want.abs() - 110 * 2.0 ** -149)[tail].max()) <= 0
+    assert float((g - want).abs()[~tail].max()) <= 2.0 ** -19
