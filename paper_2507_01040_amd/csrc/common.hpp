@@ -90,7 +90,7 @@ int device_cus();
 
 // Launch observation, for the host-side bounds checker (test
 // infrastructure): a CPU build of the library installs an observer, and every
-// launcher then hands it the launch's plan (kernel, template arguments, grid,
+// launcher of cliffconv.h's layers then hands it the launch's plan (kernel, template arguments, grid,
 // workgroup size, LDS bytes, argument block) instead of enqueueing the
 // kernel, and returns CLIFF_OK.  The checker walks the kernel's address
 // arithmetic over every workgroup and lane of the plan.  No observer is ever

@@ -9,6 +9,7 @@
 
 #include "dense_geom.hpp"
 #include "ff_common.hpp"
+#include "lds_load.hpp"
 #include "split.hpp"
 
 namespace cliff {
@@ -20,7 +21,6 @@ typedef short s4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u4 __attribute__((ext_vector_type(4)));
 typedef __bf16 b8 __attribute__((ext_vector_type(8)));
 typedef _Float16 h8 __attribute__((ext_vector_type(8)));
-typedef __attribute__((address_space(3))) void lds_void;
 
 // C[m, n] = scale sum_k A(m, k) B(n, k): operand X is [R, K] with row stride ld
 // (KM) or [K, R] with it.
@@ -149,11 +149,6 @@ struct StageOf {
     static constexpr bool KM = KM_;
 };
 
-constexpr uint32_t NOWHERE = 0x80000000u;  // past every descriptor's end: loads zeros
-
-// Until this wave's direct loads have arrived (vmcnt 0).
-__device__ inline void wait_direct() { __builtin_amdgcn_s_waitcnt(0x0f70); }
-
 // Stages of one operand's tile, from its first row and contraction value.
 template <typename T, typename SO, int NT>
 struct Operand {
@@ -176,22 +171,13 @@ struct Operand {
         }
     }
     // Piece i of L of stage s straight to LDS; slots past the last value become
-    // zeros.  The load is inline asm without outputs: as a builtin, every
-    // transposing read of LDS, of the other buffer too, waits for all of them.
-    // The caller waits (wait_direct) before the barrier that makes the stage
-    // readable.
+    // zeros.  The caller waits (wait_direct) before the barrier that makes the
+    // stage readable.
     __device__ void direct(uint32_t off, int i, int s, char* to, int tid, int wave) const
     {
-        const uint64_t address = (uint64_t)(x + (S.KM ? (int64_t)s * S.KT : (int64_t)s * S.KT * ld));
-        const u4 d = {(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)address),
-                      (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(address >> 32)) & 0xffffu, 0x7fffffffu,
-                      0x00020000u};
         const int n = left(s);
         if (n < S.KT && S.slot_k(i * NT + tid) >= n) off = NOWHERE;
-        __asm__ volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
-                         :
-                         : "s"((uint32_t)(uintptr_t)(lds_void*)to + wave * 1024 + i * NT * 16), "v"(off), "s"(d)
-                         : "memory", "m0");
+        load_to_lds(x + (S.KM ? (int64_t)s * S.KT : (int64_t)s * S.KT * ld), off, to + wave * 1024 + i * NT * 16);
     }
     __device__ int left(int s) const  // of a stage's values, those that exist
     {
