@@ -411,7 +411,9 @@ __global__ __launch_bounds__(64 * WR * WC) void product_kernel(ProductArgs p)
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave / WC * WM, wn = wave % WC * WN;
 
-    const TileId id = tile_of(blockIdx.x, (uint32_t)((p.M + BM - 1) / BM), (uint32_t)((p.N + BN - 1) / BN), p.splits);
+    const uint32_t tm = (uint32_t)((p.M + BM - 1) / BM), tn = (uint32_t)((p.N + BN - 1) / BN);
+    if (workgroup_id() >= tm * tn * p.splits) return;
+    const TileId id = tile_of(workgroup_id(), tm, tn, p.splits);
     const int64_t m0 = (int64_t)id.m * BM, n0 = (int64_t)id.n * BN, k0 = id.split * p.k_part;
     const int64_t kn = p.K - k0 < p.k_part ? p.K - k0 : p.k_part;
     const int steps = kn > 0 ? (int)((kn + KT - 1) / KT) : 0;
@@ -569,7 +571,9 @@ __global__ __launch_bounds__(256, 2) void split_product_kernel(ProductArgs p)
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave / 2 * 64, wn = wave % 2 * 64;
 
-    const TileId id = tile_of(blockIdx.x, (uint32_t)((p.M + BM - 1) / BM), (uint32_t)((p.N + BN - 1) / BN), p.splits);
+    const uint32_t tm = (uint32_t)((p.M + BM - 1) / BM), tn = (uint32_t)((p.N + BN - 1) / BN);
+    if (workgroup_id() >= tm * tn * p.splits) return;
+    const TileId id = tile_of(workgroup_id(), tm, tn, p.splits);
     const int64_t m0 = (int64_t)id.m * BM, n0 = (int64_t)id.n * BN, k0 = id.split * p.k_part;
     const int64_t kn = p.K - k0 < p.k_part ? p.K - k0 : p.k_part;
     const int steps = kn > 0 ? (int)((kn + KT - 1) / KT) : 0;
@@ -711,7 +715,7 @@ __global__ __launch_bounds__(256) void join_kernel(ProductArgs p)
     __shared__ f4 part[4][WAVES == 4 ? 64 : 1];
     const int lane = threadIdx.x & 63, wave = WAVES == 4 ? threadIdx.x >> 6 : 0;
     const int64_t nq = (p.N + 3) / 4, plane = p.M * p.N;
-    const int64_t i = WAVES == 4 ? blockIdx.x * 64ll + lane : blockIdx.x * 256ll + threadIdx.x;
+    const int64_t i = WAVES == 4 ? workgroup_id() * 64ll + lane : workgroup_id() * 256ll + threadIdx.x;
     const int64_t m = i >> 32 ? i / nq : (int64_t)((uint32_t)i / (uint32_t)nq), n = (i - m * nq) * 4;
     const int have = p.N - n < 4 ? (int)(p.N - n) : 4;
     f4 v[1] = {f4{0.f, 0.f, 0.f, 0.f}};
@@ -1339,24 +1343,27 @@ __global__ __launch_bounds__(256) void slope_kernel(DenseBackwardArgs a, T* g, f
 }
 
 // dbias: scale times the parts [part][N], joined in a fixed order: 64 columns per
-// workgroup, every 16th part per wave.
+// workgroup at a time, every 16th part per wave.
 template <typename T>
 __global__ __launch_bounds__(1024) void bias_kernel(const float* sums, int parts, int64_t N, float scale, T* dbias)
 {
     __shared__ float s[16][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t c = blockIdx.x * 64ll + lane;
-    float t = 0.f;
-    if (c < N) {
+    for (int64_t c0 = blockIdx.x * 64ll; c0 < N; c0 += gridDim.x * 64ll) {
+        const int64_t c = c0 + lane;
+        float t = 0.f;
+        if (c < N) {
 #pragma unroll 8
-        for (int i = wave; i < parts; i += 16) t += sums[i * N + c];
+            for (int i = wave; i < parts; i += 16) t += sums[i * N + c];
+        }
+        __syncthreads();  // the columns before are done with
+        s[wave][lane] = t;
+        __syncthreads();
+        if (wave || c >= N) continue;
+        t = 0.f;
+        for (int i = 0; i < 16; ++i) t += s[i][lane];
+        dbias[c] = (T)(t * scale);
     }
-    s[wave][lane] = t;
-    __syncthreads();
-    if (wave || c >= N) return;
-    t = 0.f;
-    for (int i = 0; i < 16; ++i) t += s[i][lane];
-    dbias[c] = (T)(t * scale);
 }
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
@@ -1404,8 +1411,9 @@ Cut cut(int dtype, int64_t M, int64_t N, int64_t K, bool direct)
     return best;
 }
 
-// What the kernels of few rows are for: rows and row strides (32-bit offsets).
-constexpr int64_t FEW_ROWS = 64, FEW_LD = 1 << 23;
+// What the kernels of few rows are for: rows, row strides (32-bit offsets), and
+// outputs (2^32 threads of a grid).
+constexpr int64_t FEW_ROWS = 64, FEW_LD = 1 << 23, FEW_N = 1 << 26;
 
 // The time in ns of few_rows, from bytes that a compute unit takes in, to choose
 // between it and the tiles: every workgroup reads all of A, so that with a long
@@ -1446,7 +1454,7 @@ cliff_status run(K k, const char* name, int B, int threads, int stage, const Pro
     if (debug_enabled())
         fprintf(stderr, "cliffconv: product %lld x %lld x %lld, %s tiles of %d, %lld workgroups, %d splits\n",
                 (long long)p.M, (long long)p.N, (long long)p.K, name, B, (long long)wgs, p.splits);
-    hipLaunchKernelGGL(k, dim3((unsigned)wgs), dim3(threads), lds, stream, p);
+    hipLaunchKernelGGL(k, grid_of(wgs), dim3(threads), lds, stream, p);
     return launched();
 }
 
@@ -1510,7 +1518,7 @@ cliff_status product(int dtype, ProductArgs p, hipStream_t stream)
     const Cut c = cut(dtype, p.M, p.N, p.K, direct);
     if constexpr (AKM) {
         if (p.M <= FEW_ROWS && p.K >= per16<T> && (BKM || p.N >= per16<T>) && p.lda <= FEW_LD && p.ldb <= FEW_LD &&
-            few_rows_ns<T, BKM>(p) < c.ns)
+            p.N <= FEW_N && few_rows_ns<T, BKM>(p) < c.ns)
             return few_rows<T, BKM>(p, stream);
         if (p.M >= PANEL_ROWS && p.K <= PANEL_K && p.K >= per16<T>) return panel<T, BKM>(p, stream);
     }
@@ -1532,7 +1540,7 @@ cliff_status product(int dtype, ProductArgs p, hipStream_t stream)
     const bool one = groups >= JOIN_GROUPS;
     const int64_t blocks = ceil_div(groups, one ? 256 : 64);
     if (blocks >= (int64_t)1 << 31) return CLIFF_EUNSUPPORTED;
-    hipLaunchKernelGGL((one ? join_kernel<T, 1> : join_kernel<T, 4>), dim3((unsigned)blocks), dim3(256), 0, stream, p);
+    hipLaunchKernelGGL((one ? join_kernel<T, 1> : join_kernel<T, 4>), grid_of(blocks), dim3(256), 0, stream, p);
     return launched();
 }
 
@@ -1594,7 +1602,7 @@ cliff_status launch_dense_backward(int dtype, const DenseBackwardArgs& a, hipStr
             s = launched();
         }
         if (s == CLIFF_OK && a.dbias) {
-            hipLaunchKernelGGL(bias_kernel<T>, dim3((unsigned)ceil_div(a.N, 64)), dim3(1024), 0, stream, sums,
+            hipLaunchKernelGGL(bias_kernel<T>, dim3((unsigned)std::min(ceil_div(a.N, 64), GRID_ROW)), dim3(1024), 0, stream, sums,
                                w.parts, a.N, scale, static_cast<T*>(a.dbias));
             s = launched();
         }

@@ -22,7 +22,7 @@ template <typename T>
 __global__ __launch_bounds__(256) void dropout_kernel(DropoutArgs a, uint32_t pieces, int64_t n)
 {
     constexpr int E = per16<T>;
-    const int64_t i = blockIdx.x * 256ll + threadIdx.x;
+    const int64_t i = workgroup_id() * 256ll + threadIdx.x;
     if (i >= n) return;
     const int64_t g = n >> 32 ? i / pieces : (int64_t)((uint32_t)i / pieces), r0 = g * ROWS;
     const int col = (int)(i - g * pieces) * E, have = (int)a.d - col;
@@ -79,7 +79,7 @@ cliff_status launch_dropout(int dtype, const DropoutArgs& a, hipStream_t stream)
         if (debug_enabled())
             fprintf(stderr, "cliffconv: dropout %lld x %lld, %lld workgroups\n", (long long)a.rows, (long long)a.d,
                     (long long)blocks);
-        hipLaunchKernelGGL(dropout_kernel<T>, dim3((unsigned)blocks), dim3(256), 0, stream, a, (uint32_t)pieces, n);
+        hipLaunchKernelGGL(dropout_kernel<T>, grid_of(blocks), dim3(256), 0, stream, a, (uint32_t)pieces, n);
         return launched();
     });
 }

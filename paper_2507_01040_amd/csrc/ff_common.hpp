@@ -115,6 +115,16 @@ inline cliff_status launched()
     return hipGetLastError() == hipSuccess ? CLIFF_OK : CLIFF_EDEVICE;
 }
 
+// A grid of n workgroups, and a workgroup's place in it.  HIP takes fewer than
+// 2^32 threads along an axis, so that wide grids have rows; the last row can pass
+// n, and workgroups there have nothing to do.
+constexpr int64_t GRID_ROW = 1 << 16;
+inline dim3 grid_of(int64_t n)
+{
+    return n <= GRID_ROW ? dim3((unsigned)n) : dim3((unsigned)GRID_ROW, (unsigned)((n + GRID_ROW - 1) / GRID_ROW));
+}
+__device__ inline uint32_t workgroup_id() { return blockIdx.y * (uint32_t)GRID_ROW + blockIdx.x; }
+
 // Calls f with a value of the element type of `dtype`.
 template <typename F>
 cliff_status with_type(int dtype, F f)

@@ -321,27 +321,30 @@ __global__ __launch_bounds__(256) void norm_wide_sums_kernel(NormBackwardArgs a,
 }
 
 // Joins the parts [part][2][d] in a fixed order: 64 of the 2 d columns per
-// workgroup, every 16th part per wave.
+// workgroup at a time, every 16th part per wave.
 template <typename T>
 __global__ __launch_bounds__(1024) void norm_join_kernel(NormBackwardArgs a, const float* sums, int parts)
 {
     __shared__ float s[16][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t c = blockIdx.x * 64ll + lane;
-    float v = 0.f;
-    if (c < 2 * a.d) {
+    for (int64_t c0 = blockIdx.x * 64ll; c0 < 2 * a.d; c0 += gridDim.x * 64ll) {
+        const int64_t c = c0 + lane;
+        float v = 0.f;
+        if (c < 2 * a.d) {
 #pragma unroll 8
-        for (int i = wave; i < parts; i += 16) v += sums[2 * a.d * i + c];
-    }
-    s[wave][lane] = v;
-    __syncthreads();
-    if (wave || c >= 2 * a.d) return;
-    v = 0.f;
-    for (int i = 0; i < 16; ++i) v += s[i][lane];
-    if (c < a.d) {
-        if (a.dweight) static_cast<T*>(a.dweight)[c] = (T)v;
-    } else if (a.dbias) {
-        static_cast<T*>(a.dbias)[c - a.d] = (T)v;
+            for (int i = wave; i < parts; i += 16) v += sums[2 * a.d * i + c];
+        }
+        __syncthreads();  // the columns before are done with
+        s[wave][lane] = v;
+        __syncthreads();
+        if (wave || c >= 2 * a.d) continue;
+        v = 0.f;
+        for (int i = 0; i < 16; ++i) v += s[i][lane];
+        if (c < a.d) {
+            if (a.dweight) static_cast<T*>(a.dweight)[c] = (T)v;
+        } else if (a.dbias) {
+            static_cast<T*>(a.dbias)[c - a.d] = (T)v;
+        }
     }
 }
 
@@ -465,7 +468,7 @@ cliff_status launch_layer_norm_backward(int dtype, const NormBackwardArgs& a, hi
                                0, stream, a);
         }
         if (params)
-            hipLaunchKernelGGL(norm_join_kernel<T>, dim3((unsigned)ceil_div(2 * a.d, 64)), dim3(1024), 0, stream, a,
+            hipLaunchKernelGGL(norm_join_kernel<T>, dim3((unsigned)std::min(ceil_div(2 * a.d, 64), GRID_ROW)), dim3(1024), 0, stream, a,
                                sums, (int)parts);
         return launched();
     });

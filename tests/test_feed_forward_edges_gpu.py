@@ -172,3 +172,20 @@ def test_silu_keeps_the_digits_of_its_left_tail():
     tail = v <= -2
     assert float(((g - want).abs() - 2.0 ** -19 * want.abs() - 110 * 2.0 ** -149)[tail].max()) <= 0
     assert float((g - want).abs()[~tail].max()) <= 2.0 ** -19
+
+
+def test_grids_of_several_rows():
+    # more workgroups than one row of a grid holds: every output written, and right
+    for dtype, M, K, N in ((torch.bfloat16, 1, 1, (1 << 23) + 130), (torch.float32, (1 << 23) + 1, 2, 1),
+                           (torch.float16, (1 << 23) + 129, 1, 2)):
+        d = Draw(M + N, dtype)
+        x, w = torch.ones(M, K, dtype=dtype, device="cuda:0"), torch.ones(K, N, dtype=dtype, device="cuda:0")
+        (x if M > 1 else w).copy_(torch.arange(max(M, N), device="cuda:0").remainder(251).view(-1, 1) if M > 1 else
+                                  torch.arange(N, device="cuda:0").remainder(251).view(1, -1))
+        y = torch.full((M, N), -1.0, dtype=dtype, device="cuda:0")
+        P.dense(x, w, d.vector(N) * 0, out=y)
+        assert torch.equal(y, x.sum(1, keepdim=True) * w.sum(0, keepdim=True) / K)
+    x = torch.arange((1 << 25) + 9, device="cuda:0", dtype=torch.float32).remainder_(8191).expand(9, -1)
+    x = x + torch.arange(9, device="cuda:0")[:, None]
+    y = P.dropout(x, 0.0, rng(), residual=x)
+    assert torch.equal(y, x + x)

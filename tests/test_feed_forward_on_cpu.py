@@ -157,3 +157,23 @@ def _draw(r):
 def test_drawn_calls(seed):
     r = random.Random(seed)
     _run([_draw(r) for _ in range(60)])
+
+
+def test_widest_calls():
+    # nothing runs: every size that the header allows makes launches that HIP takes
+    # (fewer than 2^32 threads along an axis)
+    sizes = (1, 3, 8, 65, 1000, 16384, 1 << 24, (1 << 27) + 8, 1 << 30, (1 << 31) - 1)
+    cases = []
+    for t in ("fp32", "bf16"):
+        for M in sizes:
+            for K in sizes:
+                for N in sizes:
+                    if max(M * K, M * N, K * N) < 1 << 40:
+                        for oi in (0, 1):
+                            cases.append(dict(op="dense", type=t, M=M, K=K, N=N, oi=oi, dry=1))
+                            cases.append(dict(op="backward", type=t, M=M, K=K, N=N, oi=oi, act=3, dry=1))
+            for d in sizes:
+                if M * d < 1 << 40:
+                    cases += [dict(op=op, type=t, rows=M, d=d, p=0.5, dry=1) for op in ("norm", "norm_backward", "dropout")]
+    for r, _ in _run(cases):
+        assert 0 < int(r.split()[2]) < 1 << 32
