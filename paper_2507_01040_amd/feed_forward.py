@@ -9,7 +9,9 @@ float32, bfloat16 or float16, one type per call, and may be views whose rows
 have one stride and contiguous features.  As everywhere in the package, torch
 provides device memory and streams only; every tensor's shape, type, layout and
 device is checked before the library is called.  ``*_plan`` functions do the
-checks once, for a call that is repeated on the same buffers.
+checks once, for a call that is repeated on the same buffers.  Calls are not
+recorded by autograd: tensors that require a gradient are refused while it
+records (not under torch.no_grad()).
 """
 from __future__ import annotations
 
@@ -99,10 +101,21 @@ def _type_of(x, name: str) -> int:
     return codes[x.dtype]
 
 
+def _check_grad(t, name: str) -> None:
+    """The calls are not recorded by autograd: a tensor that requires a gradient
+    would lose it in silence."""
+    import torch
+    if getattr(t, "requires_grad", False) and torch.is_grad_enabled():
+        raise ValueError("%s requires a gradient, which autograd does not get from this call: call it "
+                         "under torch.no_grad() or on detached tensors, and its gradient by the "
+                         "*_backward function" % name)
+
+
 def _check_dev(t, name: str, like=None, dtype=None) -> None:
     import torch
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise ValueError("%s must be a GPU tensor" % name)
+    _check_grad(t, name)
     if like is not None and t.device != like.device:
         raise ValueError("%s is on %s, not on %s with the input" % (name, t.device, like.device))
     want = dtype if dtype is not None else like.dtype if like is not None else None

@@ -157,3 +157,35 @@ def test_buffers_are_the_streams_own(library, streams, op):
             streams["recorded"].clear()
             plan(third)
             assert sorted(streams["recorded"]) == sorted((p, "handle 7") for p, _ in streams["made"])
+
+
+@pytest.mark.parametrize("op", ["dense", "dense_backward", "layer_norm", "layer_norm_backward", "dropout"])
+def test_tensors_that_require_a_gradient(library, monkeypatch, op):
+    # autograd would not see the call: refused while it records, for each tensor
+    monkeypatch.setattr(F, "_check_dev", lambda t, name, *a, **kw: F._check_grad(t, name))
+
+    def tensors():
+        x, w, r = torch.zeros(6, 8), torch.zeros(8, 5), torch.zeros(2, dtype=torch.int64)
+        dy, v, m = torch.zeros(6, 5), torch.zeros(8), torch.zeros(6)
+        return {"dense": dict(x=x, weight=w, bias=torch.zeros(5), residual=dy, out=torch.zeros(6, 5)),
+                "dense_backward": dict(dy=dy, x=x, weight=w, dx=torch.zeros(6, 8), dweight=torch.zeros(8, 5),
+                                       dbias=torch.zeros(5)),
+                "layer_norm": dict(x=x, weight=v, bias=torch.zeros(8), out=torch.zeros(6, 8)),
+                "layer_norm_backward": dict(dy=x, x=torch.zeros(6, 8), mean=m, rstd=torch.zeros(6), weight=v,
+                                            dresidual=torch.zeros(6, 8)),
+                "dropout": dict(x=x, p=0.5, rng=r, residual=torch.zeros(6, 8))}[op]
+    call = getattr(P, op)
+    call(**tensors())
+    for name, t in tensors().items():
+        if not isinstance(t, torch.Tensor) or t.dtype != torch.float32:
+            continue
+        kw = tensors()
+        kw[name].requires_grad_()
+        with pytest.raises(ValueError, match="requires a gradient"):
+            call(**kw)
+        with torch.no_grad():
+            call(**kw)
+        with torch.inference_mode():
+            call(**kw)
+        kw[name] = kw[name].detach()
+        call(**kw)
