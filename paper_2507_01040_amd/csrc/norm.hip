@@ -166,7 +166,8 @@ __global__ __launch_bounds__(wg_threads(TPR), 2) void norm_backward_kernel(NormB
         settle_rows<T, TPR, R, C>(x, t, a.d);
         settle_rows<T, TPR, R, C>(dy, t, a.d);
         if (a.dresidual) settle_rows<T, TPR, R, C>(res, t, a.d);
-        // sums of q and of q h; elements that do not exist are zeros
+        // sums of q and of q (x - mean), which rstd multiplies as a whole: elements
+        // that do not exist have q zero, and mean times rstd need not be a float
         float s[2 * R];
 #pragma unroll
         for (int r = 0; r < R; ++r) s[2 * r] = s[2 * r + 1] = 0.f;
@@ -182,15 +183,20 @@ __global__ __launch_bounds__(wg_threads(TPR), 2) void norm_backward_kernel(NormB
                 unpack16<T>(dy[r][c], dv);
 #pragma unroll
                 for (int e = 0; e < E; ++e) {
-                    const float h = (xv[e] - mean[r]) * rstd[r], q = w ? dv[e] * wf[e] : dv[e];
+                    const float u = xv[e] - mean[r], q = w ? dv[e] * wf[e] : dv[e];
                     s[2 * r] += q;
-                    s[2 * r + 1] = fmaf(q, h, s[2 * r + 1]);
-                    dw[c][e] = fmaf(dv[e], h, dw[c][e]);
+                    s[2 * r + 1] = fmaf(q, u, s[2 * r + 1]);
+                    dw[c][e] = fmaf(dv[e], u * rstd[r], dw[c][e]);
                     db[c][e] += dv[e];
                 }
             }
         }
         row_sums<TPR, 2 * R>(s, lds[turn]);
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            s[2 * r] *= inv;
+            s[2 * r + 1] *= inv * rstd[r];
+        }
 #pragma unroll
         for (int c = 0; c < C; ++c) {
             const int col = (c * TPR + t) * E, have = (int)a.d - col;
@@ -205,7 +211,7 @@ __global__ __launch_bounds__(wg_threads(TPR), 2) void norm_backward_kernel(NormB
 #pragma unroll
                 for (int e = 0; e < E; ++e) {
                     const float h = (xv[e] - mean[r]) * rstd[r], q = w ? dv[e] * wf[e] : dv[e];
-                    const float u = rstd[r] * (q - s[2 * r] * inv - h * (s[2 * r + 1] * inv));
+                    const float u = rstd[r] * (q - s[2 * r] - h * s[2 * r + 1]);
                     v[e] = a.dresidual ? v[e] + u : u;
                 }
                 if (rg + r < a.rows) store16(static_cast<T*>(a.dx) + (rg + r) * a.lddx + col, v, have);

@@ -617,7 +617,8 @@ int norm_backward(Case& k)
     Mat x, dy, res, w, dx, dw, db, mean, rstd;
     rows(k, x, "x", R, d);
     rows(k, dy, "dy", R, d);
-    x.fill(k.g, 1.5f, 0.7f);
+    if (k.f.m.count("constant")) x.fill(k.g, 0, (float)k.f.d("constant"));
+    else x.fill(k.g, 1.5f, 0.7f);
     dy.fill(k.g, 1);
     if (k.f.i("residual")) rows(k, res, "res", R, d), res.fill(k.g, 1);
     if (k.f.i("w")) w.make(k.t, 1, d, d, k.f.i("off")), w.fill(k.g, 1);

@@ -177,3 +177,11 @@ def test_widest_calls():
                     cases += [dict(op=op, type=t, rows=M, d=d, p=0.5, dry=1) for op in ("norm", "norm_backward", "dropout")]
     for r, _ in _run(cases):
         assert 0 < int(r.split()[2]) < 1 << 32
+
+
+@pytest.mark.parametrize("t", ["fp32", "bf16"])
+def test_norm_gradient_of_large_constant_rows(t):
+    # x - mean is zero in every column, though mean times rstd (eps^-0.5 = 316) is no
+    # float: columns past the row's end, which fill its last pieces, add nothing
+    _run([dict(op="norm_backward", type=t, rows=3, d=d, constant=2.0 ** 123, w=1, residual=1)
+          for d in (1, 5, 16, 130, 300, 1025, 9000)])
