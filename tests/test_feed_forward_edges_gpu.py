@@ -5,6 +5,7 @@ import torch
 
 import ff_oracle as O
 import paper_2507_01040_amd as P
+from ff_cases import LARGE_TILES
 from test_feed_forward_gpu import DTYPES, KEY, STEP, Draw, guarded, ids, rng
 
 pytestmark = pytest.mark.gpu
@@ -189,3 +190,30 @@ def test_grids_of_several_rows():
     x = x + torch.arange(9, device="cuda:0")[:, None]
     y = P.dropout(x, 0.0, rng(), residual=x)
     assert torch.equal(y, x + x)
+
+
+@pytest.mark.parametrize("dtype,order", [(torch.bfloat16, "io"), (torch.bfloat16, "oi"), (torch.float16, "io"),
+                                         (torch.float16, "oi")], ids=ids)
+def test_large_tiles(dtype, order):
+    # the 256 x 256 tiles (test_feed_forward_on_cpu.py asserts that these sizes take
+    # them): ragged edges, a last stage that is not whole, two stages, split
+    # contractions, the whole epilogue
+    for i, ((M, K, N), _, backward) in enumerate(LARGE_TILES):
+        if backward and (dtype == torch.bfloat16) != (order == "io") and i == 3:
+            continue  # (the oracle's time)
+        d = Draw(M + K + N, dtype)
+        x, w, b, res = d.rows(M, K, 8), d.weight(K, N, order), d.vector(N), d.rows(M, N, 3)
+        y, intact = guarded(M, N, dtype)
+        got, pre = P.dense(x, w, b, act=P.ACT_GELU, dropout=(0.15, rng()), residual=res, pre=True, out=y)
+        want, want_pre = O.dense(x, w, b, 2, (0.15, (KEY, STEP)), res, dtype)
+        O.check(pre, want_pre, "pre %d" % i)
+        O.check(got, want, "y %d" % i)
+        assert intact()
+        if backward:
+            dy = d.rows(M, N)
+            dx, intact = guarded(M, K, dtype)
+            dw, intact_w = _guarded_weight(order, K, N, dtype, 5)
+            got = P.dense_backward(dy, x, w, pre=pre, act=P.ACT_RELU, dx=dx, dweight=dw)
+            for g, v, name in zip(got, O.dense_backward(dy, x, w, pre, 1, None, dtype), ("dx", "dw", "db")):
+                O.check(g, v, "%s %d" % (name, i))
+            assert intact() and intact_w()

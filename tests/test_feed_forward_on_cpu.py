@@ -7,6 +7,7 @@ import random
 import pytest
 
 from cpu_kernels import build as C
+from ff_cases import LARGE_TILES
 
 TYPES = ["fp32", "bf16", "fp16"]
 
@@ -185,3 +186,14 @@ def test_norm_gradient_of_large_constant_rows(t):
     # float: columns past the row's end, which fill its last pieces, add nothing
     _run([dict(op="norm_backward", type=t, rows=3, d=d, constant=2.0 ** 123, w=1, residual=1)
           for d in (1, 5, 16, 130, 300, 1025, 9000)])
+
+
+def test_large_tiles_of_the_gpu_tests():
+    # which kernels the calls of test_feed_forward_edges_gpu.py take
+    for (M, K, N), forward, backward in LARGE_TILES:
+        for t in ("bf16", "fp16"):
+            for oi in (0, 1):
+                _run([dict(op="dense", type=t, M=M, K=K, N=N, oi=oi, dry=1)], forward)
+                if backward:
+                    _run([dict(op="backward", type=t, M=M, K=K, N=N, oi=oi, dry=1)],
+                         backward)
