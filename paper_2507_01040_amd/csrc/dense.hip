@@ -1090,7 +1090,8 @@ __global__ __launch_bounds__(512, 2) void rows_fp32_kernel(ProductArgs p)
 // 16 kk + 8 h + i, or for fp32 (whose 8 are two loads) 16 kk + 4 h + i and 8 on,
 // so that a row's two lanes read neighbours.  131072 x 128 x 512 fp32: 120 us (2.8
 // TB/s, and 145 TFLOP/s of products), 150 with bias and GELU, whose vector
-// instructions the products do not hide; bf16 42 us (4.0 TB/s).
+// instructions the products do not hide; bf16 with
+// bias 54 us, with bias and GELU 71 (3.1 and 2.4 TB/s).
 constexpr int PANEL = 128;
 template <typename T, bool BKM, int KK, bool WHOLE>
 __global__ __launch_bounds__(512, 2) void panel_kernel(ProductArgs p)
@@ -1429,7 +1430,7 @@ double few_rows_ns(const ProductArgs& p)
 }
 
 // What a product of rows (y or dx) or a weight's gradient needs for its parts.
-int64_t partial_bytes(int dtype, int64_t M, int64_t N, int64_t K, bool rows)
+int64_t partial_bytes(int dtype, int64_t M, int64_t N, int64_t K)
 {
     int64_t n = 0;
     for (int direct = 0; direct <= (dtype == CLIFF_F32 ? 0 : 1); ++direct) {
@@ -1475,10 +1476,12 @@ cliff_status few_rows(const ProductArgs& p, hipStream_t stream)
         return p.M <= 16 ? go(rows_kernel<T, BKM, 1>) : p.M <= 32 ? go(rows_kernel<T, BKM, 2>) : go(rows_kernel<T, BKM, 4>);
 }
 
-// Rows from which the panel kernel is ahead of the tiles (N 512, K 128, fp32, us:
-// 8192 rows 17.2 and 16.7 in tiles, 16384 rows 19.9 and 22.9, 131072 rows 120 and
-// 166; bf16 10.9 and 9.4, 12.2 and 11.9, 42 and 59), the contraction whose panel
-// fits LDS and whose rows fit registers, and its launch.
+// Rows from which the panel kernel is level with the tiles or ahead (us, bias alone,
+// panels and tiles; K 128, N 512: fp32 8192 rows 16.7 and 16.2, 16384 rows 19.2 and
+// 22.1, 131072 rows 119 and 156; bf16 10.8 and 9.4, 11.8 and 11.5, 54 and 64.  K 64,
+// N 256: ahead from 8192 rows.  K 128, N 128, one panel: behind by 1.5 up to 32768
+// rows, ahead from 65536), the contraction whose panel fits LDS in fp32 (in 16 bits
+// longer ones would; 131072 x 256 x 1024 bf16 takes the tiles 143), and its launch.
 constexpr int64_t PANEL_ROWS = 16384;
 constexpr int64_t PANEL_K = 128;
 
@@ -1557,14 +1560,14 @@ BackwardSpace backward_space(int dtype, int64_t M, int64_t K, int64_t N)
     w.g = 0;
     w.sums = ceil_div(M * N * (dtype == CLIFF_F32 ? 4 : 2), 256) * 256;
     w.partial = w.sums + ceil_div(w.parts * N * 4, 256) * 256;
-    w.all = w.partial + std::max({partial_bytes(dtype, M, K, N, true), partial_bytes(dtype, K, N, M, false),
-                                  partial_bytes(dtype, N, K, M, false)});
+    w.all = w.partial + std::max({partial_bytes(dtype, M, K, N), partial_bytes(dtype, K, N, M),
+                                  partial_bytes(dtype, N, K, M)});
     return w;
 }
 
 }  // namespace
 
-int64_t dense_workspace(int dtype, int64_t M, int64_t K, int64_t N) { return partial_bytes(dtype, M, N, K, true); }
+int64_t dense_workspace(int dtype, int64_t M, int64_t K, int64_t N) { return partial_bytes(dtype, M, N, K); }
 int64_t dense_backward_workspace(int dtype, int64_t M, int64_t K, int64_t N)
 {
     return backward_space(dtype, M, K, N).all;
