@@ -269,8 +269,13 @@ def _conv_dims(x, filters, k: int, name: str = "filters"):
     return B, C_in, C_out, d_image, d_filter
 
 
-def _stream_ptr(stream) -> int:
+def _stream_ptr(stream, device) -> int:
+    """The handle of a stream; None is the current one, which has to be one of
+    the tensors' device: another device's kernels would take their addresses."""
     import torch
+    if stream is None and device.type == "cuda" and device.index != torch.cuda.current_device():
+        raise ValueError("the tensors are on %s, but the current device is cuda:%d (torch.cuda.set_device)"
+                         % (device, torch.cuda.current_device()))
     s = stream if stream is not None else torch.cuda.current_stream()
     return int(s.cuda_stream)
 
@@ -355,7 +360,7 @@ def conv_nd(x, filters, bias, g: Sequence[int], act: Optional[Tuple] = None,
     st = clifford_conv_nd_algo(k, g, B, C_in, C_out, d_image, d_filter,
                                x.data_ptr(), filters.data_ptr(),
                                bias.data_ptr() if bias is not None else 0,
-                               out.data_ptr(), desc, _stream_ptr(stream), algo)
+                               out.data_ptr(), desc, _stream_ptr(stream, x.device), algo)
     if st != CLIFF_OK:
         raise CliffError(st, "clifford_conv_nd")
     return out
@@ -407,7 +412,7 @@ def conv_plan(x, filters, bias, g: Sequence[int], act: Optional[Tuple] = None,
     garr = _g_array(g)
     args = (k, garr, B, C_in, C_out, d_image, d_filter, x.data_ptr(), filters.data_ptr(),
             bias.data_ptr() if bias is not None else None, out.data_ptr(),
-            ctypes.byref(desc) if desc is not None else None, _stream_ptr(stream) or None, algo)
+            ctypes.byref(desc) if desc is not None else None, _stream_ptr(stream, x.device) or None, algo)
     return Plan(load().clifford_conv_nd_algo, args, 12, "clifford_conv_nd", out,
                 (x, filters, bias, act, garr, desc), (out,) if own_out else ())
 
@@ -443,7 +448,7 @@ def linear(x, weight, bias, g: Sequence[int], act: Optional[Tuple] = None,
     desc = _act_desc(act)
     st = clifford_linear(k, g, B, C_in, C_out, x.data_ptr(), weight.data_ptr(),
                          bias.data_ptr() if bias is not None else 0, out.data_ptr(),
-                         desc, _stream_ptr(stream))
+                         desc, _stream_ptr(stream, x.device))
     if st != CLIFF_OK:
         raise CliffError(st, "clifford_linear")
     return out
@@ -473,7 +478,7 @@ def act_nd(x, mode: int, blades: Sequence[int], weight=None, bias=None,
     _check_dev(out, "out", x.device)
     desc = _act_desc((mode, blades, weight, bias))
     st = multivector_act(nb, B, C, P, desc, x.data_ptr(), out.data_ptr(),
-                         _stream_ptr(stream))
+                         _stream_ptr(stream, x.device))
     if st != CLIFF_OK:
         raise CliffError(st, "multivector_act")
     return out
@@ -551,7 +556,7 @@ def block2(x, layer1, layer2, g: Sequence[int], out=None, workspace=None, stream
                                  b1.data_ptr() if b1 is not None else 0, d1,
                                  f2.data_ptr(), b2.data_ptr() if b2 is not None else 0,
                                  d2, workspace.data_ptr(), out.data_ptr(),
-                                 _stream_ptr(stream), path)
+                                 _stream_ptr(stream, x.device), path)
     if st != CLIFF_OK:
         raise CliffError(st, "clifford_block2_nd")
     return out
@@ -570,7 +575,7 @@ def block2_plan(x, layer1, layer2, g: Sequence[int], out=None, workspace=None, s
             ctypes.byref(d1) if d1 is not None else None, f2.data_ptr(),
             b2.data_ptr() if b2 is not None else None,
             ctypes.byref(d2) if d2 is not None else None, workspace.data_ptr(), out.data_ptr(),
-            _stream_ptr(stream) or None, path)
+            _stream_ptr(stream, x.device) or None, path)
     return Plan(load().clifford_block2_nd_path, args, 17, "clifford_block2_nd", out,
                 (x, layer1, layer2, workspace, garr, d1, d2),
                 [t for t, of in zip((workspace, out), given) if of is None])

@@ -1090,8 +1090,8 @@ __global__ __launch_bounds__(512, 2) void rows_fp32_kernel(ProductArgs p)
 // 16 kk + 8 h + i, or for fp32 (whose 8 are two loads) 16 kk + 4 h + i and 8 on,
 // so that a row's two lanes read neighbours.  131072 x 128 x 512 fp32: 120 us (2.8
 // TB/s, and 145 TFLOP/s of products), 150 with bias and GELU, whose vector
-// instructions the products do not hide; bf16 with
-// bias 54 us, with bias and GELU 71 (3.1 and 2.4 TB/s).
+// instructions the products do not hide; bf16 with bias 54 us, with bias and GELU 71
+// (3.1 and 2.4 TB/s).
 constexpr int PANEL = 128;
 template <typename T, bool BKM, int KK, bool WHOLE>
 __global__ __launch_bounds__(512, 2) void panel_kernel(ProductArgs p)

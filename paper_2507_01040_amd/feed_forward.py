@@ -231,7 +231,7 @@ class FeedForwardPlan(_pkg.Plan):
 def _plan(fn_name: str, args, out, keep, own, stream) -> FeedForwardPlan:
     """The call as a plan; args end with the stream's place.  ``own``: tensors
     allocated here, which another stream than the plan's may use."""
-    args = (*args, _pkg._stream_ptr(stream) or None)
+    args = (*args, _pkg._stream_ptr(stream, keep[0].device) or None)
     return FeedForwardPlan(getattr(_pkg.load(), fn_name), args, len(args) - 1, fn_name, out, keep, own)
 
 

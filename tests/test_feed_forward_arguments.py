@@ -32,7 +32,7 @@ class _Library:
 def library(monkeypatch):
     lib = _Library()
     monkeypatch.setattr(P, "load", lambda *a: lib)
-    monkeypatch.setattr(P, "_stream_ptr", lambda stream: 0)
+    monkeypatch.setattr(P, "_stream_ptr", lambda stream, device: 0)
     monkeypatch.setattr(F, "_check_dev", lambda *a, **kw: None)
     return lib
 

@@ -63,3 +63,14 @@ def test_calls_on_another_stream():
         assert got.data_ptr() not in places
         torch.cuda.current_stream().wait_stream(side)
         assert torch.equal(got, want)
+
+
+def test_current_device(monkeypatch):
+    # without a stream the call goes to the current device's: tensors of another one
+    # are refused
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda *a: _Stream())
+    assert P._stream_ptr(None, torch.device("cuda:0")) == 0x1234
+    assert P._stream_ptr(_Stream(), torch.device("cuda:1")) == 0x1234
+    with pytest.raises(ValueError, match="the tensors are on cuda:1, but the current device is cuda:0"):
+        P._stream_ptr(None, torch.device("cuda:1"))
