@@ -31,10 +31,10 @@ struct ProductArgs {
     const void* b;
     int64_t ldb;
     int splits;       // parts of the contraction, each by its own workgroups ...
+    float scale;
     int64_t k_part;   // ... of this many values (a multiple of the stage's)
     float* partial;   // splits > 1: fp32 [splits][M][N], joined by another kernel
     // epilogue
-    float scale;
     const void* bias;
     int act;
     DropArgs drop;
@@ -412,7 +412,7 @@ __global__ __launch_bounds__(64 * WR * WC) void product_kernel(ProductArgs p)
     const int wm = wave / WC * WM, wn = wave % WC * WN;
 
     const uint32_t tm = (uint32_t)((p.M + BM - 1) / BM), tn = (uint32_t)((p.N + BN - 1) / BN);
-    if (workgroup_id() >= tm * tn * p.splits) return;
+    if (blockIdx.y && workgroup_id() >= tm * tn * p.splits) return;
     const TileId id = tile_of(workgroup_id(), tm, tn, p.splits);
     const int64_t m0 = (int64_t)id.m * BM, n0 = (int64_t)id.n * BN, k0 = id.split * p.k_part;
     const int64_t kn = p.K - k0 < p.k_part ? p.K - k0 : p.k_part;
@@ -572,7 +572,7 @@ __global__ __launch_bounds__(256, 2) void split_product_kernel(ProductArgs p)
     const int wm = wave / 2 * 64, wn = wave % 2 * 64;
 
     const uint32_t tm = (uint32_t)((p.M + BM - 1) / BM), tn = (uint32_t)((p.N + BN - 1) / BN);
-    if (workgroup_id() >= tm * tn * p.splits) return;
+    if (blockIdx.y && workgroup_id() >= tm * tn * p.splits) return;
     const TileId id = tile_of(workgroup_id(), tm, tn, p.splits);
     const int64_t m0 = (int64_t)id.m * BM, n0 = (int64_t)id.n * BN, k0 = id.split * p.k_part;
     const int64_t kn = p.K - k0 < p.k_part ? p.K - k0 : p.k_part;
@@ -1344,27 +1344,24 @@ __global__ __launch_bounds__(256) void slope_kernel(DenseBackwardArgs a, T* g, f
 }
 
 // dbias: scale times the parts [part][N], joined in a fixed order: 64 columns per
-// workgroup at a time, every 16th part per wave.
+// workgroup, every 16th part per wave.
 template <typename T>
 __global__ __launch_bounds__(1024) void bias_kernel(const float* sums, int parts, int64_t N, float scale, T* dbias)
 {
     __shared__ float s[16][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    for (int64_t c0 = blockIdx.x * 64ll; c0 < N; c0 += gridDim.x * 64ll) {
-        const int64_t c = c0 + lane;
-        float t = 0.f;
-        if (c < N) {
+    const int64_t c = workgroup_id() * 64ll + lane;
+    float t = 0.f;
+    if (c < N) {
 #pragma unroll 8
-            for (int i = wave; i < parts; i += 16) t += sums[i * N + c];
-        }
-        __syncthreads();  // the columns before are done with
-        s[wave][lane] = t;
-        __syncthreads();
-        if (wave || c >= N) continue;
-        t = 0.f;
-        for (int i = 0; i < 16; ++i) t += s[i][lane];
-        dbias[c] = (T)(t * scale);
+        for (int i = wave; i < parts; i += 16) t += sums[i * N + c];
     }
+    s[wave][lane] = t;
+    __syncthreads();
+    if (wave || c >= N) return;
+    t = 0.f;
+    for (int i = 0; i < 16; ++i) t += s[i][lane];
+    dbias[c] = (T)(t * scale);
 }
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
@@ -1578,8 +1575,8 @@ cliff_status launch_dense(int dtype, const DenseArgs& a, hipStream_t stream)
     clear_hip_error();
     return with_type(dtype, [&](auto t) {
         using T = decltype(t);
-        ProductArgs p{a.M, a.N, a.K, a.x, a.ldx, a.w, a.ldw, 1, 0, static_cast<float*>(a.workspace),
-                      1.f, a.bias, a.act, a.drop, a.residual, a.ldr, a.pre, a.ldp, a.y, a.ldy};
+        ProductArgs p{a.M, a.N, a.K, a.x, a.ldx, a.w, a.ldw, 1, 1.f, 0, static_cast<float*>(a.workspace),
+                      a.bias, a.act, a.drop, a.residual, a.ldr, a.pre, a.ldp, a.y, a.ldy};
         return a.w_out_in ? product<T, true, true>(dtype, p, stream) : product<T, true, false>(dtype, p, stream);
     });
 }
@@ -1605,14 +1602,14 @@ cliff_status launch_dense_backward(int dtype, const DenseBackwardArgs& a, hipStr
             s = launched();
         }
         if (s == CLIFF_OK && a.dbias) {
-            hipLaunchKernelGGL(bias_kernel<T>, dim3((unsigned)std::min(ceil_div(a.N, 64), GRID_ROW)), dim3(1024), 0, stream, sums,
+            hipLaunchKernelGGL(bias_kernel<T>, grid_of(ceil_div(a.N, 64)), dim3(1024), 0, stream, sums,
                                w.parts, a.N, scale, static_cast<T*>(a.dbias));
             s = launched();
         }
         const DropArgs none{nullptr, 0, 1.f};
         auto plain = [&](int64_t M, int64_t N, int64_t K, const void* x, int64_t ldx, const void* y, int64_t ldy,
                          void* out, int64_t ldo) {
-            return ProductArgs{M, N, K, x, ldx, y, ldy, 1, 0, partial, scale / fit_slope<T>(a.act), nullptr,
+            return ProductArgs{M, N, K, x, ldx, y, ldy, 1, scale / fit_slope<T>(a.act), 0, partial, nullptr,
                                CLIFF_ACT_NONE, none, nullptr, 0, nullptr, 0, out, ldo};
         };
         if (s == CLIFF_OK && a.dx && a.M) {

@@ -191,12 +191,9 @@ __global__ __launch_bounds__(wg_threads(TPR), 2) void norm_backward_kernel(NormB
                 }
             }
         }
-        row_sums<TPR, 2 * R>(s, lds[turn]);
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-            s[2 * r] *= inv;
-            s[2 * r + 1] *= inv * rstd[r];
-        }
+        for (int r = 0; r < R; ++r) s[2 * r + 1] *= rstd[r];
+        row_sums<TPR, 2 * R>(s, lds[turn]);
 #pragma unroll
         for (int c = 0; c < C; ++c) {
             const int col = (c * TPR + t) * E, have = (int)a.d - col;
@@ -211,7 +208,7 @@ __global__ __launch_bounds__(wg_threads(TPR), 2) void norm_backward_kernel(NormB
 #pragma unroll
                 for (int e = 0; e < E; ++e) {
                     const float h = (xv[e] - mean[r]) * rstd[r], q = w ? dv[e] * wf[e] : dv[e];
-                    const float u = rstd[r] * (q - s[2 * r] - h * s[2 * r + 1]);
+                    const float u = rstd[r] * (q - s[2 * r] * inv - h * (s[2 * r + 1] * inv));
                     v[e] = a.dresidual ? v[e] + u : u;
                 }
                 if (rg + r < a.rows) store16(static_cast<T*>(a.dx) + (rg + r) * a.lddx + col, v, have);
@@ -327,30 +324,27 @@ __global__ __launch_bounds__(256) void norm_wide_sums_kernel(NormBackwardArgs a,
 }
 
 // Joins the parts [part][2][d] in a fixed order: 64 of the 2 d columns per
-// workgroup at a time, every 16th part per wave.
+// workgroup, every 16th part per wave.
 template <typename T>
 __global__ __launch_bounds__(1024) void norm_join_kernel(NormBackwardArgs a, const float* sums, int parts)
 {
     __shared__ float s[16][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    for (int64_t c0 = blockIdx.x * 64ll; c0 < 2 * a.d; c0 += gridDim.x * 64ll) {
-        const int64_t c = c0 + lane;
-        float v = 0.f;
-        if (c < 2 * a.d) {
+    const int64_t c = workgroup_id() * 64ll + lane;
+    float v = 0.f;
+    if (c < 2 * a.d) {
 #pragma unroll 8
-            for (int i = wave; i < parts; i += 16) v += sums[2 * a.d * i + c];
-        }
-        __syncthreads();  // the columns before are done with
-        s[wave][lane] = v;
-        __syncthreads();
-        if (wave || c >= 2 * a.d) continue;
-        v = 0.f;
-        for (int i = 0; i < 16; ++i) v += s[i][lane];
-        if (c < a.d) {
-            if (a.dweight) static_cast<T*>(a.dweight)[c] = (T)v;
-        } else if (a.dbias) {
-            static_cast<T*>(a.dbias)[c - a.d] = (T)v;
-        }
+        for (int i = wave; i < parts; i += 16) v += sums[2 * a.d * i + c];
+    }
+    s[wave][lane] = v;
+    __syncthreads();
+    if (wave || c >= 2 * a.d) return;
+    v = 0.f;
+    for (int i = 0; i < 16; ++i) v += s[i][lane];
+    if (c < a.d) {
+        if (a.dweight) static_cast<T*>(a.dweight)[c] = (T)v;
+    } else if (a.dbias) {
+        static_cast<T*>(a.dbias)[c - a.d] = (T)v;
     }
 }
 
@@ -474,7 +468,7 @@ cliff_status launch_layer_norm_backward(int dtype, const NormBackwardArgs& a, hi
                                0, stream, a);
         }
         if (params)
-            hipLaunchKernelGGL(norm_join_kernel<T>, dim3((unsigned)std::min(ceil_div(2 * a.d, 64), GRID_ROW)), dim3(1024), 0, stream, a,
+            hipLaunchKernelGGL(norm_join_kernel<T>, grid_of(ceil_div(2 * a.d, 64)), dim3(1024), 0, stream, a,
                                sums, (int)parts);
         return launched();
     });
