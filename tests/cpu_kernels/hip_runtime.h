@@ -47,6 +47,10 @@ struct DynamicLds {
 constexpr int WAVE = 64;
 int lane_id();
 
+// 16 bytes (nullptr: zeros) to LDS, and the wait for a thread's loads.
+void load(const char* from, char* to);
+void wait_loads();
+
 // A meeting of the wave: `in` of every lane goes to f(ins, outs), once.
 typedef void (*Meet)(const void* ins, void* outs);
 void meet(int kind, const void* in, size_t in_size, void* out, size_t out_size, Meet f);

@@ -8,7 +8,8 @@
 //
 // Input: one case per line on stdin, fields as key=value; op is dense, backward,
 // norm, norm_backward or dropout, cus the compute units that the launchers
-// assume.  dry=1: nothing runs, and tensors are addresses only; the line says what the call
+// assume; late=1: loads straight to LDS land when their thread waits for them, not
+// at once.  dry=1: nothing runs, and tensors are addresses only; the line says what the call
 // returned and the largest number of threads along an axis of a grid.
 // Output: one line per case, "ok status ..." or "FAIL ...".  stderr: "case" lines,
 // followed by what the library prints of its launches.
@@ -61,6 +62,7 @@ namespace emulate {
 
 hipError_t last_error = hipSuccess;
 bool dry = false;
+bool late = false;  // loads straight to LDS land when they are waited for
 uint64_t most_threads = 0;
 
 namespace {
@@ -78,6 +80,7 @@ struct Wave {
     alignas(128) char packed_in[WAVE * 128], packed_out[WAVE * 128];
 };
 Fiber fibers[1024];
+std::vector<std::pair<std::vector<char>, char*>> under_way[1024];  // loads of each thread
 Wave waves[16];
 char* stacks = nullptr;
 void* scheduler;
@@ -126,6 +129,7 @@ void run_group()
         f.sp = top;
     }
     for (Wave& w : waves) w.came = 0;
+    for (auto& l : under_way) l.clear();
     while (alive) {
         bool any = false;
         for (int w0 = 0; w0 < threads; w0 += WAVE) {
@@ -158,6 +162,20 @@ void run_group()
 DynamicLds::DynamicLds(void* at, size_t bytes) { dynamics().push_back({static_cast<char*>(at), bytes}); }
 
 int lane_id() { return now % WAVE; }
+
+static void land(const char* bytes, char* to) { memcpy(to, bytes, 16); }
+void load(const char* from, char* to)
+{
+    char bytes[16] = {};
+    if (from) memcpy(bytes, from, 16);
+    if (late) under_way[now].push_back({std::vector<char>(bytes, bytes + 16), to});
+    else land(bytes, to);
+}
+void wait_loads()
+{
+    for (const auto& l : under_way[now]) land(l.first.data(), l.second);
+    under_way[now].clear();
+}
 
 void meet_workgroup()
 {
@@ -714,6 +732,7 @@ int main()
         }
         cliff::assumed_cus = (int)f.i("cus", 256);
         emulate::dry = f.i("dry");
+        emulate::late = f.i("late");
         emulate::most_threads = 0;
         next_address = (uintptr_t)1 << 44;
         failure.clear();

@@ -65,11 +65,11 @@ def test_tiles(t, name):
 def test_direct_tiles(t):
     aligned = [dict(), dict(pad=8), dict(pad_x=16, pad_w=8, pad_y=1, off_y=1, pad_res=3)]
     small = [(65, 8, 8), (130, 72, 136), (128, 64, 128), (200, 136, 264), (257, 200, 96)]
-    _run([_dense(t, s, i + 3 * j, **r) for s in small for i, r in enumerate(aligned) for j in range(2)],
+    _run([_dense(t, s, i + 3 * j, late=j, **r) for s in small for i, r in enumerate(aligned) for j in range(2)],
          ["direct tiles of 128, "])
     # 256 x 256: ragged edges, a last stage that is not whole, one and two stages
     large = [(520, 1096, 512), (513, 840, 488), (1000, 600, 264), (264, 648, 1000), (257, 1048, 512)]
-    _run([_dense(t, s, i + 3 * j, cus=1, **r) for s in large for i, r in enumerate(aligned[:2]) for j in range(2)],
+    _run([_dense(t, s, i + 3 * j, cus=1, late=j, **r) for s in large for i, r in enumerate(aligned[:2]) for j in range(2)],
          ["direct tiles of 256, "])
 
 
@@ -136,6 +136,7 @@ def _draw(r):
         return int(round(a * (b / a) ** r.random()))
     op = r.choice(["dense", "dense", "backward", "backward", "norm", "norm_backward", "dropout"])
     c = dict(op=op, type=r.choice(TYPES), seed=r.randint(1, 10 ** 6), cus=r.choice([1, 2, 8, 64, 256]), p=r.choice([0, 0.3, 1]),
+             late=r.randint(0, 1),
              in_place=int(r.random() < 0.2), residual=r.randint(0, 1))
     for n in ("x", "w", "y", "pre", "res", "dy", "dx", "dw"):
         if r.random() < 0.4:
