@@ -304,6 +304,26 @@ def _empty(shape, dtype, device, stream=None):
     return t
 
 
+def _tensors(things):
+    import torch
+    for t in things:
+        if isinstance(t, torch.Tensor):
+            yield t
+        elif isinstance(t, (tuple, list)):
+            yield from _tensors(t)
+
+
+def _note_use(stream, *things):
+    """Tells torch's allocator that the tensors among ``things`` are used on
+    ``stream`` (None: the current one, as it takes them to be): one that the
+    caller frees after the call, a temporary among its arguments, is not given
+    to others before that stream is done with it."""
+    if stream is not None:
+        for t in _tensors(things):
+            if t.is_cuda:
+                t.record_stream(_torch_stream(stream, t.device))
+
+
 def from_paper_protocol(filters, bias=None):
     """Filters (N_B, C_in, C_out, d_f^k) and bias (N_B, C_out) in the paper's
     input/output protocol ("Optimization Performed", convolutional layers:
@@ -363,6 +383,7 @@ def conv_nd(x, filters, bias, g: Sequence[int], act: Optional[Tuple] = None,
                                out.data_ptr(), desc, _stream_ptr(stream, x.device), algo)
     if st != CLIFF_OK:
         raise CliffError(st, "clifford_conv_nd")
+    _note_use(stream, x, filters, bias, act, out)
     return out
 
 
@@ -373,12 +394,13 @@ class Plan:
     for, ``plan(stream)`` on another torch stream (or raw stream handle); a
     status other than CLIFF_OK raises CliffError.  The library checks its
     arguments on every call as usual.  The plan holds references to its
-    tensors and descriptors; ``plan.out`` is the output tensor.  Those of them
-    that were allocated for the plan (``own``) are its stream's: another stream
-    has to wait for that one first, as for every tensor of another stream, and
-    torch's allocator is told that they are used there."""
+    tensors and descriptors; ``plan.out`` is the output tensor.  What was
+    allocated for the plan is its stream's: another stream has to wait for that
+    one first, as for every tensor of another stream.  Torch's allocator is told
+    of every stream that a plan is made or called for (``made_for``: the stream
+    argument it was made with)."""
 
-    def __init__(self, fn, args, stream_index: int, name: str, out, keep, own=()):
+    def __init__(self, fn, args, stream_index: int, name: str, out, keep, made_for=None):
         self._fn = fn
         self._args = list(args)
         self._si = stream_index
@@ -386,14 +408,20 @@ class Plan:
         self._name = name
         self.out = out
         self._keep = keep
-        self._own = own
+        self._noted = set()
+        self._note(made_for)
+
+    def _note(self, stream):
+        handle = getattr(stream, "cuda_stream", stream)
+        if handle not in self._noted:
+            self._noted.add(handle)
+            _note_use(stream, self.out, self._keep)
 
     def __call__(self, stream=None):
         if stream is None:
             self._args[self._si] = self._stream
         else:
-            for t in self._own:
-                t.record_stream(_torch_stream(stream, t.device))
+            self._note(stream)
             handle = int(stream.cuda_stream) if hasattr(stream, "cuda_stream") else int(stream)
             self._args[self._si] = handle or None
         st = self._fn(*self._args)
@@ -406,7 +434,6 @@ def conv_plan(x, filters, bias, g: Sequence[int], act: Optional[Tuple] = None,
               out=None, stream=None, algo: int = ALGO_AUTO) -> Plan:
     """conv_nd as a Plan: the checks of conv_nd once, then each call only the
     C ABI call (``out`` is allocated here unless given)."""
-    own_out = out is None
     (k, B, C_in, C_out, d_image, d_filter), out, desc = _conv_checked(x, filters, bias, g,
                                                                        act, out, stream)
     garr = _g_array(g)
@@ -414,7 +441,7 @@ def conv_plan(x, filters, bias, g: Sequence[int], act: Optional[Tuple] = None,
             bias.data_ptr() if bias is not None else None, out.data_ptr(),
             ctypes.byref(desc) if desc is not None else None, _stream_ptr(stream, x.device) or None, algo)
     return Plan(load().clifford_conv_nd_algo, args, 12, "clifford_conv_nd", out,
-                (x, filters, bias, act, garr, desc), (out,) if own_out else ())
+                (x, filters, bias, act, garr, desc), stream)
 
 
 def linear(x, weight, bias, g: Sequence[int], act: Optional[Tuple] = None,
@@ -451,6 +478,7 @@ def linear(x, weight, bias, g: Sequence[int], act: Optional[Tuple] = None,
                          desc, _stream_ptr(stream, x.device))
     if st != CLIFF_OK:
         raise CliffError(st, "clifford_linear")
+    _note_use(stream, x, weight, bias, act, out)
     return out
 
 
@@ -481,6 +509,7 @@ def act_nd(x, mode: int, blades: Sequence[int], weight=None, bias=None,
                          _stream_ptr(stream, x.device))
     if st != CLIFF_OK:
         raise CliffError(st, "multivector_act")
+    _note_use(stream, x, weight, bias, out)
     return out
 
 
@@ -559,6 +588,7 @@ def block2(x, layer1, layer2, g: Sequence[int], out=None, workspace=None, stream
                                  _stream_ptr(stream, x.device), path)
     if st != CLIFF_OK:
         raise CliffError(st, "clifford_block2_nd")
+    _note_use(stream, x, layer1, layer2, workspace, out)
     return out
 
 
@@ -566,7 +596,6 @@ def block2_plan(x, layer1, layer2, g: Sequence[int], out=None, workspace=None, s
                 path: int = 0) -> Plan:
     """block2 as a Plan: the checks once, then each call only the C ABI call."""
     (f1, b1, a1), (f2, b2, a2) = layer1, layer2
-    given = (workspace, out)
     (k, B, C_in, C_mid, C_out, d_image, d_filter), workspace, out, d1, d2 = _block2_checked(
         x, layer1, layer2, g, out, workspace, stream)
     garr = _g_array(g)
@@ -577,8 +606,7 @@ def block2_plan(x, layer1, layer2, g: Sequence[int], out=None, workspace=None, s
             ctypes.byref(d2) if d2 is not None else None, workspace.data_ptr(), out.data_ptr(),
             _stream_ptr(stream, x.device) or None, path)
     return Plan(load().clifford_block2_nd_path, args, 17, "clifford_block2_nd", out,
-                (x, layer1, layer2, workspace, garr, d1, d2),
-                [t for t, of in zip((workspace, out), given) if of is None])
+                (x, layer1, layer2, workspace, garr, d1, d2), stream)
 
 
 def block_forward(x, layers, g: Sequence[int], outs=None, stream=None):

@@ -213,10 +213,10 @@ def _weight_order(w, name: str = "weight", like=None) -> Tuple[int, int]:
 class FeedForwardPlan(_pkg.Plan):
     """A Plan whose output may be a tuple of tensors."""
 
-    def __init__(self, fn, args, stream_index: int, name: str, out, keep, own=()):
+    def __init__(self, fn, args, stream_index: int, name: str, out, keep, made_for=None):
         # converted once: a call that is repeated is mostly this and the launch
         args = [t(a) if isinstance(a, (int, float)) else a for t, a in zip(fn.argtypes, args)]
-        super().__init__(fn, args, stream_index, name, out, keep, own)
+        super().__init__(fn, args, stream_index, name, out, keep, made_for)
         self._same_stream = functools.partial(fn, *args)
 
     def __call__(self, stream=None):
@@ -228,11 +228,11 @@ class FeedForwardPlan(_pkg.Plan):
         return super().__call__(stream)
 
 
-def _plan(fn_name: str, args, out, keep, own, stream) -> FeedForwardPlan:
-    """The call as a plan; args end with the stream's place.  ``own``: tensors
-    allocated here, which another stream than the plan's may use."""
+def _plan(fn_name: str, args, out, keep, stream) -> FeedForwardPlan:
+    """The call as a plan; args end with the stream's place."""
     args = (*args, _pkg._stream_ptr(stream, keep[0].device) or None)
-    return FeedForwardPlan(getattr(_pkg.load(), fn_name), args, len(args) - 1, fn_name, out, keep, own)
+    return FeedForwardPlan(getattr(_pkg.load(), fn_name), args, len(args) - 1, fn_name, out, keep,
+                           stream)
 
 
 class _Buffers:
@@ -241,15 +241,12 @@ class _Buffers:
 
     def __init__(self, like, stream):
         self.like, self.stream = like, stream
-        self.own = []
 
     def empty(self, given, shape, name: str, dtype=None):
         if given is not None:
             _check_dev(given, name, self.like, dtype)
             return given
-        t = _pkg._empty(shape, dtype or self.like.dtype, self.like.device, self.stream)
-        self.own.append(t)
-        return t
+        return _pkg._empty(shape, dtype or self.like.dtype, self.like.device, self.stream)
 
     def workspace(self, given, need: int):
         import torch
@@ -261,9 +258,7 @@ class _Buffers:
             return given, given.numel()
         if need == 0:
             return None, 0
-        t = _pkg._empty(need, torch.uint8, self.like.device, self.stream)
-        self.own.append(t)
-        return t, need
+        return _pkg._empty(need, torch.uint8, self.like.device, self.stream), need
 
 
 # ---------------------------------------------------------------------------
@@ -307,7 +302,7 @@ def dense_plan(x, weight, bias=None, act: int = ACT_NONE, dropout=None, residual
             _ptr(pre_t), _row_stride(pre_t, "pre") if want_pre else 0, _ptr(out),
             _row_stride(out, "out"), _ptr(ws), ws_bytes)
     return _plan("cliffconv_dense", args, (out, pre_t) if want_pre else out,
-                 (x, weight, bias, dropout, residual, pre_t, out, ws, desc), b.own, stream)
+                 (x, weight, bias, dropout, residual, pre_t, out, ws, desc), stream)
 
 
 def dense(x, weight, bias=None, act: int = ACT_NONE, dropout=None, residual=None, pre=None,
@@ -377,7 +372,7 @@ def dense_backward_plan(dy, x, weight, pre=None, act: int = ACT_NONE, dropout=No
     outs = tuple(t for t, want in ((dx, dx is not None), (dweight, dweight is not None),
                                    (dbias, bool(bias))) if want)
     return _plan("cliffconv_dense_backward", args, outs,
-                 (dy, x, weight, pre, dropout, dx, dweight, dbias, ws, desc), b.own, stream)
+                 (dy, x, weight, pre, dropout, dx, dweight, dbias, ws, desc), stream)
 
 
 def dense_backward(dy, x, weight, pre=None, act: int = ACT_NONE, dropout=None, bias: bool = True,
@@ -423,7 +418,7 @@ def layer_norm_plan(x, weight=None, bias=None, eps: float = 1e-5, out=None, mean
     args = (code, rows, d, _ptr(x), _row_stride(x, "x"), _ptr(weight), _ptr(bias), float(eps),
             _ptr(out), _row_stride(out, "out"), _ptr(mean), _ptr(rstd))
     return _plan("cliffconv_layer_norm", args, (out, mean, rstd),
-                 (x, weight, bias, out, mean, rstd), b.own, stream)
+                 (x, weight, bias, out, mean, rstd), stream)
 
 
 def layer_norm(x, weight=None, bias=None, eps: float = 1e-5, out=None, mean=None, rstd=None,
@@ -475,7 +470,7 @@ def layer_norm_backward_plan(dy, x, mean, rstd, weight=None, dresidual=None, par
             _row_stride(dresidual, "dresidual") if dresidual is not None else 0, _ptr(dx),
             _row_stride(dx, "dx"), _ptr(dweight), _ptr(dbias), _ptr(ws), ws_bytes)
     return _plan("cliffconv_layer_norm_backward", args, (dx, dweight, dbias) if params else dx,
-                 (dy, x, mean, rstd, weight, dresidual, dx, dweight, dbias, ws), b.own, stream)
+                 (dy, x, mean, rstd, weight, dresidual, dx, dweight, dbias, ws), stream)
 
 
 def layer_norm_backward(dy, x, mean, rstd, weight=None, dresidual=None, params: bool = True, dx=None,
@@ -511,7 +506,7 @@ def dropout_plan(x, p: float, rng, residual=None, out=None, stream=None) -> Feed
     args = (code, _rows_of(x.shape), x.shape[-1], _ptr(x), _row_stride(x, "x"), _ref(desc),
             _ptr(residual), _row_stride(residual, "residual") if residual is not None else 0,
             _ptr(out), _row_stride(out, "out"))
-    return _plan("cliffconv_dropout", args, out, (x, rng, residual, out, desc), b.own, stream)
+    return _plan("cliffconv_dropout", args, out, (x, rng, residual, out, desc), stream)
 
 
 def dropout(x, p: float, rng, residual: Optional[object] = None, out=None, stream=None):

@@ -125,38 +125,45 @@ def streams(monkeypatch):
     monkeypatch.setattr(torch.cuda, "current_stream", lambda *a: log["current"])
     monkeypatch.setattr(P, "_torch_stream", lambda s, d: "handle %x" % (s if isinstance(s, int) else s.cuda_stream))
     monkeypatch.setattr(torch, "empty", noted)
+    monkeypatch.setattr(torch.Tensor, "is_cuda", True)
     monkeypatch.setattr(torch.Tensor, "record_stream", lambda t, s: log["recorded"].append((t.data_ptr(), s)))
     return log
 
 
 def _calls(stream):
+    """(call, its inputs) of every operator."""
     x, w, r = torch.zeros(6, 8), torch.zeros(8, 5), torch.zeros(2, dtype=torch.int64)
-    dy, v = torch.zeros(6, 5), torch.zeros(6)
-    return {"dense": lambda: P.dense_plan(x, w, pre=True, stream=stream),
-            "dense_backward": lambda: P.dense_backward_plan(dy, x, w, stream=stream),
-            "layer_norm": lambda: P.layer_norm_plan(x, stream=stream),
-            "layer_norm_backward": lambda: P.layer_norm_backward_plan(x, x, v, v, stream=stream),
-            "dropout": lambda: P.dropout_plan(x, 0.5, r, stream=stream)}
+    dy, v, b = torch.zeros(6, 5), torch.zeros(6), torch.zeros(5)
+    return {"dense": (lambda: P.dense_plan(x, w, b, dropout=(0.5, r), residual=dy, pre=True, stream=stream),
+                      (x, w, b, r, dy)),
+            "dense_backward": (lambda: P.dense_backward_plan(dy, x, w, dropout=(0.5, r), stream=stream), (dy, x, w, r)),
+            "layer_norm": (lambda: P.layer_norm_plan(x, stream=stream), (x,)),
+            "layer_norm_backward": (lambda: P.layer_norm_backward_plan(x, x, v, v, stream=stream), (x, v)),
+            "dropout": (lambda: P.dropout_plan(x, 0.5, r, stream=stream), (x, r))}
 
 
 @pytest.mark.parametrize("op", _calls(None))
 def test_buffers_are_the_streams_own(library, streams, op):
     # memory that the current stream has freed may still be read there: what a
-    # call on another stream writes is allocated for that one
+    # call on another stream writes is allocated for that one; what it reads may be
+    # freed after the call, and is noted as used there
     for stream, name in ((None, "first"), (_Stream(), "handle 1234")):
-        call = _calls(stream)[op]
+        call, inputs = _calls(stream)[op]
         streams["made"].clear()
         streams["recorded"].clear()
         plan = call()
         assert streams["made"] and {s for _, s in streams["made"]} == {name}
         assert streams["current"] == "first"
         # and the caller, who reads it on the current stream, may free it at any time
-        assert streams["recorded"] == ([] if stream is None else [(p, "first") for p, _ in streams["made"]])
+        used = {p for p, _ in streams["made"]} | {t.data_ptr() for t in inputs}
+        assert set(streams["recorded"]) == (set() if stream is None else {(p, "first") for p, _ in streams["made"]} |
+                                            {(p, name) for p in used})
         # a plan's call on a third stream, as torch's or by its handle
-        for third in (7, type("S", (), {"cuda_stream": 7})()):
+        for third in (7, type("S", (), {"cuda_stream": 8})()):
             streams["recorded"].clear()
             plan(third)
-            assert sorted(streams["recorded"]) == sorted((p, "handle 7") for p, _ in streams["made"])
+            third = "handle %x" % getattr(third, "cuda_stream", third)
+            assert set(streams["recorded"]) == {(p, third) for p in used}
 
 
 @pytest.mark.parametrize("op", ["dense", "dense_backward", "layer_norm", "layer_norm_backward", "dropout"])
