@@ -62,15 +62,23 @@ def build() -> str:
     return EXE
 
 
-def run(cases, timeout=900):
-    """[(result line, launches' lines)] of the cases (dicts)."""
+def _run(exe, cases, timeout):
     lines = [" ".join("%s=%s" % kv for kv in c.items()) for c in cases]
     env = dict(os.environ, ASAN_OPTIONS="detect_leaks=0:detect_stack_use_after_return=0:abort_on_error=1",
                UBSAN_OPTIONS="print_stacktrace=1:halt_on_error=1")
-    r = subprocess.run([build()], input="\n".join(lines) + "\n", capture_output=True, text=True, env=env,
+    r = subprocess.run([exe], input="\n".join(lines) + "\n", capture_output=True, text=True, env=env,
                        timeout=timeout)
     if r.returncode:
-        at = r.stderr.count("\ncase ") + r.stderr.startswith("case ") - 1
+        at = ("\n" + r.stderr).count("\ncase ") - 1
         raise RuntimeError("case %s\n%s" % (lines[min(at, len(lines) - 1)], r.stderr[-6000:]))
     launches = [[s for s in part.split("\n")[1:] if s] for part in ("\n" + r.stderr).split("\ncase ")[1:]]
     return list(zip(r.stdout.strip().split("\n"), launches))
+
+
+def run(cases, timeout=900, processes=4):
+    """[(result line, launches' lines)] of the cases (dicts)."""
+    exe = build()
+    n = max(1, min(processes, len(cases) // 4))
+    with concurrent.futures.ThreadPoolExecutor(n) as ex:
+        parts = list(ex.map(lambda i: _run(exe, cases[i::n], timeout), range(n)))
+    return [parts[i % n][i // n] for i in range(len(cases))]
