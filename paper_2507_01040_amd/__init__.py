@@ -398,7 +398,8 @@ class Plan:
     allocated for the plan is its stream's: another stream has to wait for that
     one first, as for every tensor of another stream.  Torch's allocator is told
     of every stream that a plan is made or called for (``made_for``: the stream
-    argument it was made with)."""
+    argument it was made with); the stream of a raw handle has to live until the
+    plan's tensors are freed."""
 
     def __init__(self, fn, args, stream_index: int, name: str, out, keep, made_for=None):
         self._fn = fn
