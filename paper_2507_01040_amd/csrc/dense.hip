@@ -1302,9 +1302,9 @@ constexpr float fit_slope(int act)
 
 // g = keep dy f'(pre) fit_slope into g [M, N] (unless NULL), and the column sums
 // of keep dy f'(pre) over a share of the rows into sums [part][N] (unless NULL).  A
-// workgroup takes 256 columns; its four waves every fourth row each.  Bound by the vector instructions
-// of f' and the generator: 8192 x 2048 bf16, GELU and dropout, 33 us (3 TB/s); 65536
-// x 512 fp32, SiLU, 87 us (4.6 TB/s, memory).
+// workgroup takes 256 columns; its four waves every fourth row each.  Bound by the
+// vector instructions of f' and the generator: 8192 x 2048 bf16, GELU and dropout,
+// 33 us (3 TB/s); 65536 x 512 fp32, SiLU, 87 us (4.6 TB/s, memory).
 template <typename T>
 __global__ __launch_bounds__(256) void slope_kernel(DenseBackwardArgs a, T* g, float* sums, int64_t rows_per_part)
 {

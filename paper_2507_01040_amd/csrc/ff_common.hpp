@@ -201,8 +201,9 @@ __device__ inline float gelu_cdf(float v, float& e)
 
 // 1 / (1 + exp(-v)), and what it lacks to 1, as e / (1 + e) on one side of zero and
 // 1 / (1 + e) on the other, e = exp(-|v|): nothing overflows or cancels, and values
-// of the left tail keep their digits down to the smallest ones.  FINE: what the exponent's rounding takes from e
-// (4e-6 of it at |v| = 80) is put back; 16-bit results do not show it.
+// of the left tail keep their digits down to the smallest ones.  FINE: what the
+// exponent's rounding takes from e (4e-6 of it at |v| = 80) is put back; 16-bit
+// results do not show it.
 template <bool FINE>
 __device__ inline float logistic(float v, float& lacks)
 {
