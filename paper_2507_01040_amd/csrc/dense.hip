@@ -10,12 +10,12 @@
 #include "dense_geom.hpp"
 #include "ff_common.hpp"
 #include "lds_load.hpp"
+#include "rows.hpp"
 #include "split.hpp"
 
 namespace cliff {
 namespace {
 
-typedef float f4 __attribute__((ext_vector_type(4)));
 typedef float f16v __attribute__((ext_vector_type(16)));
 typedef short s4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u4 __attribute__((ext_vector_type(4)));
@@ -45,75 +45,6 @@ struct ProductArgs {
     void* y;
     int64_t ldy;
 };
-
-template <typename T>
-struct Vec4 {
-    typedef T t __attribute__((ext_vector_type(4)));
-};
-
-// Four neighbouring columns, of which some may not exist (have < 4).
-template <typename T>
-__device__ inline f4 load4(const T* p, int have)
-{
-    typename Vec4<T>::t v;
-    if (have >= 4) {
-        __builtin_memcpy(&v, p, sizeof v);
-    } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            v[e] = (T)0.f;
-            if (e < have) v[e] = p[e];
-        }
-    }
-    return __builtin_convertvector(v, f4);
-}
-template <typename T>
-__device__ inline void store4(T* p, const f4& v, int have)
-{
-    const typename Vec4<T>::t t = __builtin_convertvector(v, typename Vec4<T>::t);
-    if (have >= 4) {
-        __builtin_memcpy(p, &t, sizeof t);
-    } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (e < have) p[e] = t[e];
-    }
-}
-
-template <bool FINE>
-__device__ inline void activate4(int act, f4& v)
-{
-    switch (act) {
-#define EACH(A)                                      \
-    case A:                                          \
-        for (int e = 0; e < 4; ++e) v[e] = activate<FINE>(A, v[e]); \
-        break;
-        EACH(CLIFF_ACT_RELU)
-        EACH(CLIFF_ACT_GELU)
-        EACH(CLIFF_ACT_SILU)
-#undef EACH
-    }
-}
-template <bool FINE>
-__device__ inline void slope4(int act, f4& v, const f4& pre)
-{
-    switch (act) {
-#define EACH(A)                                                  \
-    case A:                                                      \
-        for (int e = 0; e < 4; ++e) v[e] *= activate_slope<FINE>(A, pre[e]); \
-        break;
-        EACH(CLIFF_ACT_RELU)
-        EACH(CLIFF_ACT_GELU)
-        EACH(CLIFF_ACT_SILU)
-#undef EACH
-    }
-}
-__device__ inline void drop4(const DropArgs& d, uint64_t key, uint32_t step, int64_t r, int64_t c, f4& v)
-{
-    const Words w = philox(key, step, (uint32_t)(c >> 2), r);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = w.w[e] <= d.last ? 0.f : v[e] * d.scale;
-}
 
 // Eight elements in 16-byte pieces (load16): one of a 16-bit type, two of fp32.
 template <typename T>
@@ -776,122 +707,6 @@ __device__ inline void join_waves(const ProductArgs& p, int64_t n0, const f4 (&a
     finish_rows<T, 1>(p, r, 1, n, v, ends);
 }
 
-// What the eight waves share: the workgroup's columns, and a wave's part of the
-// contraction (whole stages of KT but for the last).
-template <int KT>
-struct RowsPart {
-    int64_t n0, k0, k1;
-    int cols;
-    __device__ RowsPart(const ProductArgs& p, int columns, int wave)
-    {
-        n0 = (int64_t)xcd_run(blockIdx.x, gridDim.x) * columns;
-        cols = (int)(p.N - n0 < columns ? p.N - n0 : columns);
-        const int64_t part = (p.K + 8 * KT - 1) / (8 * KT) * KT;
-        k0 = wave * part;
-        k1 = k0 + part < p.K ? k0 + part : p.K;
-    }
-    // Calls load(stage, k) D stages ahead of use(stage).  While D more stages
-    // exist, no branch stands between a stage's load and its use: at a load that
-    // may not have been issued, the wait for an older one becomes a wait for all.
-    // A part's last values, less than a stage, come last, by load_last(stage, k).
-    template <int D, typename St, typename L, typename S, typename U>
-    __device__ void run(L load, S load_last, U use) const
-    {
-        const int n = k1 > k0 ? (int)((k1 - k0) / KT) : 0;
-        St f[D];
-        int s = 0;
-        if (n >= 2 * D) {
-#pragma unroll
-            for (int d = 0; d < D; ++d) load(f[d], k0 + d * KT);
-            do {
-#pragma unroll
-                for (int d = 0; d < D; ++d) {
-                    use(f[d]);
-                    load(f[d], k0 + (int64_t)(s + D + d) * KT);
-                }
-                s += D;
-            } while (s + 2 * D <= n);
-        } else {
-#pragma unroll
-            for (int d = 0; d < D; ++d)
-                if (d < n) load(f[d], k0 + d * KT);
-        }
-#pragma unroll
-        for (int d = 0; d < D; ++d) {
-            if (s + d < n) use(f[d]);
-            if (s + D + d < n) load(f[d], k0 + (int64_t)(s + D + d) * KT);
-        }
-#pragma unroll
-        for (int d = 0; d < D - 1; ++d)
-            if (s + D + d < n) use(f[d]);
-        const int64_t k = k0 + (int64_t)n * KT;
-        if (k >= k1) return;
-        load_last(f[0], k);
-        use(f[0]);
-    }
-};
-
-// 16 bytes at a byte offset of a lane from an address of the wave.
-template <typename T>
-__device__ inline raw16 load_at(const T* base, uint32_t offset)
-{
-    raw16 r;
-    __builtin_memcpy(&r, reinterpret_cast<const char*>(base) + offset, 16);
-    return r;
-}
-
-// A wave's piece of LDS: lines of 128 bytes, 16 of a block, in pieces of 16 bytes.
-// Loads put a line's eight pieces on neighbouring lanes, and LDS, without barriers,
-// turns them into fragments: 16 lanes that read one piece of 16 lines meet every
-// bank once.  (Fragments straight from memory have four neighbouring lanes on four
-// lines, which the L1 cache serves one at a time where lines lie a multiple of 128
-// bytes apart: 24 x 4096 x 4096 bf16 in 12.0 us instead of 7.7.)
-struct Lines {
-    uint32_t at[2];  // a lane's two pieces of a block of lines, in bytes from the first
-    template <typename T>
-    __device__ Lines(int64_t first, int64_t lines, int64_t ld, int lane, T)
-    {
-        for (int h = 0; h < 2; ++h) {
-            const int64_t l = first + 8 * h + (lane >> 3);
-            at[h] = (uint32_t)((l < lines ? l : lines - 1) * ld + per16<T> * (lane & 7)) * (uint32_t)sizeof(T);
-        }
-    }
-    Lines() = default;
-    template <typename T>
-    __device__ void load(raw16 (&v)[2], const T* base) const
-    {
-        for (int h = 0; h < 2; ++h) v[h] = load_at(base, at[h]);
-    }
-    static __device__ int byte(int line, int piece) { return line * 128 + ((piece ^ (line >> 1 & 7)) << 4); }
-    static __device__ void write(const raw16 (&v)[2], char* lds, int lane)
-    {
-        for (int h = 0; h < 2; ++h) *reinterpret_cast<raw16*>(lds + byte(8 * h + (lane >> 3), lane & 7)) = v[h];
-    }
-    static __device__ void read(raw16 (&v)[2], const char* lds, int lane)
-    {
-        for (int j = 0; j < 2; ++j) v[j] = *reinterpret_cast<const raw16*>(lds + byte(lane & 15, 4 * j + (lane >> 4)));
-    }
-    // The values before k1 of a stage that is not whole, from value k on; lines
-    // that do not exist give way to the last one here too.
-    template <typename T>
-    static __device__ void load_last(raw16 (&v)[2], const T* x, int64_t first, int64_t lines, int64_t ld, int64_t k,
-                                     int64_t k1, int lane)
-    {
-        for (int h = 0; h < 2; ++h) {
-            const int64_t l = first + 8 * h + (lane >> 3), pos = k + per16<T> * (lane & 7);
-            v[h] = load16(x + (l < lines ? l : lines - 1) * ld, pos, k1);
-            settle16<T>(v[h], pos, k1);
-        }
-    }
-};
-constexpr int LINES = 16 * 128;  // bytes of a block
-
-__device__ inline void wave_fence()
-{
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-}
-
 // 16-bit types.  B contiguous along the output is turned by the reads of LDS.
 template <typename T, bool BKM, int MB>
 __global__ __launch_bounds__(512, 2) void rows_kernel(ProductArgs p)
@@ -902,7 +717,7 @@ __global__ __launch_bounds__(512, 2) void rows_kernel(ProductArgs p)
     __shared__ __align__(16) char smem[8 * (JOIN > OWN ? JOIN : OWN)];
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const RowsPart<64> part(p, 16 * NS, wave);
+    const RowsPart<64> part(p.N, p.K, 16 * NS, wave);
     const int64_t n0 = part.n0, k1 = part.k1;
     const int cols = part.cols;
     const T* const a = static_cast<const T*>(p.a);
@@ -1011,7 +826,7 @@ __global__ __launch_bounds__(512, 2) void rows_fp32_kernel(ProductArgs p)
     __shared__ __align__(16) char smem[8 * (JOIN > OWN ? JOIN : OWN)];
     const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const RowsPart<32> part(p, 16 * NS, wave);
+    const RowsPart<32> part(p.N, p.K, 16 * NS, wave);
     const int64_t n0 = part.n0, k1 = part.k1;
     const int cols = part.cols;
     const float* const a = static_cast<const float*>(p.a);
@@ -1363,8 +1178,6 @@ __global__ __launch_bounds__(1024) void bias_kernel(const float* sums, int parts
     for (int i = 0; i < 16; ++i) t += s[i][lane];
     dbias[c] = (T)(t * scale);
 }
-
-int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // How a product is cut: tiles of 256 x 256 or 128 x 128, and parts of the
 // contraction.

@@ -1,115 +1,11 @@
 // C ABI of the feed-forward operators (cliffconv_ff.h): argument checks and
 // dispatch.  No device memory is allocated here; every call only enqueues
 // kernels on the caller's stream.
-#include <math.h>
-#include <stdint.h>
-
-#include <initializer_list>
 
 #include "cliffconv_ff.h"
 #include "ff_common.hpp"
 
-namespace {
-
 using namespace cliff;
-
-constexpr int64_t MAX_SIZE = ((int64_t)1 << 31) - 1;  // of a width or row count
-constexpr int64_t MAX_SPAN = (int64_t)1 << 40;        // elements from a matrix's first to its last
-
-bool valid_dtype(int t) { return t >= CLIFF_F32 && t <= CLIFF_F16; }
-int64_t size_of(int dtype) { return dtype == CLIFF_F32 ? 4 : 2; }
-
-// A matrix, vector (one row) or workspace of a call.
-struct Mat {
-    const void* p;
-    int64_t rows, cols, ld, elem;
-};
-
-bool bad_shape(const Mat& m)
-{
-    if (!m.p) return false;
-    if (m.ld < m.cols) return true;
-    return m.rows > 0 && (m.rows - 1) > (MAX_SPAN - 1 - m.cols) / m.ld;
-}
-
-bool misaligned(const Mat& m) { return ((uintptr_t)m.p & (uintptr_t)(m.elem - 1)) != 0; }
-
-bool overlaps(const Mat& a, const Mat& b)
-{
-    if (!a.p || !b.p || a.rows < 1 || b.rows < 1 || a.cols < 1 || b.cols < 1) return false;
-    const uintptr_t a0 = (uintptr_t)a.p, b0 = (uintptr_t)b.p;
-    const uintptr_t a1 = a0 + (uintptr_t)(((a.rows - 1) * a.ld + a.cols) * a.elem);
-    const uintptr_t b1 = b0 + (uintptr_t)(((b.rows - 1) * b.ld + b.cols) * b.elem);
-    if (a1 <= b0 || b1 <= a0) return false;
-    const uintptr_t step = (uintptr_t)(a.ld * a.elem);
-    if (step != (uintptr_t)(b.ld * b.elem)) return true;
-    // one row stride: columns of b begin `off` bytes after a's, modulo the
-    // stride, and end before a's begin again
-    const uintptr_t off = b0 >= a0 ? (b0 - a0) % step : (step - (a0 - b0) % step) % step;
-    return off < (uintptr_t)(a.cols * a.elem) || off + (uintptr_t)(b.cols * b.elem) > step;
-}
-
-bool same(const Mat& a, const Mat& b) { return a.p == b.p && a.ld == b.ld && a.elem == b.elem; }
-
-// `out` against what it must not overlap; those in `may_equal` may be the same matrix.
-bool clashes(const Mat& out, std::initializer_list<Mat> others, std::initializer_list<Mat> may_equal = {})
-{
-    for (const Mat& m : others)
-        if (overlaps(out, m)) return true;
-    for (const Mat& m : may_equal)
-        if (!same(out, m) && overlaps(out, m)) return true;
-    return false;
-}
-
-bool any_bad_shape(std::initializer_list<Mat> ms)
-{
-    for (const Mat& m : ms)
-        if (bad_shape(m)) return true;
-    return false;
-}
-
-bool any_misaligned(std::initializer_list<Mat> ms)
-{
-    for (const Mat& m : ms)
-        if (misaligned(m)) return true;
-    return false;
-}
-
-bool valid_drop(const cliff_dropout_desc* d)
-{
-    return !d || (d->p >= 0.0 && d->p <= 1.0 && (d->p == 0.0 || d->rng));
-}
-
-DropArgs to_args(const cliff_dropout_desc* d)
-{
-    DropArgs a{nullptr, 0, 1.f};
-    if (!d || d->p == 0.0) return a;
-    a.scale = d->p < 1.0 ? (float)(1.0 / (1.0 - d->p)) : 0.f;
-    const double t = nearbyint(d->p * 4294967296.0);
-    if (t < 1.0) return a;  // no word is below it
-    a.rng = d->rng;
-    a.last = (uint32_t)(t - 1.0);
-    return a;
-}
-
-Mat vec(const void* p, int64_t n, int64_t elem) { return Mat{p, 1, n, n, elem}; }
-Mat rng_of(const DropArgs& d) { return vec(d.rng, 2, 8); }
-
-cliff_status check_workspace(const void* p, int64_t have, int64_t need)
-{
-    if (need == 0) return CLIFF_OK;
-    if (!p || have < need) return CLIFF_ESCRATCH;
-    return ((uintptr_t)p & 15u) ? CLIFF_EALIGN : CLIFF_OK;
-}
-
-// Widths and row counts, and the dense matrices of them (workspaces too).
-bool valid_dense_sizes(int64_t M, int64_t K, int64_t N)
-{
-    return M >= 0 && M <= MAX_SIZE && K >= 1 && K <= MAX_SIZE && N >= 1 && N <= MAX_SIZE &&
-           M * K < MAX_SPAN && M * N < MAX_SPAN && K * N < MAX_SPAN;
-}
-
-}  // namespace
 
 extern "C" {
 

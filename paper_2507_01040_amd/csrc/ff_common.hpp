@@ -3,7 +3,10 @@
 #pragma once
 
 #include <hip/hip_runtime.h>
+#include <math.h>
 #include <stdint.h>
+
+#include <initializer_list>
 
 #include "cliffconv_ff.h"
 #include "common.hpp"
@@ -99,6 +102,106 @@ struct DropoutArgs {
     void* y;
     int64_t ldy;
 };
+
+// ---- checks of a call's arguments (host)
+
+constexpr int64_t MAX_SIZE = ((int64_t)1 << 31) - 1;  // of a width or row count
+constexpr int64_t MAX_SPAN = (int64_t)1 << 40;        // elements from a matrix's first to its last
+
+inline bool valid_dtype(int t) { return t >= CLIFF_F32 && t <= CLIFF_F16; }
+inline int64_t size_of(int dtype) { return dtype == CLIFF_F32 ? 4 : 2; }
+
+// A matrix, vector (one row) or workspace of a call.
+struct Mat {
+    const void* p;
+    int64_t rows, cols, ld, elem;
+};
+
+inline bool bad_shape(const Mat& m)
+{
+    if (!m.p) return false;
+    if (m.ld < m.cols) return true;
+    return m.rows > 0 && (m.rows - 1) > (MAX_SPAN - 1 - m.cols) / m.ld;
+}
+
+inline bool misaligned(const Mat& m) { return ((uintptr_t)m.p & (uintptr_t)(m.elem - 1)) != 0; }
+
+inline bool overlaps(const Mat& a, const Mat& b)
+{
+    if (!a.p || !b.p || a.rows < 1 || b.rows < 1 || a.cols < 1 || b.cols < 1) return false;
+    const uintptr_t a0 = (uintptr_t)a.p, b0 = (uintptr_t)b.p;
+    const uintptr_t a1 = a0 + (uintptr_t)(((a.rows - 1) * a.ld + a.cols) * a.elem);
+    const uintptr_t b1 = b0 + (uintptr_t)(((b.rows - 1) * b.ld + b.cols) * b.elem);
+    if (a1 <= b0 || b1 <= a0) return false;
+    const uintptr_t step = (uintptr_t)(a.ld * a.elem);
+    if (step != (uintptr_t)(b.ld * b.elem)) return true;
+    // one row stride: columns of b begin `off` bytes after a's, modulo the
+    // stride, and end before a's begin again
+    const uintptr_t off = b0 >= a0 ? (b0 - a0) % step : (step - (a0 - b0) % step) % step;
+    return off < (uintptr_t)(a.cols * a.elem) || off + (uintptr_t)(b.cols * b.elem) > step;
+}
+
+inline bool same(const Mat& a, const Mat& b) { return a.p == b.p && a.ld == b.ld && a.elem == b.elem; }
+
+// `out` against what it must not overlap; those in `may_equal` may be the same matrix.
+inline bool clashes(const Mat& out, std::initializer_list<Mat> others, std::initializer_list<Mat> may_equal = {})
+{
+    for (const Mat& m : others)
+        if (overlaps(out, m)) return true;
+    for (const Mat& m : may_equal)
+        if (!same(out, m) && overlaps(out, m)) return true;
+    return false;
+}
+
+inline bool any_bad_shape(std::initializer_list<Mat> ms)
+{
+    for (const Mat& m : ms)
+        if (bad_shape(m)) return true;
+    return false;
+}
+
+inline bool any_misaligned(std::initializer_list<Mat> ms)
+{
+    for (const Mat& m : ms)
+        if (misaligned(m)) return true;
+    return false;
+}
+
+inline bool valid_drop(const cliff_dropout_desc* d)
+{
+    return !d || (d->p >= 0.0 && d->p <= 1.0 && (d->p == 0.0 || d->rng));
+}
+
+inline DropArgs to_args(const cliff_dropout_desc* d)
+{
+    DropArgs a{nullptr, 0, 1.f};
+    if (!d || d->p == 0.0) return a;
+    a.scale = d->p < 1.0 ? (float)(1.0 / (1.0 - d->p)) : 0.f;
+    const double t = nearbyint(d->p * 4294967296.0);
+    if (t < 1.0) return a;  // no word is below it
+    a.rng = d->rng;
+    a.last = (uint32_t)(t - 1.0);
+    return a;
+}
+
+inline Mat vec(const void* p, int64_t n, int64_t elem) { return Mat{p, 1, n, n, elem}; }
+inline Mat rng_of(const DropArgs& d) { return vec(d.rng, 2, 8); }
+
+inline cliff_status check_workspace(const void* p, int64_t have, int64_t need)
+{
+    if (need == 0) return CLIFF_OK;
+    if (!p || have < need) return CLIFF_ESCRATCH;
+    return ((uintptr_t)p & 15u) ? CLIFF_EALIGN : CLIFF_OK;
+}
+
+// Widths and row counts, and the dense matrices of them (workspaces too).
+inline bool valid_dense_sizes(int64_t M, int64_t K, int64_t N)
+{
+    return M >= 0 && M <= MAX_SIZE && K >= 1 && K <= MAX_SIZE && N >= 1 && N <= MAX_SIZE &&
+           M * K < MAX_SPAN && M * N < MAX_SPAN && K * N < MAX_SPAN;
+}
+
+// ---- launches
 
 // Launchers (the arguments are checked): dtype is a cliff_dtype.
 cliff_status launch_dense(int dtype, const DenseArgs& a, hipStream_t stream);
@@ -246,6 +349,79 @@ __device__ inline float activate_slope(int act, float v)
     }
     }
     return 1.f;
+}
+
+// ---- four neighbouring columns
+
+typedef float f4 __attribute__((ext_vector_type(4)));
+
+template <typename T>
+struct Vec4 {
+    typedef T t __attribute__((ext_vector_type(4)));
+};
+
+// Four neighbouring columns, of which some may not exist (have < 4).
+template <typename T>
+__device__ inline f4 load4(const T* p, int have)
+{
+    typename Vec4<T>::t v;
+    if (have >= 4) {
+        __builtin_memcpy(&v, p, sizeof v);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            v[e] = (T)0.f;
+            if (e < have) v[e] = p[e];
+        }
+    }
+    return __builtin_convertvector(v, f4);
+}
+template <typename T>
+__device__ inline void store4(T* p, const f4& v, int have)
+{
+    const typename Vec4<T>::t t = __builtin_convertvector(v, typename Vec4<T>::t);
+    if (have >= 4) {
+        __builtin_memcpy(p, &t, sizeof t);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (e < have) p[e] = t[e];
+    }
+}
+
+template <bool FINE>
+__device__ inline void activate4(int act, f4& v)
+{
+    switch (act) {
+#define EACH(A)                                      \
+    case A:                                          \
+        for (int e = 0; e < 4; ++e) v[e] = activate<FINE>(A, v[e]); \
+        break;
+        EACH(CLIFF_ACT_RELU)
+        EACH(CLIFF_ACT_GELU)
+        EACH(CLIFF_ACT_SILU)
+#undef EACH
+    }
+}
+template <bool FINE>
+__device__ inline void slope4(int act, f4& v, const f4& pre)
+{
+    switch (act) {
+#define EACH(A)                                                  \
+    case A:                                                      \
+        for (int e = 0; e < 4; ++e) v[e] *= activate_slope<FINE>(A, pre[e]); \
+        break;
+        EACH(CLIFF_ACT_RELU)
+        EACH(CLIFF_ACT_GELU)
+        EACH(CLIFF_ACT_SILU)
+#undef EACH
+    }
+}
+__device__ inline void drop4(const DropArgs& d, uint64_t key, uint32_t step, int64_t r, int64_t c, f4& v)
+{
+    const Words w = philox(key, step, (uint32_t)(c >> 2), r);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = w.w[e] <= d.last ? 0.f : v[e] * d.scale;
 }
 
 // ---- 16 bytes of a row

@@ -16,32 +16,6 @@
 namespace cliff {
 namespace {
 
-constexpr int wg_threads(int TPR) { return TPR > 256 ? TPR : 256; }
-
-template <typename T>
-__device__ inline raw16 load_piece(const T* row, int col, int64_t d)
-{
-    return d < per16<T> ? load16_narrow(row, col, d) : load16(row, col, d);
-}
-template <typename T, int TPR, int R, int C>
-__device__ inline void settle_rows(raw16 (&x)[R][C], int t, int64_t d)
-{
-    if (d < per16<T> || d == (int64_t)C * TPR * per16<T>) return;
-#pragma unroll
-    for (int r = 0; r < R; ++r)
-#pragma unroll
-        for (int c = 0; c < C; ++c) settle16<T>(x[r][c], (c * TPR + t) * per16<T>, d);
-}
-
-// The elements of a vector [d] from column col on.
-template <typename T>
-__device__ inline void load_vector(const T* v, int col, int64_t d, float* to)
-{
-    raw16 r = load_piece(v, col, d);
-    if (d >= per16<T>) settle16<T>(r, col, d);
-    unpack16<T>(r, to);
-}
-
 // Rows per workgroup and pass: wg_threads / TPR groups of R.
 template <typename T, int TPR, int EL, int R>
 __global__ __launch_bounds__(wg_threads(TPR)) void norm_kernel(NormArgs a)
@@ -346,27 +320,6 @@ __global__ __launch_bounds__(1024) void norm_join_kernel(NormBackwardArgs a, con
     } else if (a.dbias) {
         static_cast<T*>(a.dbias)[c - a.d] = (T)v;
     }
-}
-
-int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
-
-// How a row is spread: calls f<TPR, EL, R>() with the smallest spread that holds
-// d elements.  16 lanes of a wave, a wave, or a workgroup per row.
-// Sixteen waves per row hold too few registers for the gradient.
-template <bool BACKWARD, typename F>
-bool with_spread(int64_t d, F&& f)
-{
-    if (d <= 16 * 8) f.template operator()<16, 8, 4>();
-    else if (d <= 16 * 16) f.template operator()<16, 16, 2>();
-    else if (d <= 64 * 8) f.template operator()<64, 8, 4>();
-    else if (d <= 64 * 16) f.template operator()<64, 16, 2>();
-    else if (d <= 256 * 8) f.template operator()<256, 8, 4>();
-    else if (d <= 256 * 16) f.template operator()<256, 16, 2>();
-    else if (d <= 512 * 16) f.template operator()<512, 16, 1>();
-    else if constexpr (BACKWARD) return false;
-    else if (d <= 1024 * 16) f.template operator()<1024, 16, 1>();
-    else return false;
-    return true;
 }
 
 // Workgroups of the gradient: each writes 2 d sums, so no more than keep the
