@@ -36,7 +36,11 @@ EXPORTED = ("clifford_conv_nd", "clifford_conv_nd_algo", "clifford_linear",
             "cliffconv_dense", "cliffconv_dense_workspace", "cliffconv_dense_backward",
             "cliffconv_dense_backward_workspace", "cliffconv_layer_norm",
             "cliffconv_layer_norm_backward", "cliffconv_layer_norm_backward_workspace",
-            "cliffconv_dropout")
+            "cliffconv_dropout",
+            "cliffconv_quantize", "cliffconv_dequantize", "cliffconv_dense_int8",
+            "cliffconv_dense_int8_workspace", "cliffconv_dense_backward_int8",
+            "cliffconv_dense_backward_int8_workspace", "cliffconv_block_norm",
+            "cliffconv_block_norm_backward", "cliffconv_block_norm_backward_workspace")
 
 
 class CliffActDesc(ctypes.Structure):
@@ -93,6 +97,7 @@ def load(path: str = LIB_PATH):
                  "clifford_block2_nd", "clifford_block2_nd_path", "clifford_block2_nd_noalloc"):
         getattr(lib, name).restype = i32
     feed_forward.declare(lib)
+    residual_block.declare(lib)
     _lib = lib
     return lib
 
@@ -630,3 +635,8 @@ from .feed_forward import (  # noqa: E402,F401
     ACT_GELU, ACT_NONE, ACT_RELU, ACT_SILU, dense, dense_backward, dense_backward_plan, dense_plan,
     dropout, dropout_plan, layer_norm, layer_norm_backward, layer_norm_backward_plan,
     layer_norm_plan)
+from . import residual_block  # noqa: E402
+from .residual_block import (  # noqa: E402,F401
+    BlockNormGradients, block_norm, block_norm_backward, block_norm_backward_plan, block_norm_plan,
+    dense_backward_int8, dense_backward_int8_plan, dense_int8, dense_int8_plan, dequantize,
+    dequantize_plan, quantize, quantize_plan)

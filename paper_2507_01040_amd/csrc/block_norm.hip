@@ -1,0 +1,728 @@
+// The norms after and before a block, its gate and the scaled residual in one pass
+// over rows, and their gradient:
+//   out = scale residual + gate n(x),   normed = n(out)
+// (n: layer norm with its weight and bias, or the same without mean).
+//
+// Bound by memory: forward reads x and the residual and writes out and normed,
+// backward reads dout, dnormed, x and out and writes dx and dresidual.  A row lies
+// in the registers of TPR threads as in layer norm (rows.hpp), between its two norms
+// in fp32.
+#include <stdio.h>
+
+#include <algorithm>
+
+#include "rows.hpp"
+
+namespace cliff {
+namespace {
+
+// What the vectors [d] hold from column col on; `otherwise` where there is none.
+template <typename T>
+__device__ inline void vector_or(const void* v, float otherwise, int col, int64_t d, float (&to)[per16<T>])
+{
+    if (v) {
+        load_vector(static_cast<const T*>(v), col, d, to);
+    } else {
+#pragma unroll
+        for (int e = 0; e < per16<T>; ++e) to[e] = otherwise;
+    }
+}
+
+// The row of the gate that belongs to a row.
+template <typename T>
+__device__ inline const T* gate_of(const void* gate, int64_t d, int64_t rows_per_gate, int64_t rows, int64_t r)
+{
+    return static_cast<const T*>(gate) + (rows_per_gate == rows ? 0 : r / rows_per_gate * d);
+}
+
+// Mean (zero with rms) and 1 / standard deviation of R rows in registers, columns
+// past the end zero.
+template <int TPR, int R, int C, int E, int LDS>
+__device__ inline void moments(const float (&v)[R][C][E], int t, int d, bool rms, float eps, float (&mean)[R],
+                               float (&rstd)[R], float (&lds)[2][LDS], int& turn)
+{
+    const float inv = 1.0f / (float)d;
+#pragma unroll
+    for (int r = 0; r < R; ++r) mean[r] = rstd[r] = 0.f;
+    if (!rms) {
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+#pragma unroll
+                for (int e = 0; e < E; ++e) mean[r] += v[r][c][e];
+        row_sums<TPR, R>(mean, lds[turn ^= 1]);
+#pragma unroll
+        for (int r = 0; r < R; ++r) mean[r] *= inv;
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const int have = d - (c * TPR + t) * E;
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                const float u = e < have ? v[r][c][e] - mean[r] : 0.f;
+                rstd[r] = fmaf(u, u, rstd[r]);
+            }
+        }
+    row_sums<TPR, R>(rstd, lds[turn ^= 1]);
+#pragma unroll
+    for (int r = 0; r < R; ++r) rstd[r] = 1.0f / sqrtf(rstd[r] * inv + eps);
+}
+
+template <typename T, int TPR, int EL, int R>
+__global__ __launch_bounds__(wg_threads(TPR)) void block_norm_kernel(BlockNormArgs a, int64_t rows_per_gate)
+{
+    constexpr int E = per16<T>, C = EL / E, G = wg_threads(TPR) / TPR;
+    __shared__ float lds[2][TPR / 64 * R + 1];
+    const int t = threadIdx.x % TPR, g = threadIdx.x / TPR, d = (int)a.d;
+    int turn = 0;
+    for (int64_t r0 = (int64_t)blockIdx.x * G * R; r0 < a.rows; r0 += (int64_t)gridDim.x * G * R) {
+        const int64_t rg = r0 + (int64_t)g * R;
+        raw16 x[R][C], res[R][C];
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            // rows that do not exist give way to the last one
+            const int64_t row = rg + r < a.rows ? rg + r : a.rows - 1;
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                const int col = (c * TPR + t) * E;
+                x[r][c] = load_piece(static_cast<const T*>(a.x) + row * a.ldx, col, d);
+                res[r][c] = load_piece(static_cast<const T*>(a.residual) + row * a.ldr, col, d);
+            }
+        }
+        settle_rows<T, TPR, R, C>(x, t, d);
+        settle_rows<T, TPR, R, C>(res, t, d);
+        float v[R][C][E], mean[R], rstd[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int c = 0; c < C; ++c) unpack16<T>(x[r][c], v[r][c]);
+        auto keep = [&](int which) {
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+                if (a.stats && t == 0 && rg + r < a.rows) {
+                    a.stats[which * a.rows + rg + r] = mean[r];
+                    a.stats[(which + 1) * a.rows + rg + r] = rstd[r];
+                }
+        };
+        if (a.after) {
+            moments<TPR>(v, t, d, a.rms, a.eps, mean, rstd, lds, turn);
+            keep(0);
+        }
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const int col = (c * TPR + t) * E, have = d - col;
+            float w[E], b[E];
+            vector_or<T>(a.weight, 1.f, col, d, w);
+            vector_or<T>(a.bias, 0.f, col, d, b);
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                const int64_t row = rg + r < a.rows ? rg + r : a.rows - 1;
+                float gate[E], u[E];
+                vector_or<T>(a.gate ? gate_of<T>(a.gate, d, rows_per_gate, a.rows, row) : nullptr, 1.f, col, d, gate);
+                unpack16<T>(res[r][c], u);
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    float h = v[r][c][e];
+                    if (a.after) h = fmaf((h - mean[r]) * rstd[r], w[e], b[e]);
+                    if (a.gate) h *= gate[e];
+                    v[r][c][e] = e < have ? fmaf(a.scale, u[e], h) : 0.f;
+                }
+                if (rg + r < a.rows) store16(static_cast<T*>(a.out) + (rg + r) * a.ldo + col, v[r][c], have);
+            }
+        }
+        if (!a.before) continue;
+        moments<TPR>(v, t, d, a.rms, a.eps, mean, rstd, lds, turn);
+        keep(2);
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const int col = (c * TPR + t) * E, have = d - col;
+            float w[E], b[E];
+            vector_or<T>(a.next_weight, 1.f, col, d, w);
+            vector_or<T>(a.next_bias, 0.f, col, d, b);
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                float u[E];
+#pragma unroll
+                for (int e = 0; e < E; ++e) u[e] = fmaf((v[r][c][e] - mean[r]) * rstd[r], w[e], b[e]);
+                if (rg + r < a.rows) store16(static_cast<T*>(a.normed) + (rg + r) * a.ldn + col, u, have);
+            }
+        }
+    }
+}
+
+// Rows that do not fit the registers: one workgroup per row, which forms out anew
+// from x and the residual for each step and writes in the last one, each column by
+// the thread that reads it (out and normed may be x or the residual).
+constexpr int WIDE = 1024;
+template <typename T>
+__global__ __launch_bounds__(WIDE) void block_norm_wide_kernel(BlockNormArgs a, int64_t rows_per_gate)
+{
+    __shared__ float lds[2][WIDE / 64];
+    int turn = 0;
+    const float inv = 1.0f / (float)a.d;
+    for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
+        const T* const x = static_cast<const T*>(a.x) + r * a.ldx;
+        const T* const res = static_cast<const T*>(a.residual) + r * a.ldr;
+        const T* const gate = a.gate ? gate_of<T>(a.gate, a.d, rows_per_gate, a.rows, r) : nullptr;
+        auto sum = [&](auto f) {
+            float s[1] = {0.f};
+            for (int64_t c = threadIdx.x; c < a.d; c += WIDE) s[0] += f(c);
+            row_sums<WIDE, 1>(s, lds[turn ^= 1]);
+            return s[0] * inv;
+        };
+        float mean = 0.f, rstd = 1.f;
+        auto measure = [&](int which, auto f) {
+            float m = 0.f;
+            if (!a.rms) m = sum(f);
+            const float q = sum([&](int64_t c) {
+                const float u = f(c) - m;
+                return u * u;
+            });
+            mean = m;
+            rstd = 1.0f / sqrtf(q + a.eps);
+            if (a.stats && threadIdx.x == 0) {
+                a.stats[which * a.rows + r] = mean;
+                a.stats[(which + 1) * a.rows + r] = rstd;
+            }
+        };
+        if (a.after) measure(0, [&](int64_t c) { return (float)x[c]; });
+        const float mean1 = mean, rstd1 = rstd;
+        auto row = [&](int64_t c) {
+            float h = (float)x[c];
+            if (a.after)
+                h = fmaf((h - mean1) * rstd1, a.weight ? (float)static_cast<const T*>(a.weight)[c] : 1.f,
+                         a.bias ? (float)static_cast<const T*>(a.bias)[c] : 0.f);
+            if (gate) h *= (float)gate[c];
+            return fmaf(a.scale, (float)res[c], h);
+        };
+        if (a.before) measure(2, row);
+        for (int64_t c = threadIdx.x; c < a.d; c += WIDE) {
+            const float v = row(c);
+            static_cast<T*>(a.out)[r * a.ldo + c] = (T)v;
+            if (a.before)
+                static_cast<T*>(a.normed)[r * a.ldn + c] =
+                    (T)fmaf((v - mean) * rstd, a.next_weight ? (float)static_cast<const T*>(a.next_weight)[c] : 1.f,
+                            a.next_bias ? (float)static_cast<const T*>(a.next_bias)[c] : 0.f);
+        }
+    }
+}
+
+// ---- the gradient
+
+// The rows are cut into parts, `per_gate` of them for each gate, and a part's sums
+// over its rows are [4][d] in the workspace:
+//   A = sum t h,  B = sum t,  C = sum dnormed k,  D = sum dnormed.
+struct Parts {
+    int64_t gates, rows_per_gate, per_gate, chunk;  // chunk: rows of a part
+    int64_t all() const { return gates * per_gate; }
+};
+
+template <typename T, int TPR, int EL, int R>
+__global__ __launch_bounds__(wg_threads(TPR), 2) void block_norm_backward_kernel(BlockNormBackwardArgs a, Parts parts,
+                                                                                 float* sums)
+{
+    constexpr int E = per16<T>, C = EL / E, NT = wg_threads(TPR), G = NT / TPR;
+    __shared__ float lds[2][TPR / 64 * 2 * R + 1];
+    __shared__ float join[G > 1 ? NT * EL : 1];
+    if (blockIdx.y && workgroup_id() >= (uint64_t)parts.gates * parts.per_gate) return;
+    const int t = threadIdx.x % TPR, g = threadIdx.x / TPR, d = (int)a.d;
+    const int64_t part = workgroup_id(), which = part / parts.per_gate, sub = part - which * parts.per_gate;
+    const int64_t begin = which * parts.rows_per_gate + sub * parts.chunk;
+    const int64_t last = (which + 1) * parts.rows_per_gate;
+    const int64_t end = begin + parts.chunk < last ? begin + parts.chunk : last;
+    const T* const gate = a.gate ? static_cast<const T*>(a.gate) + which * a.d : nullptr;
+    const float inv = 1.0f / (float)a.d;
+    float sum[4][C][E];
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int e = 0; e < E; ++e) sum[k][c][e] = 0.f;
+    int turn = 0;
+    for (int64_t r0 = begin; r0 < end; r0 += G * R) {
+        const int64_t rg = r0 + (int64_t)g * R;
+        raw16 dout[R][C], dn[R][C], x[R][C], out[R][C];
+        float mean1[R], rstd1[R], mean2[R], rstd2[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const bool row = rg + r < end;
+            const int64_t m = row ? rg + r : end - 1;
+            mean1[r] = row && a.after ? a.stats[m] : 0.f;
+            rstd1[r] = row && a.after ? a.stats[a.rows + m] : row ? 1.f : 0.f;
+            mean2[r] = row && a.dnormed ? a.stats[2 * a.rows + m] : 0.f;
+            rstd2[r] = row && a.dnormed ? a.stats[3 * a.rows + m] : 0.f;
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                const int col = (c * TPR + t) * E;
+                dout[r][c] = dn[r][c] = x[r][c] = out[r][c] = raw16{0, 0, 0, 0};
+                if (a.dout) dout[r][c] = load_piece(static_cast<const T*>(a.dout) + m * a.lddo, col, d);
+                if (a.dnormed) {
+                    dn[r][c] = load_piece(static_cast<const T*>(a.dnormed) + m * a.lddn, col, d);
+                    out[r][c] = load_piece(static_cast<const T*>(a.out) + m * a.ldo, col, d);
+                }
+                if (a.x) x[r][c] = load_piece(static_cast<const T*>(a.x) + m * a.ldx, col, d);
+                // a row that does not exist adds nothing to the sums
+                if (!row) dout[r][c] = dn[r][c] = x[r][c] = out[r][c] = raw16{0, 0, 0, 0};
+            }
+        }
+        settle_rows<T, TPR, R, C>(dout, t, d);
+        settle_rows<T, TPR, R, C>(dn, t, d);
+        settle_rows<T, TPR, R, C>(x, t, d);
+        settle_rows<T, TPR, R, C>(out, t, d);
+        // the norm before the next block: sums of q and of q (out - mean), which rstd
+        // multiplies as a whole (mean times rstd need not be a float)
+        float s[2 * R];
+        if (a.dnormed) {
+#pragma unroll
+            for (int r = 0; r < 2 * R; ++r) s[r] = 0.f;
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                float w[E];
+                vector_or<T>(a.next_weight, 1.f, (c * TPR + t) * E, d, w);
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    float n[E], o[E];
+                    unpack16<T>(dn[r][c], n);
+                    unpack16<T>(out[r][c], o);
+#pragma unroll
+                    for (int e = 0; e < E; ++e) {
+                        const float u = o[e] - mean2[r], q = n[e] * w[e];
+                        s[2 * r] += q;
+                        s[2 * r + 1] = fmaf(q, u, s[2 * r + 1]);
+                        sum[2][c][e] = fmaf(n[e], u * rstd2[r], sum[2][c][e]);
+                        sum[3][c][e] += n[e];
+                    }
+                }
+            }
+#pragma unroll
+            for (int r = 0; r < R; ++r) s[2 * r + 1] *= rstd2[r];
+            row_sums<TPR, 2 * R>(s, lds[turn ^= 1]);
+        }
+        // t, and the same sums for the norm after the block
+        float tv[R][C][E], z[2 * R];
+#pragma unroll
+        for (int r = 0; r < 2 * R; ++r) z[r] = 0.f;
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const int col = (c * TPR + t) * E, have = d - col;
+            float nw[E], w[E], gv[E];
+            vector_or<T>(a.next_weight, 1.f, col, d, nw);
+            vector_or<T>(a.weight, 1.f, col, d, w);
+            vector_or<T>(gate, 1.f, col, d, gv);
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                float n[E], o[E], xv[E], dr[E];
+                unpack16<T>(dout[r][c], tv[r][c]);
+                unpack16<T>(dn[r][c], n);
+                unpack16<T>(out[r][c], o);
+                unpack16<T>(x[r][c], xv);
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    float v = tv[r][c][e];
+                    if (a.dnormed) {
+                        const float k = (o[e] - mean2[r]) * rstd2[r];
+                        float q = n[e] * nw[e] - k * (s[2 * r + 1] * inv);
+                        if (!a.rms) q -= s[2 * r] * inv;
+                        v = fmaf(rstd2[r], q, v);
+                    }
+                    if (e >= have) v = 0.f;
+                    tv[r][c][e] = v;
+                    dr[e] = a.scale * v;
+                    const float u = xv[e] - mean1[r], q = v * gv[e] * w[e];
+                    z[2 * r] += q;
+                    z[2 * r + 1] = fmaf(q, u, z[2 * r + 1]);
+                    sum[0][c][e] = fmaf(v, u * rstd1[r], sum[0][c][e]);
+                    sum[1][c][e] += v;
+                }
+                if (rg + r < end) store16(static_cast<T*>(a.dresidual) + (rg + r) * a.lddr + col, dr, have);
+            }
+        }
+        if (a.after) {
+#pragma unroll
+            for (int r = 0; r < R; ++r) z[2 * r + 1] *= rstd1[r];
+            row_sums<TPR, 2 * R>(z, lds[turn ^= 1]);
+        }
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const int col = (c * TPR + t) * E, have = d - col;
+            float w[E], gv[E];
+            vector_or<T>(a.weight, 1.f, col, d, w);
+            vector_or<T>(gate, 1.f, col, d, gv);
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                float xv[E], dx[E];
+                unpack16<T>(x[r][c], xv);
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    float q = tv[r][c][e] * gv[e];
+                    if (a.after) {
+                        const float h = (xv[e] - mean1[r]) * rstd1[r];
+                        q = q * w[e] - h * (z[2 * r + 1] * inv);
+                        if (!a.rms) q -= z[2 * r] * inv;
+                        q *= rstd1[r];
+                    }
+                    dx[e] = q;
+                }
+                if (rg + r < end) store16(static_cast<T*>(a.dx) + (rg + r) * a.lddx + col, dx, have);
+            }
+        }
+    }
+    if (!sums) return;
+    float* const to = sums + 4 * part * a.d;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        if constexpr (G > 1) {
+            // the groups' sums of a column, in order
+            __syncthreads();
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+#pragma unroll
+                for (int e = 0; e < E; ++e) join[g * TPR * EL + (c * TPR + t) * E + e] = sum[k][c][e];
+            __syncthreads();
+            for (int col = threadIdx.x; col < d; col += NT) {
+                float v = 0.f;
+                for (int i = 0; i < G; ++i) v += join[i * TPR * EL + col];
+                to[k * a.d + col] = v;
+            }
+        } else {
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                const int col = (c * TPR + t) * E;
+#pragma unroll
+                for (int e = 0; e < E; ++e)
+                    if (col + e < d) to[k * a.d + col + e] = sum[k][c][e];
+            }
+        }
+    }
+}
+
+// Rows that do not fit the registers, in three steps: the rows' sums into row_sums
+// [rows][4] (those of the norm before, then after); the sums over rows; dx and
+// dresidual, each element by the thread that reads its inputs.
+struct WideRow {
+    float mean1, rstd1, mean2, rstd2, s1, s2, z1, z2;
+};
+template <typename T>
+__device__ inline float wide_value(const void* v, int64_t i, float otherwise)
+{
+    return v ? (float)static_cast<const T*>(v)[i] : otherwise;
+}
+// t of an element; k: of its normed value
+template <typename T>
+__device__ inline float wide_t(const BlockNormBackwardArgs& a, const WideRow& w, int64_t r, int64_t c)
+{
+    float v = wide_value<T>(a.dout, r * a.lddo + c, 0.f);
+    if (a.dnormed) {
+        const float k = ((float)static_cast<const T*>(a.out)[r * a.ldo + c] - w.mean2) * w.rstd2;
+        float q = (float)static_cast<const T*>(a.dnormed)[r * a.lddn + c] * wide_value<T>(a.next_weight, c, 1.f) - k * w.s2;
+        if (!a.rms) q -= w.s1;
+        v = fmaf(w.rstd2, q, v);
+    }
+    return v;
+}
+template <typename T>
+__device__ inline WideRow wide_row(const BlockNormBackwardArgs& a, const float* row_sums, int64_t r)
+{
+    WideRow w{0.f, 1.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    if (a.after) w.mean1 = a.stats[r], w.rstd1 = a.stats[a.rows + r];
+    if (a.dnormed) w.mean2 = a.stats[2 * a.rows + r], w.rstd2 = a.stats[3 * a.rows + r];
+    if (row_sums) w.s1 = row_sums[4 * r], w.s2 = row_sums[4 * r + 1], w.z1 = row_sums[4 * r + 2], w.z2 = row_sums[4 * r + 3];
+    return w;
+}
+
+template <typename T>
+__global__ __launch_bounds__(WIDE) void block_norm_wide_rows_kernel(BlockNormBackwardArgs a, int64_t rows_per_gate,
+                                                                    float* to)
+{
+    __shared__ float lds[2][2 * WIDE / 64];
+    int turn = 0;
+    const float inv = 1.0f / (float)a.d;
+    for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
+        WideRow w = wide_row<T>(a, nullptr, r);
+        const T* const gate = a.gate ? gate_of<T>(a.gate, a.d, rows_per_gate, a.rows, r) : nullptr;
+        if (a.dnormed) {
+            float s[2] = {0.f, 0.f};
+            for (int64_t c = threadIdx.x; c < a.d; c += WIDE) {
+                const float q = (float)static_cast<const T*>(a.dnormed)[r * a.lddn + c] * wide_value<T>(a.next_weight, c, 1.f);
+                s[0] += q;
+                s[1] = fmaf(q, (float)static_cast<const T*>(a.out)[r * a.ldo + c] - w.mean2, s[1]);
+            }
+            s[1] *= w.rstd2;
+            row_sums<WIDE, 2>(s, lds[turn ^= 1]);
+            w.s1 = s[0] * inv, w.s2 = s[1] * inv;
+        }
+        if (a.after) {
+            float s[2] = {0.f, 0.f};
+            for (int64_t c = threadIdx.x; c < a.d; c += WIDE) {
+                const float q = wide_t<T>(a, w, r, c) * wide_value<T>(gate, c, 1.f) * wide_value<T>(a.weight, c, 1.f);
+                s[0] += q;
+                s[1] = fmaf(q, (float)static_cast<const T*>(a.x)[r * a.ldx + c] - w.mean1, s[1]);
+            }
+            s[1] *= w.rstd1;
+            row_sums<WIDE, 2>(s, lds[turn ^= 1]);
+            w.z1 = s[0] * inv, w.z2 = s[1] * inv;
+        }
+        if (threadIdx.x == 0) to[4 * r] = w.s1, to[4 * r + 1] = w.s2, to[4 * r + 2] = w.z1, to[4 * r + 3] = w.z2;
+    }
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void block_norm_wide_sums_kernel(BlockNormBackwardArgs a, Parts parts,
+                                                                   const float* rows, float* sums, uint32_t blocks)
+{
+    const uint32_t id = workgroup_id();
+    const int64_t part = id / blocks, c = (id - part * blocks) * 256ll + threadIdx.x;
+    if (part >= parts.gates * parts.per_gate || c >= a.d) return;
+    const int64_t which = part / parts.per_gate, begin = which * parts.rows_per_gate + (part - which * parts.per_gate) * parts.chunk;
+    const int64_t last = (which + 1) * parts.rows_per_gate;
+    const int64_t end = begin + parts.chunk < last ? begin + parts.chunk : last;
+    float s[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int64_t r = begin; r < end; ++r) {
+        const WideRow w = wide_row<T>(a, rows, r);
+        const float t = wide_t<T>(a, w, r, c);
+        s[0] = fmaf(t, (wide_value<T>(a.x, r * a.ldx + c, 0.f) - w.mean1) * w.rstd1, s[0]);
+        s[1] += t;
+        if (a.dnormed) {
+            const float n = (float)static_cast<const T*>(a.dnormed)[r * a.lddn + c];
+            s[2] = fmaf(n, ((float)static_cast<const T*>(a.out)[r * a.ldo + c] - w.mean2) * w.rstd2, s[2]);
+            s[3] += n;
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) sums[(4 * part + k) * a.d + c] = s[k];
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void block_norm_wide_dx_kernel(BlockNormBackwardArgs a, int64_t rows_per_gate,
+                                                                 const float* rows, uint32_t blocks)
+{
+    const uint32_t id = workgroup_id();
+    const int64_t r = id / blocks, c = (id - r * blocks) * 256ll + threadIdx.x;
+    if (r >= a.rows || c >= a.d) return;
+    const WideRow w = wide_row<T>(a, rows, r);
+    const float t = wide_t<T>(a, w, r, c);
+    float q = t * (a.gate ? (float)gate_of<T>(a.gate, a.d, rows_per_gate, a.rows, r)[c] : 1.f);
+    if (a.after) {
+        const float h = ((float)static_cast<const T*>(a.x)[r * a.ldx + c] - w.mean1) * w.rstd1;
+        q = q * wide_value<T>(a.weight, c, 1.f) - h * w.z2;
+        if (!a.rms) q -= w.z1;
+        q *= w.rstd1;
+    }
+    static_cast<T*>(a.dresidual)[r * a.lddr + c] = (T)(a.scale * t);
+    static_cast<T*>(a.dx)[r * a.lddx + c] = (T)q;
+}
+
+// Joins a gate's parts in a fixed order: 64 columns per workgroup, every fourth part
+// per wave.  Writes dgate, and the sums that the gates still have to be joined of,
+// gate A, gate B, C and D, to `each` [gates][4][d]; with one gate those are the
+// results.
+template <typename T>
+__global__ __launch_bounds__(256) void block_norm_gate_kernel(BlockNormBackwardArgs a, Parts parts, const float* sums,
+                                                              float* each, uint32_t blocks)
+{
+    __shared__ float s[4][4][64];
+    const uint32_t id = workgroup_id();
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t which = id / blocks, c = (id - which * blocks) * 64ll + lane;
+    if (which >= parts.gates) return;
+    float v[4] = {0.f, 0.f, 0.f, 0.f};
+    if (c < a.d)
+        for (int64_t i = wave; i < parts.per_gate; i += 4)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[k] += sums[(4 * (which * parts.per_gate + i) + k) * a.d + c];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) s[wave][k][lane] = v[k];
+    __syncthreads();
+    if (wave || c >= a.d) return;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] = s[0][k][lane] + s[1][k][lane] + s[2][k][lane] + s[3][k][lane];
+    if (a.dgate) {
+        float g = v[0];
+        if (a.after) g = fmaf(g, wide_value<T>(a.weight, c, 1.f), wide_value<T>(a.bias, c, 0.f) * v[1]);
+        static_cast<T*>(a.dgate)[which * a.d + c] = (T)g;
+    }
+    const float gate = wide_value<T>(a.gate, which * a.d + c, 1.f);
+    v[0] *= gate;
+    v[1] *= gate;
+    if (each) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) each[(4 * which + k) * a.d + c] = v[k];
+        return;
+    }
+    void* const to[4] = {a.dweight, a.dbias, a.dnext_weight, a.dnext_bias};
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+        if (to[k]) static_cast<T*>(to[k])[c] = (T)v[k];
+}
+
+// Joins the gates' sums in a fixed order: 64 of the 4 d columns per workgroup, every
+// 16th gate per wave.
+template <typename T>
+__global__ __launch_bounds__(1024) void block_norm_join_kernel(BlockNormBackwardArgs a, const float* each, int64_t gates)
+{
+    __shared__ float s[16][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t c = workgroup_id() * 64ll + lane;
+    float v = 0.f;
+    if (c < 4 * a.d) {
+#pragma unroll 8
+        for (int64_t i = wave; i < gates; i += 16) v += each[4 * a.d * i + c];
+    }
+    s[wave][lane] = v;
+    __syncthreads();
+    if (wave || c >= 4 * a.d) return;
+    v = 0.f;
+    for (int i = 0; i < 16; ++i) v += s[i][lane];
+    const int64_t k = c / a.d;
+    void* const to = k == 0 ? a.dweight : k == 1 ? a.dbias : k == 2 ? a.dnext_weight : a.dnext_bias;
+    if (to) static_cast<T*>(to)[c - k * a.d] = (T)v;
+}
+
+template <typename T>
+struct Forward {
+    const BlockNormArgs& a;
+    int64_t rows_per_gate;
+    hipStream_t stream;
+    template <int TPR, int EL, int R>
+    void operator()()
+    {
+        // few rows: one each, for every compute unit has one
+        const int64_t cus = std::max(device_cus(), 1), groups = wg_threads(TPR) / TPR;
+        if (a.rows <= cus * groups * R)
+            launch<TPR, EL, 1>();
+        else
+            launch<TPR, EL, R>();
+    }
+    template <int TPR, int EL, int R>
+    void launch()
+    {
+        constexpr int per_pass = wg_threads(TPR) / TPR * R;
+        const int64_t blocks = std::min<int64_t>(ceil_div(a.rows, per_pass), 1 << 20);
+        if (debug_enabled())
+            fprintf(stderr, "cliffconv: block_norm %lld x %lld, %d threads per row, %lld workgroups\n",
+                    (long long)a.rows, (long long)a.d, TPR, (long long)blocks);
+        hipLaunchKernelGGL((block_norm_kernel<T, TPR, EL, R>), dim3((unsigned)blocks), dim3(wg_threads(TPR)), 0,
+                           stream, a, rows_per_gate);
+    }
+};
+
+// How the gradient's rows are cut: each part writes 4 d sums, so no more of them
+// than keep the memory busy; 16 elements of a row in a thread, and so one row.
+struct BackwardParts {
+    template <int TPR, int EL, int R>
+    void operator()()
+    {
+        rows_per_pass = wg_threads(TPR) / TPR * std::max(1, R / 2);
+    }
+    int64_t rows_per_pass = 16;
+};
+Parts cut(int64_t rows, int64_t d, int64_t gates)
+{
+    Parts p;
+    BackwardParts b;
+    const bool fits = with_spread<true>(d, b);
+    const int64_t cus = std::max(device_cus(), 1);
+    p.gates = std::max<int64_t>(gates, 1);
+    p.rows_per_gate = rows / p.gates;
+    const int64_t want = fits ? 2 * cus : std::max<int64_t>(1, ceil_div(2048, ceil_div(d, 256)));
+    p.per_gate = std::max<int64_t>(1, std::min(ceil_div(p.rows_per_gate, b.rows_per_pass), ceil_div(want, p.gates)));
+    p.chunk = ceil_div(ceil_div(p.rows_per_gate, p.per_gate), b.rows_per_pass) * b.rows_per_pass;
+    p.per_gate = std::max<int64_t>(1, p.chunk ? ceil_div(p.rows_per_gate, p.chunk) : 1);
+    return p;
+}
+
+template <typename T>
+struct Backward {
+    const BlockNormBackwardArgs& a;
+    const Parts& parts;
+    float* sums;
+    hipStream_t stream;
+    template <int TPR, int EL, int R>
+    void operator()()
+    {
+        if (debug_enabled())
+            fprintf(stderr, "cliffconv: block_norm_backward %lld x %lld, %d threads per row, %lld workgroups\n",
+                    (long long)a.rows, (long long)a.d, TPR, (long long)parts.all());
+        constexpr int RB = R / 2 > 1 ? R / 2 : 1;
+        hipLaunchKernelGGL((block_norm_backward_kernel<T, TPR, EL, RB>), grid_of(parts.all()), dim3(wg_threads(TPR)),
+                           0, stream, a, parts, sums);
+    }
+};
+
+// Workspace: the parts' sums, the gates' sums, and the sums of rows that do not fit
+// the registers.
+struct Space {
+    int64_t each, rows, all;
+};
+Space space(const Parts& p, int64_t rows, int64_t d)
+{
+    Space s;
+    BackwardParts b;
+    s.each = ceil_div(p.all() * 16 * d, 256) * 256;
+    s.rows = s.each + (p.gates > 1 ? ceil_div(p.gates * 16 * d, 256) * 256 : 0);
+    s.all = s.rows + (with_spread<true>(d, b) ? 0 : 16 * rows);
+    return s;
+}
+
+}  // namespace
+
+cliff_status launch_block_norm(int dtype, const BlockNormArgs& a, hipStream_t stream)
+{
+    clear_hip_error();
+    return with_type(dtype, [&](auto t) {
+        using T = decltype(t);
+        const int64_t rows_per_gate = a.gate ? a.rows / a.gates : a.rows;
+        if (!with_spread<false>(a.d, Forward<T>{a, rows_per_gate, stream}))
+            hipLaunchKernelGGL(block_norm_wide_kernel<T>, dim3((unsigned)std::min<int64_t>(a.rows, 1 << 20)), dim3(WIDE),
+                               0, stream, a, rows_per_gate);
+        return launched();
+    });
+}
+
+int64_t block_norm_backward_workspace(int, int64_t rows, int64_t d, int64_t gates)
+{
+    return space(cut(rows, d, gates), rows, d).all;
+}
+
+cliff_status launch_block_norm_backward(int dtype, const BlockNormBackwardArgs& a, hipStream_t stream)
+{
+    clear_hip_error();
+    return with_type(dtype, [&](auto t) {
+        using T = decltype(t);
+        const Parts parts = cut(a.rows, a.d, a.gates);
+        const Space s = space(parts, a.rows, a.d);
+        char* const ws = static_cast<char*>(a.workspace);
+        float* const sums = reinterpret_cast<float*>(ws);
+        float* const rows = reinterpret_cast<float*>(ws + s.rows);
+        const bool params = a.dgate || a.dweight || a.dbias || a.dnext_weight || a.dnext_bias;
+        const int64_t blocks = ceil_div(a.d, 256), cols = ceil_div(a.d, 64);
+        // (rows of the grid are 16 bits; matrices of 2^37 elements and more)
+        if (std::max(cols * parts.all(), a.d > 8192 ? blocks * a.rows : 0) > GRID_ROW * 0xffff) return CLIFF_EUNSUPPORTED;
+        if (a.rows && !with_spread<true>(a.d, Backward<T>{a, parts, params ? sums : nullptr, stream})) {
+            hipLaunchKernelGGL(block_norm_wide_rows_kernel<T>, dim3((unsigned)std::min<int64_t>(a.rows, 1 << 20)),
+                               dim3(WIDE), 0, stream, a, parts.rows_per_gate, rows);
+            if (params)
+                hipLaunchKernelGGL(block_norm_wide_sums_kernel<T>, grid_of(blocks * parts.all()), dim3(256), 0, stream,
+                                   a, parts, rows, sums, (uint32_t)blocks);
+            hipLaunchKernelGGL(block_norm_wide_dx_kernel<T>, grid_of(blocks * a.rows), dim3(256), 0, stream, a,
+                               parts.rows_per_gate, rows, (uint32_t)blocks);
+        }
+        if (params) {
+            float* const each = parts.gates > 1 ? reinterpret_cast<float*>(ws + s.each) : nullptr;
+            Parts join = parts;
+            if (!a.rows) join.per_gate = 0;
+            hipLaunchKernelGGL(block_norm_gate_kernel<T>, grid_of(cols * parts.gates), dim3(256), 0, stream, a, join,
+                               sums, each, (uint32_t)cols);
+            if (each && (a.dweight || a.dbias || a.dnext_weight || a.dnext_bias))
+                hipLaunchKernelGGL(block_norm_join_kernel<T>, grid_of(ceil_div(4 * a.d, 64)), dim3(1024), 0, stream, a,
+                                   each, parts.gates);
+        }
+        return launched();
+    });
+}
+
+}  // namespace cliff

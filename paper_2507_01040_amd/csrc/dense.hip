@@ -1120,8 +1120,24 @@ constexpr float fit_slope(int act)
 // workgroup takes 256 columns; its four waves every fourth row each.  Bound by the
 // vector instructions of f' and the generator: 8192 x 2048 bf16, GELU and dropout,
 // 33 us (3 TB/s); 65536 x 512 fp32, SiLU, 87 us (4.6 TB/s, memory).
-template <typename T>
-__global__ __launch_bounds__(256) void slope_kernel(DenseBackwardArgs a, T* g, float* sums, int64_t rows_per_part)
+// The pre-activations of four columns are in T, or in 8 bits with a scale for each
+// pre_groups-th of a row (EIGHT).
+template <typename T, bool EIGHT>
+__device__ inline f4 load_pre(const DenseBackwardArgs& a, const float* pre_scale, int64_t pre_groups, int64_t r, int64_t c,
+                              int have)
+{
+    if constexpr (EIGHT) {
+        Integers<4> q;
+        q.load(static_cast<const int8_t*>(a.pre) + r * a.ldp + c, have);
+        const float s = pre_scale[r * pre_groups + (pre_groups > 1 ? c / CLIFF_INT8_GROUP : 0)];
+        return f4{q.value(0, s), q.value(1, s), q.value(2, s), q.value(3, s)};
+    } else {
+        return load4(static_cast<const T*>(a.pre) + r * a.ldp + c, have);
+    }
+}
+template <typename T, bool EIGHT>
+__device__ inline void slope_rows(const DenseBackwardArgs& a, T* g, float* sums, int64_t rows_per_part,
+                                  const float* pre_scale, int64_t pre_groups)
 {
     __shared__ f4 part[4][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -1141,8 +1157,7 @@ __global__ __launch_bounds__(256) void slope_kernel(DenseBackwardArgs a, T* g, f
 #pragma unroll 4
         for (int64_t r = r0 + wave; r < r1; r += 4) {
             f4 v = load4(static_cast<const T*>(a.dy) + r * a.lddy + c, have);
-            if (a.act != CLIFF_ACT_NONE)
-                slope4<sizeof(T) == 4>(a.act, v, load4(static_cast<const T*>(a.pre) + r * a.ldp + c, have));
+            if (a.act != CLIFF_ACT_NONE) slope4<sizeof(T) == 4>(a.act, v, load_pre<T, EIGHT>(a, pre_scale, pre_groups, r, c, have));
             if (keep.rng) drop4(keep, key, step, r, c, v);
             t += v;
             if (g) store4(g + r * a.N + c, v * fit_slope<T>(a.act), have);
@@ -1156,6 +1171,25 @@ __global__ __launch_bounds__(256) void slope_kernel(DenseBackwardArgs a, T* g, f
 #pragma unroll
     for (int e = 0; e < 4; ++e)
         if (c + e < a.N) sums[blockIdx.y * a.N + c + e] = t[e];
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void slope_kernel(DenseBackwardArgs a, T* g, float* sums, int64_t rows_per_part)
+{
+    slope_rows<T, false>(a, g, sums, rows_per_part, nullptr, 0);
+}
+template <typename T>
+__global__ __launch_bounds__(256) void slope_int8_kernel(DenseBackwardInt8Args a, T* g, float* sums,
+                                                         int64_t rows_per_part)
+{
+    slope_rows<T, true>(a.dense, g, sums, rows_per_part, a.pre_scale, a.pre_groups);
+}
+
+// x in 8 bits, as the product with g reads it.
+template <typename T>
+__global__ __launch_bounds__(256) void expand_kernel(DequantizeArgs a, uint32_t pieces, int64_t n)
+{
+    dequantize_rows<T>(a, workgroup_id() * 256ll + threadIdx.x, pieces, n);
 }
 
 // dbias: scale times the parts [part][N], joined in a fixed order: 64 columns per
@@ -1394,6 +1428,45 @@ cliff_status launch_dense(int dtype, const DenseArgs& a, hipStream_t stream)
     });
 }
 
+namespace {
+
+// What follows the slopes: dbias from its partial sums, dx and dw from g.
+template <typename T>
+cliff_status finish_backward(int dtype, const DenseBackwardArgs& a, const BackwardSpace& w, const void* g, int64_t ldg,
+                             hipStream_t stream)
+{
+    char* const ws = static_cast<char*>(a.workspace);
+    float* const partial = reinterpret_cast<float*>(ws + w.partial);
+    const float scale = a.drop.rng ? a.drop.scale : 1.f;
+    cliff_status s = CLIFF_OK;
+    if (a.dbias) {
+        hipLaunchKernelGGL(bias_kernel<T>, grid_of(ceil_div(a.N, 64)), dim3(1024), 0, stream,
+                           reinterpret_cast<float*>(ws + w.sums), w.parts, a.N, scale, static_cast<T*>(a.dbias));
+        s = launched();
+    }
+    const DropArgs none{nullptr, 0, 1.f};
+    auto plain = [&](int64_t M, int64_t N, int64_t K, const void* x, int64_t ldx, const void* y, int64_t ldy,
+                     void* out, int64_t ldo) {
+        return ProductArgs{M, N, K, x, ldx, y, ldy, 1, scale / fit_slope<T>(a.act), 0, partial, nullptr,
+                           CLIFF_ACT_NONE, none, nullptr, 0, nullptr, 0, out, ldo};
+    };
+    if (s == CLIFF_OK && a.dx && a.M) {
+        const ProductArgs p = plain(a.M, a.K, a.N, g, ldg, a.w, a.ldw, a.dx, a.lddx);
+        s = a.w_out_in ? product<T, true, false>(dtype, p, stream) : product<T, true, true>(dtype, p, stream);
+    }
+    if (s == CLIFF_OK && a.dw)  // in the order of w: [K, N] = x^T g or [N, K] = g^T x
+        s = product<T, false, false>(dtype,
+                                     a.w_out_in ? plain(a.N, a.K, a.M, g, ldg, a.x, a.ldx, a.dw, a.lddw)
+                                                : plain(a.K, a.N, a.M, a.x, a.ldx, g, ldg, a.dw, a.lddw),
+                                     stream);
+    return s;
+}
+
+// x of a gradient from 8 bits in the workspace: its row stride and its place.
+int64_t expanded_ld(int64_t K) { return ceil_div(K, 8) * 8; }
+
+}  // namespace
+
 cliff_status launch_dense_backward(int dtype, const DenseBackwardArgs& a, hipStream_t stream)
 {
     clear_hip_error();
@@ -1402,39 +1475,53 @@ cliff_status launch_dense_backward(int dtype, const DenseBackwardArgs& a, hipStr
         const BackwardSpace w = backward_space(dtype, a.M, a.K, a.N);
         char* const ws = static_cast<char*>(a.workspace);
         const bool change = a.act != CLIFF_ACT_NONE || a.drop.rng;
-        const void* g = change ? ws + w.g : a.dy;
-        const int64_t ldg = change ? a.N : a.lddy;
-        float* const sums = reinterpret_cast<float*>(ws + w.sums);
-        float* const partial = reinterpret_cast<float*>(ws + w.partial);
-        const float scale = a.drop.rng ? a.drop.scale : 1.f;
         cliff_status s = CLIFF_OK;
         if (a.dbias || (change && (a.dx || a.dw))) {
             hipLaunchKernelGGL(slope_kernel<T>, dim3((unsigned)ceil_div(a.N, 256), (unsigned)w.parts), dim3(256), 0,
                                stream, a, change && (a.dx || a.dw) ? reinterpret_cast<T*>(ws + w.g) : nullptr,
-                               a.dbias ? sums : nullptr, ceil_div(a.M, w.parts));
+                               a.dbias ? reinterpret_cast<float*>(ws + w.sums) : nullptr, ceil_div(a.M, w.parts));
             s = launched();
         }
-        if (s == CLIFF_OK && a.dbias) {
-            hipLaunchKernelGGL(bias_kernel<T>, grid_of(ceil_div(a.N, 64)), dim3(1024), 0, stream, sums,
-                               w.parts, a.N, scale, static_cast<T*>(a.dbias));
+        if (s != CLIFF_OK) return s;
+        return finish_backward<T>(dtype, a, w, change ? ws + w.g : a.dy, change ? a.N : a.lddy, stream);
+    });
+}
+
+int64_t dense_backward_int8_workspace(int dtype, int64_t M, int64_t K, int64_t N)
+{
+    const int64_t x = M * expanded_ld(K) * (dtype == CLIFF_F32 ? 4 : 2);
+    return backward_space(dtype, M, K, N).all + ceil_div(x, 256) * 256;
+}
+
+cliff_status launch_dense_backward_int8(int dtype, const DenseBackwardInt8Args& a, hipStream_t stream)
+{
+    clear_hip_error();
+    return with_type(dtype, [&](auto t) {
+        using T = decltype(t);
+        DenseBackwardArgs d = a.dense;
+        const BackwardSpace w = backward_space(dtype, d.M, d.K, d.N);
+        char* const ws = static_cast<char*>(d.workspace);
+        const bool change = d.act != CLIFF_ACT_NONE || d.drop.rng;
+        cliff_status s = CLIFF_OK;
+        if (d.dbias || (change && (d.dx || d.dw))) {
+            hipLaunchKernelGGL(slope_int8_kernel<T>, dim3((unsigned)ceil_div(d.N, 256), (unsigned)w.parts), dim3(256),
+                               0, stream, a, change && (d.dx || d.dw) ? reinterpret_cast<T*>(ws + w.g) : nullptr,
+                               d.dbias ? reinterpret_cast<float*>(ws + w.sums) : nullptr, ceil_div(d.M, w.parts));
             s = launched();
         }
-        const DropArgs none{nullptr, 0, 1.f};
-        auto plain = [&](int64_t M, int64_t N, int64_t K, const void* x, int64_t ldx, const void* y, int64_t ldy,
-                         void* out, int64_t ldo) {
-            return ProductArgs{M, N, K, x, ldx, y, ldy, 1, scale / fit_slope<T>(a.act), 0, partial, nullptr,
-                               CLIFF_ACT_NONE, none, nullptr, 0, nullptr, 0, out, ldo};
-        };
-        if (s == CLIFF_OK && a.dx && a.M) {
-            const ProductArgs p = plain(a.M, a.K, a.N, g, ldg, a.w, a.ldw, a.dx, a.lddx);
-            s = a.w_out_in ? product<T, true, false>(dtype, p, stream) : product<T, true, true>(dtype, p, stream);
+        if (s == CLIFF_OK && d.dw && d.M) {
+            const int64_t ld = expanded_ld(d.K), pieces = ceil_div(d.K, per16<T>);
+            const int64_t n = pieces * ceil_div(d.M, DEQUANTIZE_ROWS), blocks = ceil_div(n, 256);
+            if (blocks >= (int64_t)1 << 31) return CLIFF_EUNSUPPORTED;
+            const DequantizeArgs x{d.M, d.K, a.x_groups, static_cast<const int8_t*>(d.x), d.ldx, a.x_scale,
+                                   ws + w.all, ld};
+            hipLaunchKernelGGL(expand_kernel<T>, grid_of(blocks), dim3(256), 0, stream, x, (uint32_t)pieces, n);
+            s = launched();
+            d.x = x.y;
+            d.ldx = ld;
         }
-        if (s == CLIFF_OK && a.dw)  // in the order of w: [K, N] = x^T g or [N, K] = g^T x
-            s = product<T, false, false>(dtype,
-                                         a.w_out_in ? plain(a.N, a.K, a.M, g, ldg, a.x, a.ldx, a.dw, a.lddw)
-                                                    : plain(a.K, a.N, a.M, a.x, a.ldx, g, ldg, a.dw, a.lddw),
-                                         stream);
-        return s;
+        if (s != CLIFF_OK) return s;
+        return finish_backward<T>(dtype, d, w, change ? ws + w.g : d.dy, change ? d.N : d.lddy, stream);
     });
 }
 

@@ -103,6 +103,92 @@ struct DropoutArgs {
     int64_t ldy;
 };
 
+struct QuantizeArgs {
+    int64_t rows, d, groups;  // groups: scales per row
+    const void* x;
+    int64_t ldx;
+    int8_t* q;
+    int64_t ldq;
+    float* scale;
+};
+
+struct DequantizeArgs {
+    int64_t rows, d, groups;
+    const int8_t* q;
+    int64_t ldq;
+    const float* scale;
+    void* y;
+    int64_t ldy;
+};
+
+struct DenseInt8Args {
+    int64_t M, K, N;
+    const int8_t* x;
+    int64_t ldx;
+    const float* x_scale;
+    const int8_t* w;
+    int64_t ldw;
+    const float* w_scale;
+    const void* bias;
+    int act;
+    const void* residual;
+    int64_t ldr;
+    void* y;
+    int64_t ldy;
+    void* workspace;
+};
+
+// x and pre of `dense` in 8 bits, with x_groups and pre_groups scales per row.
+struct DenseBackwardInt8Args {
+    DenseBackwardArgs dense;
+    const float* x_scale;
+    int64_t x_groups;
+    const float* pre_scale;
+    int64_t pre_groups;
+};
+
+struct BlockNormArgs {
+    int64_t rows, d;
+    const void* x;
+    int64_t ldx;
+    const void* residual;
+    int64_t ldr;
+    const void* gate;  // [gates, d], each for rows / gates rows; gates 0: none
+    int64_t gates;
+    float scale, eps;
+    bool after, before, rms;
+    const void *weight, *bias, *next_weight, *next_bias;
+    void* out;
+    int64_t ldo;
+    void* normed;
+    int64_t ldn;
+    float* stats;  // [4, rows]
+};
+
+struct BlockNormBackwardArgs {
+    int64_t rows, d;
+    const void* dout;
+    int64_t lddo;
+    const void* dnormed;
+    int64_t lddn;
+    const void* x;
+    int64_t ldx;
+    const void* out;
+    int64_t ldo;
+    const float* stats;
+    const void* gate;
+    int64_t gates;
+    float scale;
+    bool after, rms;
+    const void *weight, *bias, *next_weight;
+    void* dx;
+    int64_t lddx;
+    void* dresidual;
+    int64_t lddr;
+    void *dgate, *dweight, *dbias, *dnext_weight, *dnext_bias;
+    void* workspace;
+};
+
 // ---- checks of a call's arguments (host)
 
 constexpr int64_t MAX_SIZE = ((int64_t)1 << 31) - 1;  // of a width or row count
@@ -212,6 +298,15 @@ cliff_status launch_layer_norm(int dtype, const NormArgs& a, hipStream_t stream)
 cliff_status launch_layer_norm_backward(int dtype, const NormBackwardArgs& a, hipStream_t stream);
 int64_t layer_norm_backward_workspace(int dtype, int64_t rows, int64_t d);
 cliff_status launch_dropout(int dtype, const DropoutArgs& a, hipStream_t stream);
+cliff_status launch_quantize(int dtype, const QuantizeArgs& a, hipStream_t stream);
+cliff_status launch_dequantize(int dtype, const DequantizeArgs& a, hipStream_t stream);
+cliff_status launch_dense_int8(int dtype, const DenseInt8Args& a, hipStream_t stream);
+int64_t dense_int8_workspace(int64_t M, int64_t K, int64_t N);
+cliff_status launch_dense_backward_int8(int dtype, const DenseBackwardInt8Args& a, hipStream_t stream);
+int64_t dense_backward_int8_workspace(int dtype, int64_t M, int64_t K, int64_t N);
+cliff_status launch_block_norm(int dtype, const BlockNormArgs& a, hipStream_t stream);
+cliff_status launch_block_norm_backward(int dtype, const BlockNormBackwardArgs& a, hipStream_t stream);
+int64_t block_norm_backward_workspace(int dtype, int64_t rows, int64_t d, int64_t gates);
 
 inline cliff_status launched()
 {

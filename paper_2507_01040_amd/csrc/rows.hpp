@@ -37,6 +37,54 @@ __device__ inline void store16(T* p, const float* v, int have)
     }
 }
 
+// E 8-bit integers of neighbouring columns, of which some may not exist (have < E),
+// and the values that they stand for.
+template <int E>
+struct Integers {
+    uint32_t w[E / 4];
+    __device__ void load(const int8_t* p, int have)
+    {
+        if (have >= E) {
+            __builtin_memcpy(w, p, E);
+        } else {
+#pragma unroll
+            for (int i = 0; i < E / 4; ++i) w[i] = 0;
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                if (e < have) w[e / 4] |= (uint32_t)(uint8_t)p[e] << 8 * (e % 4);
+        }
+    }
+    __device__ float value(int e, float scale) const { return (float)(int8_t)(w[e / 4] >> 8 * (e % 4)) * scale; }
+};
+
+// Integers to the values that they stand for: piece i of n, the same 16 bytes of the
+// output of each of DEQUANTIZE_ROWS rows.
+constexpr int DEQUANTIZE_ROWS = 4;
+template <typename T>
+__device__ inline void dequantize_rows(const DequantizeArgs& a, int64_t i, uint32_t pieces, int64_t n)
+{
+    constexpr int E = per16<T>, ROWS = DEQUANTIZE_ROWS;
+    if (i >= n) return;
+    const int64_t g = n >> 32 ? i / pieces : (int64_t)((uint32_t)i / pieces), r0 = g * ROWS;
+    const int64_t col = (i - g * pieces) * E;
+    const int have = a.d - col < E ? (int)(a.d - col) : E;
+    Integers<E> q[ROWS];
+    float s[ROWS];
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+        const int64_t row = r0 + r < a.rows ? r0 + r : a.rows - 1;
+        q[r].load(a.q + row * a.ldq + col, have);
+        s[r] = a.scale[row * a.groups + (a.groups > 1 ? col / CLIFF_INT8_GROUP : 0)];
+    }
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+        float v[E];
+#pragma unroll
+        for (int e = 0; e < E; ++e) v[e] = q[r].value(e, s[r]);
+        if (r0 + r < a.rows) store16(static_cast<T*>(a.y) + (r0 + r) * a.ldy + col, v, have);
+    }
+}
+
 template <int CTRL>
 __device__ inline float dpp(float v)
 {
