@@ -26,6 +26,9 @@ struct Int8Args {
     int64_t lda;
     const int8_t* b;
     int64_t ldb;
+    int splits;      // parts of the contraction, each by its own workgroups ...
+    int64_t k_part;  // ... of this many values (a multiple of the stage's)
+    int* partial;    // splits > 1: [splits][M][N], joined by another kernel
     const float* a_scale;
     const float* b_scale;
     const void* bias;
@@ -41,6 +44,26 @@ __device__ inline i16v mma(const u4& x, const u4& y, const i16v& c)
     return __builtin_amdgcn_mfma_i32_32x32x32_i8(__builtin_bit_cast(i4, x), __builtin_bit_cast(i4, y), c, 0, 0, 0);
 }
 
+// Four neighbouring sums, of which some may not exist (have < 4).
+__device__ inline i4 load4i(const int* p, int have)
+{
+    i4 v = {0, 0, 0, 0};
+    if (have >= 4) __builtin_memcpy(&v, p, sizeof v);
+    else
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (e < have) v[e] = p[e];
+    return v;
+}
+__device__ inline void store4i(int* p, const i4& v, int have)
+{
+    if (have >= 4) __builtin_memcpy(p, &v, sizeof v);
+    else
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (e < have) p[e] = v[e];
+}
+
 // What a group of four columns needs besides its sums, loaded early.
 struct Ends {
     f4 scale, bias;
@@ -49,7 +72,7 @@ template <typename T>
 __device__ inline Ends load_ends(const Int8Args& p, int64_t n)
 {
     Ends e{f4{0.f, 0.f, 0.f, 0.f}, f4{0.f, 0.f, 0.f, 0.f}};
-    if (n >= p.N) return e;
+    if (n >= p.N || p.splits > 1) return e;  // (the join's)
     const int have = p.N - n < 4 ? (int)(p.N - n) : 4;
     e.scale = load4(p.b_scale + n, have);
     if (p.bias) e.bias = load4(static_cast<const T*>(p.bias) + n, have);
@@ -91,8 +114,8 @@ __device__ inline void finish_rows(const Int8Args& p, int64_t m, int step, int64
 // row.  Begins with a barrier: the stages there are done with.
 constexpr int EW = 64 + 4;  // integers per row there
 template <typename T, int MI, int NI>
-__device__ inline void write_tile(const Int8Args& p, int64_t m1, int64_t n1, const i16v (&acc)[MI][NI], char* smem,
-                                  int lane, int wave)
+__device__ inline void write_tile(const Int8Args& p, const TileId& id, int64_t m1, int64_t n1,
+                                  const i16v (&acc)[MI][NI], char* smem, int lane, int wave)
 {
     const int64_t n = n1 + 4 * (lane & 15);
     const Ends ends = load_ends<T>(p, n);
@@ -121,20 +144,139 @@ __device__ inline void write_tile(const Int8Args& p, int64_t m1, int64_t n1, con
                 i4 v[4];
 #pragma unroll
                 for (int r = 0; r < 4; ++r) v[r] = *reinterpret_cast<const i4*>(tile + (r0 + 4 * r) * EW + 4 * (lane & 15));
-                finish_rows<T, 4>(p, m1 + 32 * i + r0, 4, n, v, ends);
+                const int64_t m = m1 + 32 * i + r0;
+                if (p.splits > 1) {
+                    const int have = p.N - n < 4 ? (int)(p.N - n) : 4;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        if (m + 4 * r < p.M) store4i(p.partial + (id.split * p.M + m + 4 * r) * p.N + n, v[r], have);
+                } else {
+                    finish_rows<T, 4>(p, m, 4, n, v, ends);
+                }
             }
         }
         wave_fence();
     }
 }
 
-// 128 x 128 outputs per workgroup of 2 x 2 waves, stages of 128 contraction values
-// (slots of 16, as of 8 in 16 bits), of any alignment, one stage ahead in registers.
-constexpr int TILE = 128, KT = 128;
-template <typename T>
-__global__ __launch_bounds__(256) void int8_tile_kernel(Int8Args p)
+// BM x BN outputs per workgroup of WR x WC waves, stages of KT contraction values in
+// LDS slots of 16 (dense_geom.hpp counts them as 8 of 16 bits).  Rows that are 16-byte
+// aligned and whole slots: stages go from memory straight to LDS, one ahead in the
+// other of two buffers; the loads of a stage are spread over the products of two
+// groups, and the first fragments of the next stage are read under the last
+// products of this one, as in the product of 16-bit types (dense.hip).
+//
+// Bound by the matrix cores and LDS together, as there: a 32 x 32 x 32 product of
+// 8-bit integers takes the cycles of a 32 x 32 x 16 one of 16 bits, and its fragments
+// are as large.
+constexpr int KT = 128;
+template <typename T, int BM, int BN, int WR, int WC>
+__global__ __launch_bounds__(64 * WR * WC) void int8_direct_kernel(Int8Args p)
 {
-    constexpr int NT = 256, MI = 2, NI = 2;
+    constexpr int NT = 64 * WR * WC, WM = BM / WR, WN = BN / WC, MI = WM / 32, NI = WN / 32;
+    constexpr Stage SA{BM, KT / 2, true}, SB{BN, KT / 2, true};
+    constexpr int LA = SA.slots() / NT, LB = SB.slots() / NT, PA = SA.bytes(), BUF = PA + SB.bytes(), KK = KT / 32;
+    static_assert(WN == 64 && KK % 2 == 0 && LA == LB && LA % MI == 0, "shape");
+    extern __shared__ u4 smem4[];
+    char* const smem = reinterpret_cast<char*>(smem4);
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wm = wave / WC * WM, wn = wave % WC * WN;
+    const uint32_t tm = (uint32_t)((p.M + BM - 1) / BM), tn = (uint32_t)((p.N + BN - 1) / BN);
+    if (blockIdx.y && workgroup_id() >= tm * tn * p.splits) return;
+    const TileId id = tile_of(workgroup_id(), tm, tn, p.splits);
+    const int64_t m0 = (int64_t)id.m * BM, n0 = (int64_t)id.n * BN, k0 = id.split * p.k_part;
+    const int kn = (int)(p.K - k0 < p.k_part ? p.K - k0 : p.k_part), steps = (kn + KT - 1) / KT;
+    const int8_t* const a = p.a + m0 * p.lda + k0;
+    const int8_t* const b = p.b + n0 * p.ldb + k0;
+
+    i16v acc[MI][NI];
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+        for (int j = 0; j < NI; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[i][j][e] = 0;
+    u4 fa[2][MI], fb[2][NI];
+    auto read_one = [&](int set, const char* buf, int kk, int f) {  // columns' fragments first
+        if (f < NI)
+            fb[set][f] = *reinterpret_cast<const u4*>(buf + PA + frag_byte(SB, wn + 32 * f, 16 * kk, lane, 0));
+        else
+            fa[set][f - NI] = *reinterpret_cast<const u4*>(buf + frag_byte(SA, wm + 32 * (f - NI), 16 * kk, lane, 0));
+    };
+    // byte offsets of a thread's slots from a stage's start; rows that do not exist are
+    // zeros
+    uint32_t offa[LA], offb[LB];
+#pragma unroll
+    for (int i = 0; i < LA; ++i) {
+        const int e = i * NT + tid, ra = SA.slot_row(e), rb = SB.slot_row(e);
+        offa[i] = m0 + ra < p.M ? (uint32_t)(ra * p.lda + 2 * SA.slot_k(e)) : NOWHERE;
+        offb[i] = n0 + rb < p.N ? (uint32_t)(rb * p.ldb + 2 * SB.slot_k(e)) : NOWHERE;
+    }
+    auto load = [&](const int8_t* x, const Stage& S, uint32_t off, int i, int s, char* to) {
+        if (kn - s * KT < KT && 2 * S.slot_k(i * NT + tid) >= kn - s * KT) off = NOWHERE;
+        load_to_lds(x + (int64_t)s * KT, off, to + wave * 1024 + i * NT * 16);
+    };
+    auto load_a = [&](int s, int i) { load(a, SA, offa[i], i, s, smem + (s & 1) * BUF); };
+    auto load_b = [&](int s, int i) { load(b, SB, offb[i], i, s, smem + (s & 1) * BUF + PA); };
+    // Products of a group of 32 values, with the reads of the next one's fragments
+    // (next: its buffer) and half of the loads of a stage.  The output's columns are
+    // the matrix instruction's rows: a lane's groups of four sums are neighbours.
+    auto group = [&](int set, const char* next, int kk, auto loads) {
+        constexpr int F = MI + NI;
+#pragma unroll
+        for (int i = 0; i < MI; ++i) {
+#pragma unroll
+            for (int f = i * F / MI; f < (i + 1) * F / MI; ++f) read_one(set ^ 1, next, kk, f);
+#pragma unroll
+            for (int j = 0; j < NI; ++j) acc[i][j] = mma(fb[set][j], fa[set][i], acc[i][j]);
+#pragma unroll
+            for (int l = i * LA / MI; l < (i + 1) * LA / MI; ++l) loads(l);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    auto nothing = [](int) {};
+#pragma unroll
+    for (int i = 0; i < LA; ++i) load_a(0, i);
+#pragma unroll
+    for (int i = 0; i < LB; ++i) load_b(0, i);
+    wait_direct();
+    __syncthreads();
+    if (steps > 1)
+#pragma unroll
+        for (int i = 0; i < LA; ++i) load_a(1, i);
+#pragma unroll
+    for (int f = 0; f < MI + NI; ++f) read_one(0, smem, 0, f);
+    // Step s; whether there are one and two more.
+    auto step = [&](int s, auto one, auto two) {
+        const char* const buf = smem + (s & 1) * BUF;
+        group(0, buf, 1, [&](int i) {
+            if constexpr (one) load_b(s + 1, i);
+        });
+#pragma unroll
+        for (int kk = 1; kk + 1 < KK; ++kk) group(kk & 1, buf, kk + 1, nothing);
+        wait_direct();
+        __syncthreads();
+        // (the last step reads what no product uses)
+        group(1, smem + ((s + 1) & 1) * BUF, 0, [&](int i) {
+            if constexpr (two) load_a(s + 2, i);
+        });
+    };
+    constexpr std::true_type yes;
+    constexpr std::false_type no;
+    int s = 0;
+    for (; s + 2 < steps; ++s) step(s, yes, yes);
+    if (s + 1 < steps) step(s++, yes, no);
+    step(s, no, no);
+    write_tile<T, MI, NI>(p, id, m0 + wm, n0 + wn, acc, smem, lane, wave);
+}
+
+// The same for rows of any alignment and width: slots go through registers, one stage
+// ahead.
+template <typename T>
+__global__ __launch_bounds__(256) void int8_staged_kernel(Int8Args p)
+{
+    constexpr int TILE = 128, NT = 256, MI = 2, NI = 2;
     constexpr Stage S{TILE, KT / 2, true};
     constexpr int L = S.slots() / NT, KK = KT / 32;
     __shared__ __align__(16) char smem[2 * S.bytes() > 4 * 32 * EW * 4 ? 2 * S.bytes() : 4 * 32 * EW * 4];
@@ -142,10 +284,11 @@ __global__ __launch_bounds__(256) void int8_tile_kernel(Int8Args p)
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave / 2 * 64, wn = wave % 2 * 64;
     const uint32_t tm = (uint32_t)((p.M + TILE - 1) / TILE), tn = (uint32_t)((p.N + TILE - 1) / TILE);
-    if (blockIdx.y && workgroup_id() >= tm * tn) return;
-    const TileId id = tile_of(workgroup_id(), tm, tn, 1);
+    if (blockIdx.y && workgroup_id() >= tm * tn * p.splits) return;
+    const TileId id = tile_of(workgroup_id(), tm, tn, p.splits);
     const int64_t m0 = (int64_t)id.m * TILE, n0 = (int64_t)id.n * TILE;
-    const int K = (int)p.K, steps = (K + KT - 1) / KT;
+    const int K = (int)p.K, k0 = (int)(id.split * p.k_part), k1 = K - k0 < p.k_part ? K : k0 + (int)p.k_part;
+    const int steps = (k1 - k0 + KT - 1) / KT;
 
     i16v acc[MI][NI];
 #pragma unroll
@@ -165,11 +308,13 @@ __global__ __launch_bounds__(256) void int8_tile_kernel(Int8Args p)
         lb[i] = p.b + (n0 + r < p.N ? n0 + r : p.N - 1) * p.ldb;
         at[i] = 2 * S.slot_k(e);
     }
+    // (a part that is not the last one ends with a whole stage: pieces past its end are
+    // past the row's)
     raw16 ca[L], cb[L];
     auto fetch = [&](int s) {
 #pragma unroll
         for (int i = 0; i < L; ++i) {
-            const int k = s * KT + at[i];
+            const int k = k0 + s * KT + at[i];
             ca[i] = K < 16 ? load16_narrow(la[i], k, K) : load16(la[i], k, K);
             cb[i] = K < 16 ? load16_narrow(lb[i], k, K) : load16(lb[i], k, K);
         }
@@ -177,12 +322,12 @@ __global__ __launch_bounds__(256) void int8_tile_kernel(Int8Args p)
     fetch(0);
     for (int s = 0; s < steps; ++s) {
         __syncthreads();
+        const bool whole = k0 + (s + 1) * KT <= K;
 #pragma unroll
         for (int i = 0; i < L; ++i) {
-            const int k = s * KT + at[i];
-            if (K >= 16) {
-                settle16<int8_t>(ca[i], k, K);
-                settle16<int8_t>(cb[i], k, K);
+            if (!whole && K >= 16) {
+                settle16<int8_t>(ca[i], k0 + s * KT + at[i], K);
+                settle16<int8_t>(cb[i], k0 + s * KT + at[i], K);
             }
             *reinterpret_cast<raw16*>(smem + (i * NT + tid) * 16) = ca[i];
             *reinterpret_cast<raw16*>(smem + S.bytes() + (i * NT + tid) * 16) = cb[i];
@@ -203,27 +348,214 @@ __global__ __launch_bounds__(256) void int8_tile_kernel(Int8Args p)
                 for (int j = 0; j < NI; ++j) acc[i][j] = mma(fb[j], fa[i], acc[i][j]);
         }
     }
-    write_tile<T, MI, NI>(p, m0 + wm, n0 + wn, acc, smem, lane, wave);
+    write_tile<T, MI, NI>(p, id, m0 + wm, n0 + wn, acc, smem, lane, wave);
+}
+
+// Joins the parts of a split contraction and finishes the outputs: a thread for each
+// group of four columns, bound by the read of the parts.
+template <typename T>
+__global__ __launch_bounds__(256) void int8_join_kernel(Int8Args p)
+{
+    const int64_t nq = (p.N + 3) / 4, plane = p.M * p.N, i = workgroup_id() * 256ll + threadIdx.x;
+    const int64_t m = i >> 32 ? i / nq : (int64_t)((uint32_t)i / (uint32_t)nq), n = (i - m * nq) * 4;
+    if (m >= p.M) return;
+    const int have = p.N - n < 4 ? (int)(p.N - n) : 4, splits = p.splits;
+    Int8Args whole = p;
+    whole.splits = 1;
+    const Ends ends = load_ends<T>(whole, n);
+    const int* const q = p.partial + m * p.N + n;
+    i4 v[1] = {i4{0, 0, 0, 0}};
+#pragma unroll 4
+    for (int s = 0; s < splits; ++s) v[0] += load4i(q + s * plane, have);
+    finish_rows<T, 1>(p, m, 1, n, v, ends);
+}
+
+// Few rows (16 MB at most): bound by the read of the weight.  A workgroup streams 16
+// of its outputs' rows once, its eight waves an eighth of the contraction each, D
+// stages of 128 values ahead, and they join their sums in LDS; as for 16-bit types
+// (rows.hpp), with matrix instructions of 16 x 16 outputs and 64 values.
+template <typename T, int MB>
+__global__ __launch_bounds__(512, 2) void int8_rows_kernel(Int8Args p)
+{
+    constexpr int D = MB == 4 ? 3 : MB == 1 ? 8 : 4;  // what the registers hold
+    constexpr int W = 16 + 4, OWN = (MB + 1) * LINES, PLANE = MB * 16 * W;
+    __shared__ __align__(16) char smem[8 * (PLANE * 4 > OWN ? PLANE * 4 : OWN)];
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const RowsPart<KT> part(p.N, p.K, 16, wave);
+    const int8_t* const b = p.b + part.n0 * p.ldb;
+    i4 acc[MB];
+#pragma unroll
+    for (int i = 0; i < MB; ++i) acc[i] = i4{0, 0, 0, 0};
+    struct St {
+        raw16 x[MB][2], w[2];
+    };
+    char* const own = smem + wave * OWN;
+    Lines al[MB], bl(0, part.cols, p.ldb, lane, int8_t{});
+#pragma unroll
+    for (int i = 0; i < MB; ++i) al[i] = Lines(16 * i, p.M, p.lda, lane, int8_t{});
+    auto load = [&](St& f, int64_t k) {
+#pragma unroll
+        for (int i = 0; i < MB; ++i) al[i].load(f.x[i], p.a + k);
+        bl.load(f.w, b + k);
+    };
+    auto load_last = [&](St& f, int64_t k) {
+#pragma unroll
+        for (int i = 0; i < MB; ++i) Lines::load_last(f.x[i], p.a, 16 * i, p.M, p.lda, k, part.k1, lane);
+        Lines::load_last(f.w, b, 0, part.cols, p.ldb, k, part.k1, lane);
+    };
+    auto use = [&](St& f) {
+#pragma unroll
+        for (int i = 0; i < MB; ++i) Lines::write(f.x[i], own + i * LINES, lane);
+        Lines::write(f.w, own + MB * LINES, lane);
+        wave_fence();
+        raw16 w[2], x[MB][2];
+        Lines::read(w, own + MB * LINES, lane);
+#pragma unroll
+        for (int i = 0; i < MB; ++i) Lines::read(x[i], own + i * LINES, lane);
+        wave_fence();
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int i = 0; i < MB; ++i)
+                acc[i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i4, w[j]), __builtin_bit_cast(i4, x[i][j]),
+                                                               acc[i], 0, 0, 0);
+    };
+    part.template run<D, St>(load, load_last, use);
+
+    int* const lds = reinterpret_cast<int*>(smem);
+    const int r = threadIdx.x / 4, c = 4 * (threadIdx.x % 4);
+    const int64_t n = part.n0 + c;
+    const Ends ends = load_ends<T>(p, n);
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < MB; ++i)
+        *reinterpret_cast<i4*>(lds + wave * PLANE + (16 * i + (lane & 15)) * W + 4 * (lane >> 4)) = acc[i];
+    __syncthreads();
+    if (r >= 16 * MB || r >= p.M || n >= p.N) return;
+    i4 v[1] = {i4{0, 0, 0, 0}};
+#pragma unroll
+    for (int w = 0; w < 8; ++w) v[0] += *reinterpret_cast<const i4*>(lds + w * PLANE + r * W + c);
+    finish_rows<T, 1>(p, r, 1, n, v, ends);
+}
+
+// How a product is cut: tiles of 256 x 256 or 128 x 128, and parts of the
+// contraction, by the times in ns of a stage with one workgroup on each compute unit
+// and with as many as fit, and of a workgroup's begin and end.
+struct Cut {
+    bool large;
+    int splits;
+    int64_t k_part;
+    double ns;  // what it is expected to take
+};
+struct TileTimes {
+    int B, fit;
+    double alone, full, ends;
+};
+constexpr TileTimes T_DIRECT256{256, 1, 1300, 1300, 10000}, T_DIRECT128{128, 2, 600, 1150, 5800},
+    T_STAGED128{128, 2, 1100, 1550, 6300};
+
+Cut cut(int64_t M, int64_t N, int64_t K, bool direct)
+{
+    const int64_t cus = std::max(device_cus(), 1);
+    Cut best{false, 1, 0, 0};
+    for (int large = 0; large <= (direct ? 1 : 0); ++large) {
+        const TileTimes& t = large ? T_DIRECT256 : direct ? T_DIRECT128 : T_STAGED128;
+        const int64_t tiles = ceil_div(M, t.B) * ceil_div(N, t.B), steps = ceil_div(K, KT);
+        for (const int want : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
+            if (want > steps) break;
+            const int64_t per = ceil_div(steps, want), splits = ceil_div(steps, per);
+            const int64_t wgs = tiles * splits, rounds = wgs / (cus * t.fit), rest = wgs % (cus * t.fit);
+            double ns = rounds * (per * t.full + t.ends);
+            if (rest) ns += per * (rest <= cus ? t.alone : t.full) + t.ends;
+            // the join: a launch, and the partial sums written and read
+            if (splits > 1) ns += 4400 + (double)M * N * 4 * 2 * splits / 11700;
+            if (best.ns == 0 || ns < best.ns) best = Cut{large != 0, (int)splits, per * KT, ns};
+        }
+    }
+    return best;
+}
+
+// What the kernel of few rows is for: rows, row strides (32-bit offsets), and outputs
+// (2^32 threads of a grid).
+constexpr int64_t FEW_ROWS = 64, FEW_LD = 1 << 24, FEW_N = 1 << 26;
+
+// Its time in ns, from the bytes that a compute unit takes in: every workgroup reads
+// all of x.
+double few_rows_ns(int64_t M, int64_t N, int64_t K)
+{
+    const int rows = M <= 16 ? 16 : M <= 32 ? 32 : 64;
+    const double rounds = std::max(1., (double)ceil_div(N, 16) / std::max(device_cus(), 1));
+    return 3500 + rounds * (double)(K * (rows + 16)) / 75;
+}
+
+bool aligned_rows(const void* x, int64_t ld, int64_t width)
+{
+    return ((uintptr_t)x & 15) == 0 && ld % 16 == 0 && width % 16 == 0 && ld <= (1 << 22);
+}
+
+template <typename T>
+cliff_status int8_product(Int8Args p, hipStream_t stream)
+{
+    const bool direct = aligned_rows(p.a, p.lda, p.K) && aligned_rows(p.b, p.ldb, p.K);
+    const Cut c = cut(p.M, p.N, p.K, direct);
+    p.splits = 1;
+    const auto say = [&](const char* name, int64_t wgs) {
+        if (debug_enabled())
+            fprintf(stderr, "cliffconv: int8 product %lld x %lld x %lld, %s, %lld workgroups, %d splits\n", (long long)p.M,
+                    (long long)p.N, (long long)p.K, name, (long long)wgs, p.splits);
+    };
+    if (p.M <= FEW_ROWS && p.K >= 16 && p.lda <= FEW_LD && p.ldb <= FEW_LD && p.N <= FEW_N &&
+        few_rows_ns(p.M, p.N, p.K) < c.ns) {
+        const int64_t wgs = ceil_div(p.N, 16);
+        say("few rows", wgs);
+        const auto go = [&](auto k) { hipLaunchKernelGGL(k, dim3((unsigned)wgs), dim3(512), 0, stream, p); };
+        if (p.M <= 16) go(int8_rows_kernel<T, 1>);
+        else if (p.M <= 32) go(int8_rows_kernel<T, 2>);
+        else go(int8_rows_kernel<T, 4>);
+        return launched();
+    }
+    p.splits = c.splits;
+    p.k_part = c.k_part;
+    const int B = c.large ? 256 : 128;
+    const int64_t wgs = ceil_div(p.M, B) * ceil_div(p.N, B) * p.splits;
+    if (wgs >= (int64_t)1 << 31) return CLIFF_EUNSUPPORTED;
+    say(c.large ? "direct tiles of 256" : direct ? "direct tiles of 128" : "staged tiles of 128", wgs);
+    // LDS: two buffers of a stage, or what write_tile takes
+    if (c.large)
+        hipLaunchKernelGGL((int8_direct_kernel<T, 256, 256, 2, 4>), grid_of(wgs), dim3(512), 2 * 2 * 256 * KT, stream, p);
+    else if (direct)
+        hipLaunchKernelGGL((int8_direct_kernel<T, 128, 128, 2, 2>), grid_of(wgs), dim3(256), 2 * 2 * 128 * KT, stream, p);
+    else
+        hipLaunchKernelGGL(int8_staged_kernel<T>, grid_of(wgs), dim3(256), 0, stream, p);
+    const cliff_status s = launched();
+    if (s != CLIFF_OK || p.splits == 1) return s;
+    const int64_t blocks = ceil_div(p.M * ceil_div(p.N, 4), 256);
+    if (blocks >= (int64_t)1 << 31) return CLIFF_EUNSUPPORTED;
+    hipLaunchKernelGGL(int8_join_kernel<T>, grid_of(blocks), dim3(256), 0, stream, p);
+    return launched();
 }
 
 }  // namespace
 
-int64_t dense_int8_workspace(int64_t, int64_t, int64_t) { return 0; }
+int64_t dense_int8_workspace(int64_t M, int64_t K, int64_t N)
+{
+    int64_t n = 0;
+    for (const bool direct : {false, true}) {
+        const Cut c = cut(M, N, K, direct);
+        if (c.splits > 1) n = std::max(n, c.splits * M * N * 4);
+    }
+    return ceil_div(n, 256) * 256;
+}
 
 cliff_status launch_dense_int8(int dtype, const DenseInt8Args& a, hipStream_t stream)
 {
     clear_hip_error();
     return with_type(dtype, [&](auto t) {
         using T = decltype(t);
-        const Int8Args p{a.M, a.N, a.K, a.x, a.ldx, a.w, a.ldw, a.x_scale, a.w_scale,
-                         a.bias, a.act, a.residual, a.ldr, a.y, a.ldy};
-        const int64_t wgs = ceil_div(p.M, TILE) * ceil_div(p.N, TILE);
-        if (wgs >= (int64_t)1 << 31) return CLIFF_EUNSUPPORTED;
-        if (debug_enabled())
-            fprintf(stderr, "cliffconv: int8 product %lld x %lld x %lld, staged tiles of %d, %lld workgroups\n",
-                    (long long)p.M, (long long)p.N, (long long)p.K, TILE, (long long)wgs);
-        hipLaunchKernelGGL(int8_tile_kernel<T>, grid_of(wgs), dim3(256), 0, stream, p);
-        return launched();
+        return int8_product<T>(Int8Args{a.M, a.N, a.K, a.x, a.ldx, a.w, a.ldw, 1, 0, static_cast<int*>(a.workspace),
+                                        a.x_scale, a.w_scale, a.bias, a.act, a.residual, a.ldr, a.y, a.ldy},
+                               stream);
     });
 }
 

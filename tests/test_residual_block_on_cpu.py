@@ -186,3 +186,23 @@ def test_widest_calls():
         size = c["M"] * max(c["K"], c["N"]) if "M" in c else c["rows"] * c["d"]
         assert r.split()[1] == "0" or (r.split()[1] == "5" and size > 1 << 37), (c, r)
         assert int(r.split()[2]) < 1 << 32, (c, r)
+
+
+def test_which_kernel_an_int8_product_takes():
+    def taken(name, cases):
+        for c, (_, lines) in zip(cases, _run(cases)):
+            assert name in lines[0], (c, lines)
+        return cases
+    for i, t in enumerate(TYPES):
+        taken("few rows", [_int8(t, s, i, **r) for s in ((1, 4096, 40), (16, 1000, 17), (33, 520, 47), (64, 300, 33), (24, 16, 64))
+                           for r in (dict(), dict(pad=3), dict(off=5))])
+        taken("staged tiles of 128", [_int8(t, s, i, cus=1, **r) for s in ((65, 7, 5), (200, 130, 135), (130, 300, 260), (129, 1000, 64))
+                                      for r in (dict(), dict(pad=3), dict(pad=16, off=1))])
+        taken("direct tiles of 128", [_int8(t, s, i, late=j, **r) for s in ((65, 16, 8), (130, 144, 136), (257, 400, 96), (128, 128, 128))
+                                      for r in (dict(), dict(pad=16), dict(pad_x=32, off=16, pad_y=1)) for j in (0, 1)])
+        taken("direct tiles of 256", [_int8(t, s, i, cus=1, late=j, **r) for s in ((520, 1104, 512), (513, 848, 488), (264, 656, 1000))
+                                      for r in (dict(), dict(pad=16)) for j in (0, 1)])
+        # a contraction in parts, joined
+        for s in ((70, 2064, 72), (130, 4112, 61), (96, 3001, 250)):
+            for _, lines in _run([_int8(t, s, i + j) for j in range(4)]):
+                assert "tiles" in lines[0] and int(lines[0].rsplit(" ", 2)[1]) > 1, lines
