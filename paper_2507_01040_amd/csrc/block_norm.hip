@@ -28,6 +28,34 @@ __device__ inline void vector_or(const void* v, float otherwise, int col, int64_
     }
 }
 
+// The pieces of a vector [d] that a thread has, loaded early and unpacked where they
+// are used (of elements past the end, anything).
+template <typename T, int TPR, int C>
+struct Pieces {
+    raw16 r[C];
+    __device__ void load(const void* v, int t, int64_t d)
+    {
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const int col = (c * TPR + t) * per16<T>;
+            r[c] = raw16{0, 0, 0, 0};
+            if (v) r[c] = load_piece(static_cast<const T*>(v), col, d);
+        }
+    }
+    __device__ void get(const void* v, float otherwise, int c, int t, int64_t d, float (&to)[per16<T>]) const
+    {
+        raw16 p = r[c];
+        if (d >= per16<T>) settle16<T>(p, (c * TPR + t) * per16<T>, d);
+        unpack16<T>(p, to);
+        if (!v)
+#pragma unroll
+            for (int e = 0; e < per16<T>; ++e) to[e] = otherwise;
+    }
+};
+
+// Workgroups of the kernels here: 64 threads or fewer per row share one of 256.
+constexpr int block_threads(int TPR) { return TPR > 64 ? TPR : 256; }
+
 // The row of the gate that belongs to a row.
 template <typename T>
 __device__ inline const T* gate_of(const void* gate, int64_t d, int64_t rows_per_gate, int64_t rows, int64_t r)
@@ -72,9 +100,9 @@ __device__ inline void moments(const float (&v)[R][C][E], int t, int d, bool rms
 }
 
 template <typename T, int TPR, int EL, int R>
-__global__ __launch_bounds__(wg_threads(TPR)) void block_norm_kernel(BlockNormArgs a, int64_t rows_per_gate)
+__global__ __launch_bounds__(block_threads(TPR)) void block_norm_kernel(BlockNormArgs a, int64_t rows_per_gate)
 {
-    constexpr int E = per16<T>, C = EL / E, G = wg_threads(TPR) / TPR;
+    constexpr int E = per16<T>, C = EL / E, G = block_threads(TPR) / TPR;
     __shared__ float lds[2][TPR / 64 * R + 1];
     const int t = threadIdx.x % TPR, g = threadIdx.x / TPR, d = (int)a.d;
     int turn = 0;
@@ -91,6 +119,17 @@ __global__ __launch_bounds__(wg_threads(TPR)) void block_norm_kernel(BlockNormAr
                 x[r][c] = load_piece(static_cast<const T*>(a.x) + row * a.ldx, col, d);
                 res[r][c] = load_piece(static_cast<const T*>(a.residual) + row * a.ldr, col, d);
             }
+        }
+        // one row: its vectors are under way with it
+        constexpr bool EARLY = R == 1 && TPR < 1024;
+        Pieces<T, TPR, C> pw, pb, pg, pnw, pnb;
+        if constexpr (EARLY) {
+            const int64_t row = rg < a.rows ? rg : a.rows - 1;
+            pw.load(a.weight, t, d);
+            pb.load(a.bias, t, d);
+            pg.load(a.gate ? gate_of<T>(a.gate, d, rows_per_gate, a.rows, row) : nullptr, t, d);
+            pnw.load(a.next_weight, t, d);
+            pnb.load(a.next_bias, t, d);
         }
         settle_rows<T, TPR, R, C>(x, t, d);
         settle_rows<T, TPR, R, C>(res, t, d);
@@ -115,13 +154,20 @@ __global__ __launch_bounds__(wg_threads(TPR)) void block_norm_kernel(BlockNormAr
         for (int c = 0; c < C; ++c) {
             const int col = (c * TPR + t) * E, have = d - col;
             float w[E], b[E];
-            vector_or<T>(a.weight, 1.f, col, d, w);
-            vector_or<T>(a.bias, 0.f, col, d, b);
+            if constexpr (EARLY) {
+                pw.get(a.weight, 1.f, c, t, d, w);
+                pb.get(a.bias, 0.f, c, t, d, b);
+            } else {
+                vector_or<T>(a.weight, 1.f, col, d, w);
+                vector_or<T>(a.bias, 0.f, col, d, b);
+            }
 #pragma unroll
             for (int r = 0; r < R; ++r) {
                 const int64_t row = rg + r < a.rows ? rg + r : a.rows - 1;
                 float gate[E], u[E];
-                vector_or<T>(a.gate ? gate_of<T>(a.gate, d, rows_per_gate, a.rows, row) : nullptr, 1.f, col, d, gate);
+                if constexpr (EARLY) pg.get(a.gate, 1.f, c, t, d, gate);
+                else
+                    vector_or<T>(a.gate ? gate_of<T>(a.gate, d, rows_per_gate, a.rows, row) : nullptr, 1.f, col, d, gate);
                 unpack16<T>(res[r][c], u);
 #pragma unroll
                 for (int e = 0; e < E; ++e) {
@@ -140,8 +186,13 @@ __global__ __launch_bounds__(wg_threads(TPR)) void block_norm_kernel(BlockNormAr
         for (int c = 0; c < C; ++c) {
             const int col = (c * TPR + t) * E, have = d - col;
             float w[E], b[E];
-            vector_or<T>(a.next_weight, 1.f, col, d, w);
-            vector_or<T>(a.next_bias, 0.f, col, d, b);
+            if constexpr (EARLY) {
+                pnw.get(a.next_weight, 1.f, c, t, d, w);
+                pnb.get(a.next_bias, 0.f, c, t, d, b);
+            } else {
+                vector_or<T>(a.next_weight, 1.f, col, d, w);
+                vector_or<T>(a.next_bias, 0.f, col, d, b);
+            }
 #pragma unroll
             for (int r = 0; r < R; ++r) {
                 float u[E];
@@ -154,12 +205,30 @@ __global__ __launch_bounds__(wg_threads(TPR)) void block_norm_kernel(BlockNormAr
 }
 
 // Rows that do not fit the registers: one workgroup per row, which forms out anew
-// from x and the residual for each step and writes in the last one, each column by
+// from x and the residual for each step and writes in the last one, each piece by
 // the thread that reads it (out and normed may be x or the residual).
 constexpr int WIDE = 1024;
 template <typename T>
+__device__ inline void load_wide(const T* row, int64_t col, int64_t d, float (&v)[per16<T>])
+{
+    raw16 r = load16(row, col, d);
+    settle16<T>(r, col, d);
+    unpack16<T>(r, v);
+}
+template <typename T>
+__device__ inline void wide_vector(const void* v, float otherwise, int64_t col, int64_t d, float (&to)[per16<T>])
+{
+    if (v) {
+        load_wide(static_cast<const T*>(v), col, d, to);
+    } else {
+#pragma unroll
+        for (int e = 0; e < per16<T>; ++e) to[e] = otherwise;
+    }
+}
+template <typename T>
 __global__ __launch_bounds__(WIDE) void block_norm_wide_kernel(BlockNormArgs a, int64_t rows_per_gate)
 {
+    constexpr int E = per16<T>;
     __shared__ float lds[2][WIDE / 64];
     int turn = 0;
     const float inv = 1.0f / (float)a.d;
@@ -167,20 +236,23 @@ __global__ __launch_bounds__(WIDE) void block_norm_wide_kernel(BlockNormArgs a, 
         const T* const x = static_cast<const T*>(a.x) + r * a.ldx;
         const T* const res = static_cast<const T*>(a.residual) + r * a.ldr;
         const T* const gate = a.gate ? gate_of<T>(a.gate, a.d, rows_per_gate, a.rows, r) : nullptr;
-        auto sum = [&](auto f) {
+        // the sum over the row of what f gives for the values that `values` gives
+        auto sum = [&](auto values, auto f) {
             float s[1] = {0.f};
-            for (int64_t c = threadIdx.x; c < a.d; c += WIDE) s[0] += f(c);
+            for (int64_t c = threadIdx.x * (int64_t)E; c < a.d; c += WIDE * E) {
+                float v[E];
+                values(c, v);
+#pragma unroll
+                for (int e = 0; e < E; ++e) s[0] += c + e < a.d ? f(v[e]) : 0.f;
+            }
             row_sums<WIDE, 1>(s, lds[turn ^= 1]);
             return s[0] * inv;
         };
         float mean = 0.f, rstd = 1.f;
-        auto measure = [&](int which, auto f) {
+        auto measure = [&](int which, auto values) {
             float m = 0.f;
-            if (!a.rms) m = sum(f);
-            const float q = sum([&](int64_t c) {
-                const float u = f(c) - m;
-                return u * u;
-            });
+            if (!a.rms) m = sum(values, [](float v) { return v; });
+            const float q = sum(values, [&](float v) { return (v - m) * (v - m); });
             mean = m;
             rstd = 1.0f / sqrtf(q + a.eps);
             if (a.stats && threadIdx.x == 0) {
@@ -188,24 +260,36 @@ __global__ __launch_bounds__(WIDE) void block_norm_wide_kernel(BlockNormArgs a, 
                 a.stats[(which + 1) * a.rows + r] = rstd;
             }
         };
-        if (a.after) measure(0, [&](int64_t c) { return (float)x[c]; });
+        if (a.after) measure(0, [&](int64_t c, float (&v)[E]) { load_wide(x, c, a.d, v); });
         const float mean1 = mean, rstd1 = rstd;
-        auto row = [&](int64_t c) {
-            float h = (float)x[c];
-            if (a.after)
-                h = fmaf((h - mean1) * rstd1, a.weight ? (float)static_cast<const T*>(a.weight)[c] : 1.f,
-                         a.bias ? (float)static_cast<const T*>(a.bias)[c] : 0.f);
-            if (gate) h *= (float)gate[c];
-            return fmaf(a.scale, (float)res[c], h);
+        auto row = [&](int64_t c, float (&v)[E]) {
+            float w[E], b[E], g[E], u[E];
+            load_wide(x, c, a.d, v);
+            load_wide(res, c, a.d, u);
+            wide_vector<T>(a.weight, 1.f, c, a.d, w);
+            wide_vector<T>(a.bias, 0.f, c, a.d, b);
+            wide_vector<T>(gate, 1.f, c, a.d, g);
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                float h = v[e];
+                if (a.after) h = fmaf((h - mean1) * rstd1, w[e], b[e]);
+                v[e] = fmaf(a.scale, u[e], h * g[e]);
+            }
         };
         if (a.before) measure(2, row);
-        for (int64_t c = threadIdx.x; c < a.d; c += WIDE) {
-            const float v = row(c);
-            static_cast<T*>(a.out)[r * a.ldo + c] = (T)v;
-            if (a.before)
-                static_cast<T*>(a.normed)[r * a.ldn + c] =
-                    (T)fmaf((v - mean) * rstd, a.next_weight ? (float)static_cast<const T*>(a.next_weight)[c] : 1.f,
-                            a.next_bias ? (float)static_cast<const T*>(a.next_bias)[c] : 0.f);
+        for (int64_t c = threadIdx.x * (int64_t)E; c < a.d; c += WIDE * E) {
+            const int have = a.d - c < E ? (int)(a.d - c) : E;
+            float v[E], w[E], b[E];
+            row(c, v);
+            // (a piece that passes the end comes with columns of another thread, which may
+            // write them, and drops them)
+            store16(static_cast<T*>(a.out) + r * a.ldo + c, v, have);
+            if (!a.before) continue;
+            wide_vector<T>(a.next_weight, 1.f, c, a.d, w);
+            wide_vector<T>(a.next_bias, 0.f, c, a.d, b);
+#pragma unroll
+            for (int e = 0; e < E; ++e) v[e] = fmaf((v[e] - mean) * rstd, w[e], b[e]);
+            store16(static_cast<T*>(a.normed) + r * a.ldn + c, v, have);
         }
     }
 }
@@ -220,11 +304,13 @@ struct Parts {
     int64_t all() const { return gates * per_gate; }
 };
 
+// The next rows' loads are under way while the sums of these are joined, where the
+// registers hold both.
 template <typename T, int TPR, int EL, int R>
-__global__ __launch_bounds__(wg_threads(TPR), 2) void block_norm_backward_kernel(BlockNormBackwardArgs a, Parts parts,
-                                                                                 float* sums)
+__global__ __launch_bounds__(block_threads(TPR), TPR < 1024 ? 2 : 4) void block_norm_backward_kernel(BlockNormBackwardArgs a,
+                                                                                              Parts parts, float* sums)
 {
-    constexpr int E = per16<T>, C = EL / E, NT = wg_threads(TPR), G = NT / TPR;
+    constexpr int E = per16<T>, C = EL / E, NT = block_threads(TPR), G = NT / TPR;
     __shared__ float lds[2][TPR / 64 * 2 * R + 1];
     __shared__ float join[G > 1 ? NT * EL : 1];
     if (blockIdx.y && workgroup_id() >= (uint64_t)parts.gates * parts.per_gate) return;
@@ -242,33 +328,66 @@ __global__ __launch_bounds__(wg_threads(TPR), 2) void block_norm_backward_kernel
         for (int c = 0; c < C; ++c)
 #pragma unroll
             for (int e = 0; e < E; ++e) sum[k][c][e] = 0.f;
+    // the vectors, once for all rows: next_weight, and what t is multiplied by on its way to
+    // the norm after the block (without it to dx), gate weight
+    float nws[C][E], gws[C][E];
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        const int col = (c * TPR + t) * E;
+        float gv[E];
+        vector_or<T>(a.next_weight, 1.f, col, d, nws[c]);
+        vector_or<T>(a.weight, 1.f, col, d, gws[c]);
+        vector_or<T>(gate, 1.f, col, d, gv);
+#pragma unroll
+        for (int e = 0; e < E; ++e) gws[c][e] *= gv[e];
+    }
     int turn = 0;
-    for (int64_t r0 = begin; r0 < end; r0 += G * R) {
-        const int64_t rg = r0 + (int64_t)g * R;
+    struct Rows {
         raw16 dout[R][C], dn[R][C], x[R][C], out[R][C];
         float mean1[R], rstd1[R], mean2[R], rstd2[R];
+    };
+    auto load = [&](Rows& w, int64_t r0) {
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            const bool row = rg + r < end;
-            const int64_t m = row ? rg + r : end - 1;
-            mean1[r] = row && a.after ? a.stats[m] : 0.f;
-            rstd1[r] = row && a.after ? a.stats[a.rows + m] : row ? 1.f : 0.f;
-            mean2[r] = row && a.dnormed ? a.stats[2 * a.rows + m] : 0.f;
-            rstd2[r] = row && a.dnormed ? a.stats[3 * a.rows + m] : 0.f;
+            // rows that do not exist give way to the last one
+            const int64_t row = r0 + (int64_t)g * R + r, m = row < end ? row : end - 1;
+            w.mean1[r] = a.after ? a.stats[m] : 0.f;
+            w.rstd1[r] = a.after ? a.stats[a.rows + m] : 1.f;
+            w.mean2[r] = a.dnormed ? a.stats[2 * a.rows + m] : 0.f;
+            w.rstd2[r] = a.dnormed ? a.stats[3 * a.rows + m] : 0.f;
 #pragma unroll
             for (int c = 0; c < C; ++c) {
                 const int col = (c * TPR + t) * E;
-                dout[r][c] = dn[r][c] = x[r][c] = out[r][c] = raw16{0, 0, 0, 0};
-                if (a.dout) dout[r][c] = load_piece(static_cast<const T*>(a.dout) + m * a.lddo, col, d);
+                w.dout[r][c] = w.dn[r][c] = w.x[r][c] = w.out[r][c] = raw16{0, 0, 0, 0};
+                if (a.dout) w.dout[r][c] = load_piece(static_cast<const T*>(a.dout) + m * a.lddo, col, d);
                 if (a.dnormed) {
-                    dn[r][c] = load_piece(static_cast<const T*>(a.dnormed) + m * a.lddn, col, d);
-                    out[r][c] = load_piece(static_cast<const T*>(a.out) + m * a.ldo, col, d);
+                    w.dn[r][c] = load_piece(static_cast<const T*>(a.dnormed) + m * a.lddn, col, d);
+                    w.out[r][c] = load_piece(static_cast<const T*>(a.out) + m * a.ldo, col, d);
                 }
-                if (a.x) x[r][c] = load_piece(static_cast<const T*>(a.x) + m * a.ldx, col, d);
-                // a row that does not exist adds nothing to the sums
-                if (!row) dout[r][c] = dn[r][c] = x[r][c] = out[r][c] = raw16{0, 0, 0, 0};
+                if (a.x) w.x[r][c] = load_piece(static_cast<const T*>(a.x) + m * a.ldx, col, d);
             }
         }
+    };
+    constexpr bool AHEAD = TPR < 1024;
+    Rows now, next;
+    if constexpr (AHEAD) load(next, begin);
+    for (int64_t r0 = begin; r0 < end; r0 += G * R) {
+        const int64_t rg = r0 + (int64_t)g * R;
+        if constexpr (AHEAD) {
+            now = next;
+            if (r0 + G * R < end) load(next, r0 + G * R);
+        } else {
+            load(now, r0);
+        }
+        auto &dout = now.dout, &dn = now.dn, &x = now.x, &out = now.out;
+        auto &mean1 = now.mean1, &rstd1 = now.rstd1, &mean2 = now.mean2, &rstd2 = now.rstd2;
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+            if (rg + r >= end) {  // a row that does not exist adds nothing to the sums
+                mean1[r] = rstd1[r] = mean2[r] = rstd2[r] = 0.f;
+#pragma unroll
+                for (int c = 0; c < C; ++c) dout[r][c] = dn[r][c] = x[r][c] = out[r][c] = raw16{0, 0, 0, 0};
+            }
         settle_rows<T, TPR, R, C>(dout, t, d);
         settle_rows<T, TPR, R, C>(dn, t, d);
         settle_rows<T, TPR, R, C>(x, t, d);
@@ -281,8 +400,7 @@ __global__ __launch_bounds__(wg_threads(TPR), 2) void block_norm_backward_kernel
             for (int r = 0; r < 2 * R; ++r) s[r] = 0.f;
 #pragma unroll
             for (int c = 0; c < C; ++c) {
-                float w[E];
-                vector_or<T>(a.next_weight, 1.f, (c * TPR + t) * E, d, w);
+                const auto& w = nws[c];
 #pragma unroll
                 for (int r = 0; r < R; ++r) {
                     float n[E], o[E];
@@ -309,10 +427,7 @@ __global__ __launch_bounds__(wg_threads(TPR), 2) void block_norm_backward_kernel
 #pragma unroll
         for (int c = 0; c < C; ++c) {
             const int col = (c * TPR + t) * E, have = d - col;
-            float nw[E], w[E], gv[E];
-            vector_or<T>(a.next_weight, 1.f, col, d, nw);
-            vector_or<T>(a.weight, 1.f, col, d, w);
-            vector_or<T>(gate, 1.f, col, d, gv);
+            const auto &nw = nws[c], &gw = gws[c];
 #pragma unroll
             for (int r = 0; r < R; ++r) {
                 float n[E], o[E], xv[E], dr[E];
@@ -332,7 +447,7 @@ __global__ __launch_bounds__(wg_threads(TPR), 2) void block_norm_backward_kernel
                     if (e >= have) v = 0.f;
                     tv[r][c][e] = v;
                     dr[e] = a.scale * v;
-                    const float u = xv[e] - mean1[r], q = v * gv[e] * w[e];
+                    const float u = xv[e] - mean1[r], q = v * gw[e];
                     z[2 * r] += q;
                     z[2 * r + 1] = fmaf(q, u, z[2 * r + 1]);
                     sum[0][c][e] = fmaf(v, u * rstd1[r], sum[0][c][e]);
@@ -349,19 +464,17 @@ __global__ __launch_bounds__(wg_threads(TPR), 2) void block_norm_backward_kernel
 #pragma unroll
         for (int c = 0; c < C; ++c) {
             const int col = (c * TPR + t) * E, have = d - col;
-            float w[E], gv[E];
-            vector_or<T>(a.weight, 1.f, col, d, w);
-            vector_or<T>(gate, 1.f, col, d, gv);
+            const auto& gw = gws[c];
 #pragma unroll
             for (int r = 0; r < R; ++r) {
                 float xv[E], dx[E];
                 unpack16<T>(x[r][c], xv);
 #pragma unroll
                 for (int e = 0; e < E; ++e) {
-                    float q = tv[r][c][e] * gv[e];
+                    float q = tv[r][c][e] * gw[e];
                     if (a.after) {
                         const float h = (xv[e] - mean1[r]) * rstd1[r];
-                        q = q * w[e] - h * (z[2 * r + 1] * inv);
+                        q -= h * (z[2 * r + 1] * inv);
                         if (!a.rms) q -= z[2 * r] * inv;
                         q *= rstd1[r];
                     }
@@ -392,9 +505,14 @@ __global__ __launch_bounds__(wg_threads(TPR), 2) void block_norm_backward_kernel
 #pragma unroll
             for (int c = 0; c < C; ++c) {
                 const int col = (c * TPR + t) * E;
+                float* const at = to + k * a.d + col;
+                if (col + E <= d) {
+                    __builtin_memcpy(at, sum[k][c], sizeof sum[k][c]);
+                } else {
 #pragma unroll
-                for (int e = 0; e < E; ++e)
-                    if (col + e < d) to[k * a.d + col + e] = sum[k][c][e];
+                    for (int e = 0; e < E; ++e)
+                        if (col + e < d) at[e] = sum[k][c][e];
+                }
             }
         }
     }
@@ -402,29 +520,10 @@ __global__ __launch_bounds__(wg_threads(TPR), 2) void block_norm_backward_kernel
 
 // Rows that do not fit the registers, in three steps: the rows' sums into row_sums
 // [rows][4] (those of the norm before, then after); the sums over rows; dx and
-// dresidual, each element by the thread that reads its inputs.
+// dresidual, each piece by the thread that reads its inputs.
 struct WideRow {
     float mean1, rstd1, mean2, rstd2, s1, s2, z1, z2;
 };
-template <typename T>
-__device__ inline float wide_value(const void* v, int64_t i, float otherwise)
-{
-    return v ? (float)static_cast<const T*>(v)[i] : otherwise;
-}
-// t of an element; k: of its normed value
-template <typename T>
-__device__ inline float wide_t(const BlockNormBackwardArgs& a, const WideRow& w, int64_t r, int64_t c)
-{
-    float v = wide_value<T>(a.dout, r * a.lddo + c, 0.f);
-    if (a.dnormed) {
-        const float k = ((float)static_cast<const T*>(a.out)[r * a.ldo + c] - w.mean2) * w.rstd2;
-        float q = (float)static_cast<const T*>(a.dnormed)[r * a.lddn + c] * wide_value<T>(a.next_weight, c, 1.f) - k * w.s2;
-        if (!a.rms) q -= w.s1;
-        v = fmaf(w.rstd2, q, v);
-    }
-    return v;
-}
-template <typename T>
 __device__ inline WideRow wide_row(const BlockNormBackwardArgs& a, const float* row_sums, int64_t r)
 {
     WideRow w{0.f, 1.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
@@ -433,23 +532,65 @@ __device__ inline WideRow wide_row(const BlockNormBackwardArgs& a, const float* 
     if (row_sums) w.s1 = row_sums[4 * r], w.s2 = row_sums[4 * r + 1], w.z1 = row_sums[4 * r + 2], w.z2 = row_sums[4 * r + 3];
     return w;
 }
+template <typename T>
+__device__ inline void wide_rows(const void* m, int64_t ld, int64_t r, int64_t c, int64_t d, float (&v)[per16<T>])
+{
+    wide_vector<T>(m ? static_cast<const T*>(m) + r * ld : nullptr, 0.f, c, d, v);
+}
+// A piece of t (zero past the end); of dnormed into n and of out's normed values into k.
+template <typename T>
+__device__ inline void wide_t(const BlockNormBackwardArgs& a, const WideRow& w, int64_t r, int64_t c, float (&t)[per16<T>],
+                              float (&n)[per16<T>], float (&k)[per16<T>])
+{
+    wide_rows<T>(a.dout, a.lddo, r, c, a.d, t);
+    if (!a.dnormed) return;
+    float nw[per16<T>];
+    wide_rows<T>(a.dnormed, a.lddn, r, c, a.d, n);
+    wide_rows<T>(a.out, a.ldo, r, c, a.d, k);
+    wide_vector<T>(a.next_weight, 1.f, c, a.d, nw);
+#pragma unroll
+    for (int e = 0; e < per16<T>; ++e) {
+        k[e] = (k[e] - w.mean2) * w.rstd2;
+        float q = n[e] * nw[e] - k[e] * w.s2;
+        if (!a.rms) q -= w.s1;
+        t[e] = c + e < a.d ? fmaf(w.rstd2, q, t[e]) : 0.f;
+    }
+}
+// gate weight of a piece, without after the gate alone
+template <typename T>
+__device__ inline void wide_factor(const BlockNormBackwardArgs& a, const T* gate, int64_t c, float (&f)[per16<T>])
+{
+    float w[per16<T>];
+    wide_vector<T>(gate, 1.f, c, a.d, f);
+    wide_vector<T>(a.weight, 1.f, c, a.d, w);
+#pragma unroll
+    for (int e = 0; e < per16<T>; ++e) f[e] *= w[e];
+}
 
 template <typename T>
 __global__ __launch_bounds__(WIDE) void block_norm_wide_rows_kernel(BlockNormBackwardArgs a, int64_t rows_per_gate,
                                                                     float* to)
 {
+    constexpr int E = per16<T>;
     __shared__ float lds[2][2 * WIDE / 64];
     int turn = 0;
     const float inv = 1.0f / (float)a.d;
     for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
-        WideRow w = wide_row<T>(a, nullptr, r);
+        WideRow w = wide_row(a, nullptr, r);
         const T* const gate = a.gate ? gate_of<T>(a.gate, a.d, rows_per_gate, a.rows, r) : nullptr;
         if (a.dnormed) {
             float s[2] = {0.f, 0.f};
-            for (int64_t c = threadIdx.x; c < a.d; c += WIDE) {
-                const float q = (float)static_cast<const T*>(a.dnormed)[r * a.lddn + c] * wide_value<T>(a.next_weight, c, 1.f);
-                s[0] += q;
-                s[1] = fmaf(q, (float)static_cast<const T*>(a.out)[r * a.ldo + c] - w.mean2, s[1]);
+            for (int64_t c = threadIdx.x * (int64_t)E; c < a.d; c += WIDE * E) {
+                float n[E], o[E], nw[E];
+                wide_rows<T>(a.dnormed, a.lddn, r, c, a.d, n);
+                wide_rows<T>(a.out, a.ldo, r, c, a.d, o);
+                wide_vector<T>(a.next_weight, 1.f, c, a.d, nw);
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    const float q = n[e] * nw[e];
+                    s[0] += q;
+                    s[1] = fmaf(q, o[e] - w.mean2, s[1]);
+                }
             }
             s[1] *= w.rstd2;
             row_sums<WIDE, 2>(s, lds[turn ^= 1]);
@@ -457,10 +598,17 @@ __global__ __launch_bounds__(WIDE) void block_norm_wide_rows_kernel(BlockNormBac
         }
         if (a.after) {
             float s[2] = {0.f, 0.f};
-            for (int64_t c = threadIdx.x; c < a.d; c += WIDE) {
-                const float q = wide_t<T>(a, w, r, c) * wide_value<T>(gate, c, 1.f) * wide_value<T>(a.weight, c, 1.f);
-                s[0] += q;
-                s[1] = fmaf(q, (float)static_cast<const T*>(a.x)[r * a.ldx + c] - w.mean1, s[1]);
+            for (int64_t c = threadIdx.x * (int64_t)E; c < a.d; c += WIDE * E) {
+                float v[E], n[E], k[E], f[E], x[E];
+                wide_t<T>(a, w, r, c, v, n, k);
+                wide_factor<T>(a, gate, c, f);
+                wide_rows<T>(a.x, a.ldx, r, c, a.d, x);
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    const float q = v[e] * f[e];
+                    s[0] += q;
+                    s[1] = fmaf(q, x[e] - w.mean1, s[1]);
+                }
             }
             s[1] *= w.rstd1;
             row_sums<WIDE, 2>(s, lds[turn ^= 1]);
@@ -474,89 +622,121 @@ template <typename T>
 __global__ __launch_bounds__(256) void block_norm_wide_sums_kernel(BlockNormBackwardArgs a, Parts parts,
                                                                    const float* rows, float* sums, uint32_t blocks)
 {
+    constexpr int E = per16<T>;
     const uint32_t id = workgroup_id();
-    const int64_t part = id / blocks, c = (id - part * blocks) * 256ll + threadIdx.x;
+    const int64_t part = id / blocks, c = ((id - part * blocks) * 256ll + threadIdx.x) * E;
     if (part >= parts.gates * parts.per_gate || c >= a.d) return;
     const int64_t which = part / parts.per_gate, begin = which * parts.rows_per_gate + (part - which * parts.per_gate) * parts.chunk;
     const int64_t last = (which + 1) * parts.rows_per_gate;
     const int64_t end = begin + parts.chunk < last ? begin + parts.chunk : last;
-    float s[4] = {0.f, 0.f, 0.f, 0.f};
+    float s[4][E];
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+        for (int e = 0; e < E; ++e) s[k][e] = 0.f;
+#pragma unroll 2
     for (int64_t r = begin; r < end; ++r) {
-        const WideRow w = wide_row<T>(a, rows, r);
-        const float t = wide_t<T>(a, w, r, c);
-        s[0] = fmaf(t, (wide_value<T>(a.x, r * a.ldx + c, 0.f) - w.mean1) * w.rstd1, s[0]);
-        s[1] += t;
-        if (a.dnormed) {
-            const float n = (float)static_cast<const T*>(a.dnormed)[r * a.lddn + c];
-            s[2] = fmaf(n, ((float)static_cast<const T*>(a.out)[r * a.ldo + c] - w.mean2) * w.rstd2, s[2]);
-            s[3] += n;
+        const WideRow w = wide_row(a, rows, r);
+        float t[E], n[E], k[E], x[E];
+        wide_t<T>(a, w, r, c, t, n, k);
+        wide_rows<T>(a.x, a.ldx, r, c, a.d, x);
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            s[0][e] = fmaf(t[e], (x[e] - w.mean1) * w.rstd1, s[0][e]);
+            s[1][e] += t[e];
+            if (a.dnormed) {
+                s[2][e] = fmaf(n[e], k[e], s[2][e]);
+                s[3][e] += n[e];
+            }
         }
     }
 #pragma unroll
-    for (int k = 0; k < 4; ++k) sums[(4 * part + k) * a.d + c] = s[k];
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            if (c + e < a.d) sums[(4 * part + k) * a.d + c + e] = s[k][e];
 }
 
 template <typename T>
 __global__ __launch_bounds__(256) void block_norm_wide_dx_kernel(BlockNormBackwardArgs a, int64_t rows_per_gate,
                                                                  const float* rows, uint32_t blocks)
 {
+    constexpr int E = per16<T>;
     const uint32_t id = workgroup_id();
-    const int64_t r = id / blocks, c = (id - r * blocks) * 256ll + threadIdx.x;
+    const int64_t r = id / blocks, c = ((id - r * blocks) * 256ll + threadIdx.x) * E;
     if (r >= a.rows || c >= a.d) return;
-    const WideRow w = wide_row<T>(a, rows, r);
-    const float t = wide_t<T>(a, w, r, c);
-    float q = t * (a.gate ? (float)gate_of<T>(a.gate, a.d, rows_per_gate, a.rows, r)[c] : 1.f);
-    if (a.after) {
-        const float h = ((float)static_cast<const T*>(a.x)[r * a.ldx + c] - w.mean1) * w.rstd1;
-        q = q * wide_value<T>(a.weight, c, 1.f) - h * w.z2;
-        if (!a.rms) q -= w.z1;
-        q *= w.rstd1;
+    const int have = a.d - c < E ? (int)(a.d - c) : E;
+    const WideRow w = wide_row(a, rows, r);
+    const T* const gate = a.gate ? gate_of<T>(a.gate, a.d, rows_per_gate, a.rows, r) : nullptr;
+    float t[E], n[E], k[E], x[E], f[E];
+    wide_t<T>(a, w, r, c, t, n, k);
+    wide_rows<T>(a.x, a.ldx, r, c, a.d, x);
+    wide_factor<T>(a, gate, c, f);
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+        float q = t[e] * f[e];
+        if (a.after) {
+            q -= (x[e] - w.mean1) * w.rstd1 * w.z2;
+            if (!a.rms) q -= w.z1;
+            q *= w.rstd1;
+        }
+        x[e] = q;
+        t[e] *= a.scale;
     }
-    static_cast<T*>(a.dresidual)[r * a.lddr + c] = (T)(a.scale * t);
-    static_cast<T*>(a.dx)[r * a.lddx + c] = (T)q;
+    store16(static_cast<T*>(a.dresidual) + r * a.lddr + c, t, have);
+    store16(static_cast<T*>(a.dx) + r * a.lddx + c, x, have);
 }
 
-// Joins a gate's parts in a fixed order: 64 columns per workgroup, every fourth part
-// per wave.  Writes dgate, and the sums that the gates still have to be joined of,
-// gate A, gate B, C and D, to `each` [gates][4][d]; with one gate those are the
-// results.
+// One value of a vector [d], or what there is without one.
 template <typename T>
-__global__ __launch_bounds__(256) void block_norm_gate_kernel(BlockNormBackwardArgs a, Parts parts, const float* sums,
-                                                              float* each, uint32_t blocks)
+__device__ inline float wide_value(const void* v, int64_t i, float otherwise)
 {
-    __shared__ float s[4][4][64];
+    return v ? (float)static_cast<const T*>(v)[i] : otherwise;
+}
+
+// Joins a gate's parts in a fixed order: 16 columns per workgroup, whose threads are
+// [subset][sum][column], every SUBSETS-th part per subset.  Writes dgate, and the sums
+// that the gates still have to be joined of, gate A, gate B, C and D, to `each`
+// [gates][4][d]; with one gate those are the results.
+template <typename T, int SUBSETS>
+__global__ __launch_bounds__(64 * SUBSETS) void block_norm_gate_kernel(BlockNormBackwardArgs a, Parts parts,
+                                                                       const float* sums, float* each, uint32_t blocks)
+{
+    __shared__ float s[SUBSETS][4][16];
     const uint32_t id = workgroup_id();
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t which = id / blocks, c = (id - which * blocks) * 64ll + lane;
-    if (which >= parts.gates) return;
-    float v[4] = {0.f, 0.f, 0.f, 0.f};
-    if (c < a.d)
-        for (int64_t i = wave; i < parts.per_gate; i += 4)
-#pragma unroll
-            for (int k = 0; k < 4; ++k) v[k] += sums[(4 * (which * parts.per_gate + i) + k) * a.d + c];
-#pragma unroll
-    for (int k = 0; k < 4; ++k) s[wave][k][lane] = v[k];
+    const int lane = threadIdx.x & 15, k = threadIdx.x >> 4 & 3, subset = threadIdx.x >> 6;
+    const int64_t which = id / blocks, c = (id - which * blocks) * 16ll + lane;
+    float v = 0.f;
+    if (which < parts.gates && c < a.d) {
+        const float* const from = sums + 4 * which * parts.per_gate * a.d + k * a.d + c;
+#pragma unroll 8
+        for (int64_t i = subset; i < parts.per_gate; i += SUBSETS) v += from[4 * i * a.d];
+    }
+    s[subset][k][lane] = v;
     __syncthreads();
-    if (wave || c >= a.d) return;
+    if (which >= parts.gates || threadIdx.x >= 16 || c >= a.d) return;
+    float w[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int k = 0; k < 4; ++k) v[k] = s[0][k][lane] + s[1][k][lane] + s[2][k][lane] + s[3][k][lane];
+    for (int i = 0; i < SUBSETS; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[j] += s[i][j][lane];
     if (a.dgate) {
-        float g = v[0];
-        if (a.after) g = fmaf(g, wide_value<T>(a.weight, c, 1.f), wide_value<T>(a.bias, c, 0.f) * v[1]);
+        float g = w[0];
+        if (a.after) g = fmaf(g, wide_value<T>(a.weight, c, 1.f), wide_value<T>(a.bias, c, 0.f) * w[1]);
         static_cast<T*>(a.dgate)[which * a.d + c] = (T)g;
     }
     const float gate = wide_value<T>(a.gate, which * a.d + c, 1.f);
-    v[0] *= gate;
-    v[1] *= gate;
+    w[0] *= gate;
+    w[1] *= gate;
     if (each) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) each[(4 * which + k) * a.d + c] = v[k];
+        for (int j = 0; j < 4; ++j) each[(4 * which + j) * a.d + c] = w[j];
         return;
     }
     void* const to[4] = {a.dweight, a.dbias, a.dnext_weight, a.dnext_bias};
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
-        if (to[k]) static_cast<T*>(to[k])[c] = (T)v[k];
+    for (int j = 0; j < 4; ++j)
+        if (to[j]) static_cast<T*>(to[j])[c] = (T)w[j];
 }
 
 // Joins the gates' sums in a fixed order: 64 of the 4 d columns per workgroup, every
@@ -582,6 +762,23 @@ __global__ __launch_bounds__(1024) void block_norm_join_kernel(BlockNormBackward
     if (to) static_cast<T*>(to)[c - k * a.d] = (T)v;
 }
 
+// How a row is spread, as with_spread: eight elements in a thread, which has four sums
+// of each in the gradient, and between its two norms what registers hold of R rows.
+template <bool BACKWARD, typename F>
+bool with_block_spread(int64_t d, F&& f)
+{
+    constexpr int R = BACKWARD ? 2 : 4;
+    if (d <= 16 * 8) f.template operator()<16, 8, R>();
+    else if (d <= 32 * 8) f.template operator()<32, 8, R>();
+    else if (d <= 64 * 8) f.template operator()<64, 8, R>();
+    else if (d <= 128 * 8) f.template operator()<128, 8, R>();
+    else if (d <= 256 * 8) f.template operator()<256, 8, R>();
+    else if (d <= 512 * 8) f.template operator()<512, 8, 2>();
+    else if (d <= 1024 * 8) f.template operator()<1024, 8, 1>();
+    else return false;
+    return true;
+}
+
 template <typename T>
 struct Forward {
     const BlockNormArgs& a;
@@ -591,7 +788,7 @@ struct Forward {
     void operator()()
     {
         // few rows: one each, for every compute unit has one
-        const int64_t cus = std::max(device_cus(), 1), groups = wg_threads(TPR) / TPR;
+        const int64_t cus = std::max(device_cus(), 1), groups = block_threads(TPR) / TPR;
         if (a.rows <= cus * groups * R)
             launch<TPR, EL, 1>();
         else
@@ -600,35 +797,36 @@ struct Forward {
     template <int TPR, int EL, int R>
     void launch()
     {
-        constexpr int per_pass = wg_threads(TPR) / TPR * R;
+        constexpr int per_pass = block_threads(TPR) / TPR * R;
         const int64_t blocks = std::min<int64_t>(ceil_div(a.rows, per_pass), 1 << 20);
         if (debug_enabled())
             fprintf(stderr, "cliffconv: block_norm %lld x %lld, %d threads per row, %lld workgroups\n",
                     (long long)a.rows, (long long)a.d, TPR, (long long)blocks);
-        hipLaunchKernelGGL((block_norm_kernel<T, TPR, EL, R>), dim3((unsigned)blocks), dim3(wg_threads(TPR)), 0,
+        hipLaunchKernelGGL((block_norm_kernel<T, TPR, EL, R>), dim3((unsigned)blocks), dim3(block_threads(TPR)), 0,
                            stream, a, rows_per_gate);
     }
 };
 
-// How the gradient's rows are cut: each part writes 4 d sums, so no more of them
-// than keep the memory busy; 16 elements of a row in a thread, and so one row.
+// How the gradient's rows are cut: each part writes 4 d sums, so no more of them than
+// keep the memory busy.
 struct BackwardParts {
     template <int TPR, int EL, int R>
     void operator()()
     {
-        rows_per_pass = wg_threads(TPR) / TPR * std::max(1, R / 2);
+        rows_per_pass = block_threads(TPR) / TPR * R;
+        per_cu = std::max(1, 512 / block_threads(TPR));
     }
-    int64_t rows_per_pass = 16;
+    int64_t rows_per_pass = 16, per_cu = 2;
 };
 Parts cut(int64_t rows, int64_t d, int64_t gates)
 {
     Parts p;
     BackwardParts b;
-    const bool fits = with_spread<true>(d, b);
+    const bool fits = with_block_spread<true>(d, b);
     const int64_t cus = std::max(device_cus(), 1);
     p.gates = std::max<int64_t>(gates, 1);
     p.rows_per_gate = rows / p.gates;
-    const int64_t want = fits ? 2 * cus : std::max<int64_t>(1, ceil_div(2048, ceil_div(d, 256)));
+    const int64_t want = fits ? b.per_cu * cus : std::max<int64_t>(1, ceil_div(8 * cus, ceil_div(d, 1024)));
     p.per_gate = std::max<int64_t>(1, std::min(ceil_div(p.rows_per_gate, b.rows_per_pass), ceil_div(want, p.gates)));
     p.chunk = ceil_div(ceil_div(p.rows_per_gate, p.per_gate), b.rows_per_pass) * b.rows_per_pass;
     p.per_gate = std::max<int64_t>(1, p.chunk ? ceil_div(p.rows_per_gate, p.chunk) : 1);
@@ -647,8 +845,8 @@ struct Backward {
         if (debug_enabled())
             fprintf(stderr, "cliffconv: block_norm_backward %lld x %lld, %d threads per row, %lld workgroups\n",
                     (long long)a.rows, (long long)a.d, TPR, (long long)parts.all());
-        constexpr int RB = R / 2 > 1 ? R / 2 : 1;
-        hipLaunchKernelGGL((block_norm_backward_kernel<T, TPR, EL, RB>), grid_of(parts.all()), dim3(wg_threads(TPR)),
+        constexpr int ROWS = sizeof(T) == 4 ? 1 : R;  // what the registers hold
+        hipLaunchKernelGGL((block_norm_backward_kernel<T, TPR, EL, ROWS>), grid_of(parts.all()), dim3(block_threads(TPR)),
                            0, stream, a, parts, sums);
     }
 };
@@ -664,7 +862,7 @@ Space space(const Parts& p, int64_t rows, int64_t d)
     BackwardParts b;
     s.each = ceil_div(p.all() * 16 * d, 256) * 256;
     s.rows = s.each + (p.gates > 1 ? ceil_div(p.gates * 16 * d, 256) * 256 : 0);
-    s.all = s.rows + (with_spread<true>(d, b) ? 0 : 16 * rows);
+    s.all = s.rows + (with_block_spread<true>(d, b) ? 0 : 16 * rows);
     return s;
 }
 
@@ -676,7 +874,7 @@ cliff_status launch_block_norm(int dtype, const BlockNormArgs& a, hipStream_t st
     return with_type(dtype, [&](auto t) {
         using T = decltype(t);
         const int64_t rows_per_gate = a.gate ? a.rows / a.gates : a.rows;
-        if (!with_spread<false>(a.d, Forward<T>{a, rows_per_gate, stream}))
+        if (!with_block_spread<false>(a.d, Forward<T>{a, rows_per_gate, stream}))
             hipLaunchKernelGGL(block_norm_wide_kernel<T>, dim3((unsigned)std::min<int64_t>(a.rows, 1 << 20)), dim3(WIDE),
                                0, stream, a, rows_per_gate);
         return launched();
@@ -699,10 +897,10 @@ cliff_status launch_block_norm_backward(int dtype, const BlockNormBackwardArgs& 
         float* const sums = reinterpret_cast<float*>(ws);
         float* const rows = reinterpret_cast<float*>(ws + s.rows);
         const bool params = a.dgate || a.dweight || a.dbias || a.dnext_weight || a.dnext_bias;
-        const int64_t blocks = ceil_div(a.d, 256), cols = ceil_div(a.d, 64);
-        // (rows of the grid are 16 bits; matrices of 2^37 elements and more)
+        const int64_t blocks = ceil_div(a.d, 256 * per16<T>), cols = ceil_div(a.d, 16);
+        // (rows of the grid are 16 bits; matrices of 2^36 elements and more)
         if (std::max(cols * parts.all(), a.d > 8192 ? blocks * a.rows : 0) > GRID_ROW * 0xffff) return CLIFF_EUNSUPPORTED;
-        if (a.rows && !with_spread<true>(a.d, Backward<T>{a, parts, params ? sums : nullptr, stream})) {
+        if (a.rows && !with_block_spread<true>(a.d, Backward<T>{a, parts, params ? sums : nullptr, stream})) {
             hipLaunchKernelGGL(block_norm_wide_rows_kernel<T>, dim3((unsigned)std::min<int64_t>(a.rows, 1 << 20)),
                                dim3(WIDE), 0, stream, a, parts.rows_per_gate, rows);
             if (params)
@@ -715,8 +913,12 @@ cliff_status launch_block_norm_backward(int dtype, const BlockNormBackwardArgs& 
             float* const each = parts.gates > 1 ? reinterpret_cast<float*>(ws + s.each) : nullptr;
             Parts join = parts;
             if (!a.rows) join.per_gate = 0;
-            hipLaunchKernelGGL(block_norm_gate_kernel<T>, grid_of(cols * parts.gates), dim3(256), 0, stream, a, join,
-                               sums, each, (uint32_t)cols);
+            if (parts.per_gate >= 16)
+                hipLaunchKernelGGL((block_norm_gate_kernel<T, 16>), grid_of(cols * parts.gates), dim3(1024), 0, stream, a,
+                                   join, sums, each, (uint32_t)cols);
+            else
+                hipLaunchKernelGGL((block_norm_gate_kernel<T, 1>), grid_of(cols * parts.gates), dim3(64), 0, stream, a,
+                                   join, sums, each, (uint32_t)cols);
             if (each && (a.dweight || a.dbias || a.dnext_weight || a.dnext_bias))
                 hipLaunchKernelGGL(block_norm_join_kernel<T>, grid_of(ceil_div(4 * a.d, 64)), dim3(1024), 0, stream, a,
                                    each, parts.gates);

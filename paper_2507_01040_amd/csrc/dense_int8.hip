@@ -159,24 +159,20 @@ __device__ inline void write_tile(const Int8Args& p, const TileId& id, int64_t m
     }
 }
 
-// BM x BN outputs per workgroup of WR x WC waves, stages of KT contraction values in
+// BM x BN outputs per workgroup of WR x WC waves, stages of 64 contraction values in
 // LDS slots of 16 (dense_geom.hpp counts them as 8 of 16 bits).  Rows that are 16-byte
-// aligned and whole slots: stages go from memory straight to LDS, one ahead in the
-// other of two buffers; the loads of a stage are spread over the products of two
-// groups, and the first fragments of the next stage are read under the last
-// products of this one, as in the product of 16-bit types (dense.hip).
-//
-// Bound by the matrix cores and LDS together, as there: a 32 x 32 x 32 product of
-// 8-bit integers takes the cycles of a 32 x 32 x 16 one of 16 bits, and its fragments
-// are as large.
-constexpr int KT = 128;
+// aligned and whole slots: stages go from memory straight to LDS, three ahead in a
+// ring of four buffers, so that the wait for a stage is for loads that were issued
+// two stages before; it stands, with the barrier, between the two groups of products
+// of a stage, and the first fragments of the next stage are read under the second.
+constexpr int RING = 4, KT = 64;
 template <typename T, int BM, int BN, int WR, int WC>
 __global__ __launch_bounds__(64 * WR * WC) void int8_direct_kernel(Int8Args p)
 {
     constexpr int NT = 64 * WR * WC, WM = BM / WR, WN = BN / WC, MI = WM / 32, NI = WN / 32;
     constexpr Stage SA{BM, KT / 2, true}, SB{BN, KT / 2, true};
-    constexpr int LA = SA.slots() / NT, LB = SB.slots() / NT, PA = SA.bytes(), BUF = PA + SB.bytes(), KK = KT / 32;
-    static_assert(WN == 64 && KK % 2 == 0 && LA == LB && LA % MI == 0, "shape");
+    constexpr int LA = SA.slots() / NT, LB = SB.slots() / NT, L = LA + LB, PA = SA.bytes(), BUF = PA + SB.bytes();
+    static_assert(WN == 64 && KT == 64 && L % MI == 0, "shape");
     extern __shared__ u4 smem4[];
     char* const smem = reinterpret_cast<char*>(smem4);
     const int tid = threadIdx.x, lane = tid & 63;
@@ -206,22 +202,29 @@ __global__ __launch_bounds__(64 * WR * WC) void int8_direct_kernel(Int8Args p)
     };
     // byte offsets of a thread's slots from a stage's start; rows that do not exist are
     // zeros
-    uint32_t offa[LA], offb[LB];
+    uint32_t off[L];
 #pragma unroll
     for (int i = 0; i < LA; ++i) {
-        const int e = i * NT + tid, ra = SA.slot_row(e), rb = SB.slot_row(e);
-        offa[i] = m0 + ra < p.M ? (uint32_t)(ra * p.lda + 2 * SA.slot_k(e)) : NOWHERE;
-        offb[i] = n0 + rb < p.N ? (uint32_t)(rb * p.ldb + 2 * SB.slot_k(e)) : NOWHERE;
+        const int e = i * NT + tid, r = SA.slot_row(e);
+        off[i] = m0 + r < p.M ? (uint32_t)(r * p.lda + 2 * SA.slot_k(e)) : NOWHERE;
     }
-    auto load = [&](const int8_t* x, const Stage& S, uint32_t off, int i, int s, char* to) {
-        if (kn - s * KT < KT && 2 * S.slot_k(i * NT + tid) >= kn - s * KT) off = NOWHERE;
-        load_to_lds(x + (int64_t)s * KT, off, to + wave * 1024 + i * NT * 16);
+#pragma unroll
+    for (int i = 0; i < LB; ++i) {
+        const int e = i * NT + tid, r = SB.slot_row(e);
+        off[LA + i] = n0 + r < p.N ? (uint32_t)(r * p.ldb + 2 * SB.slot_k(e)) : NOWHERE;
+    }
+    // Load i of stage s; of stages past the last one, zeros (as many loads are under way
+    // in every step).
+    auto load = [&](int s, int i) {
+        const int l = i < LA ? i : i - LA, left = kn - s * KT;
+        const Stage& S = i < LA ? SA : SB;
+        const uint32_t o = left < KT && 2 * S.slot_k(l * NT + tid) >= left ? NOWHERE : off[i];
+        load_to_lds((i < LA ? a : b) + (int64_t)s * KT, o,
+                    smem + s % RING * BUF + (i < LA ? 0 : PA) + wave * 1024 + l * NT * 16);
     };
-    auto load_a = [&](int s, int i) { load(a, SA, offa[i], i, s, smem + (s & 1) * BUF); };
-    auto load_b = [&](int s, int i) { load(b, SB, offb[i], i, s, smem + (s & 1) * BUF + PA); };
     // Products of a group of 32 values, with the reads of the next one's fragments
-    // (next: its buffer) and half of the loads of a stage.  The output's columns are
-    // the matrix instruction's rows: a lane's groups of four sums are neighbours.
+    // (next: its buffer).  The output's columns are the matrix instruction's rows: a
+    // lane's groups of four sums are neighbours.
     auto group = [&](int set, const char* next, int kk, auto loads) {
         constexpr int F = MI + NI;
 #pragma unroll
@@ -231,58 +234,46 @@ __global__ __launch_bounds__(64 * WR * WC) void int8_direct_kernel(Int8Args p)
 #pragma unroll
             for (int j = 0; j < NI; ++j) acc[i][j] = mma(fb[set][j], fa[set][i], acc[i][j]);
 #pragma unroll
-            for (int l = i * LA / MI; l < (i + 1) * LA / MI; ++l) loads(l);
+            for (int l = i * L / MI; l < (i + 1) * L / MI; ++l) loads(l);
             __builtin_amdgcn_sched_barrier(0);
         }
     };
-    auto nothing = [](int) {};
 #pragma unroll
-    for (int i = 0; i < LA; ++i) load_a(0, i);
+    for (int s = 0; s < RING - 1; ++s)
 #pragma unroll
-    for (int i = 0; i < LB; ++i) load_b(0, i);
-    wait_direct();
+        for (int i = 0; i < L; ++i) load(s, i);
+    wait_direct_but<2 * L>();
     __syncthreads();
-    if (steps > 1)
-#pragma unroll
-        for (int i = 0; i < LA; ++i) load_a(1, i);
 #pragma unroll
     for (int f = 0; f < MI + NI; ++f) read_one(0, smem, 0, f);
-    // Step s; whether there are one and two more.
-    auto step = [&](int s, auto one, auto two) {
-        const char* const buf = smem + (s & 1) * BUF;
-        group(0, buf, 1, [&](int i) {
-            if constexpr (one) load_b(s + 1, i);
-        });
-#pragma unroll
-        for (int kk = 1; kk + 1 < KK; ++kk) group(kk & 1, buf, kk + 1, nothing);
-        wait_direct();
-        __syncthreads();
+    for (int s = 0; s < steps; ++s) {
+        group(0, smem + s % RING * BUF, 1, [](int) {});
+        wait_direct_but<L>();
+        // Every wave has the fragments of stage s - 1, whose buffer the loads now take:
+        // its products with them stand before the barrier.
+        barrier_alone();
+        __builtin_amdgcn_sched_barrier(0);
         // (the last step reads what no product uses)
-        group(1, smem + ((s + 1) & 1) * BUF, 0, [&](int i) {
-            if constexpr (two) load_a(s + 2, i);
-        });
-    };
-    constexpr std::true_type yes;
-    constexpr std::false_type no;
-    int s = 0;
-    for (; s + 2 < steps; ++s) step(s, yes, yes);
-    if (s + 1 < steps) step(s++, yes, no);
-    step(s, no, no);
+        group(1, smem + (s + 1) % RING * BUF, 0, [&](int i) { load(s + RING - 1, i); });
+    }
+    wait_direct();
     write_tile<T, MI, NI>(p, id, m0 + wm, n0 + wn, acc, smem, lane, wave);
 }
 
-// The same for rows of any alignment and width: slots go through registers, one stage
-// ahead.
-template <typename T>
-__global__ __launch_bounds__(256) void int8_staged_kernel(Int8Args p)
+// The same for rows of any alignment and width: stages of 128 values, whose slots go
+// through registers, one stage ahead.
+constexpr int KT_STAGED = 128;
+template <typename T, int TILE, int WR, int WC>
+__global__ __launch_bounds__(64 * WR * WC) void int8_staged_kernel(Int8Args p)
 {
-    constexpr int TILE = 128, NT = 256, MI = 2, NI = 2;
+    constexpr int KT = KT_STAGED, NT = 64 * WR * WC, WM = TILE / WR, WN = TILE / WC, MI = WM / 32, NI = WN / 32;
     constexpr Stage S{TILE, KT / 2, true};
-    constexpr int L = S.slots() / NT, KK = KT / 32;
-    __shared__ __align__(16) char smem[2 * S.bytes() > 4 * 32 * EW * 4 ? 2 * S.bytes() : 4 * 32 * EW * 4];
+    constexpr int L = S.slots() / NT, KK = KT / 32, EPILOGUE = WR * WC * 32 * EW * 4;
+    static_assert(WN == 64, "shape");
+    __shared__ __align__(16) char smem[2 * S.bytes() > EPILOGUE ? 2 * S.bytes() : EPILOGUE];
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int wm = wave / 2 * 64, wn = wave % 2 * 64;
+    const int wm = wave / WC * WM, wn = wave % WC * WN;
     const uint32_t tm = (uint32_t)((p.M + TILE - 1) / TILE), tn = (uint32_t)((p.N + TILE - 1) / TILE);
     if (blockIdx.y && workgroup_id() >= tm * tn * p.splits) return;
     const TileId id = tile_of(workgroup_id(), tm, tn, p.splits);
@@ -382,7 +373,7 @@ __global__ __launch_bounds__(512, 2) void int8_rows_kernel(Int8Args p)
     __shared__ __align__(16) char smem[8 * (PLANE * 4 > OWN ? PLANE * 4 : OWN)];
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const RowsPart<KT> part(p.N, p.K, 16, wave);
+    const RowsPart<128> part(p.N, p.K, 16, wave);
     const int8_t* const b = p.b + part.n0 * p.ldb;
     i4 acc[MB];
 #pragma unroll
@@ -439,29 +430,30 @@ __global__ __launch_bounds__(512, 2) void int8_rows_kernel(Int8Args p)
     finish_rows<T, 1>(p, r, 1, n, v, ends);
 }
 
-// How a product is cut: tiles of 256 x 256 or 128 x 128, and parts of the
-// contraction, by the times in ns of a stage with one workgroup on each compute unit
-// and with as many as fit, and of a workgroup's begin and end.
+// How a product is cut: square tiles, and parts of the contraction, by the times in ns
+// of 128 values with one workgroup on each compute unit and with as many as fit, and
+// of a workgroup's begin and end.
 struct Cut {
-    bool large;
-    int splits;
+    int tile, splits;
     int64_t k_part;
     double ns;  // what it is expected to take
 };
 struct TileTimes {
-    int B, fit;
+    int tile, fit;
     double alone, full, ends;
 };
-constexpr TileTimes T_DIRECT256{256, 1, 1300, 1300, 10000}, T_DIRECT128{128, 2, 600, 1150, 5800},
-    T_STAGED128{128, 2, 1100, 1550, 6300};
+// Fitted to measured times (MI355X; 44 products of 65 to 65536 rows with 1 to 32 parts
+// each, aligned and not; 15 % off on average; the cuts that they choose take 1.4 %
+// longer than the best ones, 16 % at worst).
+constexpr TileTimes T_DIRECT[] = {{256, 1, 990, 990, 11000}, {128, 3, 360, 1460, 8300}, {64, 2, 270, 410, 3200}},
+                    T_STAGED[] = {{128, 2, 740, 740, 10500}, {64, 2, 960, 1000, 1800}};
 
 Cut cut(int64_t M, int64_t N, int64_t K, bool direct)
 {
-    const int64_t cus = std::max(device_cus(), 1);
-    Cut best{false, 1, 0, 0};
-    for (int large = 0; large <= (direct ? 1 : 0); ++large) {
-        const TileTimes& t = large ? T_DIRECT256 : direct ? T_DIRECT128 : T_STAGED128;
-        const int64_t tiles = ceil_div(M, t.B) * ceil_div(N, t.B), steps = ceil_div(K, KT);
+    const int64_t cus = std::max(device_cus(), 1), steps = ceil_div(K, 128);
+    Cut best{0, 1, 0, 0};
+    const auto weigh = [&](const TileTimes& t) {
+        const int64_t tiles = ceil_div(M, t.tile) * ceil_div(N, t.tile);
         for (const int want : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
             if (want > steps) break;
             const int64_t per = ceil_div(steps, want), splits = ceil_div(steps, per);
@@ -469,10 +461,14 @@ Cut cut(int64_t M, int64_t N, int64_t K, bool direct)
             double ns = rounds * (per * t.full + t.ends);
             if (rest) ns += per * (rest <= cus ? t.alone : t.full) + t.ends;
             // the join: a launch, and the partial sums written and read
-            if (splits > 1) ns += 4400 + (double)M * N * 4 * 2 * splits / 11700;
-            if (best.ns == 0 || ns < best.ns) best = Cut{large != 0, (int)splits, per * KT, ns};
+            if (splits > 1) ns += 2800 + (double)M * N * 4 * 2 * splits / 7400;
+            if (best.ns == 0 || ns < best.ns) best = Cut{t.tile, (int)splits, per * 128, ns};
         }
-    }
+    };
+    if (direct)
+        for (const TileTimes& t : T_DIRECT) weigh(t);
+    else
+        for (const TileTimes& t : T_STAGED) weigh(t);
     return best;
 }
 
@@ -517,17 +513,18 @@ cliff_status int8_product(Int8Args p, hipStream_t stream)
     }
     p.splits = c.splits;
     p.k_part = c.k_part;
-    const int B = c.large ? 256 : 128;
-    const int64_t wgs = ceil_div(p.M, B) * ceil_div(p.N, B) * p.splits;
+    const int64_t wgs = ceil_div(p.M, c.tile) * ceil_div(p.N, c.tile) * p.splits;
     if (wgs >= (int64_t)1 << 31) return CLIFF_EUNSUPPORTED;
-    say(c.large ? "direct tiles of 256" : direct ? "direct tiles of 128" : "staged tiles of 128", wgs);
-    // LDS: two buffers of a stage, or what write_tile takes
-    if (c.large)
-        hipLaunchKernelGGL((int8_direct_kernel<T, 256, 256, 2, 4>), grid_of(wgs), dim3(512), 2 * 2 * 256 * KT, stream, p);
-    else if (direct)
-        hipLaunchKernelGGL((int8_direct_kernel<T, 128, 128, 2, 2>), grid_of(wgs), dim3(256), 2 * 2 * 128 * KT, stream, p);
-    else
-        hipLaunchKernelGGL(int8_staged_kernel<T>, grid_of(wgs), dim3(256), 0, stream, p);
+    char name[40];
+    snprintf(name, sizeof name, "%s tiles of %d", direct ? "direct" : "staged", c.tile);
+    say(name, wgs);
+    // LDS: the ring of stages, or what write_tile takes
+    const auto go = [&](auto k, int threads, int lds) { hipLaunchKernelGGL(k, grid_of(wgs), dim3(threads), lds, stream, p); };
+    if (direct && c.tile == 256) go(int8_direct_kernel<T, 256, 256, 2, 4>, 512, RING * 2 * 256 * KT);
+    else if (direct && c.tile == 128) go(int8_direct_kernel<T, 128, 128, 2, 2>, 256, RING * 2 * 128 * KT);
+    else if (direct) go(int8_direct_kernel<T, 64, 64, 2, 1>, 128, RING * 2 * 64 * KT);
+    else if (c.tile == 128) go(int8_staged_kernel<T, 128, 2, 2>, 256, 0);
+    else go(int8_staged_kernel<T, 64, 2, 1>, 128, 0);
     const cliff_status s = launched();
     if (s != CLIFF_OK || p.splits == 1) return s;
     const int64_t blocks = ceil_div(p.M * ceil_div(p.N, 4), 256);

@@ -28,4 +28,16 @@ __device__ inline void load_to_lds(const void* from, uint32_t offset, char* to)
 // Until this wave's loads have arrived (vmcnt 0).
 __device__ inline void wait_direct() { __builtin_amdgcn_s_waitcnt(0x0f70); }
 
+// Until all but the last N of them have (N < 16).
+template <int N>
+__device__ inline void wait_direct_but()
+{
+    __builtin_amdgcn_s_waitcnt(0x0f70 | N);
+    __asm__ volatile("" ::: "memory");
+}
+
+// A barrier that waits for nothing but the other waves: reads of LDS that are under
+// way stay so.
+__device__ inline void barrier_alone() { __asm__ volatile("s_barrier" ::: "memory"); }
+
 }  // namespace cliff

@@ -96,16 +96,18 @@ __device__ inline float dpp(float v)
 template <int N>
 __device__ inline float lane_sum(float v)
 {
-    static_assert(N == 16 || N == 64, "lanes");
+    static_assert(N == 16 || N == 32 || N == 64, "lanes");
     v += dpp<0xb1>(v);   // neighbours
     v += dpp<0x4e>(v);   // pairs
     v += dpp<0x141>(v);  // halves of 8, mirrored
     v += dpp<0x140>(v);  // halves of 16, mirrored
-    if constexpr (N == 64) {
+    if constexpr (N > 16) {
         const uint32_t a = __builtin_bit_cast(uint32_t, v);
         const auto s = __builtin_amdgcn_permlane16_swap(a, a, false, false);
         const uint32_t s0 = s[0], s1 = s[1];
         v = __builtin_bit_cast(float, s0) + __builtin_bit_cast(float, s1);
+    }
+    if constexpr (N > 32) {
         const uint32_t b = __builtin_bit_cast(uint32_t, v);
         const auto t = __builtin_amdgcn_permlane32_swap(b, b, false, false);
         const uint32_t t0 = t[0], t1 = t[1];
@@ -114,14 +116,14 @@ __device__ inline float lane_sum(float v)
     return v;
 }
 
-// The sums of v[0..R) over the TPR threads of a row, in every one of them: 16
+// The sums of v[0..R) over the TPR threads of a row, in every one of them: 16, 32
 // or 64 lanes, or the whole workgroup of TPR threads (then through `lds`, R
 // floats a wave, with one barrier; the caller alternates two of them).
 template <int TPR, int R>
 __device__ inline void row_sums(float (&v)[R], float* lds)
 {
 #pragma unroll
-    for (int r = 0; r < R; ++r) v[r] = lane_sum<(TPR < 64 ? 16 : 64)>(v[r]);
+    for (int r = 0; r < R; ++r) v[r] = lane_sum<(TPR < 64 ? TPR : 64)>(v[r]);
     if constexpr (TPR > 64) {
         constexpr int W = TPR / 64;
         if ((threadIdx.x & 63) == 0)

@@ -7,6 +7,17 @@
 #include "main.cpp"
 #undef main
 
+namespace emulate {
+// until only a thread's last n loads are under way
+void wait_loads_but(int n)
+{
+    auto& loads = under_way[now];
+    const size_t done = loads.size() > (size_t)n ? loads.size() - n : 0;
+    for (size_t i = 0; i < done; ++i) land(loads[i].first.data(), loads[i].second);
+    loads.erase(loads.begin(), loads.begin() + done);
+}
+}  // namespace emulate
+
 namespace {
 
 const Type I8{-1, 1, 0, 0};

@@ -7,6 +7,8 @@
 
 namespace emulate {
 
+void wait_loads_but(int n);
+
 enum { MFMA_I8 = TR16 + 1 };
 
 template <int S, typename V, typename Acc>
