@@ -99,35 +99,61 @@ __device__ inline void moments(const float (&v)[R][C][E], int t, int d, bool rms
     for (int r = 0; r < R; ++r) rstd[r] = 1.0f / sqrtf(rstd[r] * inv + eps);
 }
 
-template <typename T, int TPR, int EL, int R>
+// How the vectors and rows come.  USED: vectors where they are used, one pass over rows
+// per workgroup, several workgroups on a compute unit.  EARLY, for calls of few rows:
+// one row, its vectors under way with it.  STREAM, for rows that take a compute unit's
+// threads: a workgroup goes over many rows, vectors (but the gate) once, the next rows'
+// loads under way while the sums of these are joined.
+enum Way { USED, EARLY, STREAM };
+
+template <typename T, int TPR, int EL, int R, Way WAY>
 __global__ __launch_bounds__(block_threads(TPR)) void block_norm_kernel(BlockNormArgs a, int64_t rows_per_gate)
 {
     constexpr int E = per16<T>, C = EL / E, G = block_threads(TPR) / TPR;
     __shared__ float lds[2][TPR / 64 * R + 1];
     const int t = threadIdx.x % TPR, g = threadIdx.x / TPR, d = (int)a.d;
     int turn = 0;
-    for (int64_t r0 = (int64_t)blockIdx.x * G * R; r0 < a.rows; r0 += (int64_t)gridDim.x * G * R) {
-        const int64_t rg = r0 + (int64_t)g * R;
+    struct Rows {
         raw16 x[R][C], res[R][C];
+    };
+    auto load = [&](Rows& w, int64_t r0) {
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             // rows that do not exist give way to the last one
-            const int64_t row = rg + r < a.rows ? rg + r : a.rows - 1;
+            const int64_t rr = r0 + (int64_t)g * R + r, row = rr < a.rows ? rr : a.rows - 1;
 #pragma unroll
             for (int c = 0; c < C; ++c) {
                 const int col = (c * TPR + t) * E;
-                x[r][c] = load_piece(static_cast<const T*>(a.x) + row * a.ldx, col, d);
-                res[r][c] = load_piece(static_cast<const T*>(a.residual) + row * a.ldr, col, d);
+                w.x[r][c] = load_piece(static_cast<const T*>(a.x) + row * a.ldx, col, d);
+                w.res[r][c] = load_piece(static_cast<const T*>(a.residual) + row * a.ldr, col, d);
             }
         }
-        // one row: its vectors are under way with it
-        constexpr bool EARLY = R == 1 && TPR < 1024;
-        Pieces<T, TPR, C> pw, pb, pg, pnw, pnb;
-        if constexpr (EARLY) {
-            const int64_t row = rg < a.rows ? rg : a.rows - 1;
+    };
+    const int64_t first = (int64_t)blockIdx.x * G * R, step = (int64_t)gridDim.x * G * R;
+    Rows now, next;
+    if constexpr (WAY == STREAM) load(next, first);
+    Pieces<T, TPR, C> pw, pb, pg, pnw, pnb;
+    if constexpr (WAY == STREAM) {
+        pw.load(a.weight, t, d);
+        pb.load(a.bias, t, d);
+        pnw.load(a.next_weight, t, d);
+        pnb.load(a.next_bias, t, d);
+    }
+    for (int64_t r0 = first; r0 < a.rows; r0 += step) {
+        const int64_t rg = r0 + (int64_t)g * R;
+        if constexpr (WAY == STREAM) {
+            now = next;
+            if (r0 + step < a.rows) load(next, r0 + step);
+        } else {
+            load(now, r0);
+        }
+        auto &x = now.x, &res = now.res;
+        const int64_t row0 = rg < a.rows ? rg : a.rows - 1;
+        if constexpr (WAY != USED && R == 1)
+            pg.load(a.gate ? gate_of<T>(a.gate, d, rows_per_gate, a.rows, row0) : nullptr, t, d);
+        if constexpr (WAY == EARLY) {
             pw.load(a.weight, t, d);
             pb.load(a.bias, t, d);
-            pg.load(a.gate ? gate_of<T>(a.gate, d, rows_per_gate, a.rows, row) : nullptr, t, d);
             pnw.load(a.next_weight, t, d);
             pnb.load(a.next_bias, t, d);
         }
@@ -154,7 +180,7 @@ __global__ __launch_bounds__(block_threads(TPR)) void block_norm_kernel(BlockNor
         for (int c = 0; c < C; ++c) {
             const int col = (c * TPR + t) * E, have = d - col;
             float w[E], b[E];
-            if constexpr (EARLY) {
+            if constexpr (WAY != USED) {
                 pw.get(a.weight, 1.f, c, t, d, w);
                 pb.get(a.bias, 0.f, c, t, d, b);
             } else {
@@ -165,7 +191,7 @@ __global__ __launch_bounds__(block_threads(TPR)) void block_norm_kernel(BlockNor
             for (int r = 0; r < R; ++r) {
                 const int64_t row = rg + r < a.rows ? rg + r : a.rows - 1;
                 float gate[E], u[E];
-                if constexpr (EARLY) pg.get(a.gate, 1.f, c, t, d, gate);
+                if constexpr (WAY != USED) pg.get(a.gate, 1.f, c, t, d, gate);
                 else
                     vector_or<T>(a.gate ? gate_of<T>(a.gate, d, rows_per_gate, a.rows, row) : nullptr, 1.f, col, d, gate);
                 unpack16<T>(res[r][c], u);
@@ -186,7 +212,7 @@ __global__ __launch_bounds__(block_threads(TPR)) void block_norm_kernel(BlockNor
         for (int c = 0; c < C; ++c) {
             const int col = (c * TPR + t) * E, have = d - col;
             float w[E], b[E];
-            if constexpr (EARLY) {
+            if constexpr (WAY != USED) {
                 pnw.get(a.next_weight, 1.f, c, t, d, w);
                 pnb.get(a.next_bias, 0.f, c, t, d, b);
             } else {
@@ -328,19 +354,6 @@ __global__ __launch_bounds__(block_threads(TPR), TPR < 1024 ? 2 : 4) void block_
         for (int c = 0; c < C; ++c)
 #pragma unroll
             for (int e = 0; e < E; ++e) sum[k][c][e] = 0.f;
-    // the vectors, once for all rows: next_weight, and what t is multiplied by on its way to
-    // the norm after the block (without it to dx), gate weight
-    float nws[C][E], gws[C][E];
-#pragma unroll
-    for (int c = 0; c < C; ++c) {
-        const int col = (c * TPR + t) * E;
-        float gv[E];
-        vector_or<T>(a.next_weight, 1.f, col, d, nws[c]);
-        vector_or<T>(a.weight, 1.f, col, d, gws[c]);
-        vector_or<T>(gate, 1.f, col, d, gv);
-#pragma unroll
-        for (int e = 0; e < E; ++e) gws[c][e] *= gv[e];
-    }
     int turn = 0;
     struct Rows {
         raw16 dout[R][C], dn[R][C], x[R][C], out[R][C];
@@ -371,6 +384,19 @@ __global__ __launch_bounds__(block_threads(TPR), TPR < 1024 ? 2 : 4) void block_
     constexpr bool AHEAD = TPR < 1024;
     Rows now, next;
     if constexpr (AHEAD) load(next, begin);
+    // the vectors, once for all rows: next_weight, and what t is multiplied by on its way to
+    // the norm after the block (without it to dx), gate weight
+    float nws[C][E], gws[C][E];
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        const int col = (c * TPR + t) * E;
+        float gv[E];
+        vector_or<T>(a.next_weight, 1.f, col, d, nws[c]);
+        vector_or<T>(a.weight, 1.f, col, d, gws[c]);
+        vector_or<T>(gate, 1.f, col, d, gv);
+#pragma unroll
+        for (int e = 0; e < E; ++e) gws[c][e] *= gv[e];
+    }
     for (int64_t r0 = begin; r0 < end; r0 += G * R) {
         const int64_t rg = r0 + (int64_t)g * R;
         if constexpr (AHEAD) {
@@ -789,20 +815,21 @@ struct Forward {
     {
         // few rows: one each, for every compute unit has one
         const int64_t cus = std::max(device_cus(), 1), groups = block_threads(TPR) / TPR;
-        if (a.rows <= cus * groups * R)
-            launch<TPR, EL, 1>();
-        else
-            launch<TPR, EL, R>();
+        // 4096 columns: 8192 rows of fp32 99 us as a stream and 123 otherwise, 16384 of bf16
+        // 131 and 124
+        if constexpr (TPR * sizeof(T) > 1024) launch<TPR, EL, 1, STREAM>(1024 / TPR * cus);
+        else if (a.rows <= cus * groups * R) launch<TPR, EL, 1, EARLY>(1 << 20);
+        else launch<TPR, EL, R, USED>(1 << 20);
     }
-    template <int TPR, int EL, int R>
-    void launch()
+    template <int TPR, int EL, int R, Way WAY>
+    void launch(int64_t most)
     {
         constexpr int per_pass = block_threads(TPR) / TPR * R;
-        const int64_t blocks = std::min<int64_t>(ceil_div(a.rows, per_pass), 1 << 20);
+        const int64_t blocks = std::min(ceil_div(a.rows, per_pass), most);
         if (debug_enabled())
             fprintf(stderr, "cliffconv: block_norm %lld x %lld, %d threads per row, %lld workgroups\n",
                     (long long)a.rows, (long long)a.d, TPR, (long long)blocks);
-        hipLaunchKernelGGL((block_norm_kernel<T, TPR, EL, R>), dim3((unsigned)blocks), dim3(block_threads(TPR)), 0,
+        hipLaunchKernelGGL((block_norm_kernel<T, TPR, EL, R, WAY>), dim3((unsigned)blocks), dim3(block_threads(TPR)), 0,
                            stream, a, rows_per_gate);
     }
 };

@@ -38,39 +38,52 @@ struct Scale {
     __device__ explicit Scale(uint32_t most)
     {
         finite = most < 0x7f800000u;
-        s = __builtin_bit_cast(float, most) / 127.0f;
+        const float m = finite ? __builtin_bit_cast(float, most) : 0.f;
+        // m / 127, rounded once: the remainder of a quotient that is within a unit in the
+        // last place, times 1 / 127 rounded, gives the nearest float (Markstein 1990)
+        constexpr float R = 1.0f / 127.0f;
+        const float q = m * R;
+        s = fmaf(fmaf(-q, 127.0f, m), R, q);
         s = s > 0x1p-126f ? s : 0x1p-126f;
-        inv = finite ? 1.0f / s : 0.f;
+        inv = finite ? reciprocal(s) : 0.f;
         if (!finite) s = __builtin_nanf("");
     }
-    // The integer nearest to v / s, in the low byte.  v inv is within 2^-23 of
-    // the quotient, relative, so that only quotients within 2e-5 of the middle
-    // between two integers can go to the wrong one; those are decided by the sign
-    // of v - (k + 1/2) s, which 64 bits hold.
-    __device__ uint32_t nearest(float v) const
+    // The integer nearest to v / s.  v inv is within 3 2^-24 of the quotient, relative,
+    // so that only quotients within 3e-5 of the middle between two integers can go to
+    // the wrong one; the sign of v - (k + 1/2) s, which 64 bits hold, decides those.
+    __device__ int nearest(float v) const
     {
-        constexpr float MAGIC = 0x1.8p23f;  // its last place is one
-        const float m = fmaf(v, inv, MAGIC), n = m - MAGIC;
-        uint32_t r = __builtin_bit_cast(uint32_t, m);
-        if (fabsf(fmaf(v, inv, -n)) > 0.4999f) {
-            const float k = floorf(v * inv);
-            const double t = (double)v - ((double)k + 0.5) * (double)s;
-            const int i = (int)k;
-            r = (uint32_t)(t > 0.0 ? i + 1 : t < 0.0 ? i : i + (i & 1));
-        }
-        return r & 0xffu;
+        const float k = floorf(v * inv);
+        const double t = (double)v - ((double)k + 0.5) * (double)s;
+        const int i = (int)k;
+        return t > 0.0 ? i + 1 : t < 0.0 ? i : i + (i & 1);
     }
 };
 
-// E integers of a row's columns from `col` on, of which `have` exist.
+// E integers of a row's columns from `col` on, of which `have` exist.  Nearly all are
+// the low bytes of v inv + 1.5 2^23, whose last place is one; next to the middle
+// between two integers (one group in a thousand) they are found one by one.
 template <int E>
 __device__ inline void store_q(int8_t* to, const float (&v)[E], const Scale& s, int have)
 {
-    uint32_t w[E / 4];
+    constexpr float MAGIC = 0x1.8p23f;
+    float off = 0.f;
+    uint32_t m[E], w[E / 4];
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+        const float f = fmaf(v[e], s.inv, MAGIC);
+        m[e] = __builtin_bit_cast(uint32_t, f);
+        off = fmaxf(off, fabsf(fmaf(v[e], s.inv, MAGIC - f)));
+    }
+    if (off > 0.4999f) {
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            if (fabsf(fmaf(v[e], s.inv, MAGIC - __builtin_bit_cast(float, m[e]))) > 0.4999f) m[e] = (uint32_t)s.nearest(v[e]);
+    }
 #pragma unroll
     for (int i = 0; i < E / 4; ++i) {
-        w[i] = s.nearest(v[4 * i]) | s.nearest(v[4 * i + 1]) << 8 | s.nearest(v[4 * i + 2]) << 16 |
-               s.nearest(v[4 * i + 3]) << 24;
+        w[i] = __builtin_amdgcn_perm(__builtin_amdgcn_perm(m[4 * i + 3], m[4 * i + 2], 0x0c0c0400u),
+                                     __builtin_amdgcn_perm(m[4 * i + 1], m[4 * i], 0x0c0c0400u), 0x05040100u);
         if (!s.finite) w[i] = 0;
     }
     if (have >= E) {

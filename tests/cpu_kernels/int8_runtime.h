@@ -47,7 +47,21 @@ Acc mfma_i8(const V& a, const V& b, const Acc& c)
     return together<MFMA_I8, typename P::In, Acc, P::f>(typename P::In{a, b, c});
 }
 
+// Byte i of the result is byte selector_i of (a, b), a's bytes being 4 to 7; selector
+// 0x0c gives zero.
+inline uint32_t perm(uint32_t a, uint32_t b, uint32_t selector)
+{
+    const uint64_t both = (uint64_t)a << 32 | b;
+    uint32_t r = 0;
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t s = selector >> 8 * i & 0xff;
+        if (s < 8) r |= (uint32_t)(both >> 8 * s & 0xff) << 8 * i;
+    }
+    return r;
+}
+
 }  // namespace emulate
 
+#define __builtin_amdgcn_perm emulate::perm
 #define __builtin_amdgcn_mfma_i32_32x32x32_i8(a, b, c, x, y, z) emulate::mfma_i8<32>(a, b, c)
 #define __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, c, x, y, z) emulate::mfma_i8<16>(a, b, c)
