@@ -799,7 +799,7 @@ bool with_block_spread(int64_t d, F&& f)
     else if (d <= 64 * 8) f.template operator()<64, 8, R>();
     else if (d <= 128 * 8) f.template operator()<128, 8, R>();
     else if (d <= 256 * 8) f.template operator()<256, 8, R>();
-    else if (d <= 512 * 8) f.template operator()<512, 8, 2>();
+    else if (d <= 512 * 8) f.template operator()<512, 8, BACKWARD ? 2 : 1>();
     else if (d <= 1024 * 8) f.template operator()<1024, 8, 1>();
     else return false;
     return true;
@@ -815,9 +815,9 @@ struct Forward {
     {
         // few rows: one each, for every compute unit has one
         const int64_t cus = std::max(device_cus(), 1), groups = block_threads(TPR) / TPR;
-        // 4096 columns: 8192 rows of fp32 99 us as a stream and 123 otherwise, 16384 of bf16
-        // 131 and 124
-        if constexpr (TPR * sizeof(T) > 1024) launch<TPR, EL, 1, STREAM>(1024 / TPR * cus);
+        // (4096 columns: 8192 rows of fp32 99 us as a stream and 123 otherwise, 16384 of bf16
+        // 131 and 148)
+        if constexpr (TPR > 256) launch<TPR, EL, 1, STREAM>(1024 / TPR * cus);
         else if (a.rows <= cus * groups * R) launch<TPR, EL, 1, EARLY>(1 << 20);
         else launch<TPR, EL, R, USED>(1 << 20);
     }
