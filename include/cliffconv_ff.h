@@ -227,8 +227,11 @@ cliff_status cliffconv_dense_int8(int dtype, int64_t M, int64_t K, int64_t N, co
  *   x     int8 [M, K], row stride ldx, x_scale fp32 [M, groups] for x_group
  *   pre   int8 [M, N], row stride ldp, pre_scale fp32 [M, groups] for pre_group;
  *         both NULL where act is NONE
- * f' is taken at q scale in fp32; x is rounded to dtype before its product with g
- * (16-bit types: at most 2^-8 of each element in bf16, 2^-11 in fp16).
+ * f' is taken at q scale in fp32.  In 16-bit types one operand of dw's product is
+ * rounded: x to dtype where g is exact (NONE, ReLU), and with GELU and SiLU the scale of
+ * x times g, once, to bf16 or, in fp16, to two bf16 parts, while the integers of x are
+ * exact; that product needs |x| |g| to stay below the largest float for the largest x
+ * of each group.
  */
 int64_t cliffconv_dense_backward_int8_workspace(int dtype, int64_t M, int64_t K, int64_t N);
 cliff_status cliffconv_dense_backward_int8(

@@ -1137,7 +1137,7 @@ __device__ inline f4 load_pre(const DenseBackwardArgs& a, const float* pre_scale
 }
 template <typename T, bool EIGHT>
 __device__ inline void slope_rows(const DenseBackwardArgs& a, T* g, float* sums, int64_t rows_per_part,
-                                  const float* pre_scale, int64_t pre_groups)
+                                  const float* pre_scale, int64_t pre_groups, float* g32)
 {
     __shared__ f4 part[4][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -1161,6 +1161,8 @@ __device__ inline void slope_rows(const DenseBackwardArgs& a, T* g, float* sums,
             if (keep.rng) drop4(keep, key, step, r, c, v);
             t += v;
             if (g) store4(g + r * a.N + c, v * fit_slope<T>(a.act), have);
+            if constexpr (EIGHT)
+                if (g32) store4(g32 + r * a.N + c, v, have);
         }
     }
     if (!sums) return;
@@ -1176,13 +1178,196 @@ __device__ inline void slope_rows(const DenseBackwardArgs& a, T* g, float* sums,
 template <typename T>
 __global__ __launch_bounds__(256) void slope_kernel(DenseBackwardArgs a, T* g, float* sums, int64_t rows_per_part)
 {
-    slope_rows<T, false>(a, g, sums, rows_per_part, nullptr, 0);
+    slope_rows<T, false>(a, g, sums, rows_per_part, nullptr, 0, nullptr);
 }
 template <typename T>
 __global__ __launch_bounds__(256) void slope_int8_kernel(DenseBackwardInt8Args a, T* g, float* sums,
-                                                         int64_t rows_per_part)
+                                                         int64_t rows_per_part, float* g32)
 {
-    slope_rows<T, true>(a.dense, g, sums, rows_per_part, a.pre_scale, a.pre_groups);
+    slope_rows<T, true>(a.dense, g, sums, rows_per_part, a.pre_scale, a.pre_groups, g32);
+}
+
+// The weight's gradient of 16-bit types from x in 8 bits, where g is rounded (GELU and
+// SiLU): sum over rows of q (scale g), the integers q exactly in bf16 and scale g, from
+// g in fp32, rounded once, so that the product has one rounded operand as from x in 16
+// bits (both rounded, x and g: an error of 1.7 times the output's own rounding, not 1.4).
+// The scale goes with a row and 128 features, so a workgroup's tile has 128 of them (of
+// 128 x 128 outputs, 2 x 2 waves).  fp16 takes scale g as two bf16 parts: in fp16 it
+// could leave the range.
+//
+// Both operands go through registers, two stages of 32 rows ahead, and are converted on
+// their way to one of two LDS buffers; a step has one barrier.  Bound by the matrix
+// cores and, beside them, by the conversion.
+struct Int8Operand {
+    const int8_t* q;
+    int64_t ldq;
+    const float* scale;
+    int64_t groups;
+    const float* g;  // [rows][N]
+    int64_t ldg;
+};
+template <typename T, bool OI>
+__global__ __launch_bounds__(256, 2) void weight_int8_kernel(ProductArgs p, Int8Operand o)
+{
+    constexpr int NT = 256, KT = 32, MI = 2, NI = 2, P = __is_same(T, _Float16) ? 2 : 1;
+    using Tile = StageOf<128, KT, false>;
+    using Op = Operand<__bf16, Tile, NT>;
+    constexpr Stage S = Tile::s;
+    constexpr int L = S.slots() / NT, BYTES = S.bytes(), BUF = (1 + P) * BYTES;
+    extern __shared__ u4 smem4[];
+    char* const smem = reinterpret_cast<char*>(smem4);
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wm = wave / 2 * 64, wn = wave % 2 * 64;
+    const uint32_t tm = (uint32_t)((p.M + 127) / 128), tn = (uint32_t)((p.N + 127) / 128);
+    if (blockIdx.y && workgroup_id() >= tm * tn * p.splits) return;
+    const TileId id = tile_of(workgroup_id(), tm, tn, p.splits);
+    // features and outputs of the layer: the rows and columns of dw, or the other way
+    const int64_t k0 = (OI ? (int64_t)id.n : (int64_t)id.m) * 128, n0 = (OI ? (int64_t)id.m : (int64_t)id.n) * 128;
+    const int64_t features = OI ? p.N : p.M, outputs = OI ? p.M : p.N;
+    const int have_k = (int)(features - k0 < 128 ? features - k0 : 128), have_n = (int)(outputs - n0 < 128 ? outputs - n0 : 128);
+    const int64_t r0 = id.split * p.k_part, rows = p.K - r0 < p.k_part ? p.K - r0 : p.k_part;
+    const int steps = (int)((rows + KT - 1) / KT);
+    const int8_t* const q = o.q + r0 * o.ldq + k0;
+    const float* const g = o.g + r0 * o.ldg + n0;
+    const float* const scale = o.scale + r0 * o.groups + (o.groups > 1 ? k0 / CLIFF_INT8_GROUP : 0);
+
+    struct Fetched {
+        Integers<8> q;
+        f4 g[2];
+        float s;
+    };
+    Fetched f[2][L];
+    // Stages of whole rows in a whole tile have neither branches nor index arithmetic.
+    const int whole = have_k == 128 && have_n == 128 ? (int)(rows / KT) : 0;
+    const int8_t* at_q[L];
+    const float *at_g[L], *at_s[L];
+#pragma unroll
+    for (int i = 0; i < L; ++i) {
+        const int e = i * NT + tid, c = S.slot_row(e), r = S.slot_k(e);
+        at_q[i] = q + r * o.ldq + c;
+        at_g[i] = g + r * o.ldg + c;
+        at_s[i] = scale + r * o.groups;
+    }
+    auto fetch_one = [&](int s, Fetched (&to)[L], int i) {
+        __builtin_memcpy(to[i].q.w, at_q[i] + s * (KT * o.ldq), 8);
+        __builtin_memcpy(to[i].g, at_g[i] + s * (KT * o.ldg), 32);
+        to[i].s = at_s[i][s * (KT * o.groups)];
+    };
+    auto fetch = [&](int s, Fetched (&to)[L]) {
+        if (s >= steps) return;
+#pragma unroll
+        for (int i = 0; i < L; ++i) {
+            if (s < whole) {
+                fetch_one(s, to, i);
+                continue;
+            }
+            const int e = i * NT + tid, c = S.slot_row(e);
+            const int64_t r = (int64_t)s * KT + S.slot_k(e), row = r < rows ? r : rows - 1;
+            to[i].q.load(q + row * o.ldq + c, have_k - c);
+            to[i].g[0] = load4(g + row * o.ldg + c, have_n - c);
+            to[i].g[1] = load4(g + row * o.ldg + c + 4, have_n - c - 4);
+            to[i].s = scale[row * o.groups];
+            // (a row past the last one: zeros, whatever the last one has)
+            if (r >= rows) to[i].g[0] = to[i].g[1] = f4{0.f, 0.f, 0.f, 0.f}, to[i].s = 0.f;
+        }
+    };
+    // A slot's eight values of each operand, two at a time.
+    struct Slot {
+        b8 x, y, z;
+        __device__ void convert(const Fetched& from, int pair)
+        {
+#pragma unroll
+            for (int e = 2 * pair; e < 2 * pair + 2; ++e) {
+                x[e] = (__bf16)from.q.value(e, 1.f);
+                const float v = from.g[e / 4][e % 4] * from.s;
+                y[e] = (__bf16)v;
+                if constexpr (P == 2) z[e] = (__bf16)(v - (float)y[e]);
+            }
+        }
+        __device__ void put(char* to) const
+        {
+            *reinterpret_cast<b8*>(to) = x;
+            *reinterpret_cast<b8*>(to + BYTES) = y;
+            if constexpr (P == 2) *reinterpret_cast<b8*>(to + 2 * BYTES) = z;
+        }
+    };
+    auto put = [&](int s, const Fetched (&from)[L]) {
+#pragma unroll
+        for (int i = 0; i < L; ++i) {
+            Slot slot;
+#pragma unroll
+            for (int pair = 0; pair < 4; ++pair) slot.convert(from[i], pair);
+            slot.put(smem + (s & 1) * BUF + (i * NT + tid) * 16);
+        }
+    };
+    f16v acc[MI][NI];
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+        for (int j = 0; j < NI; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+    fetch(0, f[0]);
+    fetch(1, f[1]);
+    put(0, f[0]);
+    fetch(2, f[0]);
+    __syncthreads();
+    u4 fm[2][MI], fn[2][NI];
+    constexpr int GROUPS = KT / 16 * P;  // of products: 16 rows, a part of scale g
+    auto read = [&](int group, const char* buf) {
+        const int set = group & 1, kk = group / P, q = group % P;
+        const char* const from_m = buf + (OI ? (1 + q) * BYTES : 0);
+        const char* const from_n = buf + (OI ? 0 : (1 + q) * BYTES);
+#pragma unroll
+        for (int j = 0; j < NI; ++j) fn[set][j] = Op::frag(from_n, wn + 32 * j, 16 * kk, lane);
+#pragma unroll
+        for (int i = 0; i < MI; ++i) fm[set][i] = Op::frag(from_m, wm + 32 * i, 16 * kk, lane);
+    };
+    // Step s, with the fetched stage s + 1; plain: that and stage s + 3 are whole.  Under
+    // every product, the next group's fragments and a share of the conversion.
+    auto step = [&](int s, Fetched (&next)[L], auto plain) {
+        const char* const buf = smem + (s & 1) * BUF;
+        char* const to = smem + ((s + 1) & 1) * BUF + tid * 16;
+        if constexpr (!plain) {
+            if (s + 1 < steps) put(s + 1, next);
+            fetch(s + 3, next);
+        }
+        Slot slot;
+        read(0, buf);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int u = 0; u < 4 * GROUPS; ++u) {
+            const int group = u / 4, i = u / 2 % 2, j = u % 2;
+            acc[i][j] = mma<__bf16>(fn[group & 1][j], fm[group & 1][i], acc[i][j]);
+            if (u % 4 == 0 && group + 1 < GROUPS) read(group + 1, buf);
+            if constexpr (plain) {
+                if (u % P == 0) {
+                    const int pair = u / P;  // of eight, of both slots
+                    slot.convert(next[pair / 4], pair % 4);
+                    if (pair % 4 == 3) {
+                        slot.put(to + pair / 4 * NT * 16);
+                        fetch_one(s + 3, next, pair / 4);
+                    }
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+        __syncthreads();
+    };
+    static_assert(L == 2 && MI == 2 && NI == 2, "shares of the conversion");
+    constexpr std::true_type yes;
+    constexpr std::false_type no;
+    int s = 0;
+    for (; s + 4 < whole; s += 2) {
+        step(s, f[1], yes);
+        step(s + 1, f[0], yes);
+    }
+    for (; s < steps; s += 2) {
+        step(s, f[1], no);
+        if (s + 1 < steps) step(s + 1, f[0], no);
+    }
+    write_tile<T, MI, NI>(p, id, (int64_t)id.m * 128 + wm, (int64_t)id.n * 128 + wn, acc, smem, lane, wave);
 }
 
 // x in 8 bits, as the product with g reads it.
@@ -1290,8 +1475,9 @@ bool aligned_rows(const void* x, int64_t ld, int64_t width)
 }
 
 // Enqueues kernel k for tiles of B x B; its stages take `stage` bytes of LDS.
-template <typename K>
-cliff_status run(K k, const char* name, int B, int threads, int stage, const ProductArgs& p, hipStream_t stream)
+template <typename K, typename... More>
+cliff_status run(K k, const char* name, int B, int threads, int stage, const ProductArgs& p, hipStream_t stream,
+                 const More&... more)
 {
     const int lds = std::max(stage, threads / 64 * 32 * (64 + 4) * 4);  // or what write_tile takes
     const int64_t wgs = ceil_div(p.M, B) * ceil_div(p.N, B) * p.splits;
@@ -1299,7 +1485,7 @@ cliff_status run(K k, const char* name, int B, int threads, int stage, const Pro
     if (debug_enabled())
         fprintf(stderr, "cliffconv: product %lld x %lld x %lld, %s tiles of %d, %lld workgroups, %d splits\n",
                 (long long)p.M, (long long)p.N, (long long)p.K, name, B, (long long)wgs, p.splits);
-    hipLaunchKernelGGL(k, grid_of(wgs), dim3(threads), lds, stream, p);
+    hipLaunchKernelGGL(k, grid_of(wgs), dim3(threads), lds, stream, p, more...);
     return launched();
 }
 
@@ -1356,6 +1542,17 @@ cliff_status panel(const ProductArgs& p, hipStream_t stream)
 // waves, 128 x 2048 x 512 fp32 (16,000 groups) in 19.9 and 17.4.
 constexpr int64_t JOIN_GROUPS = 1 << 17;
 
+template <typename T>
+cliff_status join(const ProductArgs& p, hipStream_t stream)
+{
+    const int64_t groups = p.M * ceil_div(p.N, 4);
+    const bool one = groups >= JOIN_GROUPS;
+    const int64_t blocks = ceil_div(groups, one ? 256 : 64);
+    if (blocks >= (int64_t)1 << 31) return CLIFF_EUNSUPPORTED;
+    hipLaunchKernelGGL((one ? join_kernel<T, 1> : join_kernel<T, 4>), grid_of(blocks), dim3(256), 0, stream, p);
+    return launched();
+}
+
 // A product and, where its contraction is split, the join.
 template <typename T, bool AKM, bool BKM>
 cliff_status product(int dtype, ProductArgs p, hipStream_t stream)
@@ -1382,13 +1579,7 @@ cliff_status product(int dtype, ProductArgs p, hipStream_t stream)
         else
             s = run(product_kernel<T, AKM, BKM, 128, 128, 2, 2, 64, true>, "direct", 128, 256, 2 * 2 * 128 * 64 * 2, p, stream);
     }
-    if (s != CLIFF_OK || p.splits == 1) return s;
-    const int64_t groups = p.M * ceil_div(p.N, 4);
-    const bool one = groups >= JOIN_GROUPS;
-    const int64_t blocks = ceil_div(groups, one ? 256 : 64);
-    if (blocks >= (int64_t)1 << 31) return CLIFF_EUNSUPPORTED;
-    hipLaunchKernelGGL((one ? join_kernel<T, 1> : join_kernel<T, 4>), grid_of(blocks), dim3(256), 0, stream, p);
-    return launched();
+    return s != CLIFF_OK || p.splits == 1 ? s : join<T>(p, stream);
 }
 
 // Workspace of the backward pass: g, the bias's partial sums, partial products.
@@ -1462,8 +1653,47 @@ cliff_status finish_backward(int dtype, const DenseBackwardArgs& a, const Backwa
     return s;
 }
 
-// x of a gradient from 8 bits in the workspace: its row stride and its place.
+// A gradient from 8 bits has in its workspace, beside what dense_backward has, x in its
+// type with this row stride, or (weight_int8_kernel) g in fp32.
 int64_t expanded_ld(int64_t K) { return ceil_div(K, 8) * 8; }
+
+// Parts of the rows for weight_int8_kernel: a workgroup's stage of 32 rows, alone on a
+// compute unit and with a second one, and its begin and end, in ns.
+Cut weight_cut(int64_t M, int64_t K, int64_t N)
+{
+    const int64_t cus = std::max(device_cus(), 1), tiles = ceil_div(K, 128) * ceil_div(N, 128), steps = ceil_div(M, 32);
+    Cut best{false, 1, 0, 0};
+    for (const int want : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64, 96, 128, 192, 256}) {
+        if (want > steps) break;
+        const int64_t per = ceil_div(steps, want), splits = ceil_div(steps, per);
+        const int64_t wgs = tiles * splits, rounds = wgs / (cus * 2), rest = wgs % (cus * 2);
+        double ns = rounds * (per * 800 + 6000);
+        if (rest) ns += per * (rest <= cus ? 450 : 800) + 6000;
+        if (splits > 1) ns += 4400 + (double)K * N * 4 * 2 * splits / 11700;
+        if (best.ns == 0 || ns < best.ns) best = Cut{false, (int)splits, per * 32, ns};
+    }
+    return best;
+}
+
+// Whether dw comes of weight_int8_kernel: g is rounded in a type that shows it.
+bool exact_integers(int dtype, int act) { return dtype != CLIFF_F32 && (act == CLIFF_ACT_GELU || act == CLIFF_ACT_SILU); }
+
+// dw from x in 8 bits and g in fp32.
+template <typename T>
+cliff_status weight_int8(const DenseBackwardInt8Args& a, const float* g, float* partial, hipStream_t stream)
+{
+    const DenseBackwardArgs& d = a.dense;
+    const Cut c = weight_cut(d.M, d.K, d.N);
+    const int64_t M = d.w_out_in ? d.N : d.K, N = d.w_out_in ? d.K : d.N;
+    const DropArgs none{nullptr, 0, 1.f};
+    const ProductArgs p{M, N, d.M, nullptr, 0, nullptr, 0, c.splits, d.drop.rng ? d.drop.scale : 1.f, c.k_part, partial,
+                        nullptr, CLIFF_ACT_NONE, none, nullptr, 0, nullptr, 0, d.dw, d.lddw};
+    const Int8Operand o{static_cast<const int8_t*>(d.x), d.ldx, a.x_scale, a.x_groups, g, d.N};
+    const int stage = 2 * 128 * 32 * 2 * (__is_same(T, _Float16) ? 3 : 2);
+    const cliff_status s = d.w_out_in ? run(weight_int8_kernel<T, true>, "8-bit", 128, 256, stage, p, stream, o)
+                                      : run(weight_int8_kernel<T, false>, "8-bit", 128, 256, stage, p, stream, o);
+    return s == CLIFF_OK && p.splits > 1 ? join<T>(p, stream) : s;
+}
 
 }  // namespace
 
@@ -1489,8 +1719,12 @@ cliff_status launch_dense_backward(int dtype, const DenseBackwardArgs& a, hipStr
 
 int64_t dense_backward_int8_workspace(int dtype, int64_t M, int64_t K, int64_t N)
 {
-    const int64_t x = M * expanded_ld(K) * (dtype == CLIFF_F32 ? 4 : 2);
-    return backward_space(dtype, M, K, N).all + ceil_div(x, 256) * 256;
+    int64_t more = M * expanded_ld(K) * (dtype == CLIFF_F32 ? 4 : 2);
+    if (dtype != CLIFF_F32) {
+        const Cut c = weight_cut(M, K, N);
+        more = std::max(more, ceil_div(M * N * 4, 256) * 256 + (c.splits > 1 ? c.splits * K * N * 4 : 0));
+    }
+    return backward_space(dtype, M, K, N).all + ceil_div(more, 256) * 256;
 }
 
 cliff_status launch_dense_backward_int8(int dtype, const DenseBackwardInt8Args& a, hipStream_t stream)
@@ -1502,14 +1736,21 @@ cliff_status launch_dense_backward_int8(int dtype, const DenseBackwardInt8Args& 
         const BackwardSpace w = backward_space(dtype, d.M, d.K, d.N);
         char* const ws = static_cast<char*>(d.workspace);
         const bool change = d.act != CLIFF_ACT_NONE || d.drop.rng;
+        const bool exact = d.dw && d.M && exact_integers(dtype, d.act);
+        const bool g = change && (d.dx || (d.dw && !exact));
+        float* const g32 = exact ? reinterpret_cast<float*>(ws + w.all) : nullptr;
         cliff_status s = CLIFF_OK;
-        if (d.dbias || (change && (d.dx || d.dw))) {
+        if (d.dbias || g || g32) {
             hipLaunchKernelGGL(slope_int8_kernel<T>, dim3((unsigned)ceil_div(d.N, 256), (unsigned)w.parts), dim3(256),
-                               0, stream, a, change && (d.dx || d.dw) ? reinterpret_cast<T*>(ws + w.g) : nullptr,
-                               d.dbias ? reinterpret_cast<float*>(ws + w.sums) : nullptr, ceil_div(d.M, w.parts));
+                               0, stream, a, g ? reinterpret_cast<T*>(ws + w.g) : nullptr,
+                               d.dbias ? reinterpret_cast<float*>(ws + w.sums) : nullptr, ceil_div(d.M, w.parts), g32);
             s = launched();
         }
-        if (s == CLIFF_OK && d.dw && d.M) {
+        if (s == CLIFF_OK && exact) {
+            if constexpr (sizeof(T) == 2)
+                s = weight_int8<T>(a, g32, reinterpret_cast<float*>(ws + w.all + ceil_div(d.M * d.N * 4, 256) * 256), stream);
+            d.dw = nullptr;
+        } else if (s == CLIFF_OK && d.dw && d.M) {
             const int64_t ld = expanded_ld(d.K), pieces = ceil_div(d.K, per16<T>);
             const int64_t n = pieces * ceil_div(d.M, DEQUANTIZE_ROWS), blocks = ceil_div(n, 256);
             if (blocks >= (int64_t)1 << 31) return CLIFF_EUNSUPPORTED;
