@@ -64,18 +64,27 @@ __device__ inline void store4i(int* p, const i4& v, int have)
             if (e < have) p[e] = v[e];
 }
 
+// Scales whose products are normal floats, and fit any sum: within 2^-62 and 2^62.
+__device__ inline bool ordinary(float s)
+{
+    return (__builtin_bit_cast(uint32_t, s) >> 23) - 65u < 124u;  // (positive ones)
+}
+
 // What a group of four columns needs besides its sums, loaded early.
 struct Ends {
     f4 scale, bias;
+    bool ordinary;  // the scales
 };
 template <typename T>
 __device__ inline Ends load_ends(const Int8Args& p, int64_t n)
 {
-    Ends e{f4{0.f, 0.f, 0.f, 0.f}, f4{0.f, 0.f, 0.f, 0.f}};
+    Ends e{f4{0.f, 0.f, 0.f, 0.f}, f4{0.f, 0.f, 0.f, 0.f}, true};
     if (n >= p.N || p.splits > 1) return e;  // (the join's)
     const int have = p.N - n < 4 ? (int)(p.N - n) : 4;
     e.scale = load4(p.b_scale + n, have);
     if (p.bias) e.bias = load4(static_cast<const T*>(p.bias) + n, have);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) e.ordinary &= i >= have || ordinary(e.scale[i]);
     return e;
 }
 
@@ -86,26 +95,40 @@ __device__ inline void finish_rows(const Int8Args& p, int64_t m, int step, int64
     const int have = p.N - n >= 4 ? 4 : (int)(p.N - n);
     f4 res[R];
     float s[R];
+    bool plain = e.ordinary;
 #pragma unroll
-    for (int r = 0; r < R; ++r)
+    for (int r = 0; r < R; ++r) {
+        s[r] = 1.f;
         if (m + r * step < p.M) {
             s[r] = p.a_scale[m + r * step];
             if (p.residual) res[r] = load4(static_cast<const T*>(p.residual) + (m + r * step) * p.ldr + n, have);
         }
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r) plain &= ordinary(s[r]);
+    f4 u[R];
+    if (plain) {
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) u[r][i] = fmaf((float)v[r][i], s[r] * e.scale[i], e.bias[i]);
+    } else {
+        // the smaller scale first: neither product leaves fp32 where the result does not
+        // (comparisons keep a NaN)
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const bool less = s[r] < e.scale[i];
+                u[r][i] = fmaf((float)v[r][i] * (less ? s[r] : e.scale[i]), less ? e.scale[i] : s[r], e.bias[i]);
+            }
+    }
 #pragma unroll
     for (int r = 0; r < R; ++r) {
         if (m + r * step >= p.M) break;
-        f4 u;
-        // the smaller scale first: neither product leaves fp32 where the result does
-        // not (comparisons keep a NaN)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const bool less = s[r] < e.scale[i];
-            u[i] = fmaf((float)v[r][i] * (less ? s[r] : e.scale[i]), less ? e.scale[i] : s[r], e.bias[i]);
-        }
-        activate4<sizeof(T) == 4>(p.act, u);
-        if (p.residual) u += res[r];
-        store4(static_cast<T*>(p.y) + (m + r * step) * p.ldy + n, u, have);
+        activate4<sizeof(T) == 4>(p.act, u[r]);
+        if (p.residual) u[r] += res[r];
+        store4(static_cast<T*>(p.y) + (m + r * step) * p.ldy + n, u[r], have);
     }
 }
 
@@ -138,20 +161,22 @@ __device__ inline void write_tile(const Int8Args& p, const TileId& id, int64_t m
         }
         wave_fence();
         if (n < p.N) {
+// rows at a time: as many as the registers beside the accumulators hold
+            constexpr int R = MI > 1 ? 4 : 8;
 #pragma unroll 1
-            for (int h = 0; h < 2; ++h) {
+            for (int h = 0; h < 8 / R; ++h) {
                 const int r0 = 16 * h + (lane >> 4);
-                i4 v[4];
-#pragma unroll
-                for (int r = 0; r < 4; ++r) v[r] = *reinterpret_cast<const i4*>(tile + (r0 + 4 * r) * EW + 4 * (lane & 15));
                 const int64_t m = m1 + 32 * i + r0;
+                i4 v[R];
+#pragma unroll
+                for (int r = 0; r < R; ++r) v[r] = *reinterpret_cast<const i4*>(tile + (r0 + 4 * r) * EW + 4 * (lane & 15));
                 if (p.splits > 1) {
                     const int have = p.N - n < 4 ? (int)(p.N - n) : 4;
 #pragma unroll
-                    for (int r = 0; r < 4; ++r)
+                    for (int r = 0; r < R; ++r)
                         if (m + 4 * r < p.M) store4i(p.partial + (id.split * p.M + m + 4 * r) * p.N + n, v[r], have);
                 } else {
-                    finish_rows<T, 4>(p, m, 4, n, v, ends);
+                    finish_rows<T, R>(p, m, 4, n, v, ends);
                 }
             }
         }
@@ -167,7 +192,7 @@ __device__ inline void write_tile(const Int8Args& p, const TileId& id, int64_t m
 // of a stage, and the first fragments of the next stage are read under the second.
 constexpr int RING = 4, KT = 64;
 template <typename T, int BM, int BN, int WR, int WC>
-__global__ __launch_bounds__(64 * WR * WC) void int8_direct_kernel(Int8Args p)
+__global__ __launch_bounds__(64 * WR * WC, 2) void int8_direct_kernel(Int8Args p)
 {
     constexpr int NT = 64 * WR * WC, WM = BM / WR, WN = BN / WC, MI = WM / 32, NI = WN / 32;
     constexpr Stage SA{BM, KT / 2, true}, SB{BN, KT / 2, true};
@@ -264,7 +289,7 @@ __global__ __launch_bounds__(64 * WR * WC) void int8_direct_kernel(Int8Args p)
 // through registers, one stage ahead.
 constexpr int KT_STAGED = 128;
 template <typename T, int TILE, int WR, int WC>
-__global__ __launch_bounds__(64 * WR * WC) void int8_staged_kernel(Int8Args p)
+__global__ __launch_bounds__(64 * WR * WC, 2) void int8_staged_kernel(Int8Args p)
 {
     constexpr int KT = KT_STAGED, NT = 64 * WR * WC, WM = TILE / WR, WN = TILE / WC, MI = WM / 32, NI = WN / 32;
     constexpr Stage S{TILE, KT / 2, true};
