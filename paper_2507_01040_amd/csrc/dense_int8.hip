@@ -88,22 +88,28 @@ __device__ inline Ends load_ends(const Int8Args& p, int64_t n)
     return e;
 }
 
-// R rows of a group of four columns: rows m, m + step, ...
-template <typename T, int R>
-__device__ inline void finish_rows(const Int8Args& p, int64_t m, int step, int64_t n, const i4 (&v)[R], const Ends& e)
+// The scales of rows m, m + step, ...
+template <int R>
+__device__ inline void row_scales(const Int8Args& p, int64_t m, int step, float (&s)[R])
 {
-    const int have = p.N - n >= 4 ? 4 : (int)(p.N - n);
-    f4 res[R];
-    float s[R];
-    bool plain = e.ordinary;
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-        s[r] = 1.f;
-        if (m + r * step < p.M) {
-            s[r] = p.a_scale[m + r * step];
-            if (p.residual) res[r] = load4(static_cast<const T*>(p.residual) + (m + r * step) * p.ldr + n, have);
-        }
-    }
+    for (int r = 0; r < R; ++r) s[r] = p.a_scale[m + r * step < p.M ? m + r * step : p.M - 1];
+}
+
+// R rows of a group of four columns: rows m, m + step, ...  WHOLE: all of them exist (no
+// branches then, so that waits for earlier loads need not wait for these stores).
+template <typename T, int R, bool WHOLE = false>
+__device__ inline void finish_rows(const Int8Args& p, int64_t m, int step, int64_t n, const i4 (&v)[R], const Ends& e,
+                                   const float (&s)[R])
+{
+    const int have = WHOLE || p.N - n >= 4 ? 4 : (int)(p.N - n);
+    f4 res[R];
+    bool plain = e.ordinary;
+    if (p.residual)
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+            if (WHOLE || m + r * step < p.M)
+                res[r] = load4(static_cast<const T*>(p.residual) + (m + r * step) * p.ldr + n, have);
 #pragma unroll
     for (int r = 0; r < R; ++r) plain &= ordinary(s[r]);
     f4 u[R];
@@ -125,7 +131,7 @@ __device__ inline void finish_rows(const Int8Args& p, int64_t m, int step, int64
     }
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-        if (m + r * step >= p.M) break;
+        if (!WHOLE && m + r * step >= p.M) break;
         activate4<sizeof(T) == 4>(p.act, u[r]);
         if (p.residual) u[r] += res[r];
         store4(static_cast<T*>(p.y) + (m + r * step) * p.ldy + n, u[r], have);
@@ -176,7 +182,9 @@ __device__ inline void write_tile(const Int8Args& p, const TileId& id, int64_t m
                     for (int r = 0; r < R; ++r)
                         if (m + 4 * r < p.M) store4i(p.partial + (id.split * p.M + m + 4 * r) * p.N + n, v[r], have);
                 } else {
-                    finish_rows<T, R>(p, m, 4, n, v, ends);
+                    float s[R];
+                    row_scales(p, m, 4, s);
+                    finish_rows<T, R>(p, m, 4, n, v, ends, s);
                 }
             }
         }
@@ -383,7 +391,8 @@ __global__ __launch_bounds__(256) void int8_join_kernel(Int8Args p)
     i4 v[1] = {i4{0, 0, 0, 0}};
 #pragma unroll 4
     for (int s = 0; s < splits; ++s) v[0] += load4i(q + s * plane, have);
-    finish_rows<T, 1>(p, m, 1, n, v, ends);
+    const float s[1] = {p.a_scale[m]};
+    finish_rows<T, 1>(p, m, 1, n, v, ends, s);
 }
 
 // Few rows (16 MB at most): bound by the read of the weight.  A workgroup streams 16
@@ -452,7 +461,99 @@ __global__ __launch_bounds__(512, 2) void int8_rows_kernel(Int8Args p)
     i4 v[1] = {i4{0, 0, 0, 0}};
 #pragma unroll
     for (int w = 0; w < 8; ++w) v[0] += *reinterpret_cast<const i4*>(lds + w * PLANE + r * W + c);
-    finish_rows<T, 1>(p, r, 1, n, v, ends);
+    const float s[1] = {p.a_scale[r]};
+    finish_rows<T, 1>(p, r, 1, n, v, ends, s);
+}
+
+// Many rows and a short contraction: bound by the write of y (and its activation), and
+// a tile has too few stages to hide its begin and end.  So 128 outputs' weights stay in
+// LDS (a panel), and each of four waves streams blocks of 32 rows past it without
+// barriers, x from memory straight into fragments that stay for all columns, the next
+// block's loads under the work on this one.  The panel lies as [slot][column] in 16-byte slots, slot 2 kk + h
+// with the 16 values of half-wave h in product group kk, read without bank conflicts.
+constexpr int PANEL = 128, PANEL_EW = 32 + 4;
+constexpr int PANEL_WAVES = 4;
+template <typename T, int KK>
+__global__ __launch_bounds__(64 * PANEL_WAVES, 3) void int8_panel_kernel(Int8Args p)
+{
+    constexpr int SLOTS = 2 * KK * PANEL;
+    extern __shared__ u4 smem4[];
+    char* const smem = reinterpret_cast<char*>(smem4);
+    float* const scales = reinterpret_cast<float*>(smem + SLOTS * 16);
+    float* const bias = scales + PANEL;
+    const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    int* const tile = reinterpret_cast<int*>(bias + PANEL) + wave * 32 * PANEL_EW;
+    const uint32_t panels = (uint32_t)((p.N + PANEL - 1) / PANEL), t = xcd_run(blockIdx.x, gridDim.x);
+    const int64_t n0 = (int64_t)(t % panels) * PANEL, stride = (int64_t)(gridDim.x / panels) * PANEL_WAVES;
+    const int K = (int)p.K;
+    if (tid < PANEL) {
+        scales[tid] = n0 + tid < p.N ? p.b_scale[n0 + tid] : 1.f;
+        bias[tid] = p.bias && n0 + tid < p.N ? (float)static_cast<const T*>(p.bias)[n0 + tid] : 0.f;
+    }
+    for (int i = tid; i < SLOTS; i += 64 * PANEL_WAVES) {
+        const int64_t n = n0 + i % PANEL < p.N ? n0 + i % PANEL : p.N - 1;  // (columns that do not exist are not written)
+        raw16 v = load16(p.b + n * p.ldb, i / PANEL * 16, K);
+        settle16<int8_t>(v, i / PANEL * 16, K);
+        *reinterpret_cast<raw16*>(smem + i * 16) = v;
+    }
+    __syncthreads();
+
+    const int64_t blocks = (p.M + 31) / 32, b0 = (int64_t)(t / panels) * PANEL_WAVES + wave;
+    if (b0 >= blocks) return;
+    raw16 x[KK], next[KK];
+    float s[4], next_s[4];
+    // A block's rows (those that do not exist give way to the last one) and their scales.
+    auto load = [&](int64_t blk) {
+        const int64_t row = 32 * blk + (lane & 31);
+        const int8_t* const line = p.a + (row < p.M ? row : p.M - 1) * p.lda;
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) next[kk] = load16(line, 32 * kk + 16 * half, K);
+        row_scales(p, 32 * blk + (lane >> 3), 8, next_s);
+    };
+    const char* const mine = smem + (half * PANEL + (lane & 31)) * 16;
+    load(b0);
+    for (int64_t blk = b0; blk < blocks; blk += stride) {
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) {
+            x[kk] = next[kk];
+            if (K < 32 * KK) settle16<int8_t>(x[kk], 32 * kk + 16 * half, K);
+        }
+#pragma unroll
+        for (int r = 0; r < 4; ++r) s[r] = next_s[r];
+        if (blk + stride < blocks) load(blk + stride);
+        // 32 columns at a time through LDS: 8 lanes hold a row's.
+        const int64_t m = 32 * blk + (lane >> 3);
+        const bool whole = 32 * blk + 32 <= p.M && n0 + PANEL <= p.N;
+        auto finish = [&](const i16v& c, int j) {
+            wave_fence();
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+                *reinterpret_cast<i4*>(tile + (lane & 31) * PANEL_EW + 8 * g + 4 * half) =
+                    i4{c[4 * g], c[4 * g + 1], c[4 * g + 2], c[4 * g + 3]};
+            wave_fence();
+            i4 v[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                v[r] = *reinterpret_cast<const i4*>(tile + ((lane >> 3) + 8 * r) * PANEL_EW + 4 * (lane & 7));
+            const int c0 = 32 * j + 4 * (lane & 7);
+            Ends e{*reinterpret_cast<const f4*>(scales + c0), *reinterpret_cast<const f4*>(bias + c0), true};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) e.ordinary &= ordinary(e.scale[i]);
+            if (whole) finish_rows<T, 4, true>(p, m, 8, n0 + c0, v, e, s);
+            else if (n0 + c0 < p.N) finish_rows<T, 4>(p, m, 8, n0 + c0, v, e, s);
+        };
+#pragma unroll 1
+        for (int j = 0; j < PANEL / 32; ++j) {
+            i16v acc;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[e] = 0;
+#pragma unroll
+            for (int kk = 0; kk < KK; ++kk)
+                acc = mma(*reinterpret_cast<const u4*>(mine + (2 * kk * PANEL + 32 * j) * 16), __builtin_bit_cast(u4, x[kk]), acc);
+            finish(acc, j);
+        }
+    }
 }
 
 // How a product is cut: square tiles, and parts of the contraction, by the times in ns
@@ -510,6 +611,12 @@ double few_rows_ns(int64_t M, int64_t N, int64_t K)
     return 3500 + rounds * (double)(K * (rows + 16)) / 75;
 }
 
+// The longest contraction of the panel kernel, and rows and outputs from which it is level
+// with the tiles or ahead (us, panels and tiles, bf16, K 128: 2048 x 2048 outputs 7.2 and
+// 7.5, 4096 x 512 6.6 and 6.5, 16384 x 128 6.7 and 7.3, 65536 x 512 22.4 and 32.9; 8192 x
+// 128 6.4 and 5.6; 20000 x 1000 with K 256, which would fit too, 30.9 and 26.4).
+constexpr int64_t PANEL_K = 128, PANEL_ROWS = 2048, PANEL_OUTPUTS = 1 << 21;
+
 bool aligned_rows(const void* x, int64_t ld, int64_t width)
 {
     return ((uintptr_t)x & 15) == 0 && ld % 16 == 0 && width % 16 == 0 && ld <= (1 << 22);
@@ -534,6 +641,19 @@ cliff_status int8_product(Int8Args p, hipStream_t stream)
         if (p.M <= 16) go(int8_rows_kernel<T, 1>);
         else if (p.M <= 32) go(int8_rows_kernel<T, 2>);
         else go(int8_rows_kernel<T, 4>);
+        return launched();
+    }
+    const int64_t panels = ceil_div(p.N, PANEL);
+    if (p.M >= PANEL_ROWS && p.M * p.N >= PANEL_OUTPUTS && p.K <= PANEL_K && p.K >= 16 && panels < 1 << 22) {
+        const int64_t cus = std::max(device_cus(), 1);
+        const int64_t wgs = panels * std::min(std::max<int64_t>(1, 3 * cus / panels), ceil_div(p.M, 32 * PANEL_WAVES));
+        say("panels", wgs);
+        const auto go = [&](auto k, int KK) {
+            const int lds = 2 * KK * PANEL * 16 + (2 * PANEL + PANEL_WAVES * 32 * PANEL_EW) * 4;
+            hipLaunchKernelGGL(k, dim3((unsigned)wgs), dim3(64 * PANEL_WAVES), lds, stream, p);
+        };
+        if (p.K <= 64) go(int8_panel_kernel<T, 2>, 2);
+        else go(int8_panel_kernel<T, 4>, 4);
         return launched();
     }
     p.splits = c.splits;

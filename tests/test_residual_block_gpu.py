@@ -22,7 +22,7 @@ def exactly(q, scale, x, group):
 
 
 ROWS = [(1, 1), (1, 4096), (3, 7), (5, 128), (7, 129), (300, 8), (33, 777), (64, 1024), (17, 2049), (4, 8192), (3, 8193), (2, 20001),
-        (4099, 128), (1001, 260)]
+        (4099, 128), (1001, 260), (1100, 2100), (700, 5000)]
 
 
 @pytest.mark.parametrize("group", [None, 128])
@@ -100,7 +100,7 @@ class Eight(Draw):
 SIZES = [(1, 64, 64), (1, 1, 1), (3, 7, 5), (1, 4096, 512), (2, 520, 1000), (16, 2048, 96), (17, 96, 129), (24, 1024, 256), (32, 64, 72),
          (33, 65, 63), (64, 256, 128), (65, 16, 257), (127, 136, 320), (128, 128, 128), (130, 1040, 264), (255, 64, 511),
          (256, 512, 256), (257, 208, 513), (520, 784, 1032), (1000, 33, 40), (4099, 64, 24), (9, 3001, 16), (300, 16384, 8),
-         (520, 2064, 1024), (20000, 128, 200), (16390, 100, 130), (64, 16384, 48)]
+         (520, 2064, 1024), (20000, 128, 200), (16390, 100, 130), (64, 16384, 48), (2050, 17, 1030), (9001, 112, 257)]
 
 
 def _int8(dtype, size, i, pad=0, offset=0):
