@@ -1187,17 +1187,20 @@ __global__ __launch_bounds__(256) void slope_int8_kernel(DenseBackwardInt8Args a
     slope_rows<T, true>(a.dense, g, sums, rows_per_part, a.pre_scale, a.pre_groups, g32);
 }
 
-// The weight's gradient of 16-bit types from x in 8 bits, where g is rounded (GELU and
-// SiLU): sum over rows of q (scale g), the integers q exactly in bf16 and scale g, from
-// g in fp32, rounded once, so that the product has one rounded operand as from x in 16
+// The weight's gradient from x in 8 bits: sum over rows of q (scale g), the integers q
+// exactly in bf16 and scale g from g in fp32.  bf16, where g is rounded (GELU and SiLU),
+// rounds scale g instead, so that the product has one rounded operand as from x in 16
 // bits (both rounded, x and g: an error of 1.7 times the output's own rounding, not 1.4).
+// fp16 takes scale g as two bf16 parts, for in fp16 it could leave the range, and fp32
+// as three (split.hpp), three products instead of the six of two split operands.
 // The scale goes with a row and 128 features, so a workgroup's tile has 128 of them (of
-// 128 x 128 outputs, 2 x 2 waves).  fp16 takes scale g as two bf16 parts: in fp16 it
-// could leave the range.
+// 128 x 128 outputs, 2 x 2 waves).
 //
 // Both operands go through registers, two stages of 32 rows ahead, and are converted on
 // their way to one of two LDS buffers; a step has one barrier.  Bound by the matrix
 // cores and, beside them, by the conversion.
+template <typename T>
+constexpr int weight_parts = sizeof(T) == 4 ? 3 : __is_same(T, _Float16) ? 2 : 1;
 struct Int8Operand {
     const int8_t* q;
     int64_t ldq;
@@ -1209,7 +1212,7 @@ struct Int8Operand {
 template <typename T, bool OI>
 __global__ __launch_bounds__(256, 2) void weight_int8_kernel(ProductArgs p, Int8Operand o)
 {
-    constexpr int NT = 256, KT = 32, MI = 2, NI = 2, P = __is_same(T, _Float16) ? 2 : 1;
+    constexpr int NT = 256, KT = 32, MI = 2, NI = 2, P = weight_parts<T>;
     using Tile = StageOf<128, KT, false>;
     using Op = Operand<__bf16, Tile, NT>;
     constexpr Stage S = Tile::s;
@@ -1274,22 +1277,28 @@ __global__ __launch_bounds__(256, 2) void weight_int8_kernel(ProductArgs p, Int8
     };
     // A slot's eight values of each operand, two at a time.
     struct Slot {
-        b8 x, y, z;
+        b8 x, y[P];
         __device__ void convert(const Fetched& from, int pair)
         {
 #pragma unroll
             for (int e = 2 * pair; e < 2 * pair + 2; ++e) {
                 x[e] = (__bf16)from.q.value(e, 1.f);
-                const float v = from.g[e / 4][e % 4] * from.s;
-                y[e] = (__bf16)v;
-                if constexpr (P == 2) z[e] = (__bf16)(v - (float)y[e]);
+                float v = from.g[e / 4][e % 4] * from.s;
+                if constexpr (P == 3) v *= SPLIT_SCALE;
+#pragma unroll
+                for (int q = 0; q < P; ++q) {
+                    y[q][e] = (__bf16)v;
+                    const float part = (float)y[q][e];
+                    // (an infinity has no rest; three parts are found out by their NaN)
+                    v = P == 2 && fabsf(part) == __builtin_inff() ? 0.f : v - part;
+                }
             }
         }
         __device__ void put(char* to) const
         {
             *reinterpret_cast<b8*>(to) = x;
-            *reinterpret_cast<b8*>(to + BYTES) = y;
-            if constexpr (P == 2) *reinterpret_cast<b8*>(to + 2 * BYTES) = z;
+#pragma unroll
+            for (int q = 0; q < P; ++q) *reinterpret_cast<b8*>(to + (1 + q) * BYTES) = y[q];
         }
     };
     auto put = [&](int s, const Fetched (&from)[L]) {
@@ -1366,6 +1375,43 @@ __global__ __launch_bounds__(256, 2) void weight_int8_kernel(ProductArgs p, Int8
     for (; s < steps; s += 2) {
         step(s, f[1], no);
         if (s + 1 < steps) step(s + 1, f[0], no);
+    }
+    if constexpr (P == 3) {
+        // Sums that are infinite or NaN, or that the parts cannot hold, again as fp32
+        // products, operands straight from memory (this wave's tile).
+        float z = 0.f;
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+#pragma unroll
+            for (int j = 0; j < NI; ++j) {
+                acc[i][j] *= 1.0f / SPLIT_SCALE;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) z = fmaf(acc[i][j][e], 0.f, z);
+            }
+        if (__ballot(z != 0.f)) {
+#pragma unroll
+            for (int i = 0; i < MI; ++i)
+#pragma unroll
+                for (int j = 0; j < NI; ++j)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+            auto at = [&](bool left, int c, int64_t r) {  // an element of x or of g
+                if (r >= rows || c >= (left ? have_k : have_n)) return 0.f;
+                return left ? (float)q[r * o.ldq + c] * scale[r * o.groups] : g[r * o.ldg + c];
+            };
+            for (int64_t r = lane >> 5; r - (lane >> 5) < rows; r += 2) {
+                float va[MI], vb[NI];
+#pragma unroll
+                for (int i = 0; i < MI; ++i) va[i] = at(!OI, wm + 32 * i + (lane & 31), r);
+#pragma unroll
+                for (int j = 0; j < NI; ++j) vb[j] = at(OI, wn + 32 * j + (lane & 31), r);
+#pragma unroll
+                for (int i = 0; i < MI; ++i)
+#pragma unroll
+                    for (int j = 0; j < NI; ++j)
+                        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(vb[j], va[i], acc[i][j], 0, 0, 0);
+            }
+        }
     }
     write_tile<T, MI, NI>(p, id, (int64_t)id.m * 128 + wm, (int64_t)id.n * 128 + wn, acc, smem, lane, wave);
 }
@@ -1675,12 +1721,12 @@ Cut weight_cut(int64_t M, int64_t K, int64_t N)
     return best;
 }
 
-// Whether dw comes of weight_int8_kernel: g is rounded in a type that shows it.
-bool exact_integers(int dtype, int act) { return dtype != CLIFF_F32 && (act == CLIFF_ACT_GELU || act == CLIFF_ACT_SILU); }
+// Whether dw comes of weight_int8_kernel: in fp32, and where g is rounded.
+bool exact_integers(int dtype, int act) { return dtype == CLIFF_F32 || act == CLIFF_ACT_GELU || act == CLIFF_ACT_SILU; }
 
 // dw from x in 8 bits and g in fp32.
 template <typename T>
-cliff_status weight_int8(const DenseBackwardInt8Args& a, const float* g, float* partial, hipStream_t stream)
+cliff_status weight_int8(const DenseBackwardInt8Args& a, const float* g, int64_t ldg, float* partial, hipStream_t stream)
 {
     const DenseBackwardArgs& d = a.dense;
     const Cut c = weight_cut(d.M, d.K, d.N);
@@ -1688,8 +1734,8 @@ cliff_status weight_int8(const DenseBackwardInt8Args& a, const float* g, float* 
     const DropArgs none{nullptr, 0, 1.f};
     const ProductArgs p{M, N, d.M, nullptr, 0, nullptr, 0, c.splits, d.drop.rng ? d.drop.scale : 1.f, c.k_part, partial,
                         nullptr, CLIFF_ACT_NONE, none, nullptr, 0, nullptr, 0, d.dw, d.lddw};
-    const Int8Operand o{static_cast<const int8_t*>(d.x), d.ldx, a.x_scale, a.x_groups, g, d.N};
-    const int stage = 2 * 128 * 32 * 2 * (__is_same(T, _Float16) ? 3 : 2);
+    const Int8Operand o{static_cast<const int8_t*>(d.x), d.ldx, a.x_scale, a.x_groups, g, ldg};
+    const int stage = 2 * 128 * 32 * 2 * (1 + weight_parts<T>);
     const cliff_status s = d.w_out_in ? run(weight_int8_kernel<T, true>, "8-bit", 128, 256, stage, p, stream, o)
                                       : run(weight_int8_kernel<T, false>, "8-bit", 128, 256, stage, p, stream, o);
     return s == CLIFF_OK && p.splits > 1 ? join<T>(p, stream) : s;
@@ -1719,11 +1765,10 @@ cliff_status launch_dense_backward(int dtype, const DenseBackwardArgs& a, hipStr
 
 int64_t dense_backward_int8_workspace(int dtype, int64_t M, int64_t K, int64_t N)
 {
-    int64_t more = M * expanded_ld(K) * (dtype == CLIFF_F32 ? 4 : 2);
-    if (dtype != CLIFF_F32) {
-        const Cut c = weight_cut(M, K, N);
-        more = std::max(more, ceil_div(M * N * 4, 256) * 256 + (c.splits > 1 ? c.splits * K * N * 4 : 0));
-    }
+    const Cut c = weight_cut(M, K, N);
+    int64_t more = c.splits > 1 ? c.splits * K * N * 4 : 0;
+    if (dtype != CLIFF_F32)  // g in fp32 and the parts, or x
+        more = std::max(ceil_div(M * N * 4, 256) * 256 + more, M * expanded_ld(K) * 2);
     return backward_space(dtype, M, K, N).all + ceil_div(more, 256) * 256;
 }
 
@@ -1734,11 +1779,12 @@ cliff_status launch_dense_backward_int8(int dtype, const DenseBackwardInt8Args& 
         using T = decltype(t);
         DenseBackwardArgs d = a.dense;
         const BackwardSpace w = backward_space(dtype, d.M, d.K, d.N);
-        char* const ws = static_cast<char*>(d.workspace);
+        char *const ws = static_cast<char*>(d.workspace), *const more = ws + w.all;
         const bool change = d.act != CLIFF_ACT_NONE || d.drop.rng;
         const bool exact = d.dw && d.M && exact_integers(dtype, d.act);
-        const bool g = change && (d.dx || (d.dw && !exact));
-        float* const g32 = exact ? reinterpret_cast<float*>(ws + w.all) : nullptr;
+        // g in the type, for dx and a product with x in it; fp32 has the one g
+        const bool g = change && (d.dx || (d.dw && (!exact || sizeof(T) == 4)));
+        float* const g32 = exact && sizeof(T) == 2 ? reinterpret_cast<float*>(more) : nullptr;
         cliff_status s = CLIFF_OK;
         if (d.dbias || g || g32) {
             hipLaunchKernelGGL(slope_int8_kernel<T>, dim3((unsigned)ceil_div(d.N, 256), (unsigned)w.parts), dim3(256),
@@ -1747,22 +1793,22 @@ cliff_status launch_dense_backward_int8(int dtype, const DenseBackwardInt8Args& 
             s = launched();
         }
         if (s == CLIFF_OK && exact) {
-            if constexpr (sizeof(T) == 2)
-                s = weight_int8<T>(a, g32, reinterpret_cast<float*>(ws + w.all + ceil_div(d.M * d.N * 4, 256) * 256), stream);
+            const float* const from = g32 ? g32 : static_cast<const float*>(change ? ws + w.g : d.dy);
+            char* const partial = g32 ? more + ceil_div(d.M * d.N * 4, 256) * 256 : more;
+            s = weight_int8<T>(a, from, g32 || change ? d.N : d.lddy, reinterpret_cast<float*>(partial), stream);
             d.dw = nullptr;
         } else if (s == CLIFF_OK && d.dw && d.M) {
             const int64_t ld = expanded_ld(d.K), pieces = ceil_div(d.K, per16<T>);
             const int64_t n = pieces * ceil_div(d.M, DEQUANTIZE_ROWS), blocks = ceil_div(n, 256);
             if (blocks >= (int64_t)1 << 31) return CLIFF_EUNSUPPORTED;
-            const DequantizeArgs x{d.M, d.K, a.x_groups, static_cast<const int8_t*>(d.x), d.ldx, a.x_scale,
-                                   ws + w.all, ld};
+            const DequantizeArgs x{d.M, d.K, a.x_groups, static_cast<const int8_t*>(d.x), d.ldx, a.x_scale, more, ld};
             hipLaunchKernelGGL(expand_kernel<T>, grid_of(blocks), dim3(256), 0, stream, x, (uint32_t)pieces, n);
             s = launched();
             d.x = x.y;
             d.ldx = ld;
         }
         if (s != CLIFF_OK) return s;
-        return finish_backward<T>(dtype, d, w, change ? ws + w.g : d.dy, change ? d.N : d.lddy, stream);
+        return finish_backward<T>(dtype, d, w, change ? static_cast<const void*>(ws + w.g) : d.dy, change ? d.N : d.lddy, stream);
     });
 }
 

@@ -13,7 +13,8 @@ from . import build as B
 
 OUT = os.path.join(B.OUT, "block")
 EXE = os.path.join(OUT, "cpu_block_kernels")
-OWN = ["main.cpp", "block_main.cpp", "run_dense.cpp", "run_int8.cpp", "hip_runtime.h", "int8_runtime.h", "lds_load.hpp"]
+OWN = ["main.cpp", "block_main.cpp", "run_dense.cpp", "run_int8.cpp", "hip_runtime.h", "int8_runtime.h", "block_lds_load.hpp"]
+AS = {"hip_runtime.h": "hip/hip_runtime.h", "block_lds_load.hpp": "lds_load.hpp"}  # names in the build
 TAKEN = B.TAKEN + ["ff_block_api.cpp", "quantize.hip", "dense_int8.hip", "block_norm.hip"]
 UNITS = ["block_main.cpp", "run_dense.cpp", "run_int8.cpp", "quantize.hip", "block_norm.hip", "norm.hip", "dropout.hip",
          "ff_api.cpp", "ff_block_api.cpp"]
@@ -37,7 +38,7 @@ def build() -> str:
     for f in TAKEN:
         shutil.copy(os.path.join(B.CSRC, f), src)
     for f in OWN:
-        shutil.copy(os.path.join(B.HERE, f), os.path.join(src, "hip") if f == "hip_runtime.h" else src)
+        shutil.copy(os.path.join(B.HERE, f), os.path.join(src, AS.get(f, f)))
 
     def compile_one(unit):
         obj = os.path.join(OUT, unit + ".o")

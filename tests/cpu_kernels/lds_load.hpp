@@ -15,11 +15,5 @@ inline void load_to_lds(const void* from, uint32_t offset, char* to)
     emulate::load(outside ? nullptr : static_cast<const char*>(from) + offset, to + 16 * emulate::lane_id());
 }
 inline void wait_direct() { emulate::wait_loads(); }
-inline void barrier_alone() { emulate::meet_workgroup(); }
-template <int N>
-void wait_direct_but()
-{
-    emulate::wait_loads_but(N);
-}
 
 }  // namespace cliff
