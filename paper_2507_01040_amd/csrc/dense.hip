@@ -1703,18 +1703,25 @@ cliff_status finish_backward(int dtype, const DenseBackwardArgs& a, const Backwa
 // type with this row stride, or (weight_int8_kernel) g in fp32.
 int64_t expanded_ld(int64_t K) { return ceil_div(K, 8) * 8; }
 
-// Parts of the rows for weight_int8_kernel: a workgroup's stage of 32 rows, alone on a
-// compute unit and with a second one, and its begin and end, in ns.
-Cut weight_cut(int64_t M, int64_t K, int64_t N)
+// Parts of the rows for weight_int8_kernel, by the times in ns of a workgroup's stage of
+// 32 rows, alone on a compute unit and with a second one, and of its begin and end
+// (MI355X, one, two and three parts of scale g; tiles that are not whole wait for their
+// loads: 20000 x 300 x 300 bf16 75 us in 24 parts and 58 in 96).
+struct StageTimes {
+    double alone, full;
+};
+constexpr StageTimes T_WEIGHT[] = {{930, 1640}, {500, 760}, {760, 1230}}, T_WEIGHT_EDGES{2400, 3000};  // by cliff_dtype
+Cut weight_cut(int dtype, int64_t M, int64_t K, int64_t N)
 {
     const int64_t cus = std::max(device_cus(), 1), tiles = ceil_div(K, 128) * ceil_div(N, 128), steps = ceil_div(M, 32);
+    const StageTimes& t = K % 128 || N % 128 ? T_WEIGHT_EDGES : T_WEIGHT[dtype];
     Cut best{false, 1, 0, 0};
     for (const int want : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64, 96, 128, 192, 256}) {
         if (want > steps) break;
         const int64_t per = ceil_div(steps, want), splits = ceil_div(steps, per);
         const int64_t wgs = tiles * splits, rounds = wgs / (cus * 2), rest = wgs % (cus * 2);
-        double ns = rounds * (per * 800 + 6000);
-        if (rest) ns += per * (rest <= cus ? 450 : 800) + 6000;
+        double ns = rounds * (per * t.full + 6000);
+        if (rest) ns += per * (rest <= cus ? t.alone : t.full) + 6000;
         if (splits > 1) ns += 4400 + (double)K * N * 4 * 2 * splits / 11700;
         if (best.ns == 0 || ns < best.ns) best = Cut{false, (int)splits, per * 32, ns};
     }
@@ -1726,10 +1733,10 @@ bool exact_integers(int dtype, int act) { return dtype == CLIFF_F32 || act == CL
 
 // dw from x in 8 bits and g in fp32.
 template <typename T>
-cliff_status weight_int8(const DenseBackwardInt8Args& a, const float* g, int64_t ldg, float* partial, hipStream_t stream)
+cliff_status weight_int8(int dtype, const DenseBackwardInt8Args& a, const float* g, int64_t ldg, float* partial, hipStream_t stream)
 {
     const DenseBackwardArgs& d = a.dense;
-    const Cut c = weight_cut(d.M, d.K, d.N);
+    const Cut c = weight_cut(dtype, d.M, d.K, d.N);
     const int64_t M = d.w_out_in ? d.N : d.K, N = d.w_out_in ? d.K : d.N;
     const DropArgs none{nullptr, 0, 1.f};
     const ProductArgs p{M, N, d.M, nullptr, 0, nullptr, 0, c.splits, d.drop.rng ? d.drop.scale : 1.f, c.k_part, partial,
@@ -1765,7 +1772,7 @@ cliff_status launch_dense_backward(int dtype, const DenseBackwardArgs& a, hipStr
 
 int64_t dense_backward_int8_workspace(int dtype, int64_t M, int64_t K, int64_t N)
 {
-    const Cut c = weight_cut(M, K, N);
+    const Cut c = weight_cut(dtype, M, K, N);
     int64_t more = c.splits > 1 ? c.splits * K * N * 4 : 0;
     if (dtype != CLIFF_F32)  // g in fp32 and the parts, or x
         more = std::max(ceil_div(M * N * 4, 256) * 256 + more, M * expanded_ld(K) * 2);
@@ -1795,7 +1802,7 @@ cliff_status launch_dense_backward_int8(int dtype, const DenseBackwardInt8Args& 
         if (s == CLIFF_OK && exact) {
             const float* const from = g32 ? g32 : static_cast<const float*>(change ? ws + w.g : d.dy);
             char* const partial = g32 ? more + ceil_div(d.M * d.N * 4, 256) * 256 : more;
-            s = weight_int8<T>(a, from, g32 || change ? d.N : d.lddy, reinterpret_cast<float*>(partial), stream);
+            s = weight_int8<T>(dtype, a, from, g32 || change ? d.N : d.lddy, reinterpret_cast<float*>(partial), stream);
             d.dw = nullptr;
         } else if (s == CLIFF_OK && d.dw && d.M) {
             const int64_t ld = expanded_ld(d.K), pieces = ceil_div(d.K, per16<T>);
