@@ -6,7 +6,9 @@
 // Bound by memory: forward reads x and the residual and writes out and normed,
 // backward reads dout, dnormed, x and out and writes dx and dresidual.  A row lies
 // in the registers of TPR threads as in layer norm (rows.hpp), between its two norms
-// in fp32.
+// in fp32.  524288 x 128 fp32 forward 216 us (5.0 TB/s), 8192 x 4096 fp32 99 (5.4);
+// backward 16384 x 4096 bf16 171 us with its sums (4.7 TB/s), 266 with sixteen columns in
+// a thread, vectors loaded anew for each row and no loads ahead; 4 x 4096 bf16 5.4 us.
 #include <stdio.h>
 
 #include <algorithm>
