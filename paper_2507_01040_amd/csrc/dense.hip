@@ -1703,7 +1703,7 @@ cliff_status finish_backward(int dtype, const DenseBackwardArgs& a, const Backwa
 
 // A gradient from 8 bits has in its workspace, beside what dense_backward has, x in its
 // type with this row stride, or (weight_int8_kernel) g in fp32.
-int64_t expanded_ld(int64_t K) { return ceil_div(K, 8) * 8; }
+int64_t expanded_ld(int64_t K) { return ceil_div(K, 8) * 8; }  // (16-bit types)
 
 // Parts of the rows for weight_int8_kernel, by the times in ns of a workgroup's stage of
 // 32 rows, alone on a compute unit and with a second one, and of its begin and end
@@ -1791,7 +1791,7 @@ cliff_status launch_dense_backward_int8(int dtype, const DenseBackwardInt8Args& 
         char *const ws = static_cast<char*>(d.workspace), *const more = ws + w.all;
         const bool change = d.act != CLIFF_ACT_NONE || d.drop.rng;
         const bool exact = d.dw && d.M && exact_integers(dtype, d.act);
-        // g in the type, for dx and a product with x in it; fp32 has the one g
+        // g in the type, for dx and for dw where it is not in fp32 beside it
         const bool g = change && (d.dx || (d.dw && (!exact || sizeof(T) == 4)));
         float* const g32 = exact && sizeof(T) == 2 ? reinterpret_cast<float*>(more) : nullptr;
         cliff_status s = CLIFF_OK;
@@ -1806,16 +1806,18 @@ cliff_status launch_dense_backward_int8(int dtype, const DenseBackwardInt8Args& 
             char* const partial = g32 ? more + ceil_div(d.M * d.N * 4, 256) * 256 : more;
             s = weight_int8<T>(dtype, a, from, g32 || change ? d.N : d.lddy, reinterpret_cast<float*>(partial), stream);
             d.dw = nullptr;
-        } else if (s == CLIFF_OK && d.dw && d.M) {
-            const int64_t ld = expanded_ld(d.K), pieces = ceil_div(d.K, per16<T>);
-            const int64_t n = pieces * ceil_div(d.M, DEQUANTIZE_ROWS), blocks = ceil_div(n, 256);
-            if (blocks >= (int64_t)1 << 31) return CLIFF_EUNSUPPORTED;
-            const DequantizeArgs x{d.M, d.K, a.x_groups, static_cast<const int8_t*>(d.x), d.ldx, a.x_scale, more, ld};
-            hipLaunchKernelGGL(expand_kernel<T>, grid_of(blocks), dim3(256), 0, stream, x, (uint32_t)pieces, n);
-            s = launched();
-            d.x = x.y;
-            d.ldx = ld;
         }
+        if constexpr (sizeof(T) == 2)
+            if (s == CLIFF_OK && d.dw && d.M) {  // x as the product with g reads it
+                const int64_t ld = expanded_ld(d.K), pieces = ceil_div(d.K, per16<T>);
+                const int64_t n = pieces * ceil_div(d.M, DEQUANTIZE_ROWS), blocks = ceil_div(n, 256);
+                if (blocks >= (int64_t)1 << 31) return CLIFF_EUNSUPPORTED;
+                const DequantizeArgs x{d.M, d.K, a.x_groups, static_cast<const int8_t*>(d.x), d.ldx, a.x_scale, more, ld};
+                hipLaunchKernelGGL(expand_kernel<T>, grid_of(blocks), dim3(256), 0, stream, x, (uint32_t)pieces, n);
+                s = launched();
+                d.x = x.y;
+                d.ldx = ld;
+            }
         if (s != CLIFF_OK) return s;
         return finish_backward<T>(dtype, d, w, change ? static_cast<const void*>(ws + w.g) : d.dy, change ? d.N : d.lddy, stream);
     });
