@@ -294,6 +294,22 @@ def test_block_norm_gradient_in_place(dtype):
         assert torch.equal(alone.dx, want.dx) and torch.equal(alone.dresidual, want.dresidual) and alone[2:] == (None,) * 5
 
 
+@pytest.mark.parametrize("size", [r for r in ROWS if r[0]], ids=str)
+@pytest.mark.parametrize("dtype", DTYPES, ids=ids)
+def test_block_norm_gradient_with_a_gate_for_every_row(dtype, size):
+    for i, (after, before) in enumerate(((True, True), (True, False), (False, True))):
+        c = _norm_case(dtype, size, 4 + i, after=after, before=before, gate=Draw(9, dtype).rows(*size))
+        if not after:
+            c["weight"] = c["bias"] = None
+        if not before:
+            c["next_weight"] = c["next_bias"] = None
+        k = _gradient(c, size, dtype, i)
+        got = P.block_norm_backward(**k)
+        _check_gradient(k, got, dtype)
+        again = P.block_norm_backward(**k)
+        assert all(a is b is None or torch.equal(a, b) for a, b in zip(got, again))
+
+
 @pytest.mark.parametrize("rms", [False, True])
 @pytest.mark.parametrize("gates", [1, 3])
 def test_block_norm_gradient_against_differences(gates, rms):

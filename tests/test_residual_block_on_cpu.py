@@ -112,6 +112,20 @@ def test_block_norm_gradient(t):
     _run(cases)
 
 
+@pytest.mark.parametrize("t", TYPES)
+def test_block_norm_gradient_with_a_gate_for_every_row(t):
+    cases = []
+    for i, (R, d) in enumerate(NORM_WIDTHS[1:]):
+        for j, r in enumerate(RAGGED):
+            for after, before in ((1, 1), (1, 0), (0, 1)):
+                c = _norm("block_norm_backward", t, R, d, i, j, alias=(0, 0, 1, 2, 0, 1)[j], no_dout=int(j == 4 and before),
+                          no_params=int(j == 3), pad_dy=j, pad_dn=j, **r)
+                cases.append(dict(c, gates=max(R, 1), after=after, before=before))
+    if t != "fp16":  # (which has no 2^60)
+        cases += [dict(op="block_norm_backward", type=t, rows=3, d=d, constant=2.0 ** 60, w=1, gates=3) for d in (1, 5, 130, 1025, 8191)]
+    _run(cases)
+
+
 @pytest.mark.parametrize("t", ["fp32", "bf16"])
 def test_block_norm_gradient_of_large_constant_rows(t):
     # x - mean is zero in every column, though mean times rstd (eps^-0.5 = 316) is no
