@@ -119,13 +119,13 @@ __device__ inline void finish_rows(const Int8Args& p, int64_t m, int step, int64
 #pragma unroll
             for (int i = 0; i < 4; ++i) u[r][i] = fmaf((float)v[r][i], s[r] * e.scale[i], e.bias[i]);
     } else {
-        // the smaller scale first: neither product leaves fp32 where the result does not
-        // (comparisons keep a NaN)
+        // the scale of smaller magnitude first: neither product leaves fp32 where the result
+        // does not (comparisons keep a NaN)
 #pragma unroll
         for (int r = 0; r < R; ++r)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const bool less = s[r] < e.scale[i];
+                const bool less = fabsf(s[r]) < fabsf(e.scale[i]);
                 u[r][i] = fmaf((float)v[r][i] * (less ? s[r] : e.scale[i]), less ? e.scale[i] : s[r], e.bias[i]);
             }
     }

@@ -122,6 +122,10 @@ int dense_int8(Case& k)
     const float size = (float)(1 / (80 * sqrt((double)K)));
     fill_scales(k, xs, M, 1, 1.f);
     fill_scales(k, ws, N, 1, size / 80);
+    if (const int far = (int)k.f.i("far"); far && !emulate::dry) {  // of both signs, far from one: 2^far and 2^-far
+        for (int64_t i = 0; i < M; ++i) xs.set(0, i, (float)(ldexp(xs.get(0, i), far) * (i % 2 ? -1 : 1)));
+        for (int64_t i = 0; i < N; ++i) ws.set(0, i, (float)(ldexp(ws.get(0, i), -far) * (i / 2 % 2 ? -1 : 1)));
+    }
     if (k.f.i("bias")) b.make(k.t, 1, N, N, k.f.i("off")), b.fill(k.g, 1);
     if (k.f.i("residual") && !in_place) rows(k, res, "res", M, N), res.fill(k.g, 1);
     rows(k, y, "y", M, N);
