@@ -337,8 +337,8 @@ struct Parts {
 // EACH: every row has a gate of its own, which comes and whose gradient
 //   weight A + bias B = v (h weight + bias)
 // goes with the row, and the sums over all rows are of gate A and gate B at once
-// (65536 x 1024 bf16: 210 us, and 2288 with the sums of each gate in memory; 16384 x
-// 4096: 198 and 2158, of the 146 with one gate for all rows).
+// (bf16, both norms with their vectors: 65536 x 1024 in 238 us, and 2459 with the sums of
+// each gate in memory; 16384 x 4096 in 226 and 2341; one gate for all rows 186 and 171).
 template <typename T, int TPR, int EL, int R, bool EACH>
 __global__ __launch_bounds__(block_threads(TPR), TPR < 1024 ? 2 : 4) void block_norm_backward_kernel(BlockNormBackwardArgs a,
                                                                                               Parts parts, float* sums)
@@ -839,8 +839,8 @@ struct Forward {
     {
         // few rows: one each, for every compute unit has one
         const int64_t cus = std::max(device_cus(), 1), groups = block_threads(TPR) / TPR;
-        // (4096 columns: 8192 rows of fp32 99 us as a stream and 123 otherwise, 16384 of bf16
-        // 131 and 148)
+        // (4096 columns: 8192 rows of fp32 99 us as a stream and 121 otherwise, 16384 of bf16
+        // 111 and 174)
         if constexpr (TPR > 256) launch<TPR, EL, 1, STREAM>(1024 / TPR * cus);
         else if (a.rows <= cus * groups * R) launch<TPR, EL, 1, EARLY>(1 << 20);
         else launch<TPR, EL, R, USED>(1 << 20);

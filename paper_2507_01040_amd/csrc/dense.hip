@@ -1115,13 +1115,8 @@ constexpr float fit_slope(int act)
     return __is_same(T, _Float16) && (act == CLIFF_ACT_GELU || act == CLIFF_ACT_SILU) ? FIT_SLOPE : 1.f;
 }
 
-// g = keep dy f'(pre) fit_slope into g [M, N] (unless NULL), and the column sums
-// of keep dy f'(pre) over a share of the rows into sums [part][N] (unless NULL).  A
-// workgroup takes 256 columns; its four waves every fourth row each.  Bound by the
-// vector instructions of f' and the generator: 8192 x 2048 bf16, GELU and dropout,
-// 33 us (3 TB/s); 65536 x 512 fp32, SiLU, 87 us (4.6 TB/s, memory).
-// The pre-activations of four columns are in T, or in 8 bits with a scale for each
-// pre_groups-th of a row (EIGHT).
+// The pre-activations of four columns, in T, or in 8 bits with pre_groups scales a row
+// (EIGHT).
 template <typename T, bool EIGHT>
 __device__ inline f4 load_pre(const DenseBackwardArgs& a, const float* pre_scale, int64_t pre_groups, int64_t r, int64_t c,
                               int have)
@@ -1135,6 +1130,13 @@ __device__ inline f4 load_pre(const DenseBackwardArgs& a, const float* pre_scale
         return load4(static_cast<const T*>(a.pre) + r * a.ldp + c, have);
     }
 }
+
+// g = keep dy f'(pre) fit_slope into g [M, N] (unless NULL), and the column sums
+// of keep dy f'(pre) over a share of the rows into sums [part][N] (unless NULL); with
+// EIGHT also keep dy f'(pre) in fp32 into g32 [M, N] (unless NULL).  A workgroup takes
+// 256 columns; its four waves every fourth row each.  Bound by the vector instructions
+// of f' and the generator: 8192 x 2048 bf16, GELU and dropout, 33 us (3 TB/s); 65536 x
+// 512 fp32, SiLU, 87 us (4.6 TB/s, memory).
 template <typename T, bool EIGHT>
 __device__ inline void slope_rows(const DenseBackwardArgs& a, T* g, float* sums, int64_t rows_per_part,
                                   const float* pre_scale, int64_t pre_groups, float* g32)
