@@ -231,7 +231,7 @@ cliff_status cliffconv_dense_int8(int dtype, int64_t M, int64_t K, int64_t N, co
  * rounded: x to dtype where g is exact (NONE, ReLU), and with GELU and SiLU the scale of
  * x times g, once, to bf16 or, in fp16, to two bf16 parts, while the integers of x are
  * exact; that product needs |x| |g| to stay below the largest float for the largest x
- * of each group.
+ * of each group, and loses bits where scale |g| is below the smallest normal one.
  */
 int64_t cliffconv_dense_backward_int8_workspace(int dtype, int64_t M, int64_t K, int64_t N);
 cliff_status cliffconv_dense_backward_int8(
